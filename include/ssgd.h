@@ -211,6 +211,8 @@ int ssgd_sketch_merge(ssgd_ctx* ctx, const float* tables, float* merged, void* s
  * order, in fp32, of the decoded q16[w][j][b].  The rest of the pipeline runs on `merged` unchanged. */
 #define SSGD_FMT_F16  0
 #define SSGD_FMT_BF16 1
+#define SSGD_FMT_F32  2  /* the training operators below */
+#define SSGD_FMT_E4M3 3  /* ssgd_adamw_step's 8-bit states */
 int ssgd_sketch_quantize16(ssgd_ctx* ctx, const float* tables, int32_t fmt, uint16_t* q16, void* stream);
 int ssgd_sketch_merge16(ssgd_ctx* ctx, const uint16_t* q16, int32_t fmt, float* merged, void* stream);
 
@@ -319,6 +321,86 @@ int ssgd_launch_count(const ssgd_ctx* ctx, int64_t* out);
 /* Waits for the stream, then returns SSGD_EDEVICE if a kernel recorded an error since the last call
  * (the flag is cleared), SSGD_ECUDA if the stream reports a CUDA error, else SSGD_OK. */
 int ssgd_status(ssgd_ctx* ctx, void* stream);
+
+/* ---- operators of the training step around the compression ------------------------------------------------------
+ *
+ * The gradient that ssgd_step compresses comes out of a model's layers and loss, and the parameters that are not
+ * sketched (Section 5 of the paper leaves bias terms uncompressed) need an ordinary optimizer step.  These entry
+ * points have no context: everything they read or write is an argument.  They allocate nothing, check their arguments
+ * before anything is launched, and only enqueue work on `stream` (they can be captured in a CUDA graph).
+ *
+ * Element formats are SSGD_FMT_*; all arithmetic is fp32, results are rounded to nearest even once.  Bases need the
+ * alignment of their element type only (SSGD_EALIGN); rows may have any stride ld >= n (elements).  Bases and
+ * strides that are multiples of 16 bytes are fastest.  Values may be anything: infinities and NaN follow the formulas.
+ */
+
+/* Layer norm over the last dimension of x [rows][n] (any of the three formats):
+ *   mean = 1/n sum x,  rstd = (1/n sum (x - mean)^2 + eps)^-1/2,  y = (x - mean) rstd w + b
+ * w, b: [n] in fmt_w, which is SSGD_FMT_F32 or fmt_x; either may be NULL (1 and 0).  y: [rows][n] in fmt_x, may be x
+ * itself (same ld).  stats: [2][rows] fp32, mean then rstd: what the backward pass wants.  1 <= n <= 2^24, rows >= 0. */
+int ssgd_layer_norm(const void* x, int64_t ld_x, int32_t fmt_x, const void* w, const void* b, int32_t fmt_w,
+                    int64_t rows, int64_t n, float eps, void* y, int64_t ld_y, float* stats, void* stream);
+/* Its gradient.  With h = (x - mean) rstd and a = dy w:
+ *   dx = rstd (a - 1/n sum a - h 1/n sum a h)      [rows][n] in fmt_x; may be dy itself (same ld)
+ *   dw = sum over rows of dy h,  db = sum over rows of dy      [n] fp32 (so they can be a piece of a row of g); either
+ *        may be NULL; accumulate != 0 adds to what is there
+ * The sums over rows are added in a fixed order.  workspace: device memory of at least
+ * ssgd_layer_norm_backward_workspace(rows, n) bytes, 16-byte aligned, free again once the stream has passed. */
+int ssgd_layer_norm_backward_workspace(int64_t rows, int64_t n, size_t* out_bytes);
+int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int32_t fmt_x, const void* w,
+                             int32_t fmt_w, const float* stats, int64_t rows, int64_t n, void* dx, int64_t ld_dx,
+                             float* dw, float* db, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Log probabilities of given tokens.  For each row of logits [rows][vocab], z = scale * logits (scale > 0, e.g. 1 /
+ * temperature), lse = log sum e^z, p = e^(z - lse):
+ *   stats [3][rows] fp32   logp = z[id] - lse;  entropy = -sum p log p;  lse
+ *   top_idx, top_logp [rows][top]   the `top` (0 .. SSGD_MAX_TOP) largest logits, larger first, equal ones by smaller
+ *                                   index (NaN counts as the largest), and their log probabilities
+ * ids: [rows] of 4 or 8 bytes each (ids_bytes).  An id outside [0, vocab) is ignored: its logp is 0 and has no gradient.
+ * A logit of -inf has probability 0.  A row of nothing else has lse = -inf, entropy 0, every log probability -inf and
+ * the gradient 0.  A NaN or +inf makes its row's statistics NaN.  1 <= vocab <= 2^30. */
+#define SSGD_MAX_TOP 32
+int ssgd_token_logprobs(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes, int64_t rows,
+                        int64_t vocab, float scale, int32_t top, float* stats, int32_t* top_idx, float* top_logp,
+                        void* stream);
+/* The gradient with respect to the logits of sum(d_logp logp) + sum(d_entropy entropy) + sum(d_top top_logp):
+ *   dlogits_j = scale (d_logp [j = id] + sum_m d_top_m [j = top_idx_m] - p_j (d_logp + sum_m d_top_m + d_entropy (log p_j + entropy)))
+ * lse, entropy: [rows], as the forward pass wrote them.  d_logp, d_entropy: [rows], either may be NULL (0).  top_idx, d_top:
+ * [rows][top].  A top_idx outside [0, vocab) adds to the sum only.  dlogits: [rows][vocab] in fmt; may be logits itself
+ * (same ld). */
+int ssgd_token_logprobs_backward(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes,
+                                 int64_t rows, int64_t vocab, float scale, const float* lse, const float* entropy,
+                                 const float* d_logp, const float* d_entropy, int32_t top, const int32_t* top_idx,
+                                 const float* d_top, void* dlogits, int64_t ld_d, void* stream);
+
+/* One AdamW step (decoupled weight decay) over `count` tensors, each contiguous, in one launch per 384 tensors:
+ *   g <- g * grad_scale (device fp32 scalar, NULL: 1)
+ *   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - b1^step) * m / (sqrt(v) / sqrt(1 - b2^step) + eps),   step = 1, 2, ...
+ * p: SSGD_FMT_F32 or SSGD_FMT_BF16.  g: fp32, binary16 or bfloat16.  copy: NULL, or (fp32 p only) a copy of the new p
+ * in fmt_copy (SSGD_FMT_BF16 or SSGD_FMT_F16).  No two of these buffers may overlap.
+ * States, fmt_state: SSGD_FMT_F32, m and v fp32 [n], scales unused; or SSGD_FMT_E4M3, one byte per element: every
+ * SSGD_ADAMW_BLOCK consecutive elements share an fp32 scale (m_scale, v_scale: [ceil(n / SSGD_ADAMW_BLOCK)]), m stands
+ * for code * m_scale and v for (code * v_scale)^2, the new scale being the block's largest magnitude / 448.  Zero codes
+ * and scales are the initial state.  A positive sqrt(v) is never stored as 0.  A value that is not finite is stored as NaN.
+ * stochastic != 0: e4m3 states and bfloat16 parameters are rounded up or down with the probability that makes them
+ * right on average, by a hash of (seed, the tensor's place in the list, the element's index): give every step another
+ * seed.  stochastic == 0: to nearest. */
+#define SSGD_ADAMW_BLOCK 256
+typedef struct {
+    void* p;
+    const void* g;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* copy;
+    int64_t n;
+} ssgd_adamw_tensor;
+int ssgd_adamw_step(const ssgd_adamw_tensor* tensors, int32_t count, int32_t fmt_p, int32_t fmt_g, int32_t fmt_state,
+                    int32_t fmt_copy, double lr, double beta1, double beta2, double eps, double weight_decay,
+                    int64_t step, const float* grad_scale, int32_t stochastic, uint64_t seed, void* stream);
 
 const char* ssgd_strerror(int code);
 const char* ssgd_last_error(const ssgd_ctx* ctx); /* text of the last CUDA error seen, or "" */

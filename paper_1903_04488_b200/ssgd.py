@@ -21,11 +21,14 @@ PRUNE_AUTO, PRUNE_OFF, PRUNE_ON, PRUNE_EARLY_EXIT, PRUNE_FUSED = 0, 1, 2, 3, 4
 STREAM_AUTO, STREAM_EVICT_FIRST, STREAM_L2_ONLY = 0, 1, 2
 ZERO_DEFERRED, ZERO_EAGER = 0, 1
 SCHED_AUTO, SCHED_COORDINATE_MAJOR, SCHED_WORKER_MAJOR = 0, 1, 2
-FMT_F16, FMT_BF16 = 0, 1
+FMT_F16, FMT_BF16, FMT_F32, FMT_E4M3 = 0, 1, 2, 3
+MAX_TOP = 32
+ADAMW_BLOCK = 256
 MAX_R = 15
 
 # name -> argument types, exactly the declarations of include/ssgd.h
 _vp, _i64, _i32, _u64, _f32, _sz = C.c_void_p, C.c_int64, C.c_int32, C.c_uint64, C.c_float, C.c_size_t
+_f64 = C.c_double
 SIGNATURES = {
     "ssgd_create": [C.POINTER(_vp), _i64, _i32, _i64, _i64, _i32, _u64],
     "ssgd_destroy": [_vp],
@@ -63,6 +66,15 @@ SIGNATURES = {
     "ssgd_get_stage_times": [_vp, _vp, C.POINTER(C.c_double), C.POINTER(_i64)],
     "ssgd_launch_count": [_vp, C.POINTER(_i64)],
     "ssgd_status": [_vp, _vp],
+    # operators of the training step (train_ops.py)
+    "ssgd_layer_norm": [_vp, _i64, _i32, _vp, _vp, _i32, _i64, _i64, _f32, _vp, _i64, _vp, _vp],
+    "ssgd_layer_norm_backward_workspace": [_i64, _i64, C.POINTER(_sz)],
+    "ssgd_layer_norm_backward": [_vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _sz,
+                                 _vp],
+    "ssgd_token_logprobs": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _i32, _vp, _vp, _vp, _vp],
+    "ssgd_token_logprobs_backward": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
+                                     _i64, _vp],
+    "ssgd_adamw_step": [_vp, _i32, _i32, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _f64, _i64, _vp, _i32, _u64, _vp],
 }
 
 _lib = None
