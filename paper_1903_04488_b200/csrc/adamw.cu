@@ -172,27 +172,58 @@ __global__ void __launch_bounds__(THREADS) k_adamw_f32(const __grid_constant__ T
 
 // ---- states in 8 bits --------------------------------------------------------------------------------
 
-__device__ __forceinline__ float e4m3_value(uint32_t code) {
-    __half_raw r = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3);
-    return __half2float(__half(r));
+// Two e4m3 codes (lower byte first) as numbers
+__device__ __forceinline__ float2 e4m3_pair(uint32_t codes) {
+    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
+    return __half22float2(__half2(r));
 }
 
-// y = magnitude / scale in [0, 448], rounded down after u in [0, 1) units of its last place is added.  With
-// e = max(exponent, -6) a unit is 2^(e - 3); n = floor(y / unit + u) in 0..16 and 8 (e + 6) + n is the code, whose carry
-// into the exponent comes out by itself.  (A y above 448 by a rounding error stays at the largest code.)
-__device__ __forceinline__ uint32_t e4m3_code(float y, float u) {
-    const uint32_t e = max(__float_as_uint(y) & 0x7f800000u, 121u << 23);
-    const float per_unit = __uint_as_float((257u << 23) - e);          // 1 / unit
-    const uint32_t n = __float_as_uint(__fadd_rd(fmaf(y, per_unit, u), 8388608.f)) & 31u;
-    return min((e >> 20) - 968u + n, 126u);
+// Rounding to e4m3 in the bits of fp32.  y in [-448, 448] times 2^-120 is an fp32 number (a subnormal where e4m3 has
+// subnormals) whose exponent and first three fraction bits ARE the code, at bit 20: adding a dither in [0, 2^20) to the bits
+// and dropping the lower 20 rounds up with the probability of the dropped part, carries into the exponent included.
+// Shifted left by 4 with the sign put in front, the upper byte of the result is the code.
+__device__ __forceinline__ uint32_t e4m3_in_top_byte(float y, uint32_t dither) {
+    const uint32_t x = __float_as_uint(y * 0x1p-120f) + dither;
+    return ((x << 4) & 0x7fffffffu) | (x & 0x80000000u);
+}
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+__device__ __forceinline__ float sqrt_fast(float x) {
+    float y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ float warp_max(float x) {         // of magnitudes, which order like their bits; NaN above all
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
+}
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float2 (&f)[4]) {
+    if constexpr (sizeof(T) == 2) {
+        unpack_pairs(load_vec_stream<T, 8>(p), f);
+    } else {
+        const Vec<T, 4> a = load_vec_stream<T, 4>(p), b = load_vec_stream<T, 4>(p + 4);
+        f[0] = make_float2(a.e[0], a.e[1]); f[1] = make_float2(a.e[2], a.e[3]);
+        f[2] = make_float2(b.e[0], b.e[1]); f[3] = make_float2(b.e[2], b.e[3]);
+    }
 }
 
-__device__ __forceinline__ float finite_magnitude(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
-
-// A warp owns one block of 256 elements: lane l the elements 8 l .. 8 l + 7 when everything is aligned for it (VEC),
+// A warp owns one block of 256 elements: lane l the elements 8 l .. 8 l + 7 when everything is aligned for it (VECTOR),
 // otherwise the elements l, l + 32, ...  The codes and scales are the same either way.
-template <typename P, typename G, int CAP, bool VECTOR>
-__device__ __forceinline__ void block8(const Table<CAP>& T, const Entry& E, int64_t block, bool stochastic) {
+template <typename P, typename G, int CAP, bool STOCHASTIC, bool VECTOR>
+__device__ __forceinline__ void block8(const Table<CAP>& T, const Entry& E, int64_t block) {
     const Hyper& h = T.h;
     const int lane = threadIdx.x & 31;
     const int64_t base = block * QBLOCK, n = E.n;
@@ -200,100 +231,108 @@ __device__ __forceinline__ void block8(const Table<CAP>& T, const Entry& E, int6
     const G* g = static_cast<const G*>(E.g) + base;
     uint8_t* mc = static_cast<uint8_t*>(E.m) + base;
     uint8_t* vc = static_cast<uint8_t*>(E.v) + base;
-    const int left = n - base < QBLOCK ? (int)(n - base) : QBLOCK;
+    const int left = VECTOR ? QBLOCK : n - base < QBLOCK ? (int)(n - base) : QBLOCK;
     auto at = [&](int j) { return VECTOR ? lane * 8 + j : lane + 32 * j; };
-    float fp[8], fg[8], fm[8], fr[8];
-    const float gs = h.grad_scale ? *h.grad_scale : 1.f, ms = E.ms[block], vs = E.vs[block];
-    if (VECTOR && left == QBLOCK) {
-        union { uint2 r; uint8_t c[8]; } cm, cv;
-        cm.r = *reinterpret_cast<const uint2*>(mc + lane * 8);
-        cv.r = *reinterpret_cast<const uint2*>(vc + lane * 8);
-        if constexpr (sizeof(P) == 2) {
-            unpack(load_vec<P, 8>(p + lane * 8), fp);
-        } else {
-            const Vec<P, 4> a = load_vec<P, 4>(p + lane * 8), b = load_vec<P, 4>(p + lane * 8 + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { fp[j] = a.e[j]; fp[4 + j] = b.e[j]; }
-        }
-        if constexpr (sizeof(G) == 2) {
-            unpack(load_vec_stream<G, 8>(g + lane * 8), fg);
-        } else {
-            const Vec<G, 4> a = load_vec_stream<G, 4>(g + lane * 8), b = load_vec_stream<G, 4>(g + lane * 8 + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { fg[j] = a.e[j]; fg[4 + j] = b.e[j]; }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { fm[j] = e4m3_value(cm.c[j]); fr[j] = e4m3_value(cv.c[j]); }
+    float2 fp[4], fg[4], fm[4], fr[4];
+    if (VECTOR) {
+        const uint2 cm = *reinterpret_cast<const uint2*>(mc + lane * 8), cv = *reinterpret_cast<const uint2*>(vc + lane * 8);
+        load8(p + lane * 8, fp);
+        load8(g + lane * 8, fg);
+        fm[0] = e4m3_pair(cm.x & 0xffffu); fm[1] = e4m3_pair(cm.x >> 16); fm[2] = e4m3_pair(cm.y & 0xffffu); fm[3] = e4m3_pair(cm.y >> 16);
+        fr[0] = e4m3_pair(cv.x & 0xffffu); fr[1] = e4m3_pair(cv.x >> 16); fr[2] = e4m3_pair(cv.y & 0xffffu); fr[3] = e4m3_pair(cv.y >> 16);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = at(j);
-            const bool in = i < left;
-            fp[j] = in ? to_f32(p[i]) : 0.f;
-            fg[j] = in ? to_f32(g[i]) : 0.f;
-            fm[j] = in ? e4m3_value(mc[i]) : 0.f;
-            fr[j] = in ? e4m3_value(vc[i]) : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            const int i0 = at(2 * j), i1 = at(2 * j + 1);
+            fp[j] = make_float2(i0 < left ? to_f32(p[i0]) : 0.f, i1 < left ? to_f32(p[i1]) : 0.f);
+            fg[j] = make_float2(i0 < left ? to_f32(g[i0]) : 0.f, i1 < left ? to_f32(g[i1]) : 0.f);
+            fm[j] = e4m3_pair((i0 < left ? mc[i0] : 0u) | (i1 < left ? mc[i1] : 0u) << 8);
+            fr[j] = e4m3_pair((i0 < left ? vc[i0] : 0u) | (i1 < left ? vc[i1] : 0u) << 8);
         }
     }
-    float am = 0.f, ar = 0.f;
+    const float gs = h.grad_scale ? *h.grad_scale : 1.f;
+    const float2 ms = both(E.ms[block] * h.b1), vs = both(E.vs[block]);
+    float am = 0.f, ar = 0.f, ap = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float gj = fg[j] * gs, r0 = fr[j] * vs;
-        const float m = fmaf(fm[j] * ms, h.b1, gj * h.omb1);
-        const float v = fmaf(r0 * r0, h.b2, gj * gj * h.omb2);
-        const float r = sqrtf(v);
-        fp[j] = fmaf(fp[j], h.keep, -h.step_size * (m / fmaf(r, h.inv_bc2, h.eps)));
+    for (int j = 0; j < 4; ++j) {
+        const float2 gj = mul2(fg[j], both(gs)), r0 = mul2(fr[j], vs);
+        const float2 m = fma2(fm[j], ms, mul2(gj, both(h.omb1)));
+        const float2 v = fma2(mul2(r0, r0), both(h.b2), mul2(mul2(gj, gj), both(h.omb2)));
+        const float2 r = make_float2(sqrt_fast(v.x), sqrt_fast(v.y));
+        const float2 denom = fma2(r, both(h.inv_bc2), both(h.eps));
+        const float2 q = make_float2(__fdividef(m.x, denom.x), __fdividef(m.y, denom.y));
+        fp[j] = fma2(q, both(-h.step_size), mul2(fp[j], both(h.keep)));
         fm[j] = m;
         fr[j] = r;
-        am = fmaxf(am, finite_magnitude(m));
-        ar = fmaxf(ar, finite_magnitude(r));
+        am = max_nan(am, max_nan(fabsf(m.x), fabsf(m.y)));
+        ar = max_nan(ar, max_nan(r.x, r.y));
+        if (sizeof(P) == 2) ap = max_nan(ap, max_nan(fabsf(fp[j].x), fabsf(fp[j].y)));
     }
-    // magnitudes order like their bit patterns
-    am = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(am)));
-    ar = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(ar)));
-    const float least = 0x1p-100f;                         // below it 448 / x overflows: the block is held as zeros
-    const float im = am < least ? 0.f : 448.f / am, ir = ar < least ? 0.f : 448.f / ar;
+    am = warp_max(am);
+    ar = warp_max(ar);
+    // rare: a value that is not finite.  It must not count for the scale, and its code is NaN.
+    const bool odd = !(am < INFINITY && ar < INFINITY);
+    if (odd) {
+        am = ar = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            am = fmaxf(am, fmaxf(finite(fm[j].x) ? fabsf(fm[j].x) : 0.f, finite(fm[j].y) ? fabsf(fm[j].y) : 0.f));
+            ar = fmaxf(ar, fmaxf(finite(fr[j].x) ? fr[j].x : 0.f, finite(fr[j].y) ? fr[j].y : 0.f));
+        }
+        am = warp_max(am);
+        ar = warp_max(ar);
+    }
+    // Below 2^-100 the block is held as zeros.  448 * (1 / x) is good to 2 units: the dither's 16 bits leave room for 7
+    // before the largest magnitude could round past 448.
+    const float least = 0x1p-100f;
+    const float2 im = both(am < least ? 0.f : 448.f * rcp_fast(am)), ir = both(ar < least ? 0.f : 448.f * rcp_fast(ar));
     if (lane == 0) {
-        E.ms[block] = am < least ? 0.f : am / 448.f;
-        E.vs[block] = ar < least ? 0.f : ar / 448.f;
+        E.ms[block] = am < least ? 0.f : am * (1.f / 448.f);
+        E.vs[block] = ar < least ? 0.f : ar * (1.f / 448.f);
     }
     uint32_t code_m[8], code_v[8], word[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        word[j] = stochastic ? dither_word(E.key, base + at(j)) : 0u;
+        word[j] = STOCHASTIC ? dither_word(E.key, base + at(j)) : 0u;
         // 16 bits of dither each, in the middle of their interval; without a seed 1/2: to nearest
-        const float um = stochastic ? __uint_as_float(((word[j] << 7) & 0x007fff80u) | 0x3f800040u) - 1.f : 0.5f;
-        const float uv = stochastic ? __uint_as_float(((word[j] >> 9) & 0x007fff80u) | 0x3f800040u) - 1.f : 0.5f;
-        const uint32_t sign = (__float_as_uint(fm[j]) >> 24) & 0x80u;
-        code_m[j] = e4m3_code(fabsf(fm[j]) * im, um);
-        if (fm[j] < 0.f) code_m[j] |= sign;
-        code_v[j] = e4m3_code(fr[j] * ir, uv);
-        if (fr[j] > 0.f) code_v[j] = max(code_v[j], 1u);
-        if (!(fabsf(fm[j]) < INFINITY)) code_m[j] = 0x7fu;
-        if (!(fabsf(fr[j]) < INFINITY)) code_v[j] = 0x7fu;
+        const uint32_t dm = STOCHASTIC ? ((word[j] << 4) & 0xffff0u) | 8u : 0x80000u;
+        const uint32_t dv = STOCHASTIC ? ((word[j] >> 12) & 0xffff0u) | 8u : 0x80000u;
+        const float2 ym = mul2(fm[j / 2], im), yr = mul2(fr[j / 2], ir);
+        code_m[j] = e4m3_in_top_byte(j & 1 ? ym.y : ym.x, dm);
+        // a positive value keeps at least the smallest code
+        const uint32_t x = __float_as_uint((j & 1 ? yr.y : yr.x) * 0x1p-120f) + dv;
+        code_v[j] = max(x, min(__float_as_uint(j & 1 ? fr[j / 2].y : fr[j / 2].x), 1u << 20)) << 4;
+        if (odd) {
+            if (!finite(j & 1 ? fm[j / 2].y : fm[j / 2].x)) code_m[j] = 0x7fu << 24;
+            if (!finite(j & 1 ? fr[j / 2].y : fr[j / 2].x)) code_v[j] = 0x7fu << 24;
+        }
     }
-    if (VECTOR && left == QBLOCK) {
-        union { uint2 r; uint8_t c[8]; } cm, cv;
+    uint32_t np[8];                                          // bfloat16 parameters: the new value in the upper half
+    if constexpr (sizeof(P) == 2) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { cm.c[j] = (uint8_t)code_m[j]; cv.c[j] = (uint8_t)code_v[j]; }
-        *reinterpret_cast<uint2*>(mc + lane * 8) = cm.r;
-        *reinterpret_cast<uint2*>(vc + lane * 8) = cv.r;
+        for (int j = 0; j < 8; ++j) {
+            const float x = j & 1 ? fp[j / 2].y : fp[j / 2].x;
+            np[j] = STOCHASTIC ? __float_as_uint(x) + ((word[j] * 0x9E3779B9u) >> 16) : (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x)) << 16;
+            if (STOCHASTIC && !(ap < INFINITY) && !finite(x)) np[j] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x)) << 16;
+        }
+    }
+    if (VECTOR) {
+        *reinterpret_cast<uint2*>(mc + lane * 8) = make_uint2(top_bytes(code_m[0], code_m[1], code_m[2], code_m[3]),
+                                                              top_bytes(code_m[4], code_m[5], code_m[6], code_m[7]));
+        *reinterpret_cast<uint2*>(vc + lane * 8) = make_uint2(top_bytes(code_v[0], code_v[1], code_v[2], code_v[3]),
+                                                              top_bytes(code_v[4], code_v[5], code_v[6], code_v[7]));
         if constexpr (sizeof(P) == 2) {
-            Vec<P, 8> o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o.e[j] = round_param<P>(fp[j], stochastic, word[j]);
-            store_vec<P, 8>(p + lane * 8, o);
+            *reinterpret_cast<uint4*>(p + lane * 8) = make_uint4(__byte_perm(np[0], np[1], 0x7632), __byte_perm(np[2], np[3], 0x7632),
+                                                                 __byte_perm(np[4], np[5], 0x7632), __byte_perm(np[6], np[7], 0x7632));
         } else {
-            Vec<P, 4> a, b;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { a.e[j] = fp[j]; b.e[j] = fp[4 + j]; }
-            store_vec<P, 4>(p + lane * 8, a);
-            store_vec<P, 4>(p + lane * 8 + 4, b);
+            float4* o = reinterpret_cast<float4*>(p + lane * 8);
+            o[0] = make_float4(fp[0].x, fp[0].y, fp[1].x, fp[1].y);
+            o[1] = make_float4(fp[2].x, fp[2].y, fp[3].x, fp[3].y);
         }
         if (E.copy) {
             Vec<unsigned short, 8> c;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) c.e[j] = round_copy(fp[j], h.copy_f16);
+            for (int j = 0; j < 8; ++j) c.e[j] = round_copy(j & 1 ? fp[j / 2].y : fp[j / 2].x, h.copy_f16);
             store_vec<unsigned short, 8>(static_cast<unsigned short*>(E.copy) + base + lane * 8, c);
         }
     } else {
@@ -301,10 +340,12 @@ __device__ __forceinline__ void block8(const Table<CAP>& T, const Entry& E, int6
         for (int j = 0; j < 8; ++j) {
             const int i = at(j);
             if (i < left) {
-                mc[i] = (uint8_t)code_m[j];
-                vc[i] = (uint8_t)code_v[j];
-                p[i] = round_param<P>(fp[j], stochastic, word[j]);
-                if (E.copy) static_cast<unsigned short*>(E.copy)[base + i] = round_copy(fp[j], h.copy_f16);
+                const float x = j & 1 ? fp[j / 2].y : fp[j / 2].x;
+                mc[i] = (uint8_t)(code_m[j] >> 24);
+                vc[i] = (uint8_t)(code_v[j] >> 24);
+                if constexpr (sizeof(P) == 2) p[i] = __ushort_as_bfloat16((unsigned short)(np[j] >> 16));
+                else p[i] = x;
+                if (E.copy) static_cast<unsigned short*>(E.copy)[base + i] = round_copy(x, h.copy_f16);
             }
         }
     }
@@ -316,8 +357,8 @@ __global__ void __launch_bounds__(THREADS) k_adamw_8bit(const __grid_constant__ 
     const Entry& E = T.t[k];
     const int64_t block = (int64_t)(blockIdx.x - T.first[k]) * (THREADS / 32) + (threadIdx.x >> 5);
     if (block * QBLOCK >= E.n) return;
-    if (E.head == 0) block8<P, G, CAP, true>(T, E, block, STOCHASTIC);
-    else block8<P, G, CAP, false>(T, E, block, STOCHASTIC);
+    if (E.head == 0 && block * QBLOCK + QBLOCK <= E.n) block8<P, G, CAP, STOCHASTIC, true>(T, E, block);
+    else block8<P, G, CAP, STOCHASTIC, false>(T, E, block);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------

@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/ssgd.h"
 
@@ -65,6 +66,67 @@ __device__ __forceinline__ Vec<T, VEC> pack(const float (&f)[VEC]) {
     Vec<T, VEC> v;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) v.e[i] = from_f32<T>(f[i]);
+    return v;
+}
+
+// Pairs of fp32 numbers: one instruction works on both (rounding each like the scalar operation).
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// VEC elements as pairs in fp32; a single element has 0 beside it.
+template <int VEC> constexpr int PAIRS = (VEC + 1) / 2;
+template <typename T, int VEC>
+__device__ __forceinline__ void unpack_pairs(const Vec<T, VEC>& v, float2 (&f)[PAIRS<VEC>]) {
+    if constexpr (VEC == 1) {
+        f[0] = make_float2(to_f32(v.e[0]), 0.f);
+    } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    } else if constexpr (std::is_same<T, __half>::value) {
+        const __half2* h = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) f[i] = __half22float2(h[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) f[i] = make_float2(v.e[2 * i], v.e[2 * i + 1]);
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Vec<T, VEC> pack_pairs(const float2 (&f)[PAIRS<VEC>]) {
+    Vec<T, VEC> v;
+    if constexpr (VEC == 1) {
+        v.e[0] = from_f32<T>(f[0].x);
+    } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) h[i] = __floats2bfloat162_rn(f[i].x, f[i].y);
+    } else if constexpr (std::is_same<T, __half>::value) {
+        __half2* h = reinterpret_cast<__half2*>(&v);
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) h[i] = __floats2half2_rn(f[i].x, f[i].y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) { v.e[2 * i] = f[i].x; v.e[2 * i + 1] = f[i].y; }
+    }
     return v;
 }
 

@@ -44,17 +44,57 @@ __device__ __forceinline__ float group_sum(float x, float* slot) {
 
 // w or b at column `col`, VEC of them, in fp32 or in the row's format
 template <typename T, int VEC>
-__device__ __forceinline__ void load_param(const void* w, bool w_f32, int col, float (&f)[VEC]) {
+__device__ __forceinline__ void load_param(const void* w, bool w_f32, int col, float2 (&f)[PAIRS<VEC>]) {
     if (w_f32) {
         const float* p = static_cast<const float*>(w) + col;
         if constexpr (VEC == 8) {
             const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+            f[0] = make_float2(a.x, a.y); f[1] = make_float2(a.z, a.w);
+            f[2] = make_float2(b.x, b.y); f[3] = make_float2(b.z, b.w);
         } else {
-            unpack(load_vec<float, VEC>(p), f);
+            unpack_pairs(load_vec<float, VEC>(p), f);
         }
     } else {
-        unpack(load_vec<T, VEC>(static_cast<const T*>(w) + col), f);
+        unpack_pairs(load_vec<T, VEC>(static_cast<const T*>(w) + col), f);
+    }
+}
+
+// y = (x - mean) rstd w + b of one vector
+template <typename T, int VEC, typename A>
+__device__ __forceinline__ Vec<T, VEC> normalised(const Vec<T, VEC>& v, const A& args, int col, float2 minus_mean, float2 rstd) {
+    float2 f[PAIRS<VEC>], w[PAIRS<VEC>];
+    unpack_pairs(v, f);
+#pragma unroll
+    for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = mul2(add2(f[i], minus_mean), rstd);
+    if (args.w) {
+        load_param<T, VEC>(args.w, args.w_f32, col, w);
+#pragma unroll
+        for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = mul2(f[i], w[i]);
+    }
+    if (args.b) {
+        load_param<T, VEC>(args.b, args.w_f32, col, w);
+#pragma unroll
+        for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = add2(f[i], w[i]);
+    }
+    return pack_pairs<T, VEC>(f);
+}
+// sum of a vector's elements, and of their squared deviations, added to s
+template <typename T, int VEC>
+__device__ __forceinline__ void add_sum(const Vec<T, VEC>& v, float2& s) {
+    float2 f[PAIRS<VEC>];
+    unpack_pairs(v, f);
+#pragma unroll
+    for (int i = 0; i < PAIRS<VEC>; ++i) s = add2(s, f[i]);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void add_squares(const Vec<T, VEC>& v, float2 minus_mean, float2& q) {
+    float2 f[PAIRS<VEC>];
+    unpack_pairs(v, f);
+#pragma unroll
+    for (int i = 0; i < PAIRS<VEC>; ++i) {
+        float2 d = add2(f[i], minus_mean);
+        if (VEC == 1) d.y = 0.f;
+        q = fma2(d, d, q);
     }
 }
 
@@ -76,55 +116,27 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm(const NormA
     const T* x = static_cast<const T*>(A.x) + row * A.ld_x;
     const int nv = A.n / VEC;
     Vec<T, VEC> v[NV];
-    float s = 0.f;
+    float2 s = both(0.f), q = both(0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = t + j * G;
         if (i < nv) v[j] = load_vec_stream<T, VEC>(x + (int64_t)i * VEC);
     }
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        if (t + j * G < nv) {
-            float f[VEC];
-            unpack(v[j], f);
+    for (int j = 0; j < NV; ++j)
+        if (t + j * G < nv) add_sum(v[j], s);
+    const float mean = group_sum<G>(s.x + s.y, slot[0]) / (float)A.n;
+    const float2 minus_mean = both(-mean);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s += f[e];
-        }
-    }
-    const float mean = group_sum<G>(s, slot[0]) / (float)A.n;
-    float q = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        if (t + j * G < nv) {
-            float f[VEC];
-            unpack(v[j], f);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) { const float d = f[e] - mean; q = fmaf(d, d, q); }
-        }
-    }
-    const float rstd = 1.0f / sqrtf(group_sum<G>(q, slot[1]) / (float)A.n + A.eps);
+    for (int j = 0; j < NV; ++j)
+        if (t + j * G < nv) add_squares(v[j], minus_mean, q);
+    const float rstd = 1.0f / sqrtf(group_sum<G>(q.x + q.y, slot[1]) / (float)A.n + A.eps);
     if (t == 0) { A.stats[row] = mean; A.stats[A.rows + row] = rstd; }
     T* y = static_cast<T*>(A.y) + row * A.ld_y;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = t + j * G;
-        if (i < nv) {
-            float f[VEC], w[VEC], b[VEC];
-            unpack(v[j], f);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = (f[e] - mean) * rstd;
-            if (A.w) {
-                load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] *= w[e];
-            }
-            if (A.b) {
-                load_param<T, VEC>(A.b, A.w_f32, i * VEC, b);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] += b[e];
-            }
-            store_vec<T, VEC>(y + (int64_t)i * VEC, pack<T, VEC>(f));
-        }
+        if (i < nv) store_vec<T, VEC>(y + (int64_t)i * VEC, normalised(v[j], A, i * VEC, minus_mean, both(rstd)));
     }
 }
 
@@ -137,38 +149,16 @@ __global__ void __launch_bounds__(WIDE) k_layer_norm_wide(const NormArgs A) {
     const int64_t row = blockIdx.x;
     const T* x = static_cast<const T*>(A.x) + row * A.ld_x;
     const int nv = A.n / VEC;
-    float s = 0.f, q = 0.f, f[VEC];
-    for (int i = t; i < nv; i += WIDE) {
-        unpack(load_vec<T, VEC>(x + (int64_t)i * VEC), f);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) s += f[e];
-    }
-    const float mean = group_sum<WIDE>(s, slot[0]) / (float)A.n;
-    for (int i = t; i < nv; i += WIDE) {
-        unpack(load_vec<T, VEC>(x + (int64_t)i * VEC), f);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) { const float d = f[e] - mean; q = fmaf(d, d, q); }
-    }
-    const float rstd = 1.0f / sqrtf(group_sum<WIDE>(q, slot[1]) / (float)A.n + A.eps);
+    float2 s = both(0.f), q = both(0.f);
+    for (int i = t; i < nv; i += WIDE) add_sum(load_vec<T, VEC>(x + (int64_t)i * VEC), s);
+    const float mean = group_sum<WIDE>(s.x + s.y, slot[0]) / (float)A.n;
+    const float2 minus_mean = both(-mean);
+    for (int i = t; i < nv; i += WIDE) add_squares(load_vec<T, VEC>(x + (int64_t)i * VEC), minus_mean, q);
+    const float rstd = 1.0f / sqrtf(group_sum<WIDE>(q.x + q.y, slot[1]) / (float)A.n + A.eps);
     if (t == 0) { A.stats[row] = mean; A.stats[A.rows + row] = rstd; }
     T* y = static_cast<T*>(A.y) + row * A.ld_y;
-    for (int i = t; i < nv; i += WIDE) {
-        float w[VEC], b[VEC];
-        unpack(load_vec<T, VEC>(x + (int64_t)i * VEC), f);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = (f[e] - mean) * rstd;
-        if (A.w) {
-            load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] *= w[e];
-        }
-        if (A.b) {
-            load_param<T, VEC>(A.b, A.w_f32, i * VEC, b);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] += b[e];
-        }
-        store_vec<T, VEC>(y + (int64_t)i * VEC, pack<T, VEC>(f));
-    }
+    for (int i = t; i < nv; i += WIDE)
+        store_vec<T, VEC>(y + (int64_t)i * VEC, normalised(load_vec<T, VEC>(x + (int64_t)i * VEC), A, i * VEC, minus_mean, both(rstd)));
 }
 
 // ---- backward ----------------------------------------------------------------------------------------
@@ -188,21 +178,59 @@ struct NormBackArgs {
     float* row_sums;     // wide rows: [rows][2]
 };
 
+// h = (x - mean) rstd and a = dy w of one vector, and what it adds to the four sums
+template <int P>
+struct BackTerms { float2 h[P], a[P]; };
+template <typename T, int VEC>
+__device__ __forceinline__ BackTerms<PAIRS<VEC>> back_terms(const Vec<T, VEC>& x, const Vec<T, VEC>& dy, const float2 (&w)[PAIRS<VEC>],
+                                                            float2 minus_mean, float2 rstd, float2& c1, float2& c2,
+                                                            float2* dw, float2* db) {
+    BackTerms<PAIRS<VEC>> r;
+    float2 d[PAIRS<VEC>];
+    unpack_pairs(x, r.h);
+    unpack_pairs(dy, d);
+#pragma unroll
+    for (int i = 0; i < PAIRS<VEC>; ++i) {
+        r.h[i] = mul2(add2(r.h[i], minus_mean), rstd);
+        r.a[i] = mul2(d[i], w[i]);
+        c1 = add2(c1, r.a[i]);
+        c2 = fma2(r.a[i], r.h[i], c2);
+        if (dw) {
+            dw[i] = fma2(d[i], r.h[i], dw[i]);
+            db[i] = add2(db[i], d[i]);
+        }
+    }
+    return r;
+}
+// dx = rstd a - rstd c1 - h (rstd c2)
+template <typename T, int VEC>
+__device__ __forceinline__ Vec<T, VEC> back_result(const BackTerms<PAIRS<VEC>>& r, float2 rstd, float2 minus_c1, float2 minus_c2) {
+    float2 f[PAIRS<VEC>];
+#pragma unroll
+    for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = mul2(fma2(r.h[i], minus_c2, add2(r.a[i], minus_c1)), rstd);
+    return pack_pairs<T, VEC>(f);
+}
+
 template <typename T, int VEC, int G, int E>
 __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_back(const NormBackArgs A) {
-    constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS;
+    constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS, P = PAIRS<VEC>;
     extern __shared__ float smem[];                    // G = 32: [8][2][n] partial sums at the end
     __shared__ float2 slot[2][32];
     const int t = threadIdx.x % G, sub = threadIdx.x / G;
     const int nv = A.n / VEC;
     const float inv_n = 1.0f / (float)A.n;
-    float dw[E], db[E];
+    float2 dw[NV][P], db[NV][P], w[NV][P];
 #pragma unroll
-    for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) { dw[j][i] = db[j][i] = both(0.f); w[j][i] = both(1.f); }
+        if (A.w && t + j * G < nv) load_param<T, VEC>(A.w, A.w_f32, (t + j * G) * VEC, w[j]);
+    }
+    // the next row's vectors are on their way while this row is summed and written
     Vec<T, VEC> vx[NV], vd[NV];
+    float mean = 0.f, rstd = 0.f;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     int64_t row = (int64_t)blockIdx.x * ROWS + sub;
-    int turn = 0;
     auto fetch = [&](int64_t r) {
         const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
         const T* d = static_cast<const T*>(A.dy) + r * A.ld_dy;
@@ -214,97 +242,63 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_back(const 
                 vd[j] = load_vec_stream<T, VEC>(d + (int64_t)i * VEC);
             }
         }
+        mean = A.stats[r];
+        rstd = A.stats[A.rows + r];
     };
+    if (row < A.rows) fetch(row);
+    int turn = 0;
     for (; row < A.rows; row += step) {
-        fetch(row);
-        const float mean = A.stats[row], rstd = A.stats[A.rows + row];
-        float c1 = 0.f, c2 = 0.f;
+        float2 c1 = both(0.f), c2 = both(0.f);
+        BackTerms<P> r[NV];
+        const float2 scale = both(rstd);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = t + j * G;
-            if (i < nv) {
-                float fx[VEC], fd[VEC], w[VEC];
-                unpack(vx[j], fx);
-                unpack(vd[j], fd);
-                if (A.w) load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float h = (fx[e] - mean) * rstd;
-                    const float a = A.w ? fd[e] * w[e] : fd[e];
-                    c1 += a;
-                    c2 = fmaf(a, h, c2);
-                    dw[j * VEC + e] = fmaf(fd[e], h, dw[j * VEC + e]);
-                    db[j * VEC + e] += fd[e];
-                }
-            }
-        }
-        c1 = warp_sum(c1);
-        c2 = warp_sum(c2);
+        for (int j = 0; j < NV; ++j)
+            if (t + j * G < nv) r[j] = back_terms<T, VEC>(vx[j], vd[j], w[j], both(-mean), scale, c1, c2, dw[j], db[j]);
+        if (row + step < A.rows) fetch(row + step);
+        float s1 = warp_sum(c1.x + c1.y), s2 = warp_sum(c2.x + c2.y);
         if constexpr (G > 32) {
             const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
             constexpr int NW = GroupShape<G>::WARPS;
-            if (lane == 0) slot[turn][warp] = make_float2(c1, c2);
+            if (lane == 0) slot[turn][warp] = make_float2(s1, s2);
             __syncthreads();
-            const float2 p = lane < NW ? slot[turn][lane] : make_float2(0.f, 0.f);
-            c1 = warp_sum(p.x);
-            c2 = warp_sum(p.y);
+            float2 p = lane < NW ? slot[turn][lane] : both(0.f);
+#pragma unroll
+            for (int o = NW / 2; o > 0; o >>= 1)
+                p = add2(p, make_float2(__shfl_xor_sync(0xffffffffu, p.x, o), __shfl_xor_sync(0xffffffffu, p.y, o)));
+            s1 = __shfl_sync(0xffffffffu, p.x, 0);
+            s2 = __shfl_sync(0xffffffffu, p.y, 0);
             turn ^= 1;
         }
-        c1 *= inv_n;
-        c2 *= inv_n;
         T* dx = static_cast<T*>(A.dx) + row * A.ld_dx;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int i = t + j * G;
-            if (i < nv) {
-                float fx[VEC], fd[VEC], w[VEC];
-                unpack(vx[j], fx);
-                unpack(vd[j], fd);
-                if (A.w) load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float h = (fx[e] - mean) * rstd;
-                    const float a = A.w ? fd[e] * w[e] : fd[e];
-                    fd[e] = rstd * (a - c1 - h * c2);
-                }
-                store_vec<T, VEC>(dx + (int64_t)i * VEC, pack<T, VEC>(fd));
-            }
+            if (i < nv)
+                store_vec<T, VEC>(dx + (int64_t)i * VEC, back_result<T, VEC>(r[j], scale, both(-s1 * inv_n), both(-s2 * inv_n)));
         }
     }
     if (!A.partial) return;
     float* out = A.partial + (int64_t)blockIdx.x * 2 * A.n;
-    if constexpr (G == 32) {
-        // the block's 8 warps add up in shared memory first
-        float* mine = smem + (int64_t)sub * 2 * A.n;
+    float* mine = G == 32 ? smem + (int64_t)sub * 2 * A.n : out;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = t + j * G;
-            if (i < nv) {
+    for (int j = 0; j < NV; ++j) {
+        const int i = t + j * G;
+        if (i < nv) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    mine[i * VEC + e] = dw[j * VEC + e];
-                    mine[A.n + i * VEC + e] = db[j * VEC + e];
-                }
+            for (int e = 0; e < VEC; ++e) {
+                mine[i * VEC + e] = e & 1 ? dw[j][e / 2].y : dw[j][e / 2].x;
+                mine[A.n + i * VEC + e] = e & 1 ? db[j][e / 2].y : db[j][e / 2].x;
             }
         }
+    }
+    if constexpr (G == 32) {
+        // the block's 8 warps add up in shared memory first
         __syncthreads();
         for (int c = threadIdx.x; c < 2 * A.n; c += GroupShape<G>::BLOCK) {
             float s = 0.f;
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) s += smem[(int64_t)r * 2 * A.n + c];
             out[c] = s;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = t + j * G;
-            if (i < nv) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    out[i * VEC + e] = dw[j * VEC + e];
-                    out[A.n + i * VEC + e] = db[j * VEC + e];
-                }
-            }
         }
     }
 }
@@ -316,76 +310,71 @@ __global__ void __launch_bounds__(WIDE) k_norm_back_sums(const NormBackArgs A) {
     const int64_t row = blockIdx.x;
     const T* x = static_cast<const T*>(A.x) + row * A.ld_x;
     const T* d = static_cast<const T*>(A.dy) + row * A.ld_dy;
-    const float mean = A.stats[row], rstd = A.stats[A.rows + row];
+    const float2 minus_mean = both(-A.stats[row]), rstd = both(A.stats[A.rows + row]);
     const int nv = A.n / VEC;
-    float c1 = 0.f, c2 = 0.f;
+    float2 c1 = both(0.f), c2 = both(0.f);
     for (int i = threadIdx.x; i < nv; i += WIDE) {
-        float fx[VEC], fd[VEC], w[VEC];
-        unpack(load_vec<T, VEC>(x + (int64_t)i * VEC), fx);
-        unpack(load_vec<T, VEC>(d + (int64_t)i * VEC), fd);
-        if (A.w) load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
+        float2 w[PAIRS<VEC>];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float a = A.w ? fd[e] * w[e] : fd[e];
-            c1 += a;
-            c2 = fmaf(a, (fx[e] - mean) * rstd, c2);
-        }
+        for (int k = 0; k < PAIRS<VEC>; ++k) w[k] = both(1.f);
+        if (A.w) load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
+        back_terms<T, VEC>(load_vec<T, VEC>(x + (int64_t)i * VEC), load_vec<T, VEC>(d + (int64_t)i * VEC), w, minus_mean, rstd, c1, c2,
+                           nullptr, nullptr);
     }
-    c1 = group_sum<WIDE>(c1, slot[0]);
-    c2 = group_sum<WIDE>(c2, slot[1]);
+    const float s1 = group_sum<WIDE>(c1.x + c1.y, slot[0]), s2 = group_sum<WIDE>(c2.x + c2.y, slot[1]);
     if (threadIdx.x == 0) {
-        A.row_sums[2 * row] = c1 / (float)A.n;
-        A.row_sums[2 * row + 1] = c2 / (float)A.n;
+        A.row_sums[2 * row] = s1 / (float)A.n;
+        A.row_sums[2 * row + 1] = s2 / (float)A.n;
     }
 }
 
 // Second pass: blockIdx.x is a slab of 256 vectors of columns, blockIdx.y a share of the rows.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) k_norm_back_slab(const NormBackArgs A) {
+    constexpr int P = PAIRS<VEC>;
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= A.n / VEC) return;
     const int64_t col = (int64_t)i * VEC;
-    float dw[VEC], db[VEC], w[VEC];
+    float2 dw[P], db[P], w[P];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) { dw[e] = db[e] = 0.f; w[e] = 1.f; }
+    for (int e = 0; e < P; ++e) { dw[e] = db[e] = both(0.f); w[e] = both(1.f); }
     if (A.w) load_param<T, VEC>(A.w, A.w_f32, (int)col, w);
     for (int64_t row = blockIdx.y; row < A.rows; row += gridDim.y) {
-        float fx[VEC], fd[VEC];
-        unpack(load_vec_stream<T, VEC>(static_cast<const T*>(A.x) + row * A.ld_x + col), fx);
-        unpack(load_vec_stream<T, VEC>(static_cast<const T*>(A.dy) + row * A.ld_dy + col), fd);
-        const float mean = A.stats[row], rstd = A.stats[A.rows + row];
-        const float c1 = A.row_sums[2 * row], c2 = A.row_sums[2 * row + 1];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float h = (fx[e] - mean) * rstd;
-            dw[e] = fmaf(fd[e], h, dw[e]);
-            db[e] += fd[e];
-            fd[e] = rstd * (fd[e] * w[e] - c1 - h * c2);
-        }
-        store_vec<T, VEC>(static_cast<T*>(A.dx) + row * A.ld_dx + col, pack<T, VEC>(fd));
+        float2 c1 = both(0.f), c2 = both(0.f);
+        const float2 rstd = both(A.stats[A.rows + row]);
+        const BackTerms<P> r =
+            back_terms<T, VEC>(load_vec_stream<T, VEC>(static_cast<const T*>(A.x) + row * A.ld_x + col),
+                               load_vec_stream<T, VEC>(static_cast<const T*>(A.dy) + row * A.ld_dy + col), w,
+                               both(-A.stats[row]), rstd, c1, c2, dw, db);
+        store_vec<T, VEC>(static_cast<T*>(A.dx) + row * A.ld_dx + col,
+                          back_result<T, VEC>(r, rstd, both(-A.row_sums[2 * row]), both(-A.row_sums[2 * row + 1])));
     }
     if (!A.partial) return;
     float* out = A.partial + (int64_t)blockIdx.y * 2 * A.n;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-        out[col + e] = dw[e];
-        out[A.n + col + e] = db[e];
+        out[col + e] = e & 1 ? dw[e / 2].y : dw[e / 2].x;
+        out[A.n + col + e] = e & 1 ? db[e / 2].y : db[e / 2].x;
     }
 }
 
-// dw[c], db[c] = sum over the blocks' partials, in a fixed order: 32 columns per block, 8 warps share the partials.
-__global__ void __launch_bounds__(256) k_norm_reduce(const float* partial, int parts, int n, float* dw, float* db, int accumulate) {
-    __shared__ float s[8][32];
+// dw[c], db[c] = sum over the blocks' partials, in a fixed order: 32 columns per block, its warps share the partials.
+constexpr int REDUCE_WARPS = 16;
+__global__ void __launch_bounds__(REDUCE_WARPS * 32) k_norm_reduce(const float* partial, int parts, int n, float* dw, float* db,
+                                                                   int accumulate) {
+    __shared__ float s[REDUCE_WARPS][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;              // 0 .. 2n - 1
     float a = 0.f;
-    if (c < 2 * n)
-        for (int p = warp; p < parts; p += 8) a += partial[(int64_t)p * 2 * n + c];
+    if (c < 2 * n) {
+#pragma unroll 8
+        for (int p = warp; p < parts; p += REDUCE_WARPS) a += partial[(int64_t)p * 2 * n + c];
+    }
     s[warp][lane] = a;
     __syncthreads();
     if (warp == 0 && c < 2 * n) {
 #pragma unroll
-        for (int k = 1; k < 8; ++k) a += s[k][lane];
+        for (int k = 1; k < REDUCE_WARPS; ++k) a += s[k][lane];
         float* out = c < n ? dw : db;
         if (out) {
             const int at = c < n ? c : c - n;
@@ -430,8 +419,9 @@ int launch_norm(const NormArgs& A, cudaStream_t st) {
         k_layer_norm<T, VEC, G, E><<<(unsigned)grid, GroupShape<G>::BLOCK, 0, st>>>(A);                             \
         return launched();                                                                                          \
     } while (0)
+    constexpr int LONG = VEC == 1 ? 32 : 64;           // a vector of one element wastes half of a pair's registers
     if (n <= 32 * 16) NORM(32, 16);
-    if (n <= 32 * 64) NORM(32, 64);
+    if (n <= 32 * LONG) NORM(32, LONG);
     if (n <= 128 * 32) NORM(128, 32);
     if (n <= 256 * 32) NORM(256, 32);
     if (n <= 512 * 32) NORM(512, 32);
@@ -442,7 +432,7 @@ int launch_norm(const NormArgs& A, cudaStream_t st) {
 }
 
 constexpr int64_t PART_BLOCKS = 148 * 4;         // at most so many partial sums of dw and db
-constexpr int BACK_MAX_N = 512 * 16;             // rows up to here stay in a block's registers
+constexpr int BACK_NARROW = 512 * 8;             // rows up to here stay in a block's registers, whatever the format
 
 template <typename T, int VEC>
 int launch_norm_back(const NormBackArgs& A, int sms, int* parts, cudaStream_t st) {
@@ -462,10 +452,12 @@ int launch_norm_back(const NormBackArgs& A, int sms, int* parts, cudaStream_t st
         *parts = (int)grid;                                                                                         \
         return launched();                                                                                          \
     } while (0)
-    if (n <= 32 * 16) NORM_BACK(32, 16);
-    if (n <= 128 * 16) NORM_BACK(128, 16);
-    if (n <= 256 * 16) NORM_BACK(256, 16);
-    if (n <= BACK_MAX_N) NORM_BACK(512, 16);
+    // 16 elements of 16 bits per thread or 8 of 32 bits: with their sums and the next row's on the way, 128 registers
+    constexpr int E = sizeof(T) == 4 || VEC == 1 ? 8 : 16;
+    if (n <= 32 * E) NORM_BACK(32, E);
+    if (n <= 128 * E) NORM_BACK(128, E);
+    if (n <= 256 * E) NORM_BACK(256, E);
+    if (n <= 512 * E) NORM_BACK(512, E);
 #undef NORM_BACK
     if (A.rows > 0x7fffffff) return SSGD_EINVAL;
     k_norm_back_sums<T, VEC><<<(unsigned)A.rows, WIDE, 0, st>>>(A);
@@ -519,7 +511,7 @@ int ssgd_layer_norm_backward_workspace(int64_t rows, int64_t n, size_t* out_byte
     if (rows < 0 || n < 1 || n > MAX_N || !out_bytes) return SSGD_EINVAL;
     const int64_t parts = rows < PART_BLOCKS ? rows : PART_BLOCKS;
     size_t bytes = (size_t)parts * 2 * (size_t)n * 4;
-    if (n > BACK_MAX_N) bytes += (size_t)rows * 2 * 4;
+    if (n > BACK_NARROW) bytes += (size_t)rows * 2 * 4;
     *out_bytes = bytes;
     return SSGD_OK;
 }
@@ -551,13 +543,13 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
     NormBackArgs A{dy, ld_dy, x, ld_x, w, fmt_w == SSGD_FMT_F32, stats, rows, (int32_t)n, dx, ld_dx, nullptr, nullptr};
     float* base = static_cast<float*>(workspace);
     A.row_sums = base;
-    if (n > BACK_MAX_N) base += 2 * rows;
+    if (n > BACK_NARROW) base += 2 * rows;
     A.partial = dw || db ? base : nullptr;
     const int vec = vec_of(es, n, {dy, x, dx}, {ld_dy, ld_x, ld_dx}, {w}, A.w_f32);
     int parts = 0;
     e = BY_FORMAT(launch_norm_back, fmt_x, vec, A, sms, &parts, st);
     if (e || !A.partial) return e;
-    k_norm_reduce<<<(unsigned)((2 * n + 31) / 32), 256, 0, st>>>(A.partial, parts, (int)n, dw, db, accumulate);
+    k_norm_reduce<<<(unsigned)((2 * n + 31) / 32), REDUCE_WARPS * 32, 0, st>>>(A.partial, parts, (int)n, dw, db, accumulate);
     return launched();
 }
 

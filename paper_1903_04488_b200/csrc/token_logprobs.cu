@@ -129,20 +129,55 @@ template <typename T> struct Granules {
     __device__ __forceinline__ bool whole(int32_t i) const { return first(i) >= 0 && first(i) + VEC <= n; }
 };
 
-// The maximum of a granule (NaN if it holds one)
-template <typename T>
-__device__ __forceinline__ float max_of(const Vec<T, 16 / sizeof(T)>& v) {
-    if constexpr (sizeof(T) == 4) {
-        return max_nan(max_nan(v.e[0], v.e[1]), max_nan(v.e[2], v.e[3]));
-    } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-        const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-        return max_nan(__low2float(m), __high2float(m));
-    } else {
-        const __half2* h = reinterpret_cast<const __half2*>(&v);
-        const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-        return max_nan(__low2float(m), __high2float(m));
+// Running maximum of the elements of granules, two at a time (NaN if one is)
+template <typename T> struct PairMax;
+template <> struct PairMax<float> {
+    float2 m;
+    __device__ __forceinline__ explicit PairMax(float x) : m(both(x)) {}
+    __device__ __forceinline__ void add(const Vec<float, 4>& v) {
+        m.x = max_nan(m.x, max_nan(v.e[0], v.e[1]));
+        m.y = max_nan(m.y, max_nan(v.e[2], v.e[3]));
     }
+    __device__ __forceinline__ float value() const { return max_nan(m.x, m.y); }
+};
+template <> struct PairMax<__nv_bfloat16> {
+    __nv_bfloat162 m;
+    __device__ __forceinline__ explicit PairMax(float x) : m(__float2bfloat162_rn(x)) {}
+    __device__ __forceinline__ void add(const Vec<__nv_bfloat16, 8>& v) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        m = __hmax2_nan(m, __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    }
+    __device__ __forceinline__ float value() const { return max_nan(__low2float(m), __high2float(m)); }
+};
+template <> struct PairMax<__half> {
+    __half2 m;
+    __device__ __forceinline__ explicit PairMax(float x) : m(__float2half2_rn(x)) {}
+    __device__ __forceinline__ void add(const Vec<__half, 8>& v) {
+        const __half2* h = reinterpret_cast<const __half2*>(&v);
+        m = __hmax2_nan(m, __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    }
+    __device__ __forceinline__ float value() const { return max_nan(__low2float(m), __high2float(m)); }
+};
+
+// A granule with everything below `low` raised to it (low is a number of the format)
+__device__ __forceinline__ Vec<float, 4> raised(Vec<float, 4> v, float low) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v.e[e] = fmaxf(v.e[e], low);
+    return v;
+}
+__device__ __forceinline__ Vec<__nv_bfloat16, 8> raised(Vec<__nv_bfloat16, 8> v, float low) {
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+    const __nv_bfloat162 l = __float2bfloat162_rn(low);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __hmax2(h[e], l);
+    return v;
+}
+__device__ __forceinline__ Vec<__half, 8> raised(Vec<__half, 8> v, float low) {
+    __half2* h = reinterpret_cast<__half2*>(&v);
+    const __half2 l = __float2half2_rn(low);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __hmax2(h[e], l);
+    return v;
 }
 
 // A value no larger than m - 160 / c and below every element that could matter: elements under it are raised to it, so
@@ -160,28 +195,33 @@ template <> __device__ __forceinline__ float floor_for<__half>(float m, float c)
 template <typename T, int U>
 __device__ __forceinline__ void add_granules(Sums& a, float& low, const Vec<T, 16 / sizeof(T)> (&v)[U], int have, float c) {
     constexpr int VEC = 16 / sizeof(T);
-    float m = a.m;
+    PairMax<T> top(a.m);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (u < have) m = max_nan(m, max_of<T>(v[u]));
+        if (u < have) top.add(v[u]);
+    const float m = top.value();
     if (!(m == a.m)) {
         rebase(a, m, c);
         low = fabsf(m) < fast_limit<T>() ? floor_for<T>(m, c) : NEG_INF;
     }
     if (low > NEG_INF) {
+        const float2 minus_m = both(-a.m), c2 = both(c);
+        float2 s = both(0.f), w = both(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u < have) {
-                float f[VEC];
-                unpack(v[u], f);
+                float2 f[VEC / 2];
+                unpack_pairs(raised(v[u], low), f);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float d = (fmaxf(f[e], low) - a.m) * c, x = ex2(d);
-                    a.s += x;
-                    a.w = fmaf(x, d, a.w);
+                for (int e = 0; e < VEC / 2; ++e) {
+                    const float2 d = mul2(add2(f[e], minus_m), c2), x = make_float2(ex2(d.x), ex2(d.y));
+                    s = add2(s, x);
+                    w = fma2(x, d, w);
                 }
             }
         }
+        a.s += s.x + s.y;
+        a.w += w.x + w.y;
     } else {
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -394,7 +434,7 @@ struct LogprobBackArgs {
 
 constexpr int BACK_U = 2;
 
-template <typename T>
+template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBackArgs A) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ int32_t special[MAX_TOP + 1];
@@ -420,17 +460,19 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBa
     const float g_logp = counted && A.d_logp ? A.d_logp[row] : 0.f;
     float sum = g_logp;
     for (int i = 0; i < A.top; ++i) sum += A.d_top[row * A.top + i];
-    const float g_h = A.d_entropy ? A.d_entropy[row] : 0.f;
+    const float g_h = ENTROPY ? A.d_entropy[row] : 0.f;
     const float lse = A.lse[row];
-    const bool none = lse == NEG_INF;                     // an empty row: p = 0 everywhere
-    const float h = A.d_entropy ? A.entropy[row] : 0.f;
+    const float minus_lse = lse == NEG_INF ? NEG_INF : -lse;   // of an empty row: p = 0 everywhere
+    const float h = ENTROPY ? A.entropy[row] : 0.f;
     const float scale = A.scale;
     const float base = -scale * fmaf(g_h, h, sum), slope = -scale * g_h;
-    // gradient of one logit without the columns' own terms: p (base + slope log p)
-    auto grad = [&](float x) {
-        const float logp = none ? NEG_INF : fmaf(x, scale, -lse);
-        const float p = ex2(logp * LOG2E);
-        return A.d_entropy ? p * fmaf(slope, fmaxf(logp, -200.f), base) : p * base;
+    // gradient of two logits without the columns' own terms: p (base + slope log p)
+    auto grad = [&](float2 x) {
+        float2 logp = fma2(x, both(scale), both(minus_lse));
+        const float2 t = mul2(logp, both(LOG2E)), p = make_float2(ex2(t.x), ex2(t.y));
+        if (!ENTROPY) return mul2(p, both(base));
+        logp = make_float2(fmaxf(logp.x, -200.f), fmaxf(logp.y, -200.f));
+        return mul2(p, fma2(logp, both(slope), both(base)));
     };
     // the columns with a term of their own that this CTA writes
     const int nspecial = A.top + (counted ? 1 : 0);
@@ -452,19 +494,19 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBa
             if (i < G.count) {
                 const int32_t at = G.first(i);
                 if (G.whole(i)) {
-                    float f[VEC];
-                    unpack(v[u], f);
+                    float2 f[VEC / 2];
+                    unpack_pairs(v[u], f);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) f[e] = grad(f[e]);
-                    store_vec<T, VEC>(out + at, pack<T, VEC>(f));
+                    for (int e = 0; e < VEC / 2; ++e) f[e] = grad(f[e]);
+                    store_vec<T, VEC>(out + at, pack_pairs<T, VEC>(f));
                 } else {
                     for (int e = 0; e < VEC; ++e)
-                        if (at + e >= 0 && at + e < A.vocab) out[at + e] = from_f32<T>(grad(to_f32(z[at + e])));
+                        if (at + e >= 0 && at + e < A.vocab) out[at + e] = from_f32<T>(grad(both(to_f32(z[at + e]))).x);
                 }
             }
         }
     } else {
-        for (int32_t j = lo + t; j < hi; j += THREADS) out[j] = from_f32<T>(grad(to_f32(z[j])));
+        for (int32_t j = lo + t; j < hi; j += THREADS) out[j] = from_f32<T>(grad(both(to_f32(z[j]))).x);
     }
     if (nspecial == 0) return;                            // the same for the whole CTA
     __syncthreads();
@@ -472,7 +514,7 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBa
         float own = 0.f;
         for (int i = 0; i < nspecial; ++i)
             if (special[i] == col) own += extra[i];
-        out[col] = from_f32<T>(fmaf(scale, own, grad(z_fix)));
+        out[col] = from_f32<T>(fmaf(scale, own, grad(both(z_fix)).x));
     }
 }
 
@@ -508,7 +550,8 @@ int launch_logprobs_back(LogprobBackArgs A, cudaStream_t st) {
     constexpr int VEC = 16 / sizeof(T);
     A.chunks = (A.vocab + 2 * VEC - 2 + THREADS * BACK_U * VEC - 1) / (THREADS * BACK_U * VEC);   // whatever the phase
     if (A.rows * A.chunks > 0x7fffffff) return SSGD_EINVAL;
-    k_token_logprobs_back<T><<<(unsigned)(A.rows * A.chunks), THREADS, 0, st>>>(A);
+    if (A.d_entropy) k_token_logprobs_back<T, true><<<(unsigned)(A.rows * A.chunks), THREADS, 0, st>>>(A);
+    else k_token_logprobs_back<T, false><<<(unsigned)(A.rows * A.chunks), THREADS, 0, st>>>(A);
     return launched();
 }
 
