@@ -359,7 +359,7 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
  *                                   index (NaN counts as the largest), and their log probabilities
  * ids: [rows] of 4 or 8 bytes each (ids_bytes).  An id outside [0, vocab) is ignored: its logp is 0 and has no gradient.
  * A logit of -inf has probability 0.  A row of nothing else has lse = -inf, entropy 0, every log probability -inf and
- * the gradient 0.  A NaN or +inf makes its row's statistics NaN.  1 <= vocab <= 2^30. */
+ * the gradient 0.  A NaN or +inf makes its row's statistics NaN.  1 <= vocab <= 2^27. */
 #define SSGD_MAX_TOP 32
 int ssgd_token_logprobs(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes, int64_t rows,
                         int64_t vocab, float scale, int32_t top, float* stats, int32_t* top_idx, float* top_logp,

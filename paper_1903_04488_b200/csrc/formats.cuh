@@ -130,6 +130,35 @@ __device__ __forceinline__ Vec<T, VEC> pack_pairs(const float2 (&f)[PAIRS<VEC>])
     return v;
 }
 
+// Largest over the warp, NaN if any lane has one
+__device__ __forceinline__ float warp_max_nan(float x) {
+    float y;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+// BYTES (4, 8 or 16, both sides aligned to it) on their way from global to shared memory while the thread goes on.  A
+// thread that reads only what it has copied itself needs no barrier: the wait below is enough.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* shared, const void* global) {
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(shared);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(global) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(global), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most N of this thread's committed groups are still on their way
+template <int N>
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Programmatic dependent launch: a kernel launched with launch_after may start while its predecessor in the stream drains; it
+// sees what that wrote once successor_wait has returned.
+__device__ __forceinline__ void successor_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void successor_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Host side -----------------------------------------------------------------------------------------
 
 inline int fmt_bytes(int32_t fmt) {
@@ -150,6 +179,20 @@ inline int sm_count_of_current_device(int* out) {
     }
     *out = known[dev];
     return SSGD_OK;
+}
+
+template <typename... P, typename... A>
+int launch_after(cudaStream_t st, void (*kernel)(P...), dim3 grid, int block, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
 }
 
 inline int launched() { return cudaGetLastError() == cudaSuccess ? SSGD_OK : SSGD_ECUDA; }

@@ -7,6 +7,8 @@
 // Both are bound by HBM: two streams of rows x n elements forward, three backward, a dozen operations per element.
 // So a row is read once and stays in registers (in its own format) from the first sum to the result: the variance is
 // the mean of squared deviations from the mean already known, not a difference of large sums.
+#include <algorithm>
+
 #include "formats.cuh"
 
 using namespace ssgd;
@@ -20,12 +22,6 @@ template <int G> struct GroupShape {
     static constexpr int ROWS = BLOCK / G;
     static constexpr int WARPS = G / 32;
 };
-
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
 
 // Sum over the group, known to every thread of it.  `slot` [WARPS] is not used again before the next barrier but one.
 template <int G>
@@ -178,108 +174,203 @@ struct NormBackArgs {
     float* row_sums;     // wide rows: [rows][2]
 };
 
-// h = (x - mean) rstd and a = dy w of one vector, and what it adds to the four sums
-template <int P>
-struct BackTerms { float2 h[P], a[P]; };
+// What a vector adds to the row's two sums (of a and a h) and to the columns' sums over the rows
 template <typename T, int VEC>
-__device__ __forceinline__ BackTerms<PAIRS<VEC>> back_terms(const Vec<T, VEC>& x, const Vec<T, VEC>& dy, const float2 (&w)[PAIRS<VEC>],
-                                                            float2 minus_mean, float2 rstd, float2& c1, float2& c2,
-                                                            float2* dw, float2* db) {
-    BackTerms<PAIRS<VEC>> r;
-    float2 d[PAIRS<VEC>];
-    unpack_pairs(x, r.h);
+__device__ __forceinline__ void back_sums(const Vec<T, VEC>& x, const Vec<T, VEC>& dy, const float2 (&w)[PAIRS<VEC>], float2 minus_mean,
+                                          float2 rstd, float2& c1, float2& c2, float2* dw, float2* db) {
+    float2 h[PAIRS<VEC>], d[PAIRS<VEC>];
+    unpack_pairs(x, h);
     unpack_pairs(dy, d);
 #pragma unroll
     for (int i = 0; i < PAIRS<VEC>; ++i) {
-        r.h[i] = mul2(add2(r.h[i], minus_mean), rstd);
-        r.a[i] = mul2(d[i], w[i]);
-        c1 = add2(c1, r.a[i]);
-        c2 = fma2(r.a[i], r.h[i], c2);
+        h[i] = mul2(add2(h[i], minus_mean), rstd);
+        const float2 a = mul2(d[i], w[i]);
+        c1 = add2(c1, a);
+        c2 = fma2(a, h[i], c2);
         if (dw) {
-            dw[i] = fma2(d[i], r.h[i], dw[i]);
+            dw[i] = fma2(d[i], h[i], dw[i]);
             db[i] = add2(db[i], d[i]);
         }
     }
-    return r;
 }
-// dx = rstd a - rstd c1 - h (rstd c2)
+// dx = rstd (dy w - c1 - (x - mean) (rstd c2))
 template <typename T, int VEC>
-__device__ __forceinline__ Vec<T, VEC> back_result(const BackTerms<PAIRS<VEC>>& r, float2 rstd, float2 minus_c1, float2 minus_c2) {
-    float2 f[PAIRS<VEC>];
+__device__ __forceinline__ Vec<T, VEC> back_result(const Vec<T, VEC>& x, const Vec<T, VEC>& dy, const float2 (&w)[PAIRS<VEC>],
+                                                   float2 minus_mean, float2 rstd, float2 minus_c1, float2 minus_c2) {
+    float2 f[PAIRS<VEC>], d[PAIRS<VEC>];
+    unpack_pairs(x, f);
+    unpack_pairs(dy, d);
+    const float2 k = mul2(minus_c2, rstd);
 #pragma unroll
-    for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = mul2(fma2(r.h[i], minus_c2, add2(r.a[i], minus_c1)), rstd);
+    for (int i = 0; i < PAIRS<VEC>; ++i)
+        f[i] = mul2(fma2(add2(f[i], minus_mean), k, fma2(d[i], w[i], minus_c1)), rstd);
     return pack_pairs<T, VEC>(f);
 }
 
-template <typename T, int VEC, int G, int E>
-__global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_back(const NormBackArgs A) {
-    constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS, P = PAIRS<VEC>;
-    extern __shared__ float smem[];                    // G = 32: [8][2][n] partial sums at the end
-    __shared__ float2 slot[2][32];
-    const int t = threadIdx.x % G, sub = threadIdx.x / G;
+// Sums of V values (a power of two up to 8) over the warp at once: in each of the first steps a lane hands half of its values
+// to its partner and goes on with the other half.  Value i ends up in the lanes l with l / (32 / V) = i.
+template <int V>
+__device__ __forceinline__ float warp_sums(float (&v)[V]) {
+    const int lane = threadIdx.x & 31;
+    int o = 16;
+#pragma unroll
+    for (int half = V / 2; half > 0; half >>= 1, o >>= 1) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const float keep = upper ? v[i + half] : v[i], give = upper ? v[i] : v[i + half];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    float x = v[0];
+#pragma unroll
+    for (; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// R rows at a time: the latency of their sums' way through the warps and the block is paid once for all of them.  The next R
+// rows are on their way into shared memory meanwhile; a thread copies what it will read itself.  (Vectors of 2 bytes
+// cannot be copied this way: they are read when they are needed.)
+//
+// Measured at 16384 x 4096 in bfloat16 (us, rows at a time x blocks per SM): 1 x 2 85.9, 2 x 2 80.9, 4 x 2 (128 registers: spills)
+// 81.2, 4 x 1 73.8.  Without the ring, the next row in registers: 88.6; the rows ahead asked into L2: 86.
+constexpr int STAGES = 2;
+template <int G> constexpr int ROWS_AT_ONCE = G < 512 ? 4 : 2;     // what the ring's shared memory allows
+template <typename T, int VEC> constexpr bool STAGED = sizeof(T) * VEC >= 4;
+template <typename T, int VEC, int G, int E, int R> constexpr size_t RING_BYTES =
+    STAGED<T, VEC> ? (size_t)STAGES * R * 2 * E * sizeof(T) * GroupShape<G>::BLOCK : 0;
+
+// FULL: every thread has E elements (n = G E), so no column needs a check.
+template <typename T, int VEC, int G, int E, int R, bool FULL>
+__global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 256 ? 2 : 1) k_layer_norm_back(const NormBackArgs A) {
+    constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS, P = PAIRS<VEC>, NW = GroupShape<G>::WARPS, BLOCK = GroupShape<G>::BLOCK;
+    constexpr bool RING = STAGED<T, VEC>;
+    extern __shared__ __align__(16) float smem[];      // the ring; G = 32: [8][2][n] partial sums at the end
+    __shared__ __align__(16) float slot[2][NW][2 * R];
+    const int t = threadIdx.x % G, sub = threadIdx.x / G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int nv = A.n / VEC;
     const float inv_n = 1.0f / (float)A.n;
+    auto mine_here = [&](int j) { return FULL || t + j * G < nv; };
     float2 dw[NV][P], db[NV][P], w[NV][P];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
         for (int i = 0; i < P; ++i) { dw[j][i] = db[j][i] = both(0.f); w[j][i] = both(1.f); }
-        if (A.w && t + j * G < nv) load_param<T, VEC>(A.w, A.w_f32, (t + j * G) * VEC, w[j]);
+        if (A.w && mine_here(j)) load_param<T, VEC>(A.w, A.w_f32, (t + j * G) * VEC, w[j]);
     }
-    // the next row's vectors are on their way while this row is summed and written
-    Vec<T, VEC> vx[NV], vd[NV];
-    float mean = 0.f, rstd = 0.f;
-    const int64_t step = (int64_t)gridDim.x * ROWS;
-    int64_t row = (int64_t)blockIdx.x * ROWS + sub;
-    auto fetch = [&](int64_t r) {
-        const T* x = static_cast<const T*>(A.x) + r * A.ld_x;
-        const T* d = static_cast<const T*>(A.dy) + r * A.ld_dy;
+    const int64_t step = (int64_t)gridDim.x * ROWS * R;
+    int64_t row = ((int64_t)blockIdx.x * ROWS + sub) * R;
+    // this thread's part of the rows in work: dx and (RING: of the rows to be sent next, else of those in work) x, dy
+    const T* x = static_cast<const T*>(A.x) + t * VEC + row * A.ld_x;
+    const T* dy = static_cast<const T*>(A.dy) + t * VEC + row * A.ld_dy;
+    T* dx = static_cast<T*>(A.dx) + t * VEC + row * A.ld_dx;
+    Vec<T, VEC>* ring = reinterpret_cast<Vec<T, VEC>*>(smem) + threadIdx.x;      // [stage][row][x, dy][j], BLOCK apart
+    auto place = [&](int stage, int k, int which, int j) { return ring + (((stage * R + k) * 2 + which) * NV + j) * BLOCK; };
+    auto send = [&](int64_t r, int stage) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = t + j * G;
-            if (i < nv) {
-                vx[j] = load_vec_stream<T, VEC>(x + (int64_t)i * VEC);
-                vd[j] = load_vec_stream<T, VEC>(d + (int64_t)i * VEC);
+        for (int k = 0; k < R; ++k) {
+            if (r + k < A.rows) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    if (mine_here(j)) {
+                        copy_async<sizeof(T) * VEC>(place(stage, k, 0, j), x + k * A.ld_x + j * G * VEC);
+                        copy_async<sizeof(T) * VEC>(place(stage, k, 1, j), dy + k * A.ld_dy + j * G * VEC);
+                    }
+                }
             }
         }
-        mean = A.stats[r];
-        rstd = A.stats[A.rows + r];
+        x += step * A.ld_x;
+        dy += step * A.ld_dy;
+        copy_async_commit();
     };
-    if (row < A.rows) fetch(row);
-    int turn = 0;
-    for (; row < A.rows; row += step) {
-        float2 c1 = both(0.f), c2 = both(0.f);
-        BackTerms<P> r[NV];
-        const float2 scale = both(rstd);
+    auto read_x = [&](int stage, int k, int j) {
+        if constexpr (RING) return *place(stage, k, 0, j);
+        else return load_vec<T, VEC>(x + k * A.ld_x + j * G * VEC);
+    };
+    auto read_dy = [&](int stage, int k, int j) {
+        if constexpr (RING) return *place(stage, k, 1, j);
+        else return load_vec<T, VEC>(dy + k * A.ld_dy + j * G * VEC);
+    };
+    if constexpr (RING) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (t + j * G < nv) r[j] = back_terms<T, VEC>(vx[j], vd[j], w[j], both(-mean), scale, c1, c2, dw[j], db[j]);
-        if (row + step < A.rows) fetch(row + step);
-        float s1 = warp_sum(c1.x + c1.y), s2 = warp_sum(c2.x + c2.y);
-        if constexpr (G > 32) {
-            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-            constexpr int NW = GroupShape<G>::WARPS;
-            if (lane == 0) slot[turn][warp] = make_float2(s1, s2);
+        for (int s = 0; s < STAGES - 1; ++s) send(row + s * step, s);
+    }
+    float next_mean[R], next_rstd[R];
+    auto next_stats = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            next_mean[k] = r + k < A.rows ? A.stats[r + k] : 0.f;
+            next_rstd[k] = r + k < A.rows ? A.stats[A.rows + r + k] : 0.f;
+        }
+    };
+    next_stats(row);
+    int turn = 0, stage = 0;
+    // R rows, all of them there (ALL) or not
+    auto rows_in_work = [&](auto all, int have) {
+        constexpr bool ALL = decltype(all)::value;
+        float2 minus_mean[R], rstd[R];
+        float sums[2 * R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) { minus_mean[k] = both(-next_mean[k]); rstd[k] = both(next_rstd[k]); }
+        next_stats(row + step);
+        if constexpr (RING) {
+            send(row + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+            copy_async_wait<STAGES - 1>();
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            float2 c1 = both(0.f), c2 = both(0.f);
+            if (ALL || k < have) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (mine_here(j))
+                        back_sums<T, VEC>(read_x(stage, k, j), read_dy(stage, k, j), w[j], minus_mean[k], rstd[k], c1, c2, dw[j], db[j]);
+            }
+            sums[2 * k] = c1.x + c1.y;
+            sums[2 * k + 1] = c2.x + c2.y;
+        }
+        const float mine = warp_sums<2 * R>(sums);
+        constexpr int SPREAD = 32 / (2 * R);
+        if constexpr (G == 32) {
+#pragma unroll
+            for (int i = 0; i < 2 * R; ++i) sums[i] = __shfl_sync(0xffffffffu, mine, i * SPREAD);
+        } else {
+            if (lane % SPREAD == 0) slot[turn][warp][lane / SPREAD] = mine;
             __syncthreads();
-            float2 p = lane < NW ? slot[turn][lane] : both(0.f);
+            float2 total[R];
 #pragma unroll
-            for (int o = NW / 2; o > 0; o >>= 1)
-                p = add2(p, make_float2(__shfl_xor_sync(0xffffffffu, p.x, o), __shfl_xor_sync(0xffffffffu, p.y, o)));
-            s1 = __shfl_sync(0xffffffffu, p.x, 0);
-            s2 = __shfl_sync(0xffffffffu, p.y, 0);
+            for (int k = 0; k < R; ++k) total[k] = both(0.f);
+#pragma unroll
+            for (int q = 0; q < NW; ++q)
+#pragma unroll
+                for (int k = 0; k < R; ++k) total[k] = add2(total[k], *reinterpret_cast<const float2*>(&slot[turn][q][2 * k]));
+#pragma unroll
+            for (int k = 0; k < R; ++k) { sums[2 * k] = total[k].x; sums[2 * k + 1] = total[k].y; }
             turn ^= 1;
         }
-        T* dx = static_cast<T*>(A.dx) + row * A.ld_dx;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int i = t + j * G;
-            if (i < nv)
-                store_vec<T, VEC>(dx + (int64_t)i * VEC, back_result<T, VEC>(r[j], scale, both(-s1 * inv_n), both(-s2 * inv_n)));
+        for (int k = 0; k < R; ++k) {
+            if (ALL || k < have) {
+                const float2 m1 = both(-sums[2 * k] * inv_n), m2 = both(-sums[2 * k + 1] * inv_n);
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (mine_here(j))
+                        store_vec<T, VEC>(dx + k * A.ld_dx + j * G * VEC,
+                                          back_result<T, VEC>(read_x(stage, k, j), read_dy(stage, k, j), w[j], minus_mean[k], rstd[k], m1, m2));
+            }
         }
-    }
+        dx += step * A.ld_dx;
+        if constexpr (!RING) { x += step * A.ld_x; dy += step * A.ld_dy; }
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+    };
+    for (; row + R <= A.rows; row += step) rows_in_work(std::true_type{}, R);
+    if (R > 1 && row < A.rows) rows_in_work(std::false_type{}, (int)(A.rows - row));
+    if constexpr (RING) copy_async_wait<0>();
+    successor_may_start();                             // k_norm_reduce waits for the partial sums by itself
     if (!A.partial) return;
     float* out = A.partial + (int64_t)blockIdx.x * 2 * A.n;
     float* mine = G == 32 ? smem + (int64_t)sub * 2 * A.n : out;
+    if (G == 32) __syncthreads();                      // every warp is done with the ring
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = t + j * G;
@@ -292,7 +383,7 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_back(const 
         }
     }
     if constexpr (G == 32) {
-        // the block's 8 warps add up in shared memory first
+        // the block's 8 warps add up in shared memory
         __syncthreads();
         for (int c = threadIdx.x; c < 2 * A.n; c += GroupShape<G>::BLOCK) {
             float s = 0.f;
@@ -318,7 +409,7 @@ __global__ void __launch_bounds__(WIDE) k_norm_back_sums(const NormBackArgs A) {
 #pragma unroll
         for (int k = 0; k < PAIRS<VEC>; ++k) w[k] = both(1.f);
         if (A.w) load_param<T, VEC>(A.w, A.w_f32, i * VEC, w);
-        back_terms<T, VEC>(load_vec<T, VEC>(x + (int64_t)i * VEC), load_vec<T, VEC>(d + (int64_t)i * VEC), w, minus_mean, rstd, c1, c2,
+        back_sums<T, VEC>(load_vec<T, VEC>(x + (int64_t)i * VEC), load_vec<T, VEC>(d + (int64_t)i * VEC), w, minus_mean, rstd, c1, c2,
                            nullptr, nullptr);
     }
     const float s1 = group_sum<WIDE>(c1.x + c1.y, slot[0]), s2 = group_sum<WIDE>(c2.x + c2.y, slot[1]);
@@ -341,13 +432,12 @@ __global__ void __launch_bounds__(256) k_norm_back_slab(const NormBackArgs A) {
     if (A.w) load_param<T, VEC>(A.w, A.w_f32, (int)col, w);
     for (int64_t row = blockIdx.y; row < A.rows; row += gridDim.y) {
         float2 c1 = both(0.f), c2 = both(0.f);
-        const float2 rstd = both(A.stats[A.rows + row]);
-        const BackTerms<P> r =
-            back_terms<T, VEC>(load_vec_stream<T, VEC>(static_cast<const T*>(A.x) + row * A.ld_x + col),
-                               load_vec_stream<T, VEC>(static_cast<const T*>(A.dy) + row * A.ld_dy + col), w,
-                               both(-A.stats[row]), rstd, c1, c2, dw, db);
+        const float2 minus_mean = both(-A.stats[row]), rstd = both(A.stats[A.rows + row]);
+        const Vec<T, VEC> vx = load_vec_stream<T, VEC>(static_cast<const T*>(A.x) + row * A.ld_x + col);
+        const Vec<T, VEC> vd = load_vec_stream<T, VEC>(static_cast<const T*>(A.dy) + row * A.ld_dy + col);
+        back_sums<T, VEC>(vx, vd, w, minus_mean, rstd, c1, c2, dw, db);
         store_vec<T, VEC>(static_cast<T*>(A.dx) + row * A.ld_dx + col,
-                          back_result<T, VEC>(r, rstd, both(-A.row_sums[2 * row]), both(-A.row_sums[2 * row + 1])));
+                          back_result<T, VEC>(vx, vd, w, minus_mean, rstd, both(-A.row_sums[2 * row]), both(-A.row_sums[2 * row + 1])));
     }
     if (!A.partial) return;
     float* out = A.partial + (int64_t)blockIdx.y * 2 * A.n;
@@ -359,13 +449,14 @@ __global__ void __launch_bounds__(256) k_norm_back_slab(const NormBackArgs A) {
 }
 
 // dw[c], db[c] = sum over the blocks' partials, in a fixed order: 32 columns per block, its warps share the partials.
-constexpr int REDUCE_WARPS = 16;
+constexpr int REDUCE_WARPS = 32;
 __global__ void __launch_bounds__(REDUCE_WARPS * 32) k_norm_reduce(const float* partial, int parts, int n, float* dw, float* db,
                                                                    int accumulate) {
     __shared__ float s[REDUCE_WARPS][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;              // 0 .. 2n - 1
     float a = 0.f;
+    successor_wait();
     if (c < 2 * n) {
 #pragma unroll 8
         for (int p = warp; p < parts; p += REDUCE_WARPS) a += partial[(int64_t)p * 2 * n + c];
@@ -440,15 +531,21 @@ int launch_norm_back(const NormBackArgs& A, int sms, int* parts, cudaStream_t st
     int64_t grid = 0;
 #define NORM_BACK(G, E)                                                                                             \
     do {                                                                                                            \
-        const size_t smem = G == 32 && A.partial ? (size_t)GroupShape<G>::ROWS * 2 * n * 4 : 0;                     \
-        int per_sm = 0;                                                                                             \
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_layer_norm_back<T, VEC, G, E>,                 \
-                                                          GroupShape<G>::BLOCK, smem) != cudaSuccess || per_sm < 1) \
+        constexpr int R = ROWS_AT_ONCE<G>;                                                                          \
+        constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
+        auto kernel = WIDEST && n == G * E ? k_layer_norm_back<T, VEC, G, E, R, WIDEST> : k_layer_norm_back<T, VEC, G, E, R, false>; \
+        constexpr int TILE = GroupShape<G>::ROWS * R;                                                               \
+        size_t smem = RING_BYTES<T, VEC, G, E, R>;                                                                  \
+        if (G == 32) smem = std::max(smem, (size_t)GroupShape<G>::ROWS * 2 * n * 4);                                \
+        if (smem > 40 * 1024 &&                                                                                     \
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)    \
             return SSGD_ECUDA;                                                                                      \
-        grid = (A.rows + GroupShape<G>::ROWS - 1) / GroupShape<G>::ROWS;                                            \
-        if (grid > (int64_t)sms * per_sm) grid = (int64_t)sms * per_sm;                                             \
-        if (grid > PART_BLOCKS) grid = PART_BLOCKS;                                                                 \
-        k_layer_norm_back<T, VEC, G, E><<<(unsigned)grid, GroupShape<G>::BLOCK, smem, st>>>(A);                     \
+        int per_sm = 0;                                                                                             \
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, GroupShape<G>::BLOCK, smem) != cudaSuccess || \
+            per_sm < 1)                                                                                             \
+            return SSGD_ECUDA;                                                                                      \
+        grid = std::min({(A.rows + TILE - 1) / TILE, (int64_t)sms * per_sm, PART_BLOCKS});                          \
+        kernel<<<(unsigned)grid, GroupShape<G>::BLOCK, smem, st>>>(A);                                              \
         *parts = (int)grid;                                                                                         \
         return launched();                                                                                          \
     } while (0)
@@ -549,8 +646,8 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
     int parts = 0;
     e = BY_FORMAT(launch_norm_back, fmt_x, vec, A, sms, &parts, st);
     if (e || !A.partial) return e;
-    k_norm_reduce<<<(unsigned)((2 * n + 31) / 32), REDUCE_WARPS * 32, 0, st>>>(A.partial, parts, (int)n, dw, db, accumulate);
-    return launched();
+    return launch_after(st, k_norm_reduce, dim3((unsigned)((2 * n + 31) / 32)), REDUCE_WARPS * 32, A.partial, parts, (int)n, dw, db,
+                        accumulate);
 }
 
 }  // extern "C"

@@ -77,18 +77,12 @@ __device__ __forceinline__ void add_careful(Sums& a, float z, float c) {
     if (e > 0.f || e != e) a.w = fmaf(e, d, a.w);
 }
 
-// b joins a (another thread's or another CTA's part of the row)
-__device__ __forceinline__ void join(Sums& a, Sums b, float c) {
-    const float m = max_nan(a.m, b.m);
+// The sums of all lanes, relative to their common maximum, in every lane
+__device__ __forceinline__ void join_warp(Sums& a, float c) {
+    const float m = warp_max_nan(a.m);
     if (!(m == a.m)) rebase(a, m, c);
-    if (!(m == b.m)) rebase(b, m, c);
-    a.s += b.s;
-    a.w += b.w;
-}
-
-__device__ __forceinline__ Sums shuffle_xor(const Sums& a, int o) {
-    return Sums{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o),
-                __shfl_xor_sync(0xffffffffu, a.w, o)};
+    a.s = warp_sum(a.s);
+    a.w = warp_sum(a.w);
 }
 
 // Sort keys: larger key = earlier.  Upper half the logit's order, lower half the index inverted; 0 = no entry.
@@ -269,8 +263,7 @@ __device__ __forceinline__ uint32_t sort32(uint32_t x) {
 }
 
 struct Shared {
-    Sums part[WARPS];
-    Sums total;                       // this CTA's part of the row
+    Sums part[WARPS];                 // part[0] is the CTA's in the end
     uint64_t list[WARPS][MAX_TOP];    // list[0] is the CTA's in the end
     uint32_t bound[WARPS];
     int32_t picked[THREADS];
@@ -346,24 +339,33 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs(const LogprobArgs A,
     constexpr int VEC = 16 / sizeof(T), U = 4;
     __shared__ Shared sh;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const int64_t row = (int64_t)blockIdx.x / split;
-    const int part = blockIdx.x % split;
+    // split is a power of two
+    const int shift = __ffs(split) - 1, part = blockIdx.x & (split - 1);
+    const int64_t row = blockIdx.x >> shift;
     const T* z = static_cast<const T*>(A.logits) + row * A.ld;
     const Granules<T> G(z, A.vocab);
-    const int32_t per = (G.count + split - 1) / split;
+    const int32_t per = (G.count + split - 1) >> shift;
     const int32_t g0 = min(part * per, G.count), g1 = min(g0 + per, G.count);
     const float c = A.scale * LOG2E;
     int64_t id = -1;
     if (part == 0 && t == 0) id = id_of(A.ids, A.ids64, row);
     Sums a{NEG_INF, 0.f, 0.f};
     float low = NEG_INF;
+    const int32_t whole0 = G.phase ? 1 : 0, whole1 = G.whole(G.count - 1) ? G.count : G.count - 1;
     for (int32_t b0 = g0; b0 < g1; b0 += THREADS * U) {
         Vec<T, VEC> v[U];
+        if (b0 >= whole0 && b0 + THREADS * U <= min(whole1, g1)) {
+            const T* p = z + G.first(b0 + t);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_vec_stream<T, VEC>(p + u * (THREADS * VEC));
+            add_granules<T, U>(a, low, v, U, c);
+            continue;
+        }
         const int have = (g1 - b0 + THREADS - 1) / THREADS;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t i = b0 + u * THREADS + t, at = G.first(i);
-            if (i < g1 && G.whole(i)) {
+            if (i >= whole0 && i < min(whole1, g1)) {
                 v[u] = load_vec_stream<T, VEC>(z + at);
             } else {
 #pragma unroll
@@ -381,21 +383,23 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs(const LogprobArgs A,
     float z_id = 0.f;
     if (counted) z_id = to_f32(z[id]);
     // join: warp, CTA, cluster
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) join(a, shuffle_xor(a, o), c);
+    join_warp(a, c);
     if (lane == 0) sh.part[warp] = a;
     if (TOP) best_of_segment<T>(sh, G, g0, g1, thread_max, has, A.top);
     __syncthreads();
-    if (t == 0) {
-        for (int i = 1; i < WARPS; ++i) join(a, sh.part[i], c);
-        sh.total = a;
+    if (warp == 0) {
+        a = lane < WARPS ? sh.part[lane] : Sums{NEG_INF, 0.f, 0.f};
+        join_warp(a, c);
+        __syncwarp();
+        if (lane == 0) sh.part[0] = a;
     }
     cg::cluster_group cluster = cg::this_cluster();
     if (split > 1) cluster.sync();
-    else __syncthreads();
     if (part == 0 && warp == 0) {
-        a = sh.total;
-        for (int i = 1; i < split; ++i) join(a, *cluster.map_shared_rank(&sh.total, i), c);
+        if (split > 1) {
+            a = lane < split ? *cluster.map_shared_rank(&sh.part[0], lane < split ? lane : 0) : Sums{NEG_INF, 0.f, 0.f};
+            join_warp(a, c);
+        }
         const float log2s = log2f(a.s);
         const bool none = a.s == 0.f;                      // every logit is -inf
         auto logp_of = [&](float x) {
@@ -423,7 +427,8 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs(const LogprobArgs A,
 struct LogprobBackArgs {
     const void* logits; int64_t ld;
     const void* ids; bool ids64;
-    int64_t rows; int32_t vocab; int32_t chunks;
+    int64_t rows; int32_t vocab;
+    int32_t per;           // granules per CTA, a multiple of THREADS
     float scale;
     const float* lse; const float* entropy;
     const float* d_logp; const float* d_entropy;      // either may be NULL
@@ -432,28 +437,21 @@ struct LogprobBackArgs {
     bool same_phase;       // rows of logits and of the result lie alike within 16 bytes
 };
 
-constexpr int BACK_U = 2;
+constexpr int BACK_U = 4;
 
+// CTA (row, part) writes `per` granules of a row.
 template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBackArgs A) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ int32_t special[MAX_TOP + 1];
     __shared__ float extra[MAX_TOP + 1];
     const int t = threadIdx.x;
-    const int64_t row = (int64_t)blockIdx.x / A.chunks;
-    const int chunk = blockIdx.x % A.chunks;
+    const int64_t row = blockIdx.x;
     const T* z = static_cast<const T*>(A.logits) + row * A.ld;
     T* out = static_cast<T*>(A.out) + row * A.ld_out;
-    Granules<T> G(z, A.vocab);
-    const int32_t g0 = chunk * (THREADS * BACK_U);
-    Vec<T, VEC> v[BACK_U];
-    if (A.same_phase) {
-#pragma unroll
-        for (int u = 0; u < BACK_U; ++u) {
-            const int32_t i = g0 + u * THREADS + t;
-            if (i < G.count && G.whole(i)) v[u] = load_vec_stream<T, VEC>(z + G.first(i));
-        }
-    }
+    const Granules<T> G(z, A.vocab);
+    const int32_t g0 = (int32_t)blockIdx.y * A.per, g1 = min(g0 + A.per, G.count);
+    if (g0 >= g1) return;                                 // the last part, where the phase needs no further granule
     // the row's constants
     const int64_t id = A.ids ? id_of(A.ids, A.ids64, row) : -1;
     const bool counted = id >= 0 && id < A.vocab;
@@ -474,6 +472,7 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBa
         logp = make_float2(fmaxf(logp.x, -200.f), fmaxf(logp.y, -200.f));
         return mul2(p, fma2(logp, both(slope), both(base)));
     };
+    auto one = [&](float x) { return from_f32<T>(grad(both(x)).x); };
     // the columns with a term of their own that this CTA writes
     const int nspecial = A.top + (counted ? 1 : 0);
     int32_t col = -1;
@@ -482,31 +481,49 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBa
         special[t] = col;
         extra[t] = t < A.top ? A.d_top[row * A.top + t] : g_logp;
     }
-    const int32_t lo = max(g0 * VEC - G.phase, 0), hi = min((g0 + THREADS * BACK_U) * VEC - G.phase, A.vocab);
+    const int32_t lo = max(G.first(g0), 0), hi = min(G.first(g1), A.vocab);
     const bool fix = t < nspecial && col >= lo && col < hi;
     float z_fix = 0.f;
     if (fix) z_fix = to_f32(z[col]);                      // before the result, which may lie in the same place, is written
     __syncthreads();
     if (A.same_phase) {
+        const int32_t whole0 = G.phase ? 1 : 0, whole1 = min(G.whole(G.count - 1) ? G.count : G.count - 1, g1);
+        for (int32_t b0 = g0; b0 < g1; b0 += THREADS * BACK_U) {
+            const int32_t at = G.first(b0 + t);
+            Vec<T, VEC> v[BACK_U];
+            float2 f[VEC / 2];
+            if (b0 >= whole0 && b0 + THREADS * BACK_U <= whole1) {
 #pragma unroll
-        for (int u = 0; u < BACK_U; ++u) {
-            const int32_t i = g0 + u * THREADS + t;
-            if (i < G.count) {
-                const int32_t at = G.first(i);
-                if (G.whole(i)) {
-                    float2 f[VEC / 2];
+                for (int u = 0; u < BACK_U; ++u) v[u] = load_vec_stream<T, VEC>(z + at + u * (THREADS * VEC));
+#pragma unroll
+                for (int u = 0; u < BACK_U; ++u) {
                     unpack_pairs(v[u], f);
 #pragma unroll
                     for (int e = 0; e < VEC / 2; ++e) f[e] = grad(f[e]);
-                    store_vec<T, VEC>(out + at, pack_pairs<T, VEC>(f));
-                } else {
-                    for (int e = 0; e < VEC; ++e)
-                        if (at + e >= 0 && at + e < A.vocab) out[at + e] = from_f32<T>(grad(both(to_f32(z[at + e]))).x);
+                    store_vec<T, VEC>(out + at + u * (THREADS * VEC), pack_pairs<T, VEC>(f));
+                }
+                continue;
+            }
+#pragma unroll
+            for (int u = 0; u < BACK_U; ++u) {
+                const int32_t i = b0 + u * THREADS + t;
+                if (i >= whole0 && i < whole1) v[u] = load_vec_stream<T, VEC>(z + G.first(i));
+            }
+#pragma unroll
+            for (int u = 0; u < BACK_U; ++u) {
+                const int32_t i = b0 + u * THREADS + t;
+                if (i >= whole0 && i < whole1) {
+                    unpack_pairs(v[u], f);
+#pragma unroll
+                    for (int e = 0; e < VEC / 2; ++e) f[e] = grad(f[e]);
+                    store_vec<T, VEC>(out + G.first(i), pack_pairs<T, VEC>(f));
+                } else if (i < g1) {
+                    for (int32_t j = max(G.first(i), 0); j < min(G.first(i) + VEC, A.vocab); ++j) out[j] = one(to_f32(z[j]));
                 }
             }
         }
     } else {
-        for (int32_t j = lo + t; j < hi; j += THREADS) out[j] = from_f32<T>(grad(both(to_f32(z[j]))).x);
+        for (int32_t j = lo + t; j < hi; j += THREADS) out[j] = one(to_f32(z[j]));
     }
     if (nspecial == 0) return;                            // the same for the whole CTA
     __syncthreads();
@@ -546,16 +563,23 @@ int launch_logprobs(const LogprobArgs& A, int split, cudaStream_t st) {
 }
 
 template <typename T>
-int launch_logprobs_back(LogprobBackArgs A, cudaStream_t st) {
+int launch_logprobs_back(LogprobBackArgs A, int sms, cudaStream_t st) {
     constexpr int VEC = 16 / sizeof(T);
-    A.chunks = (A.vocab + 2 * VEC - 2 + THREADS * BACK_U * VEC - 1) / (THREADS * BACK_U * VEC);   // whatever the phase
-    if (A.rows * A.chunks > 0x7fffffff) return SSGD_EINVAL;
-    if (A.d_entropy) k_token_logprobs_back<T, true><<<(unsigned)(A.rows * A.chunks), THREADS, 0, st>>>(A);
-    else k_token_logprobs_back<T, false><<<(unsigned)(A.rows * A.chunks), THREADS, 0, st>>>(A);
+    const int64_t granules = (A.vocab + 2 * VEC - 2) / VEC;             // whatever the phase
+    // Whole batches per CTA, 4 of them where that still makes 8 CTAs per SM: the row's constants cost a CTA as much as
+    // a batch.
+    int64_t batches = 4;
+    while (batches > 1 && A.rows * ((granules + batches * THREADS * BACK_U - 1) / (batches * THREADS * BACK_U)) < 8 * sms) batches /= 2;
+    A.per = (int32_t)(batches * THREADS * BACK_U);
+    const int64_t parts = (granules + A.per - 1) / A.per;
+    if (parts > 65535) return SSGD_EINVAL;
+    const dim3 grid((unsigned)A.rows, (unsigned)parts);
+    if (A.d_entropy) k_token_logprobs_back<T, true><<<grid, THREADS, 0, st>>>(A);
+    else k_token_logprobs_back<T, false><<<grid, THREADS, 0, st>>>(A);
     return launched();
 }
 
-constexpr int64_t MAX_VOCAB = (int64_t)1 << 30;
+constexpr int64_t MAX_VOCAB = (int64_t)1 << 27;
 
 int check_logits(const void* logits, int64_t ld, int32_t fmt, int64_t rows, int64_t vocab, float scale, int32_t top) {
     if (rows < 0 || rows > 0x0fffffff || vocab < 1 || vocab > MAX_VOCAB || ld < vocab) return SSGD_EINVAL;
@@ -602,12 +626,14 @@ int ssgd_token_logprobs_backward(const void* logits, int64_t ld, int32_t fmt, co
     if (!aligned_to(ids, ids_bytes) || !aligned_to(dlogits, es) || !aligned_to(lse, 4) || !aligned_to(entropy, 4) ||
         !aligned_to(d_logp, 4) || !aligned_to(d_entropy, 4) || !aligned_to(top_idx, 4) || !aligned_to(d_top, 4))
         return SSGD_EALIGN;
+    int sms = 0;
+    if ((e = sm_count_of_current_device(&sms))) return e;
     LogprobBackArgs A{logits, ld, ids, ids_bytes == 8, rows, (int32_t)vocab, 0, scale, lse, entropy, d_logp, d_entropy,
                       top, top_idx, d_top, dlogits, ld_d, false};
     A.same_phase = addr(logits) % 16 == addr(dlogits) % 16 && (rows == 1 || (ld - ld_d) * es % 16 == 0);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return fmt == SSGD_FMT_F32 ? launch_logprobs_back<float>(A, st)
-         : fmt == SSGD_FMT_F16 ? launch_logprobs_back<__half>(A, st) : launch_logprobs_back<__nv_bfloat16>(A, st);
+    return fmt == SSGD_FMT_F32 ? launch_logprobs_back<float>(A, sms, st)
+         : fmt == SSGD_FMT_F16 ? launch_logprobs_back<__half>(A, sms, st) : launch_logprobs_back<__nv_bfloat16>(A, sms, st);
 }
 
 }  // extern "C"

@@ -10,6 +10,8 @@ of a call are on the current CUDA device.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import operator
 
 import numpy as np
 import torch
@@ -18,8 +20,9 @@ from . import ssgd as S
 
 _FMT = {torch.float32: S.FMT_F32, torch.float16: S.FMT_F16, torch.bfloat16: S.FMT_BF16}
 _ID_BYTES = {torch.int64: 8, torch.int32: 4}
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
-    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+# the current stream and device, without the objects that torch.cuda's functions make of them
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _chk(code: int, what: str) -> None:
@@ -31,9 +34,32 @@ def _device(t: torch.Tensor, name: str) -> int:
     if not t.is_cuda:
         raise TypeError(f"{name}: need a CUDA tensor")
     dev = t.get_device()
-    if dev != torch.cuda.current_device():
-        raise ValueError(f"{name}: on device {dev}, but the current device is {torch.cuda.current_device()}")
+    if dev != _current_device():
+        raise ValueError(f"{name}: on device {dev}, but the current device is {_current_device()}")
     return dev
+
+
+_PROTO: dict[int, torch.Tensor] = {}
+
+
+def _f32(dev: int, shape) -> torch.Tensor:
+    """An uninitialised float32 tensor (new_empty costs half of what torch.empty with a type and a device does)."""
+    proto = _PROTO.get(dev)
+    if proto is None:
+        proto = _PROTO[dev] = torch.empty(0, dtype=torch.float32, device=f"cuda:{dev}")
+    return proto.new_empty(shape)
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """An uninitialised contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(rows: int, n: int) -> int:
+    out = S._sz()
+    _chk(S.lib().ssgd_layer_norm_backward_workspace(rows, n, C.byref(out)), "ssgd_layer_norm_backward_workspace")
+    return out.value
 
 
 def _rows(t: torch.Tensor, name: str, dev: int | None = None) -> tuple[int, int, int]:
@@ -88,14 +114,14 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     wp = _flat(weight, param.dtype, n, "weight", dev) if weight is not None else None
     bp = _flat(bias, param.dtype, n, "bias", dev) if bias is not None else None
     if out is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = _like(x)
         ld_y = n
     else:
         if out.shape != x.shape or out.dtype != x.dtype:
             raise TypeError("out: need x's shape and type")
         y = out
         ld_y = _rows(out, "out", dev)[2]
-    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    stats = _f32(dev, (2, rows))
     _chk(S.lib().ssgd_layer_norm(x.data_ptr(), ld, fmt, wp, bp, fmt_w, rows, n, eps, y.data_ptr(), ld_y, stats.data_ptr(),
                                  _raw_stream(dev)), "ssgd_layer_norm")
     return y, stats
@@ -117,7 +143,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     fmt_w = fmt if weight is None else _format(weight, "weight")
     wp = _flat(weight, weight.dtype, n, "weight", dev) if weight is not None else None
     if dx is None:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = _like(x)
         ld_dx = n
     else:
         if dx.shape != x.shape or dx.dtype != x.dtype:
@@ -127,17 +153,15 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
         if accumulate and (dw is None or db is None):
             raise ValueError("accumulate: needs dw and db")
         if dw is None:
-            dw = torch.empty(n, dtype=torch.float32, device=x.device)
+            dw = _f32(dev, (n,))
         if db is None:
-            db = torch.empty(n, dtype=torch.float32, device=x.device)
-    lib = S.lib()
-    nbytes = S._sz()
-    _chk(lib.ssgd_layer_norm_backward_workspace(rows, n, C.byref(nbytes)), "ssgd_layer_norm_backward_workspace")
-    ws = torch.empty(nbytes.value, dtype=torch.uint8, device=x.device)
-    _chk(lib.ssgd_layer_norm_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ld, fmt, wp, fmt_w,
-                                      _flat(stats, torch.float32, 2 * rows, "stats", dev), rows, n, dx.data_ptr(), ld_dx,
-                                      _flat(dw, torch.float32, n, "dw", dev), _flat(db, torch.float32, n, "db", dev),
-                                      1 if accumulate else 0, ws.data_ptr(), nbytes.value, _raw_stream(dev)),
+            db = _f32(dev, (n,))
+    nbytes = _norm_workspace(rows, n)
+    ws = _f32(dev, (nbytes // 4,))
+    _chk(S.lib().ssgd_layer_norm_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ld, fmt, wp, fmt_w,
+                                          _flat(stats, torch.float32, 2 * rows, "stats", dev), rows, n, dx.data_ptr(), ld_dx,
+                                          _flat(dw, torch.float32, n, "dw", dev), _flat(db, torch.float32, n, "db", dev),
+                                          1 if accumulate else 0, ws.data_ptr(), nbytes, _raw_stream(dev)),
          "ssgd_layer_norm_backward")
     return dx, dw, db
 
@@ -177,11 +201,11 @@ def token_logprobs(logits: torch.Tensor, ids: torch.Tensor, *, top: int = 0, sca
     if id_bytes is None:
         raise TypeError("ids: need int64 or int32")
     ids_p = _flat(ids, ids.dtype, rows, "ids", dev)
-    stats = torch.empty((3, rows), dtype=torch.float32, device=logits.device)
+    stats = _f32(dev, (3, rows))
     top_idx = top_logp = None
     if top > 0:
         top_idx = torch.empty((rows, top), dtype=torch.int32, device=logits.device)
-        top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device)
+        top_logp = _f32(dev, (rows, top))
     _chk(S.lib().ssgd_token_logprobs(logits.data_ptr(), ld, fmt, ids_p, id_bytes, rows, vocab, scale, top, stats.data_ptr(),
                                      top_idx.data_ptr() if top > 0 else None, top_logp.data_ptr() if top > 0 else None,
                                      _raw_stream(dev)), "ssgd_token_logprobs")
@@ -212,7 +236,7 @@ def token_logprobs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.
             raise TypeError("top_idx: need [rows][top]")
         top = top_idx.shape[1]
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        out = _like(logits)
         ld_out = vocab
     else:
         if out.shape != logits.shape or out.dtype != logits.dtype:
@@ -231,6 +255,10 @@ def token_logprobs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.
 # ---- AdamW over many tensors -------------------------------------------------------------------------
 
 _P, _G, _M, _V, _MS, _VS, _COPY, _N = range(8)     # the fields of ssgd_adamw_tensor, 8 bytes each
+_dtype_of = operator.attrgetter("dtype")
+_is_none = functools.partial(operator.is_, None)
+_numel, _is_contiguous, _get_device, _data_ptr = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device,
+                                                  torch.Tensor.data_ptr)
 
 
 class AdamW:
@@ -276,8 +304,9 @@ class AdamW:
             raise TypeError("copies: bfloat16 or float16, and only of float32 params")
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.step_count = step_count
-        self._dev, self._sizes = dev, sizes
+        self._dev, self._sizes, self._sizes_u64 = dev, sizes, np.array(sizes, dtype=np.uint64)
         self._desc = np.zeros((len(params), 8), dtype=np.uint64)
+        self._desc_p = self._desc.ctypes.data
         self._desc[:, _N] = sizes
         columns = [(_P, params, dtype, sizes, "params"), (_M, self.m, sdtype, sizes, "m"), (_V, self.v, sdtype, sizes, "v")]
         if small:
@@ -298,27 +327,31 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError("grads: need one tensor per parameter")
         dev = self._dev
-        if dev != torch.cuda.current_device():
+        if dev != _current_device():
             raise ValueError(f"grads: the parameters are on device {dev}, which is not the current one")
         desc, sizes = self._desc, self._sizes
-        dtype = next((g.dtype for g in grads if g is not None), torch.float32)
+        skipped = any(map(_is_none, grads))
+        given = [g for g in grads if g is not None] if skipped else grads
+        # what every gradient has to be, checked list by list (a Python statement per tensor would cost more than the launch)
+        dtypes = set(map(_dtype_of, given))
+        dtype = next(iter(dtypes), torch.float32)
         fmt_g = _FMT.get(dtype)
         if fmt_g is None:
             raise TypeError("grads: need float32, bfloat16 or float16")
-        addresses = []
-        skipped = False
-        for g, n in zip(grads, sizes):
-            if g is None:
-                skipped = True
-                addresses.append(0)
-            elif g.dtype == dtype and g.numel() == n and g.is_contiguous() and g.get_device() == dev:
-                addresses.append(g.data_ptr())
-            else:
-                raise TypeError(f"grads[{len(addresses)}]: need a contiguous tensor of {n} elements of {dtype} on CUDA device {dev}")
-        desc[:, _G] = addresses
-        desc[:, _N] = [n if a else 0 for n, a in zip(sizes, addresses)] if skipped else sizes
+        want = [n for g, n in zip(grads, sizes) if g is not None] if skipped else sizes
+        if len(dtypes) > 1 or list(map(_numel, given)) != want or not all(map(_is_contiguous, given)) or \
+                any(map(dev.__ne__, map(_get_device, given))):
+            for i, (g, n) in enumerate(zip(grads, sizes)):
+                if g is not None and (g.dtype != dtype or g.numel() != n or not g.is_contiguous() or g.get_device() != dev):
+                    raise TypeError(f"grads[{i}]: need a contiguous tensor of {n} elements of {dtype} on CUDA device {dev}")
+        if skipped:
+            desc[:, _G] = [0 if g is None else g.data_ptr() for g in grads]
+            desc[:, _N] = [0 if g is None else n for g, n in zip(grads, sizes)]
+        else:
+            desc[:, _G] = list(map(_data_ptr, grads))
+            desc[:, _N] = self._sizes_u64
         fmt_p, fmt_s, fmt_c = self._fmt
-        _chk(S.lib().ssgd_adamw_step(desc.ctypes.data, len(sizes), fmt_p, fmt_g, fmt_s, fmt_c, self.lr if lr is None else lr,
+        _chk(S.lib().ssgd_adamw_step(self._desc_p, len(sizes), fmt_p, fmt_g, fmt_s, fmt_c, self.lr if lr is None else lr,
                                      self.betas[0], self.betas[1], self.eps, self.weight_decay, self.step_count + 1,
                                      _flat(grad_scale, torch.float32, 1, "grad_scale", dev), 0 if seed is None else 1,
                                      0 if seed is None else seed & 0xFFFFFFFFFFFFFFFF, _raw_stream(dev)), "ssgd_adamw_step")
