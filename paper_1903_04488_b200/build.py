@@ -1,8 +1,9 @@
-"""Builds libssgd.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Builds libssgd.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and the Python module _train_ops beside it.
 
     python -m paper_1903_04488_b200.build [--force] [--verbose]
 
-Every .cu under csrc/ is one translation unit; they are compiled in parallel and linked into one library.
+Every .cu under csrc/ is one translation unit; they are compiled in parallel and linked into one library.  train_ops.cpp
+is the binding of the training operators, a Python module over torch's headers that is linked to the library.
 """
 from __future__ import annotations
 
@@ -16,6 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libssgd.so")
+BINDING = os.path.join(HERE, "_train_ops.so")
 OBJ = os.path.join(HERE, "build")
 
 NVCC_FLAGS = [
@@ -38,8 +40,29 @@ def stale() -> bool:
     return os.path.getmtime(LIB) < max(os.path.getmtime(p) for p in _deps())
 
 
+def build_binding(force: bool = False) -> str:
+    """Compile _train_ops.so (g++, torch's headers) and link it to libssgd.so, which lies beside it."""
+    src = os.path.join(CSRC, "train_ops.cpp")
+    newest = max(os.path.getmtime(p) for p in [src] + glob.glob(os.path.join(INCLUDE, "*.h")))
+    if force or not os.path.exists(BINDING) or os.path.getmtime(BINDING) < newest:
+        import sysconfig
+
+        import torch
+        from torch.utils import cpp_extension
+        libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+        includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"],
+                                                    os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
+        tmp = BINDING + ".tmp.%d" % os.getpid()
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+        cmd += [a for i in includes for a in ("-isystem", i)] + [src, "-o", tmp, "-L", HERE, "-l:libssgd.so", "-L", libs]
+        cmd += ["-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
+        subprocess.check_call(cmd)
+        os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ and link libssgd.so (nvcc cross-compiles; no GPU needed)."""
+    """Compile every .cu under csrc/ and link libssgd.so (nvcc cross-compiles; no GPU needed), then the binding."""
     if force or stale():
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
         os.makedirs(OBJ, exist_ok=True)
@@ -58,6 +81,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + ".tmp.%d" % os.getpid()
         subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", tmp] + objs)
         os.replace(tmp, LIB)
+    build_binding(force)
     return LIB
 
 
