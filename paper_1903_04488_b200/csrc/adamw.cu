@@ -417,14 +417,12 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
     }
 }
 
-#ifndef MBX
-#define MBX 3
-#endif
+
 // A warp takes BLOCKS8 blocks, 8 apart (its neighbours have those between); the next one is read while one is computed.  The
 // chunk's 32 scales are read and written as a whole: a store of 4 bytes per block made the kernel's memory traffic alone
 // 206 instead of 144 us at 90M elements.
 template <typename P, typename G, int CAP, bool STOCHASTIC>
-__global__ void __launch_bounds__(THREADS, MBX) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {
+__global__ void __launch_bounds__(THREADS, 3) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {
     constexpr int WARPS = THREADS / 32, STEP = WARPS * QBLOCK;
     static_assert(WARPS * BLOCKS8 == 32, "a lane per scale");
     __shared__ float scales[2][32];

@@ -7,10 +7,10 @@
 // rises.  A row is cut into granules of 16 aligned bytes (its first and last may be partial, so any base and stride will
 // do); granule i of a segment belongs to thread i mod THREADS.
 //
-// Alternatives: the k-th largest of the threads' maxima bounds the k-th largest logit from below, so only threads whose
-// maximum reaches it can hold one of the k.  Their granules -- k threads' worth when logits are distinct -- are read
-// again (from L2) and fed into a sorted list per warp.  Order: larger logit first, then smaller index; a NaN counts as
-// the largest; -0 and +0 are equal.
+// Alternatives: the threads' maxima bound the k-th largest logit from below, so only threads whose maximum reaches the bound
+// can hold one of the k.  Their granules -- those of some 20 to 60 of 256 threads -- are read again (from L2), and the
+// logits that reach the bound are sorted, 32 to a warp, and merged.  Order: larger logit first, then smaller index; a NaN
+// counts as the largest; -0 and +0 are equal.
 //
 // Few rows: a cluster of CTAs shares a row and joins through distributed shared memory, so there is still one launch
 // and no scratch.
@@ -28,8 +28,6 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int WARPS = THREADS / 32;
 constexpr int MAX_TOP = SSGD_MAX_TOP;       // one entry per lane of a warp
 static_assert(MAX_TOP == 32, "a warp's list has an entry per lane");
 constexpr float LOG2E = 1.4426950408889634f;
@@ -48,23 +46,31 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
 }
 
 // Largest magnitude of a format for which the fast path below is taken, with room for the floor.
-template <typename T> __device__ __forceinline__ float fast_limit() { return 1e37f; }
+template <typename T> __device__ __forceinline__ float fast_limit() { return 1e30f; }
 template <> __device__ __forceinline__ float fast_limit<__half>() { return 6e4f; }
 
-// The running sums of one thread, relative to its maximum logit m, in powers of two: with d = (z - m) c, c = scale * log2 e,
-// s = sum 2^d and w = sum 2^d d.  The difference comes first: z c alone overflows at the lowest values that masks use.
+// The running sums of one thread, relative to its maximum logit m, in powers of two: with c = scale * log2 e, shift = m c and
+// d = z c - shift, s = sum 2^d and w = sum 2^d d.  shift is rounded, but as every d is taken from the same shift that only
+// moves the reference.  Beyond HUGE_LOGIT, where masks put their lowest values, z c would overflow: there d = (z - m) c, and
+// nothing from there has weight beside a smaller logit.
 struct Sums {
-    float m, s, w;
+    float m, shift, s, w;
 };
+constexpr float HUGE_LOGIT = 1e30f;
+
+__device__ __forceinline__ Sums no_sums() { return Sums{NEG_INF, NEG_INF, 0.f, 0.f}; }
+__device__ __forceinline__ bool ordinary(float m, float shift) { return fabsf(m) < HUGE_LOGIT && fabsf(shift) < HUGE_LOGIT; }
 
 __device__ __forceinline__ void rebase(Sums& a, float m, float c) {
+    const float shift = __fmul_rn(m, c);
     if (a.m > NEG_INF || a.m != a.m) {
-        const float delta = (a.m - m) * c, f = ex2(delta);
+        const float delta = ordinary(m, shift) ? a.shift - shift : (a.m - m) * c, f = ex2(delta);
         a.w = f * fmaf(delta, a.s, a.w);
         if (f == 0.f && a.s == a.s && a.w != a.w) a.w = 0.f;   // 0 * -inf: the old part has vanished
         a.s *= f;
     }
     a.m = m;
+    a.shift = shift;
 }
 
 // Any values: infinities, NaN, magnitudes near the end of the format.
@@ -72,7 +78,7 @@ __device__ __forceinline__ void add_careful(Sums& a, float z, float c) {
     const float m = max_nan(a.m, z);
     if (!(m == a.m)) rebase(a, m, c);
     if (z == NEG_INF && a.m == a.m) return;                // contributes nothing, whatever the maximum
-    const float d = (z - a.m) * c, e = ex2(d);
+    const float d = ordinary(a.m, a.shift) ? fmaf(z, c, -a.shift) : (z - a.m) * c, e = ex2(d);
     a.s += e;
     if (e > 0.f || e != e) a.w = fmaf(e, d, a.w);
 }
@@ -174,54 +180,65 @@ __device__ __forceinline__ Vec<__half, 8> raised(Vec<__half, 8> v, float low) {
     return v;
 }
 
-// A value no larger than m - 160 / c and below every element that could matter: elements under it are raised to it, so
-// that -inf does not make 0 * -inf.  2^-160 is zero in fp32.
-template <typename T> __device__ __forceinline__ float floor_for(float m, float c) { return __fsub_rd(m, __fdiv_ru(160.f, c)); }
-template <> __device__ __forceinline__ float floor_for<__nv_bfloat16>(float m, float c) {
-    return __bfloat162float(__float2bfloat16_rd(__fsub_rd(m, __fdiv_ru(160.f, c))));
+// A value no larger than m - reach, reach = 160 / c rounded up, and below every element that could matter: elements under it
+// are raised to it, so that -inf does not make 0 * -inf.  2^-160 is zero in fp32.
+template <typename T> __device__ __forceinline__ float floor_for(float m, float reach) { return __fsub_rd(m, reach); }
+template <> __device__ __forceinline__ float floor_for<__nv_bfloat16>(float m, float reach) {
+    return __bfloat162float(__float2bfloat16_rd(__fsub_rd(m, reach)));
 }
-template <> __device__ __forceinline__ float floor_for<__half>(float m, float c) {
-    return __half2float(__float2half_rd(__fsub_rd(m, __fdiv_ru(160.f, c))));
+template <> __device__ __forceinline__ float floor_for<__half>(float m, float reach) {
+    return __half2float(__float2half_rd(__fsub_rd(m, reach)));
 }
 
-// Elements that are not there are -inf: they change neither the maximum nor the sums.  `have` <= U is the same for the
-// whole CTA.
+// What a thread carries along a row
+struct Running {
+    Sums a;
+    float low;           // elements below it are raised to it; -inf: they are taken one by one
+    float c, reach;
+};
+
+template <typename T>
+__device__ __noinline__ Sums add_granule_carefully(Sums a, Vec<T, 16 / sizeof(T)> v, float c) {
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) add_careful(a, to_f32(v.e[e]), c);
+    return a;
+}
+
+// Granules v[0] .. v[have - 1] (`have` is the same for the whole CTA).  Elements that are not there are -inf: they change neither
+// the maximum nor the sums.
 template <typename T, int U>
-__device__ __forceinline__ void add_granules(Sums& a, float& low, const Vec<T, 16 / sizeof(T)> (&v)[U], int have, float c) {
+__device__ __forceinline__ void add_granules(Running& r, const Vec<T, 16 / sizeof(T)> (&v)[U], int have) {
     constexpr int VEC = 16 / sizeof(T);
-    PairMax<T> top(a.m);
+    PairMax<T> top(r.a.m);
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (u < have) top.add(v[u]);
     const float m = top.value();
-    if (!(m == a.m)) {
-        rebase(a, m, c);
-        low = fabsf(m) < fast_limit<T>() ? floor_for<T>(m, c) : NEG_INF;
+    if (!(m == r.a.m)) {
+        rebase(r.a, m, r.c);
+        r.low = fabsf(m) < fast_limit<T>() && ordinary(m, r.a.shift) ? floor_for<T>(m, r.reach) : NEG_INF;
     }
-    if (low > NEG_INF) {
-        const float2 minus_m = both(-a.m), c2 = both(c);
+    if (r.low > NEG_INF) {
+        const float2 minus_shift = both(-r.a.shift), c2 = both(r.c);
         float2 s = both(0.f), w = both(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u < have) {
                 float2 f[VEC / 2];
-                unpack_pairs(raised(v[u], low), f);
+                unpack_pairs(raised(v[u], r.low), f);
 #pragma unroll
                 for (int e = 0; e < VEC / 2; ++e) {
-                    const float2 d = mul2(add2(f[e], minus_m), c2), x = make_float2(ex2(d.x), ex2(d.y));
+                    const float2 d = fma2(f[e], c2, minus_shift), x = make_float2(ex2(d.x), ex2(d.y));
                     s = add2(s, x);
                     w = fma2(x, d, w);
                 }
             }
         }
-        a.s += s.x + s.y;
-        a.w += w.x + w.y;
+        r.a.s += s.x + s.y;
+        r.a.w += w.x + w.y;
     } else {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (u < have)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) add_careful(a, to_f32(v[u].e[e]), c);
+            if (u < have) r.a = add_granule_carefully<T>(r.a, v[u], r.c);
     }
 }
 
@@ -248,65 +265,63 @@ __device__ __forceinline__ uint64_t merge(uint64_t a, uint64_t b) {
     return a;
 }
 // Lane l gets the l-th largest of the warp's values.
-__device__ __forceinline__ uint32_t sort32(uint32_t x) {
+__device__ __forceinline__ uint64_t sort32(uint64_t x) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int k = 2; k <= 32; k <<= 1) {
 #pragma unroll
         for (int o = k >> 1; o > 0; o >>= 1) {
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, x, o);
+            const uint64_t other = __shfl_xor_sync(0xffffffffu, x, o);
             const bool keep_larger = ((lane & o) == 0) == ((lane & k) == 0);
-            x = keep_larger ? max(x, other) : min(x, other);
+            x = keep_larger == (x > other) ? x : other;
         }
     }
     return x;
 }
 
+constexpr int CANDIDATES = 256;
+
+template <int NT>
 struct Shared {
-    Sums part[WARPS];                 // part[0] is the CTA's in the end
-    uint64_t list[WARPS][MAX_TOP];    // list[0] is the CTA's in the end
-    uint32_t bound[WARPS];
-    int32_t picked[THREADS];
-    int32_t npicked;
+    Sums part[8];                     // part[0] is the CTA's in the end
+    uint64_t list[8][MAX_TOP];        // list[0] is the CTA's in the end
+    uint64_t candidate[CANDIDATES];
+    uint32_t bound[8];
+    int32_t picked[NT];
+    int32_t npicked, ncandidates;
 };
 
-// The CTA's best of its segment [g0, g1) into sh.list[0], in order, at least k of them (0 where there are fewer).
+// The order of the elements of a granule (0 where there is none)
 template <typename T>
-__device__ void best_of_segment(Shared& sh, const Granules<T>& G, int32_t g0, int32_t g1, float thread_max, bool has, int k) {
+__device__ __forceinline__ void orders_of(const Granules<T>& G, int32_t i, bool there, uint32_t (&order)[16 / sizeof(T)]) {
     constexpr int VEC = 16 / sizeof(T);
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const uint32_t mine = has ? order_of(thread_max) : 0u;
-    // Each warp has ceil(k / WARPS) threads whose maximum reaches its bound, so k logits reach the least of the bounds.
-    const uint32_t sorted = sort32(mine);
-    if (lane == (k + WARPS - 1) / WARPS - 1) sh.bound[warp] = sorted;
-    if (t == 0) sh.npicked = 0;
-    __syncthreads();
-    uint32_t bound = sh.bound[0];
+    const int32_t at = G.first(i);
 #pragma unroll
-    for (int i = 1; i < WARPS; ++i) bound = min(bound, sh.bound[i]);
-    if (has && mine >= bound) sh.picked[atomicAdd(&sh.npicked, 1)] = t;
-    __syncthreads();
+    for (int e = 0; e < VEC; ++e) order[e] = 0;
+    if (!there) return;
+    if (G.whole(i)) {
+        const Vec<T, VEC> v = load_vec<T, VEC>(G.row + at);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) order[e] = order_of(to_f32(v.e[e]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (at + e >= 0 && at + e < G.n) order[e] = order_of(to_f32(G.row[at + e]));
+    }
+}
+
+// Rare: more than CANDIDATES logits reach the bound (many equal ones, or a few threads with nearly all the large ones).  Each
+// warp goes through the granules of the picked threads and inserts one by one into its list.
+template <typename T, int NT>
+__device__ __noinline__ uint64_t best_one_by_one(const Shared<NT>& sh, const Granules<T>& G, int32_t g0, int32_t g1, uint32_t bound, int k) {
+    constexpr int VEC = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint64_t list = 0, last = 0;                           // lane's entry of the warp's list; the k-th entry
-    const int np = sh.npicked;
-    for (int q = warp; q < np; q += WARPS) {
-        const int owner = sh.picked[q];
-        for (int32_t base = g0 + owner; base < g1; base += 32 * THREADS) {
-            const int32_t i = base + lane * THREADS;
-            const int32_t at = G.first(i);
+    for (int q = warp; q < sh.npicked; q += NT / 32) {
+        for (int32_t base = g0 + sh.picked[q]; base < g1; base += 32 * NT) {
+            const int32_t i = base + lane * NT, at = G.first(i);
             uint32_t order[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) order[e] = 0;
-            if (i < g1) {
-                if (G.whole(i)) {
-                    const Vec<T, VEC> v = load_vec<T, VEC>(G.row + at);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) order[e] = order_of(to_f32(v.e[e]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        if (at + e >= 0 && at + e < G.n) order[e] = order_of(to_f32(G.row[at + e]));
-                }
-            }
+            orders_of<T>(G, i, i < g1, order);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 uint32_t todo = __ballot_sync(0xffffffffu, order[e] >= bound && order[e] >= (uint32_t)(last >> 32) && order[e] != 0);
@@ -323,9 +338,72 @@ __device__ void best_of_segment(Shared& sh, const Granules<T>& G, int32_t g0, in
             }
         }
     }
-    sh.list[warp][lane] = list;
+    return list;
+}
+
+// The CTA's best of its segment [g0, g1) into sh.list[0], in order, at least k of them (0 where there are fewer).
+template <typename T, int NT>
+__device__ __forceinline__ void best_of_segment(Shared<NT>& sh, const Granules<T>& G, int32_t g0, int32_t g1, float thread_max, int k) {
+    constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const bool has = g0 + t < g1;
+    const uint32_t mine = has ? order_of(thread_max) : 0u;
+    // The q-th largest maximum of each warp whose 32 threads all have granules, q = ceil(k / number of those warps): k logits
+    // reach the least of these.  (No such warp: every logit is a candidate, fewer than 32 granules.)
+    const int full = min((g1 - g0) / 32, WARPS);
+    if (warp < full) {
+        uint32_t left = mine, best = 0;
+        for (int q = 0; q < k; q += full) {
+            best = __reduce_max_sync(0xffffffffu, left);
+            const uint32_t who = __ballot_sync(0xffffffffu, left == best);
+            if (lane == __ffs(who) - 1) left = 0;
+        }
+        if (lane == 0) sh.bound[warp] = best;
+    }
+    if (t == 0) sh.npicked = sh.ncandidates = 0;
+    __syncthreads();
+    uint32_t bound = full ? 0xffffffffu : 0u;
+    for (int i = 0; i < full; ++i) bound = min(bound, sh.bound[i]);
+    if (has && mine >= bound) sh.picked[atomicAdd(&sh.npicked, 1)] = t;
+    __syncthreads();
+    // all threads share the granules of the picked ones, a power of two of lanes to one of them
+    const int each = (g1 - g0 + NT - 1) / NT, np = sh.npicked;
+    const int log_lanes = each >= 32 ? 5 : 32 - __clz(each - 1);      // each = 1: no bits
+    for (int q = (warp << (5 - log_lanes)) + (lane >> log_lanes); q < np; q += WARPS << (5 - log_lanes)) {
+        const int32_t owner = sh.picked[q];
+        for (int j = lane & ((1 << log_lanes) - 1); j < each; j += 1 << log_lanes) {
+            const int32_t i = g0 + owner + j * NT;
+            if (i >= g1) break;
+            if (G.whole(i)) {                              // mostly there is nothing in it
+                PairMax<T> top(NEG_INF);
+                top.add(load_vec<T, VEC>(G.row + G.first(i)));
+                if (order_of(top.value()) < bound) continue;
+            }
+            uint32_t order[VEC];
+            orders_of<T>(G, i, true, order);
 #pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                if (order[e] >= bound && order[e] != 0) {
+                    const int at = atomicAdd(&sh.ncandidates, 1);
+                    if (at < CANDIDATES) sh.candidate[at] = ((uint64_t)order[e] << 32) | (0xffffffffu - (uint32_t)(G.first(i) + e));
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const int n = sh.ncandidates;
+    int lists = WARPS;
+    uint64_t list = 0;
+    if (n <= CANDIDATES) {
+        lists = min((n + 31) / 32, WARPS);
+        if (warp < lists) list = sort32(t < n ? sh.candidate[t] : 0);
+        for (int at = t + NT; at - lane < n; at += NT) list = merge(list, sort32(at < n ? sh.candidate[at] : 0));
+    } else {
+        list = best_one_by_one<T, NT>(sh, G, g0, g1, bound, k);
+    }
+    sh.list[warp][lane] = list;
     for (int half = WARPS / 2; half > 0; half >>= 1) {
+        if (half >= lists) continue;                       // the same for the whole CTA
         __syncthreads();
         if (warp < half) {
             list = merge(list, sh.list[warp + half][lane]);
@@ -334,10 +412,13 @@ __device__ void best_of_segment(Shared& sh, const Granules<T>& G, int32_t g0, in
     }
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(THREADS) k_token_logprobs(const LogprobArgs A, int split) {
-    constexpr int VEC = 16 / sizeof(T), U = 4;
-    __shared__ Shared sh;
+// At 4096 x 32000 in bfloat16 50 us, 5.2 TB/s.  Per logit 8.5 instructions, one of them a 2^x, of which an SM has 16 a cycle:
+// 36 us for these alone.  The latency of the loads is covered by other CTAs, 6 of 256 threads per SM (with 4: 56 us, 5: 51; the
+// next batch in registers while one is summed, 3 CTAs: 69).
+template <typename T, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, 6 * 256 / NT) k_token_logprobs(const LogprobArgs A, int split) {
+    constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32, U = 4;
+    __shared__ Shared<NT> sh;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     // split is a power of two
     const int shift = __ffs(split) - 1, part = blockIdx.x & (split - 1);
@@ -349,35 +430,39 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs(const LogprobArgs A,
     const float c = A.scale * LOG2E;
     int64_t id = -1;
     if (part == 0 && t == 0) id = id_of(A.ids, A.ids64, row);
-    Sums a{NEG_INF, 0.f, 0.f};
-    float low = NEG_INF;
-    const int32_t whole0 = G.phase ? 1 : 0, whole1 = G.whole(G.count - 1) ? G.count : G.count - 1;
-    for (int32_t b0 = g0; b0 < g1; b0 += THREADS * U) {
-        Vec<T, VEC> v[U];
-        if (b0 >= whole0 && b0 + THREADS * U <= min(whole1, g1)) {
-            const T* p = z + G.first(b0 + t);
+    Running r{no_sums(), NEG_INF, c, __fdiv_ru(160.f, c)};
+    // granules [whole0, whole1) of the segment are vectors; the row's first and last may be parts of one
+    const int32_t whole0 = g0 == 0 && G.phase ? 1 : g0, whole1 = g1 == G.count && !G.whole(G.count - 1) ? g1 - 1 : g1;
+    {
+        int32_t i = g0 + t;
+        const T* p = z + G.first(i);
+        int32_t b0 = g0;
+        if (whole0 == g0) {
+            for (; b0 + NT * U <= whole1; b0 += NT * U, i += NT * U, p += NT * U * VEC) {
+                Vec<T, VEC> v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = load_vec_stream<T, VEC>(p + u * (THREADS * VEC));
-            add_granules<T, U>(a, low, v, U, c);
-            continue;
-        }
-        const int have = (g1 - b0 + THREADS - 1) / THREADS;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t i = b0 + u * THREADS + t, at = G.first(i);
-            if (i >= whole0 && i < min(whole1, g1)) {
-                v[u] = load_vec_stream<T, VEC>(z + at);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[u].e[e] = from_f32<T>(NEG_INF);
-                    if (i < g1 && at + e >= 0 && at + e < A.vocab) v[u].e[e] = z[at + e];
-                }
+                for (int u = 0; u < U; ++u) v[u] = load_vec_stream<T, VEC>(p + u * (NT * VEC));
+                add_granules<T, U>(r, v, U);
             }
         }
-        add_granules<T, U>(a, low, v, have, c);
+        for (; b0 < whole1; b0 += NT * U, i += NT * U, p += NT * U * VEC) {
+            Vec<T, VEC> v[U];
+            const int have = (whole1 - b0 + NT - 1) / NT;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[u].e[e] = from_f32<T>(NEG_INF);
+                if (i + u * NT >= whole0 && i + u * NT < whole1) v[u] = load_vec_stream<T, VEC>(p + u * (NT * VEC));
+            }
+            add_granules<T, U>(r, v, have);
+        }
     }
-    const bool has = g0 + t < g1;
+    auto partial = [&](int32_t i) {
+        for (int32_t at = max(G.first(i), 0); at < min(G.first(i) + VEC, A.vocab); ++at) add_careful(r.a, to_f32(z[at]), c);
+    };
+    if (whole0 > g0 && t == 0) partial(0);
+    if (whole1 < g1 && whole1 >= whole0 && (whole1 - g0) % NT == t) partial(whole1);
+    Sums& a = r.a;
     const float thread_max = a.m;
     const bool counted = id >= 0 && id < A.vocab;          // an id outside the vocabulary is ignored
     float z_id = 0.f;
@@ -385,38 +470,53 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs(const LogprobArgs A,
     // join: warp, CTA, cluster
     join_warp(a, c);
     if (lane == 0) sh.part[warp] = a;
-    if (TOP) best_of_segment<T>(sh, G, g0, g1, thread_max, has, A.top);
+    if (TOP) best_of_segment<T, NT>(sh, G, g0, g1, thread_max, A.top);
     __syncthreads();
     if (warp == 0) {
-        a = lane < WARPS ? sh.part[lane] : Sums{NEG_INF, 0.f, 0.f};
+        a = lane < WARPS ? sh.part[lane] : no_sums();
         join_warp(a, c);
-        __syncwarp();
         if (lane == 0) sh.part[0] = a;
     }
     cg::cluster_group cluster = cg::this_cluster();
-    if (split > 1) cluster.sync();
+    if (split > 1) {
+        cluster.sync();
+        if (TOP && part == 0) {
+            // the CTAs' lists, two by two
+            for (int q = warp; q < split / 2; q += WARPS) {
+                const uint64_t one = cluster.map_shared_rank(&sh.list[0][0], 2 * q)[lane];
+                const uint64_t two = cluster.map_shared_rank(&sh.list[0][0], 2 * q + 1)[lane];
+                sh.candidate[q * 32 + lane] = merge(one, two);
+            }
+            for (int half = split / 4; half > 0; half >>= 1) {
+                __syncthreads();
+                for (int q = warp; q < half; q += WARPS)
+                    sh.candidate[q * 32 + lane] = merge(sh.candidate[q * 32 + lane], sh.candidate[(q + half) * 32 + lane]);
+            }
+        }
+    }
     if (part == 0 && warp == 0) {
         if (split > 1) {
-            a = lane < split ? *cluster.map_shared_rank(&sh.part[0], lane < split ? lane : 0) : Sums{NEG_INF, 0.f, 0.f};
+            a = lane < split ? *cluster.map_shared_rank(&sh.part[0], lane < split ? lane : 0) : no_sums();
             join_warp(a, c);
         }
         const float log2s = log2f(a.s);
         const bool none = a.s == 0.f;                      // every logit is -inf
+        // relative to the reference that the sums have: log p = (x c - shift) - log2 s in powers of two; in powers of e from the
+        // start where that would overflow
+        const bool plain = ordinary(a.m, a.shift);
         auto logp_of = [&](float x) {
-            return none || (x == NEG_INF && a.s == a.s) ? NEG_INF : fmaf(x - a.m, A.scale, -log2s * LN2);
+            if (none || (x == NEG_INF && a.s == a.s)) return NEG_INF;
+            return plain && fabsf(x) < HUGE_LOGIT ? (fmaf(x, c, -a.shift) - log2s) * LN2 : fmaf(x - a.m, A.scale, -log2s * LN2);
         };
         if (lane == 0) {
             A.stats[row] = counted ? logp_of(z_id) : 0.f;
             A.stats[A.rows + row] = none ? 0.f : (log2s - a.w / a.s) * LN2;
-            A.stats[2 * A.rows + row] = none ? NEG_INF : fmaf(a.m, A.scale, log2s * LN2);
+            A.stats[2 * A.rows + row] = none ? NEG_INF : plain ? (a.shift + log2s) * LN2 : fmaf(a.m, A.scale, log2s * LN2);
         }
-        if (TOP) {
-            uint64_t list = sh.list[0][lane];
-            for (int i = 1; i < split; ++i) list = merge(list, cluster.map_shared_rank(&sh.list[0][0], i)[lane]);
-            if (lane < A.top) {
-                A.top_idx[row * A.top + lane] = (int32_t)(0xffffffffu - (uint32_t)list);
-                A.top_logp[row * A.top + lane] = logp_of(logit_of(list));
-            }
+        if (TOP && lane < A.top) {
+            const uint64_t key = split > 1 ? sh.candidate[lane] : sh.list[0][lane];
+            A.top_idx[row * A.top + lane] = (int32_t)(0xffffffffu - (uint32_t)key);
+            A.top_logp[row * A.top + lane] = logp_of(logit_of(key));
         }
     }
     if (split > 1) cluster.sync();                         // nobody leaves while its shared memory is read
@@ -437,7 +537,7 @@ struct LogprobBackArgs {
     bool same_phase;       // rows of logits and of the result lie alike within 16 bytes
 };
 
-constexpr int BACK_U = 4;
+constexpr int THREADS = 256, BACK_U = 4;
 
 // CTA (row, part) writes `per` granules of a row.
 template <typename T, bool ENTROPY>
@@ -537,19 +637,23 @@ __global__ void __launch_bounds__(THREADS) k_token_logprobs_back(const LogprobBa
 
 // ---- host side ---------------------------------------------------------------------------------------
 
-// CTAs that share a row: enough of them for all SMs, while each still has two granules per thread.
-int split_for(int64_t rows, int64_t vocab, int es, int sms) {
-    const int64_t granules = vocab * es / 16;
+// CTAs that share a row: enough of them for 4 per SM, while each still has two granules per thread.  Measured at 300 x 50001
+// fp32 (us, without / with 5 alternatives): up to 2 per SM 18.7 / 27.4, 4 16.7 / 22.9, 8 19.9 / 28.2.
+int split_for(int64_t rows, int64_t granules, int sms) {
     int split = 1;
-    while (split < 8 && rows * split < 2 * sms && granules / (split * 2) >= 2 * THREADS) split *= 2;
+    while (split < 8 && rows * split < 4 * sms && granules / (split * 2) >= 2 * 256) split *= 2;
     return split;
 }
 
-template <typename T>
-int launch_logprobs(const LogprobArgs& A, int split, cudaStream_t st) {
+// Rows of up to this many granules are left to CTAs of 64 threads where there are enough rows: what a CTA spends on a row's joins
+// does not depend on its length.  Measured (us, 64 / 256 threads): 3641 x 6156 binary16 (770 granules) 17.3 / 20.7, with 5
+// alternatives 28.7 / 36.9; 1637 x 5325 fp32 (1332) with 20 26.9 / 24.6; 4096 x 32000 bfloat16 (4000) 57.4 / 50.0.
+constexpr int64_t SHORT_ROW = 1024;
+template <typename T, int NT>
+int launch_logprobs_nt(const LogprobArgs& A, int split, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(A.rows * split));
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(NT);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -557,9 +661,17 @@ int launch_logprobs(const LogprobArgs& A, int split, cudaStream_t st) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = split > 1 ? 1 : 0;
-    const cudaError_t e = A.top ? cudaLaunchKernelEx(&cfg, k_token_logprobs<T, true>, A, split)
-                                : cudaLaunchKernelEx(&cfg, k_token_logprobs<T, false>, A, split);
+    const cudaError_t e = A.top ? cudaLaunchKernelEx(&cfg, k_token_logprobs<T, true, NT>, A, split)
+                                : cudaLaunchKernelEx(&cfg, k_token_logprobs<T, false, NT>, A, split);
     return e == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
+}
+
+template <typename T>
+int launch_logprobs(const LogprobArgs& A, int sms, cudaStream_t st) {
+    const int64_t granules = ((int64_t)A.vocab * sizeof(T) + 15) / 16;
+    const int split = split_for(A.rows, granules, sms);
+    if (granules <= SHORT_ROW && A.rows >= 4 * sms) return launch_logprobs_nt<T, 64>(A, 1, st);
+    return launch_logprobs_nt<T, 256>(A, split, st);
 }
 
 template <typename T>
@@ -607,10 +719,9 @@ int ssgd_token_logprobs(const void* logits, int64_t ld, int32_t fmt, const void*
     int sms = 0;
     if ((e = sm_count_of_current_device(&sms))) return e;
     const LogprobArgs A{logits, ld, ids, ids_bytes == 8, rows, (int32_t)vocab, scale, top, stats, top_idx, top_logp};
-    const int split = split_for(rows, vocab, fmt_bytes(fmt), sms);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return fmt == SSGD_FMT_F32 ? launch_logprobs<float>(A, split, st)
-         : fmt == SSGD_FMT_F16 ? launch_logprobs<__half>(A, split, st) : launch_logprobs<__nv_bfloat16>(A, split, st);
+    return fmt == SSGD_FMT_F32 ? launch_logprobs<float>(A, sms, st)
+         : fmt == SSGD_FMT_F16 ? launch_logprobs<__half>(A, sms, st) : launch_logprobs<__nv_bfloat16>(A, sms, st);
 }
 
 int ssgd_token_logprobs_backward(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes,
