@@ -23,6 +23,27 @@ template <int G> struct GroupShape {
     static constexpr int WARPS = G / 32;
 };
 
+// Sums of V values (a power of two up to 8) over the warp at once: in each of the first steps a lane hands half of its values
+// to its partner and goes on with the other half.  Value i ends up in the lanes l with l / (32 / V) = i.
+template <int V>
+__device__ __forceinline__ float warp_sums(float (&v)[V]) {
+    const int lane = threadIdx.x & 31;
+    int o = 16;
+#pragma unroll
+    for (int half = V / 2; half > 0; half >>= 1, o >>= 1) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const float keep = upper ? v[i + half] : v[i], give = upper ? v[i] : v[i + half];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    float x = v[0];
+#pragma unroll
+    for (; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
 // Sum over the group, known to every thread of it.  `slot` [WARPS] is not used again before the next barrier but one.
 template <int G>
 __device__ __forceinline__ float group_sum(float x, float* slot) {
@@ -32,10 +53,14 @@ __device__ __forceinline__ float group_sum(float x, float* slot) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (lane == 0) slot[warp] = x;
     __syncthreads();
-    float s = lane < NW ? slot[lane] : 0.f;
+    if constexpr (NW <= 8) {
+        float s = slot[0];
 #pragma unroll
-    for (int o = NW / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return __shfl_sync(0xffffffffu, s, 0);
+        for (int i = 1; i < NW; ++i) s += slot[i];
+        return s;
+    } else {
+        return warp_sum(lane < NW ? slot[lane] : 0.f);
+    }
 }
 
 // w or b at column `col`, VEC of them, in fp32 or in the row's format
@@ -58,19 +83,23 @@ __device__ __forceinline__ void load_param(const void* w, bool w_f32, int col, f
 // y = (x - mean) rstd w + b of one vector
 template <typename T, int VEC, typename A>
 __device__ __forceinline__ Vec<T, VEC> normalised(const Vec<T, VEC>& v, const A& args, int col, float2 minus_mean, float2 rstd) {
-    float2 f[PAIRS<VEC>], w[PAIRS<VEC>];
+    float2 f[PAIRS<VEC>], w[PAIRS<VEC>], b[PAIRS<VEC>];
     unpack_pairs(v, f);
 #pragma unroll
     for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = mul2(add2(f[i], minus_mean), rstd);
-    if (args.w) {
+    if (args.w && args.b) {
+        load_param<T, VEC>(args.w, args.w_f32, col, w);
+        load_param<T, VEC>(args.b, args.w_f32, col, b);
+#pragma unroll
+        for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = fma2(f[i], w[i], b[i]);
+    } else if (args.w) {
         load_param<T, VEC>(args.w, args.w_f32, col, w);
 #pragma unroll
         for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = mul2(f[i], w[i]);
-    }
-    if (args.b) {
-        load_param<T, VEC>(args.b, args.w_f32, col, w);
+    } else if (args.b) {
+        load_param<T, VEC>(args.b, args.w_f32, col, b);
 #pragma unroll
-        for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = add2(f[i], w[i]);
+        for (int i = 0; i < PAIRS<VEC>; ++i) f[i] = add2(f[i], b[i]);
     }
     return pack_pairs<T, VEC>(f);
 }
@@ -102,38 +131,221 @@ struct NormArgs {
     float* stats;        // [2][rows]: mean, rstd
 };
 
-template <typename T, int VEC, int G, int E>
+// FULL: every thread has E elements (n = G E), so no column needs a check.
+template <typename T, int VEC, int G, int E, bool FULL>
 __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm(const NormArgs A) {
     constexpr int NV = E / VEC;
     __shared__ float slot[2][32];
     const int t = threadIdx.x % G;
     const int64_t row = (int64_t)blockIdx.x * GroupShape<G>::ROWS + threadIdx.x / G;
     if (row >= A.rows) return;                         // a whole warp (G = 32) or nobody
-    const T* x = static_cast<const T*>(A.x) + row * A.ld_x;
+    const T* x = static_cast<const T*>(A.x) + row * A.ld_x + t * VEC;
     const int nv = A.n / VEC;
+    auto mine_here = [&](int j) { return FULL || t + j * G < nv; };
     Vec<T, VEC> v[NV];
     float2 s = both(0.f), q = both(0.f);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = t + j * G;
-        if (i < nv) v[j] = load_vec_stream<T, VEC>(x + (int64_t)i * VEC);
-    }
+    for (int j = 0; j < NV; ++j)
+        if (mine_here(j)) v[j] = load_vec_stream<T, VEC>(x + j * G * VEC);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        if (t + j * G < nv) add_sum(v[j], s);
+        if (mine_here(j)) add_sum(v[j], s);
     const float mean = group_sum<G>(s.x + s.y, slot[0]) / (float)A.n;
     const float2 minus_mean = both(-mean);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        if (t + j * G < nv) add_squares(v[j], minus_mean, q);
+        if (mine_here(j)) add_squares(v[j], minus_mean, q);
     const float rstd = 1.0f / sqrtf(group_sum<G>(q.x + q.y, slot[1]) / (float)A.n + A.eps);
     if (t == 0) { A.stats[row] = mean; A.stats[A.rows + row] = rstd; }
-    T* y = static_cast<T*>(A.y) + row * A.ld_y;
+    T* y = static_cast<T*>(A.y) + row * A.ld_y + t * VEC;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (mine_here(j)) store_vec<T, VEC>(y + j * G * VEC, normalised(v[j], A, (t + j * G) * VEC, minus_mean, both(rstd)));
+}
+
+// A row at a time, rows blockIdx, blockIdx + grid, ... to a block: the threads keep their columns of w and b, and the next row is
+// on its way into registers while one is worked on.  For few rows (everything is asked for at once: 6.0 us for one row of
+// 2048, 8.1 through the ring below) and for fp32 (8192 x 2048 20.9 us, through the ring 24.7).
+template <typename T, int VEC, int G, int E, bool FULL>
+__global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_rows(const NormArgs A) {
+    constexpr int NV = E / VEC, P = PAIRS<VEC>;
+    __shared__ float slot[2][32];
+    const int t = threadIdx.x % G;
+    const int64_t step = (int64_t)gridDim.x * GroupShape<G>::ROWS;
+    int64_t row = (int64_t)blockIdx.x * GroupShape<G>::ROWS + threadIdx.x / G;
+    const int nv = A.n / VEC;
+    auto mine_here = [&](int j) { return FULL || t + j * G < nv; };
+    const T* x = static_cast<const T*>(A.x) + row * A.ld_x + t * VEC;
+    T* y = static_cast<T*>(A.y) + row * A.ld_y + t * VEC;
+    Vec<T, VEC> v[NV];
+    auto fetch = [&]() {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (mine_here(j)) v[j] = load_vec_stream<T, VEC>(x + j * G * VEC);
+        x += step * A.ld_x;
+    };
+    if (row < A.rows) fetch();
+    float2 w[NV][P], b[NV][P];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int i = t + j * G;
-        if (i < nv) store_vec<T, VEC>(y + (int64_t)i * VEC, normalised(v[j], A, i * VEC, minus_mean, both(rstd)));
+#pragma unroll
+        for (int i = 0; i < P; ++i) { w[j][i] = both(1.f); b[j][i] = both(0.f); }
+        if (A.w && mine_here(j)) load_param<T, VEC>(A.w, A.w_f32, (t + j * G) * VEC, w[j]);
+        if (A.b && mine_here(j)) load_param<T, VEC>(A.b, A.w_f32, (t + j * G) * VEC, b[j]);
     }
+    const float inv_n = 1.f / (float)A.n;
+#pragma unroll 1
+    for (; row < A.rows; row += step) {
+        Vec<T, VEC> now[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) now[j] = v[j];
+        if (row + step < A.rows) fetch();
+        float2 s = both(0.f), q = both(0.f);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (mine_here(j)) add_sum(now[j], s);
+        const float mean = group_sum<G>(s.x + s.y, slot[0]) * inv_n;
+        const float2 minus_mean = both(-mean);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (mine_here(j)) add_squares(now[j], minus_mean, q);
+        const float rstd = 1.0f / sqrtf(group_sum<G>(q.x + q.y, slot[1]) * inv_n + A.eps);
+        if (t == 0) { A.stats[row] = mean; A.stats[A.rows + row] = rstd; }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (mine_here(j)) {
+                float2 f[P];
+                unpack_pairs(now[j], f);
+#pragma unroll
+                for (int i = 0; i < P; ++i) f[i] = fma2(mul2(add2(f[i], minus_mean), both(rstd)), w[j][i], b[j][i]);
+                store_vec<T, VEC>(y + j * G * VEC, pack_pairs<T, VEC>(f));
+            }
+        }
+        y += step * A.ld_y;
+    }
+}
+
+// Several rows at once, and more of them to a block: the threads keep their columns of w and b, which L1 would have to serve
+// again for every row (twice as many bytes as the row, if they are fp32 and it is not); the latency of the sums' way through
+// warps and block is paid once for R rows; and the next R rows are on their way into shared memory meanwhile.  A thread
+// copies what it will read itself.  (Vectors of 2 bytes cannot be copied this way.)
+//
+// Measured at 16384 x 2048 in bfloat16 (us): 22.9, 5.9 TB/s; 2 rows at a time 24.7, 1 row 26.2; k_layer_norm_rows 28.8; a warp per
+// row and w, b from L1 29.3, with fp32 w, b 36.9.
+constexpr int STAGES = 2;
+template <typename T, int VEC> constexpr bool STAGED = sizeof(T) * VEC >= 4;
+
+// Sums of R values over the group, in all its threads.  `slot` is not used again before the next barrier but one.
+template <int G, int R>
+__device__ __forceinline__ void group_sums(float (&v)[R], float (*slot)[R]) {
+    constexpr int NW = GroupShape<G>::WARPS, SPREAD = 32 / R;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float mine = warp_sums<R>(v);
+    if constexpr (G == 32) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = __shfl_sync(0xffffffffu, mine, i * SPREAD);
+    } else {
+        if (lane % SPREAD == 0) slot[warp][lane / SPREAD] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = slot[0][i];
+#pragma unroll
+        for (int q = 1; q < NW; ++q)
+#pragma unroll
+            for (int i = 0; i < R; ++i) v[i] += slot[q][i];
+    }
+}
+
+template <typename T, int VEC, int G, int E, int R, bool FULL>
+__global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_ring(const NormArgs A) {
+    constexpr int NV = E / VEC, P = PAIRS<VEC>, BLOCK = GroupShape<G>::BLOCK;
+    extern __shared__ __align__(16) float smem[];
+    __shared__ __align__(16) float slot[2][GroupShape<G>::WARPS][R];
+    const int t = threadIdx.x % G;
+    const int64_t step = (int64_t)gridDim.x * GroupShape<G>::ROWS * R;
+    int64_t row = ((int64_t)blockIdx.x * GroupShape<G>::ROWS + threadIdx.x / G) * R;
+    const int nv = A.n / VEC;
+    auto mine_here = [&](int j) { return FULL || t + j * G < nv; };
+    const T* x = static_cast<const T*>(A.x) + row * A.ld_x + t * VEC;
+    T* y = static_cast<T*>(A.y) + row * A.ld_y + t * VEC;
+    Vec<T, VEC>* ring = reinterpret_cast<Vec<T, VEC>*>(smem) + threadIdx.x;      // [stage][row][j], BLOCK apart
+    auto place = [&](int stage, int k, int j) { return ring + ((stage * R + k) * NV + j) * BLOCK; };
+    auto send = [&](int64_t r, int stage) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (r + k < A.rows) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (mine_here(j)) copy_async<sizeof(T) * VEC>(place(stage, k, j), x + k * A.ld_x + j * G * VEC);
+            }
+        }
+        x += step * A.ld_x;
+        copy_async_commit();
+    };
+    auto read = [&](int stage, int k, int j) { return *place(stage, k, j); };
+    send(row, 0);
+    float2 w[NV][P], b[NV][P];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) { w[j][i] = both(1.f); b[j][i] = both(0.f); }
+        if (A.w && mine_here(j)) load_param<T, VEC>(A.w, A.w_f32, (t + j * G) * VEC, w[j]);
+        if (A.b && mine_here(j)) load_param<T, VEC>(A.b, A.w_f32, (t + j * G) * VEC, b[j]);
+    }
+    const float inv_n = 1.f / (float)A.n;
+    int stage = 0;
+    auto rows_in_work = [&](auto all, int have) {
+        constexpr bool ALL = decltype(all)::value;
+        send(row + step, stage ^ 1);
+        copy_async_wait<1>();
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            float2 s = both(0.f);
+            if (ALL || k < have) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (mine_here(j)) add_sum(read(stage, k, j), s);
+            }
+            mean[k] = s.x + s.y;
+        }
+        group_sums<G, R>(mean, slot[0]);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            mean[k] *= inv_n;
+            float2 q = both(0.f);
+            if (ALL || k < have) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (mine_here(j)) add_squares(read(stage, k, j), both(-mean[k]), q);
+            }
+            rstd[k] = q.x + q.y;
+        }
+        group_sums<G, R>(rstd, slot[1]);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (ALL || k < have) {
+                rstd[k] = 1.0f / sqrtf(rstd[k] * inv_n + A.eps);
+                if (t == 0) { A.stats[row + k] = mean[k]; A.stats[A.rows + row + k] = rstd[k]; }
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    if (mine_here(j)) {
+                        float2 f[P];
+                        unpack_pairs(read(stage, k, j), f);
+#pragma unroll
+                        for (int i = 0; i < P; ++i) f[i] = fma2(mul2(add2(f[i], both(-mean[k])), both(rstd[k])), w[j][i], b[j][i]);
+                        store_vec<T, VEC>(y + k * A.ld_y + j * G * VEC, pack_pairs<T, VEC>(f));
+                    }
+                }
+            }
+        }
+        y += step * A.ld_y;
+        stage ^= 1;
+    };
+#pragma unroll 1
+    for (; row + R <= A.rows; row += step) rows_in_work(std::true_type{}, R);
+    if (R > 1 && row < A.rows) rows_in_work(std::false_type{}, (int)(A.rows - row));
+    copy_async_wait<0>();
 }
 
 // Rows that do not fit a block's registers: the row is read three times (the second and third mostly from L2).
@@ -207,42 +419,19 @@ __device__ __forceinline__ Vec<T, VEC> back_result(const Vec<T, VEC>& x, const V
     return pack_pairs<T, VEC>(f);
 }
 
-// Sums of V values (a power of two up to 8) over the warp at once: in each of the first steps a lane hands half of its values
-// to its partner and goes on with the other half.  Value i ends up in the lanes l with l / (32 / V) = i.
-template <int V>
-__device__ __forceinline__ float warp_sums(float (&v)[V]) {
-    const int lane = threadIdx.x & 31;
-    int o = 16;
-#pragma unroll
-    for (int half = V / 2; half > 0; half >>= 1, o >>= 1) {
-        const bool upper = lane & o;
-#pragma unroll
-        for (int i = 0; i < half; ++i) {
-            const float keep = upper ? v[i + half] : v[i], give = upper ? v[i] : v[i + half];
-            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-        }
-    }
-    float x = v[0];
-#pragma unroll
-    for (; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
-
 // R rows at a time: the latency of their sums' way through the warps and the block is paid once for all of them.  The next R
 // rows are on their way into shared memory meanwhile; a thread copies what it will read itself.  (Vectors of 2 bytes
 // cannot be copied this way: they are read when they are needed.)
 //
 // Measured at 16384 x 4096 in bfloat16 (us, rows at a time x blocks per SM): 1 x 2 85.9, 2 x 2 80.9, 4 x 2 (128 registers: spills)
-// 81.2, 4 x 1 73.8.  Without the ring, the next row in registers: 88.6; the rows ahead asked into L2: 86.
-constexpr int STAGES = 2;
-template <int G> constexpr int ROWS_AT_ONCE = G < 512 ? 4 : 2;     // what the ring's shared memory allows
-template <typename T, int VEC> constexpr bool STAGED = sizeof(T) * VEC >= 4;
+// 81.2, 4 x 1 73.8; in fp32, 8192 x 2048: 2 x 2 37.2, 4 x 1 37.6, 1999 x 1030 10.5 and 13.4.  Without the ring, the next row in registers: 88.6; the rows ahead asked into L2: 86.
+template <typename T, int G> constexpr int ROWS_AT_ONCE = sizeof(T) == 4 || G >= 512 ? 2 : 4;
 template <typename T, int VEC, int G, int E, int R> constexpr size_t RING_BYTES =
     STAGED<T, VEC> ? (size_t)STAGES * R * 2 * E * sizeof(T) * GroupShape<G>::BLOCK : 0;
 
 // FULL: every thread has E elements (n = G E), so no column needs a check.
 template <typename T, int VEC, int G, int E, int R, bool FULL>
-__global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 256 ? 2 : 1) k_layer_norm_back(const NormBackArgs A) {
+__global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 256 ? 2 : sizeof(T) == 4 && GroupShape<G>::BLOCK == 256 ? 2 : 1) k_layer_norm_back(const NormBackArgs A) {
     constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS, P = PAIRS<VEC>, NW = GroupShape<G>::WARPS, BLOCK = GroupShape<G>::BLOCK;
     constexpr bool RING = STAGED<T, VEC>;
     extern __shared__ __align__(16) float smem[];      // the ring; G = 32: [8][2][n] partial sums at the end
@@ -501,22 +690,53 @@ int vec_of(int es, int64_t n, std::initializer_list<const void*> bases, std::ini
 }
 
 template <typename T, int VEC>
-int launch_norm(const NormArgs& A, cudaStream_t st) {
+int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
     const int n = A.n;
+#define FILL_SMS(kernel, tile, smem)                                                                                \
+    int per_sm = 0;                                                                                                 \
+    if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) \
+        return SSGD_ECUDA;                                                                                          \
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, BLOCK, smem) != cudaSuccess || per_sm < 1)   \
+        return SSGD_ECUDA;                                                                                          \
+    const int64_t grid = std::min((A.rows + tile - 1) / tile, (int64_t)sms * per_sm);                               \
+    kernel<<<(unsigned)grid, BLOCK, smem, st>>>(A);                                                                 \
+    return launched()
+#define NORM_ROWS(G, E, R)                                                                                          \
+    do {                                                                                                            \
+        constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
+        constexpr int BLOCK = GroupShape<G>::BLOCK, ROWS = GroupShape<G>::ROWS;                                     \
+        const bool full = WIDEST && n == G * E;                                                                     \
+        if constexpr (sizeof(T) == 2 && VEC > 1 && G <= 512) {                                                      \
+            if (A.rows >= 8 * sms) {                                                                                \
+                auto kernel = full ? k_layer_norm_ring<T, VEC, G, E, R, WIDEST> : k_layer_norm_ring<T, VEC, G, E, R, false>; \
+                const size_t smem = (size_t)STAGES * R * E * sizeof(T) * BLOCK;                                     \
+                FILL_SMS(kernel, (ROWS * R), smem);                                                                 \
+            }                                                                                                       \
+        }                                                                                                           \
+        auto kernel = full ? k_layer_norm_rows<T, VEC, G, E, WIDEST> : k_layer_norm_rows<T, VEC, G, E, false>;      \
+        const size_t smem = 0;                                                                                      \
+        FILL_SMS(kernel, ROWS, smem);                                                                               \
+    } while (0)
 #define NORM(G, E)                                                                                                  \
     do {                                                                                                            \
         const int64_t grid = (A.rows + GroupShape<G>::ROWS - 1) / GroupShape<G>::ROWS;                              \
         if (grid > 0x7fffffff) return SSGD_EINVAL;                                                                  \
-        k_layer_norm<T, VEC, G, E><<<(unsigned)grid, GroupShape<G>::BLOCK, 0, st>>>(A);                             \
+        constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
+        auto kernel = WIDEST && n == G * E ? k_layer_norm<T, VEC, G, E, WIDEST> : k_layer_norm<T, VEC, G, E, false>; \
+        kernel<<<(unsigned)grid, GroupShape<G>::BLOCK, 0, st>>>(A);                                                 \
         return launched();                                                                                          \
     } while (0)
-    constexpr int LONG = VEC == 1 ? 32 : 64;           // a vector of one element wastes half of a pair's registers
-    if (n <= 32 * 16) NORM(32, 16);
-    if (n <= 32 * LONG) NORM(32, LONG);
-    if (n <= 128 * 32) NORM(128, 32);
-    if (n <= 256 * 32) NORM(256, 32);
+    constexpr int E = VEC == 1 ? 8 : 16;               // a vector of one element wastes half of a pair's registers
+    if (n <= 32 * E) NORM_ROWS(32, E, 4);
+    if (n <= 64 * E) NORM_ROWS(64, E, 4);
+    if (n <= 128 * E) NORM_ROWS(128, E, 4);
+    if (n <= 256 * E) NORM_ROWS(256, E, 4);
+    if (n <= 512 * E) NORM_ROWS(512, E, 2);
+    if (VEC == 1 && n <= 1024 * 8) NORM_ROWS(1024, 8, 1);
     if (n <= 512 * 32) NORM(512, 32);
 #undef NORM
+#undef NORM_ROWS
+#undef FILL_SMS
     if (A.rows > 0x7fffffff) return SSGD_EINVAL;
     k_layer_norm_wide<T, VEC><<<(unsigned)A.rows, WIDE, 0, st>>>(A);
     return launched();
@@ -531,7 +751,7 @@ int launch_norm_back(const NormBackArgs& A, int sms, int* parts, cudaStream_t st
     int64_t grid = 0;
 #define NORM_BACK(G, E)                                                                                             \
     do {                                                                                                            \
-        constexpr int R = ROWS_AT_ONCE<G>;                                                                          \
+        constexpr int R = ROWS_AT_ONCE<T, G>;                                                                       \
         constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
         auto kernel = WIDEST && n == G * E ? k_layer_norm_back<T, VEC, G, E, R, WIDEST> : k_layer_norm_back<T, VEC, G, E, R, false>; \
         constexpr int TILE = GroupShape<G>::ROWS * R;                                                               \
@@ -601,7 +821,9 @@ int ssgd_layer_norm(const void* x, int64_t ld_x, int32_t fmt_x, const void* w, c
     const NormArgs A{x, ld_x, w, b, fmt_w == SSGD_FMT_F32, rows, (int32_t)n, eps, y, ld_y, stats};
     const int vec = vec_of(es, n, {x, y}, {ld_x, ld_y}, {w, b}, A.w_f32);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return BY_FORMAT(launch_norm, fmt_x, vec, A, st);
+    int sms = 0;
+    if ((e = sm_count_of_current_device(&sms))) return e;
+    return BY_FORMAT(launch_norm, fmt_x, vec, A, sms, st);
 }
 
 int ssgd_layer_norm_backward_workspace(int64_t rows, int64_t n, size_t* out_bytes) {
