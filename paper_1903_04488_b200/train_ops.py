@@ -24,7 +24,7 @@ _FMT = {torch.float32: S.FMT_F32, torch.float16: S.FMT_F16, torch.bfloat16: S.FM
 _native = None
 
 
-def _load():
+def native():
     """The native module.  Raises if it, or the library, has not been built."""
     global _native
     if _native is None:
@@ -47,7 +47,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     """(y, stats): layer norm over the last dimension of x, and each row's mean and 1 / standard deviation, [2][rows] fp32.
 
     weight, bias: [n], float32 or x's type, both the same.  out: where y goes (x's shape and type; may be x itself)."""
-    return (_native or _load()).layer_norm(x, weight, bias, eps, out)
+    return (_native or native()).layer_norm(x, weight, bias, eps, out)
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, stats: torch.Tensor, *,
@@ -57,7 +57,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
 
     dx, dw, db: where the results go (dx may be dy itself; dw and db may be pieces of a flat gradient).  accumulate adds
     dw and db to what is there."""
-    return (_native or _load()).layer_norm_backward(dy, x, weight, stats, dx, dw, db, accumulate, need_params)
+    return (_native or native()).layer_norm_backward(dy, x, weight, stats, dx, dw, db, accumulate, need_params)
 
 
 # ---- log probabilities of given tokens ---------------------------------------------------------------
@@ -86,7 +86,7 @@ class TokenLogprobs:
 def token_logprobs(logits: torch.Tensor, ids: torch.Tensor, *, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
     """Log probability of ids[row] under softmax(scale * logits[row]), the distribution's entropy, log sum exp and the
     `top` best alternatives.  logits [rows][vocab]; ids [rows] int64 or int32 (outside the vocabulary: ignored)."""
-    return TokenLogprobs(*(_native or _load()).token_logprobs(logits, ids, top, scale))
+    return TokenLogprobs(*(_native or native()).token_logprobs(logits, ids, top, scale))
 
 
 def token_logprobs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.Tensor, d_logp: torch.Tensor | None, *,
@@ -95,7 +95,7 @@ def token_logprobs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.
                             out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient with respect to the logits of sum(d_logp logp) + sum(d_entropy entropy) + sum(d_top top_logp), in the
     logits' type.  lse, entropy, top_idx: from the forward pass with the same scale.  out may be the logits themselves."""
-    return (_native or _load()).token_logprobs_backward(logits, ids, lse, d_logp, entropy, d_entropy, top_idx, d_top, scale, out)
+    return (_native or native()).token_logprobs_backward(logits, ids, lse, d_logp, entropy, d_entropy, top_idx, d_top, scale, out)
 
 
 # ---- AdamW over many tensors -------------------------------------------------------------------------
@@ -175,6 +175,6 @@ class AdamW:
         """One step.  grads: one contiguous tensor per parameter (float32, bfloat16 or float16, all the same type), None
         for a parameter that is left alone.  seed: round e4m3 states and bfloat16 parameters stochastically with it (another
         one every step).  grad_scale: float32 scalar on the device that multiplies every gradient."""
-        (_native or _load()).adamw_step(self._desc_p, grads, self._dev, *self._fmt, self.lr if lr is None else lr, *self.betas,
+        (_native or native()).adamw_step(self._desc_p, grads, self._dev, *self._fmt, self.lr if lr is None else lr, *self.betas,
                                         self.eps, self.weight_decay, self.step_count + 1, grad_scale, seed, len(self.params))
         self.step_count += 1
