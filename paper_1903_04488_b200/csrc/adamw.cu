@@ -30,8 +30,7 @@ constexpr int FEW_TENSORS = 40;            // 3 KB: small arguments cost less to
 constexpr int QBLOCK = SSGD_ADAMW_BLOCK;   // elements per scale
 constexpr int UNROLL32 = 2;                // vectors of 4 per thread and chunk (fp32 states)
 constexpr int CHUNK32 = THREADS * 4 * UNROLL32;
-constexpr int BLOCKS8 = 4;                 // blocks of 256 per warp and chunk (8-bit states)
-constexpr int CHUNK8 = (THREADS / 32) * BLOCKS8 * QBLOCK;
+constexpr int MAX_BLOCKS8 = 8;             // blocks of 256 per warp and chunk (8-bit states): up to this many
 
 struct Entry {
     void* p; const void* g; void* m; void* v; float* ms; float* vs; void* copy;
@@ -44,6 +43,7 @@ struct Hyper {
     float sqrt_b2, sqrt_omb2;
     const float* grad_scale;
     int32_t copy_f16;    // the copy is binary16, else bfloat16
+    int32_t blocks8;     // blocks per warp and chunk (8-bit states)
 };
 template <int CAP>
 struct Table {
@@ -183,10 +183,17 @@ __device__ __forceinline__ float2 e4m3_pair(uint32_t codes) {
 // Rounding to e4m3 in the bits of fp32.  y in [-448, 448] times 2^-120 is an fp32 number (a subnormal where e4m3 has
 // subnormals) whose exponent and first three fraction bits ARE the code, at bit 20: adding a dither in [0, 2^20) to the bits
 // and dropping the lower 20 rounds up with the probability of the dropped part, carries into the exponent included.
-// Shifted left by 4 with the sign put in front, the upper byte of the result is the code.
-__device__ __forceinline__ uint32_t e4m3_in_top_byte(uint32_t x) { return ((x << 4) & 0x7fffffffu) | (x & 0x80000000u); }
-__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+// The codes of four such sums x (sign in front), in one word.  Two at a time: their upper halves side by side and shifted left by
+// 4, each half's upper byte is a code once the sign is put in front of it again.
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t e4m3_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    const uint32_t ab = __byte_perm(a, b, 0x7632), cd = __byte_perm(c, d, 0x7632);
+    uint32_t lo = ab << 4, hi = cd << 4;
+    if (SIGNED) {
+        lo = (lo & 0x7fff7fffu) | (ab & 0x80008000u);
+        hi = (hi & 0x7fff7fffu) | (cd & 0x80008000u);
+    }
+    return __byte_perm(lo, hi, 0x7531);
 }
 __device__ __forceinline__ float sqrt_fast(float x) {
     float y;
@@ -230,15 +237,35 @@ __device__ __forceinline__ void eight(const Vec<T, 16 / sizeof(T)> (&v)[sizeof(T
         f[2] = make_float2(v[1].e[0], v[1].e[1]); f[3] = make_float2(v[1].e[2], v[1].e[3]);
     }
 }
+// A block on its way through shared memory; each lane copies what it will read itself
+template <typename P, typename G>
+struct alignas(16) Staged {
+    Vec<P, 16 / sizeof(P)> p[sizeof(P) / 2][32];
+    Vec<G, 16 / sizeof(G)> g[sizeof(G) / 2][32];
+    uint2 m[32], v[32];
+};
 // `at`: the lane's first element within the chunk
 template <typename P, typename G>
-__device__ __forceinline__ void fetch(Block<P, G>& b, const Chunk<P, G>& C, uint32_t at) {
+__device__ __forceinline__ void send(Staged<P, G>& s, const Chunk<P, G>& C, uint32_t at) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int k = 0; k < (int)sizeof(P) / 2; ++k) b.p[k] = load_vec_stream<P, 16 / sizeof(P)>(C.p + at + k * 4);
+    for (int k = 0; k < (int)sizeof(P) / 2; ++k) copy_async<16>(&s.p[k][lane], C.p + at + k * 4);
 #pragma unroll
-    for (int k = 0; k < (int)sizeof(G) / 2; ++k) b.g[k] = load_vec_stream<G, 16 / sizeof(G)>(C.g + at + k * 4);
-    b.m = __ldcs(reinterpret_cast<const uint2*>(C.m + at));
-    b.v = __ldcs(reinterpret_cast<const uint2*>(C.v + at));
+    for (int k = 0; k < (int)sizeof(G) / 2; ++k) copy_async<16>(&s.g[k][lane], C.g + at + k * 4);
+    copy_async<8>(&s.m[lane], C.m + at);
+    copy_async<8>(&s.v[lane], C.v + at);
+}
+template <typename P, typename G>
+__device__ __forceinline__ Block<P, G> taken(const Staged<P, G>& s) {
+    const int lane = threadIdx.x & 31;
+    Block<P, G> b;
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(P) / 2; ++k) b.p[k] = s.p[k][lane];
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(G) / 2; ++k) b.g[k] = s.g[k][lane];
+    b.m = s.m[lane];
+    b.v = s.v[lane];
+    return b;
 }
 
 // The step's constants in the form the 8-bit kernel uses them
@@ -355,25 +382,23 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
                 dv = upper & 0xffff0u;
                 if (sizeof(P) == 2) np[q] = __float_as_uint(part(fp, j)) + (((r ^ (r >> 16)) * 0x9E3779B9u) >> 16);
             }
-            code_m[q] = e4m3_in_top_byte(__float_as_uint(j & 1 ? ym.y : ym.x) + dm + 8u);
+            code_m[q] = __float_as_uint(j & 1 ? ym.y : ym.x) + dm + 8u;
             code_v[q] = __float_as_uint(j & 1 ? yr.y : yr.x) + dv + 8u;
-            least_v = min(least_v, code_v[q]);
+            if (q & 1) least_v = __vimin3_u32(least_v, code_v[q - 1], code_v[q]);
         }
         if (least_v < 1u << 20) {                            // a positive value keeps at least the smallest code
 #pragma unroll
             for (int q = 0; q < 4; ++q) code_v[q] = max(code_v[q], part(fr, half * 4 + q) > 0.f ? 1u << 20 : 0u);
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) code_v[q] <<= 4;
-        if (odd) {
+        if (odd) {                                           // the format's NaN, 0x7f
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (!finite(part(fm, half * 4 + q))) code_m[q] = 0x7fu << 24;
-                if (!finite(part(fr, half * 4 + q))) code_v[q] = 0x7fu << 24;
+                if (!finite(part(fm, half * 4 + q))) code_m[q] = 0x7fu << 20;
+                if (!finite(part(fr, half * 4 + q))) code_v[q] = 0x7fu << 20;
             }
         }
-        out_m[half] = top_bytes(code_m[0], code_m[1], code_m[2], code_m[3]);
-        out_v[half] = top_bytes(code_v[0], code_v[1], code_v[2], code_v[3]);
+        out_m[half] = e4m3_codes<true>(code_m[0], code_m[1], code_m[2], code_m[3]);
+        out_v[half] = e4m3_codes<false>(code_v[0], code_v[1], code_v[2], code_v[3]);
         if constexpr (sizeof(P) == 2) {                      // bfloat16 parameters: the new value in the upper half of a word
             if (!STOCHASTIC || odd) {                        // to nearest, or what is not finite, which no dither may touch
 #pragma unroll
@@ -418,47 +443,55 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
 }
 
 
-// A warp takes BLOCKS8 blocks, 8 apart (its neighbours have those between); the next one is read while one is computed.  The
-// chunk's 32 scales are read and written as a whole: a store of 4 bytes per block made the kernel's memory traffic alone
+// A warp takes h.blocks8 blocks, 8 apart (its neighbours have those between); the next one is on its way while one is computed.
+// The chunk's scales are read and written as a whole: a store of 4 bytes per block made the kernel's memory traffic alone
 // 206 instead of 144 us at 90M elements.
+constexpr int STAGES8 = 2;
 template <typename P, typename G, int CAP, bool STOCHASTIC>
-__global__ void __launch_bounds__(THREADS, 3) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {
+__global__ void __launch_bounds__(THREADS, 4) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {
     constexpr int WARPS = THREADS / 32, STEP = WARPS * QBLOCK;
-    static_assert(WARPS * BLOCKS8 == 32, "a lane per scale");
-    __shared__ float scales[2][32];
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float scales[2][WARPS * MAX_BLOCKS8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Staged<P, G>* ring = reinterpret_cast<Staged<P, G>*>(smem) + warp * STAGES8;
     const int k = tensor_of(T, blockIdx.x);
     const Entry& E = T.t[k];
-    const int64_t chunk = blockIdx.x - T.first[k], begin = chunk * CHUNK8;
-    const bool vectors = E.head == 0;
+    const int nb = T.h.blocks8, nscales = WARPS * nb, size = STEP * nb;
+    const int64_t chunk = blockIdx.x - T.first[k], begin = chunk * size;
     const Chunk<P, G> C{static_cast<P*>(E.p) + begin, static_cast<const G*>(E.g) + begin, static_cast<uint8_t*>(E.m) + begin,
                         static_cast<uint8_t*>(E.v) + begin, E.copy ? static_cast<unsigned short*>(E.copy) + begin : nullptr,
-                        E.n - begin < CHUNK8 ? (int32_t)(E.n - begin) : CHUNK8};
+                        E.n - begin < size ? (int32_t)(E.n - begin) : size};
     const uint32_t index = E.key ^ (uint32_t)begin ^ ((uint32_t)((uint64_t)begin >> 32) * 0x9E3779B9u);
+    const int32_t vectors = E.head == 0 ? C.n / QBLOCK * QBLOCK : 0;    // blocks up to here are whole and aligned
     int32_t first = warp * QBLOCK;
-    Block<P, G> in;
-    if (vectors && first + QBLOCK <= C.n) fetch(in, C, first + lane * 8);
-    float* const mine = (warp == 0 ? E.ms : E.vs) + chunk * (WARPS * BLOCKS8) + lane;    // warps 0 and 1 look after the scales
-    const bool scale_here = warp < 2 && lane * QBLOCK < C.n;
-    if (scale_here) scales[warp][lane] = *mine;
+#pragma unroll
+    for (int s = 0; s < STAGES8 - 1; ++s) {
+        if (s < nb && first + s * STEP < vectors) send(ring[s], C, first + s * STEP + lane * 8);
+        copy_async_commit();
+    }
+    const int which = threadIdx.x >= THREADS / 2, mine = threadIdx.x % (THREADS / 2);     // one scale to a thread
+    float* const scale = (which ? E.vs : E.ms) + chunk * nscales + mine;
+    const bool has_scale = mine < nscales && mine * QBLOCK < C.n;
+    if (has_scale) scales[which][mine] = *scale;
     const float gs = T.h.grad_scale ? *T.h.grad_scale : 1.f;
-    const float sqrt_omb2 = T.h.sqrt_omb2;
-    const Hyper8 h{T.h.b1, T.h.omb1 * gs, T.h.sqrt_b2, sqrt_omb2 * gs, T.h.keep, -T.h.step_size, T.h.inv_bc2, T.h.eps};
+    const Hyper8 h{T.h.b1, T.h.omb1 * gs, T.h.sqrt_b2, T.h.sqrt_omb2 * gs, T.h.keep, -T.h.step_size, T.h.inv_bc2, T.h.eps};
     __syncthreads();
+    int stage = 0;
 #pragma unroll 1
-    for (int i = 0; i < BLOCKS8 && first < C.n; ++i, first += STEP) {
+    for (int i = 0; i < nb && first < C.n; ++i, first += STEP) {
         float& ms = scales[0][i * WARPS + warp];
         float& vs = scales[1][i * WARPS + warp];
-        if (vectors && first + QBLOCK <= C.n) {
-            const Block<P, G> now = in;
-            if (i + 1 < BLOCKS8 && first + STEP + QBLOCK <= C.n) fetch(in, C, first + STEP + lane * 8);
-            block8<P, G, STOCHASTIC, true>(h, index, C, first, now, T.h.copy_f16, ms, vs);
-        } else {
-            block8<P, G, STOCHASTIC, false>(h, index, C, first, in, T.h.copy_f16, ms, vs);
-        }
+        const int32_t later = first + (STAGES8 - 1) * STEP;
+        if (i + STAGES8 - 1 < nb && later < vectors) send(ring[stage == 0 ? STAGES8 - 1 : stage - 1], C, later + lane * 8);
+        copy_async_commit();
+        copy_async_wait<STAGES8 - 1>();
+        if (first < vectors) block8<P, G, STOCHASTIC, true>(h, index, C, first, taken(ring[stage]), T.h.copy_f16, ms, vs);
+        else block8<P, G, STOCHASTIC, false>(h, index, C, first, Block<P, G>{}, T.h.copy_f16, ms, vs);
+        stage = stage == STAGES8 - 1 ? 0 : stage + 1;
     }
+    copy_async_wait<0>();
     __syncthreads();
-    if (scale_here) *mine = scales[warp][lane];
+    if (has_scale) *scale = scales[which][mine];
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
@@ -490,7 +523,7 @@ int launch_group(const ssgd_adamw_tensor* t, int32_t first, int32_t count, bool 
         e.key = mix(key + (uint32_t)i);
         e.head = head_of(t[i], sizeof(P), sizeof(G), small ? 1 : 4, small ? 8 : 4, !small);
         T.first[k++] = (uint32_t)chunks;
-        const int64_t chunk = small ? CHUNK8 : CHUNK32;
+        const int64_t chunk = small ? (int64_t)(THREADS / 32) * QBLOCK * h.blocks8 : CHUNK32;
         // the last chunk of a tensor takes what the head has pushed out of the others
         const int64_t body = e.head > 0 ? (e.n > e.head ? e.n - e.head : 1) : e.n;
         chunks += (uint64_t)((body + chunk - 1) / chunk);
@@ -500,8 +533,11 @@ int launch_group(const ssgd_adamw_tensor* t, int32_t first, int32_t count, bool 
     T.first[k] = (uint32_t)chunks;
     T.count = k;
     if (small) {
-        if (stochastic) k_adamw_8bit<P, G, CAP, true><<<(unsigned)chunks, THREADS, 0, st>>>(T);
-        else k_adamw_8bit<P, G, CAP, false><<<(unsigned)chunks, THREADS, 0, st>>>(T);
+        auto kernel = stochastic ? k_adamw_8bit<P, G, CAP, true> : k_adamw_8bit<P, G, CAP, false>;
+        const int smem = (int)sizeof(Staged<P, G>) * (THREADS / 32) * STAGES8;
+        if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+            return SSGD_ECUDA;
+        kernel<<<(unsigned)chunks, THREADS, smem, st>>>(T);
     } else {
         if (stochastic && sizeof(P) == 2) k_adamw_f32<P, G, CAP, true><<<(unsigned)chunks, THREADS, 0, st>>>(T);
         else k_adamw_f32<P, G, CAP, false><<<(unsigned)chunks, THREADS, 0, st>>>(T);
@@ -561,6 +597,18 @@ extern "C" int ssgd_adamw_step(const ssgd_adamw_tensor* tensors, int32_t count, 
     h.eps = (float)eps;
     h.grad_scale = grad_scale;
     h.copy_f16 = fmt_copy == SSGD_FMT_F16;
+    h.blocks8 = 1;
+    int64_t blocks = 0;
+    for (int32_t i = 0; i < count; ++i) blocks += (tensors[i].n + QBLOCK - 1) / QBLOCK;
+    if (blocks == 0) return SSGD_OK;
+    if (small) {
+        // As many blocks to a warp as leave 4 CTAs to an SM: one after the other they take a microsecond each, but share a CTA's
+        // start and end.  8 blocks / 1 block: 79,247 elements in 22 tensors 12.4 / 5.1 us; 8 / 4 blocks: 90M 175 / 182.
+        int sms = 0;
+        const int e = sm_count_of_current_device(&sms);
+        if (e) return e;
+        while (h.blocks8 < MAX_BLOCKS8 && blocks >= (int64_t)h.blocks8 * 2 * (THREADS / 32) * 4 * sms) h.blocks8 *= 2;
+    }
     const uint32_t key = mix(mix((uint32_t)seed) ^ (uint32_t)(seed >> 32));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool sr = stochastic != 0;
