@@ -181,6 +181,23 @@ inline int sm_count_of_current_device(int* out) {
     return SSGD_OK;
 }
 
+// CTAs of a kernel that fit an SM at once (asked once per kernel and device: the answer does not change, and asking costs as
+// much as a launch).  `known` belongs to the kernel; smem above 40 KB is opted into on the way.
+template <typename K>
+inline int residency(K kernel, int block, size_t smem, int (&known)[64], int* out) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SSGD_ECUDA;
+    if (!known[dev]) {
+        int n = 0;
+        if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+            return SSGD_ECUDA;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem) != cudaSuccess || n < 1) return SSGD_ECUDA;
+        known[dev] = n;      // the same value whichever thread stores it
+    }
+    *out = known[dev];
+    return SSGD_OK;
+}
+
 template <typename... P, typename... A>
 int launch_after(cudaStream_t st, void (*kernel)(P...), dim3 grid, int block, A... args) {
     cudaLaunchConfig_t cfg{};

@@ -9,9 +9,12 @@
 // the mean of squared deviations from the mean already known, not a difference of large sums.
 #include <algorithm>
 
+#include <cooperative_groups.h>
+
 #include "formats.cuh"
 
 using namespace ssgd;
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -384,6 +387,7 @@ struct NormBackArgs {
     void* dx; int64_t ld_dx;
     float* partial;      // [grid][2][n]; NULL: neither dw nor db is wanted
     float* row_sums;     // wide rows: [rows][2]
+    int32_t slab;        // columns per CTA of a cluster
 };
 
 // What a vector adds to the row's two sums (of a and a h) and to the columns' sums over the rows
@@ -429,15 +433,21 @@ template <typename T, int G> constexpr int ROWS_AT_ONCE = sizeof(T) == 4 || G >=
 template <typename T, int VEC, int G, int E, int R> constexpr size_t RING_BYTES =
     STAGED<T, VEC> ? (size_t)STAGES * R * 2 * E * sizeof(T) * GroupShape<G>::BLOCK : 0;
 
-// FULL: every thread has E elements (n = G E), so no column needs a check.
-template <typename T, int VEC, int G, int E, int R, bool FULL>
+// FULL: every thread has E elements (n = G E), so no column needs a check.  SHARED: a cluster of CTAs shares the rows, each with a
+// slab of A.slab columns; their sums of a row meet in distributed shared memory.
+template <typename T, int VEC, int G, int E, int R, bool FULL, bool SHARED>
 __global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 256 ? 2 : sizeof(T) == 4 && GroupShape<G>::BLOCK == 256 ? 2 : 1) k_layer_norm_back(const NormBackArgs A) {
     constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS, P = PAIRS<VEC>, NW = GroupShape<G>::WARPS, BLOCK = GroupShape<G>::BLOCK;
     constexpr bool RING = STAGED<T, VEC>;
     extern __shared__ __align__(16) float smem[];      // the ring; G = 32: [8][2][n] partial sums at the end
     __shared__ __align__(16) float slot[2][NW][2 * R];
+    __shared__ __align__(16) float across[2][8][2 * R];    // SHARED: each CTA's sums
+    cg::cluster_group cluster = cg::this_cluster();
     const int t = threadIdx.x % G, sub = threadIdx.x / G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int nv = A.n / VEC;
+    const int parts = SHARED ? (int)cluster.num_blocks() : 1, part = SHARED ? (int)cluster.block_rank() : 0;
+    const int col0 = SHARED ? part * A.slab : 0, here = SHARED ? min(A.slab, A.n - col0) : A.n;
+    const int64_t block = SHARED ? blockIdx.x / parts : blockIdx.x, blocks = SHARED ? gridDim.x / parts : gridDim.x;
+    const int nv = here / VEC;
     const float inv_n = 1.0f / (float)A.n;
     auto mine_here = [&](int j) { return FULL || t + j * G < nv; };
     float2 dw[NV][P], db[NV][P], w[NV][P];
@@ -445,14 +455,14 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 2
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
         for (int i = 0; i < P; ++i) { dw[j][i] = db[j][i] = both(0.f); w[j][i] = both(1.f); }
-        if (A.w && mine_here(j)) load_param<T, VEC>(A.w, A.w_f32, (t + j * G) * VEC, w[j]);
+        if (A.w && mine_here(j)) load_param<T, VEC>(A.w, A.w_f32, col0 + (t + j * G) * VEC, w[j]);
     }
-    const int64_t step = (int64_t)gridDim.x * ROWS * R;
-    int64_t row = ((int64_t)blockIdx.x * ROWS + sub) * R;
+    const int64_t step = blocks * ROWS * R;
+    int64_t row = (block * ROWS + sub) * R;
     // this thread's part of the rows in work: dx and (RING: of the rows to be sent next, else of those in work) x, dy
-    const T* x = static_cast<const T*>(A.x) + t * VEC + row * A.ld_x;
-    const T* dy = static_cast<const T*>(A.dy) + t * VEC + row * A.ld_dy;
-    T* dx = static_cast<T*>(A.dx) + t * VEC + row * A.ld_dx;
+    const T* x = static_cast<const T*>(A.x) + col0 + t * VEC + row * A.ld_x;
+    const T* dy = static_cast<const T*>(A.dy) + col0 + t * VEC + row * A.ld_dy;
+    T* dx = static_cast<T*>(A.dx) + col0 + t * VEC + row * A.ld_dx;
     Vec<T, VEC>* ring = reinterpret_cast<Vec<T, VEC>*>(smem) + threadIdx.x;      // [stage][row][x, dy][j], BLOCK apart
     auto place = [&](int stage, int k, int which, int j) { return ring + (((stage * R + k) * 2 + which) * NV + j) * BLOCK; };
     auto send = [&](int64_t r, int stage) {
@@ -493,6 +503,7 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 2
         }
     };
     next_stats(row);
+    if constexpr (SHARED) cluster.sync();              // all are there before any of them is written to
     int turn = 0, stage = 0;
     // R rows, all of them there (ALL) or not
     auto rows_in_work = [&](auto all, int have) {
@@ -535,6 +546,20 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 2
                 for (int k = 0; k < R; ++k) total[k] = add2(total[k], *reinterpret_cast<const float2*>(&slot[turn][q][2 * k]));
 #pragma unroll
             for (int k = 0; k < R; ++k) { sums[2 * k] = total[k].x; sums[2 * k + 1] = total[k].y; }
+            if constexpr (SHARED) {
+                // to every CTA of the cluster; read behind its barrier, and not written again before the next but one
+                if ((int)threadIdx.x < parts) {
+                    float2* to = reinterpret_cast<float2*>(cluster.map_shared_rank(&across[turn][part][0], threadIdx.x));
+#pragma unroll
+                    for (int k = 0; k < R; ++k) to[k] = total[k];
+                }
+                cluster.sync();
+#pragma unroll
+                for (int i = 0; i < 2 * R; ++i) sums[i] = across[turn][0][i];
+                for (int q = 1; q < parts; ++q)
+#pragma unroll
+                    for (int i = 0; i < 2 * R; ++i) sums[i] += across[turn][q][i];
+            }
             turn ^= 1;
         }
 #pragma unroll
@@ -555,9 +580,10 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 2
     for (; row + R <= A.rows; row += step) rows_in_work(std::true_type{}, R);
     if (R > 1 && row < A.rows) rows_in_work(std::false_type{}, (int)(A.rows - row));
     if constexpr (RING) copy_async_wait<0>();
+    if constexpr (SHARED) cluster.sync();              // nobody leaves while others write to its shared memory
     successor_may_start();                             // k_norm_reduce waits for the partial sums by itself
     if (!A.partial) return;
-    float* out = A.partial + (int64_t)blockIdx.x * 2 * A.n;
+    float* out = A.partial + block * 2 * A.n + col0;
     float* mine = G == 32 ? smem + (int64_t)sub * 2 * A.n : out;
     if (G == 32) __syncthreads();                      // every warp is done with the ring
 #pragma unroll
@@ -689,18 +715,20 @@ int vec_of(int es, int64_t n, std::initializer_list<const void*> bases, std::ini
     return 1;
 }
 
+// A grid that fills the SMs; `smem` depends on the kernel alone
+template <typename K>
+int launch_filling(K kernel, const NormArgs& A, int block, int64_t tile, size_t smem, int (&known)[64], int sms, cudaStream_t st) {
+    int per_sm = 0;
+    const int e = residency(kernel, block, smem, known, &per_sm);
+    if (e) return e;
+    const int64_t grid = std::min((A.rows + tile - 1) / tile, (int64_t)sms * per_sm);
+    kernel<<<(unsigned)grid, block, smem, st>>>(A);
+    return launched();
+}
+
 template <typename T, int VEC>
 int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
     const int n = A.n;
-#define FILL_SMS(kernel, tile, smem)                                                                                \
-    int per_sm = 0;                                                                                                 \
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) \
-        return SSGD_ECUDA;                                                                                          \
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, BLOCK, smem) != cudaSuccess || per_sm < 1)   \
-        return SSGD_ECUDA;                                                                                          \
-    const int64_t grid = std::min((A.rows + tile - 1) / tile, (int64_t)sms * per_sm);                               \
-    kernel<<<(unsigned)grid, BLOCK, smem, st>>>(A);                                                                 \
-    return launched()
 #define NORM_ROWS(G, E, R)                                                                                          \
     do {                                                                                                            \
         constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
@@ -708,14 +736,14 @@ int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
         const bool full = WIDEST && n == G * E;                                                                     \
         if constexpr (sizeof(T) == 2 && VEC > 1 && G <= 512) {                                                      \
             if (A.rows >= 8 * sms) {                                                                                \
+                static int known[2][64];                                                                            \
                 auto kernel = full ? k_layer_norm_ring<T, VEC, G, E, R, WIDEST> : k_layer_norm_ring<T, VEC, G, E, R, false>; \
-                const size_t smem = (size_t)STAGES * R * E * sizeof(T) * BLOCK;                                     \
-                FILL_SMS(kernel, (ROWS * R), smem);                                                                 \
+                return launch_filling(kernel, A, BLOCK, ROWS * R, (size_t)STAGES * R * E * sizeof(T) * BLOCK, known[full], sms, st); \
             }                                                                                                       \
         }                                                                                                           \
+        static int known[2][64];                                                                                    \
         auto kernel = full ? k_layer_norm_rows<T, VEC, G, E, WIDEST> : k_layer_norm_rows<T, VEC, G, E, false>;      \
-        const size_t smem = 0;                                                                                      \
-        FILL_SMS(kernel, ROWS, smem);                                                                               \
+        return launch_filling(kernel, A, BLOCK, ROWS, 0, known[full], sms, st);                                     \
     } while (0)
 #define NORM(G, E)                                                                                                  \
     do {                                                                                                            \
@@ -736,45 +764,71 @@ int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
     if (n <= 512 * 32) NORM(512, 32);
 #undef NORM
 #undef NORM_ROWS
-#undef FILL_SMS
     if (A.rows > 0x7fffffff) return SSGD_EINVAL;
     k_layer_norm_wide<T, VEC><<<(unsigned)A.rows, WIDE, 0, st>>>(A);
     return launched();
 }
 
 constexpr int64_t PART_BLOCKS = 148 * 4;         // at most so many partial sums of dw and db
-constexpr int BACK_NARROW = 512 * 8;             // rows up to here stay in a block's registers, whatever the format
+constexpr int BACK_NARROW = 8 * 256 * 8;         // rows up to here never need the sums of k_norm_back_sums
 
 template <typename T, int VEC>
-int launch_norm_back(const NormBackArgs& A, int sms, int* parts, cudaStream_t st) {
+int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
     const int n = A.n;
     int64_t grid = 0;
 #define NORM_BACK(G, E)                                                                                             \
     do {                                                                                                            \
-        constexpr int R = ROWS_AT_ONCE<T, G>;                                                                       \
+        constexpr int R = ROWS_AT_ONCE<T, G>, BLOCK = GroupShape<G>::BLOCK, TILE = GroupShape<G>::ROWS * R;         \
         constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
-        auto kernel = WIDEST && n == G * E ? k_layer_norm_back<T, VEC, G, E, R, WIDEST> : k_layer_norm_back<T, VEC, G, E, R, false>; \
-        constexpr int TILE = GroupShape<G>::ROWS * R;                                                               \
+        static int known[2][64];                                                                                    \
+        const bool full = WIDEST && n == G * E;                                                                     \
+        auto kernel = full ? k_layer_norm_back<T, VEC, G, E, R, WIDEST, false> : k_layer_norm_back<T, VEC, G, E, R, false, false>; \
         size_t smem = RING_BYTES<T, VEC, G, E, R>;                                                                  \
-        if (G == 32) smem = std::max(smem, (size_t)GroupShape<G>::ROWS * 2 * n * 4);                                \
-        if (smem > 40 * 1024 &&                                                                                     \
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)    \
-            return SSGD_ECUDA;                                                                                      \
+        if (G == 32) smem = std::max(smem, (size_t)GroupShape<G>::ROWS * 2 * G * E * 4);                            \
         int per_sm = 0;                                                                                             \
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, GroupShape<G>::BLOCK, smem) != cudaSuccess || \
-            per_sm < 1)                                                                                             \
-            return SSGD_ECUDA;                                                                                      \
+        const int e = residency(kernel, BLOCK, smem, known[full], &per_sm);                                         \
+        if (e) return e;                                                                                            \
         grid = std::min({(A.rows + TILE - 1) / TILE, (int64_t)sms * per_sm, PART_BLOCKS});                          \
-        kernel<<<(unsigned)grid, GroupShape<G>::BLOCK, smem, st>>>(A);                                              \
+        kernel<<<(unsigned)grid, BLOCK, smem, st>>>(A);                                                             \
         *parts = (int)grid;                                                                                         \
         return launched();                                                                                          \
     } while (0)
-    // 16 elements of 16 bits per thread or 8 of 32 bits: with their sums and the next row's on the way, 128 registers
+    // 16 elements of 16 bits per thread or 8 of 32 bits: with their sums, 128 registers
     constexpr int E = sizeof(T) == 4 || VEC == 1 ? 8 : 16;
     if (n <= 32 * E) NORM_BACK(32, E);
     if (n <= 128 * E) NORM_BACK(128, E);
     if (n <= 256 * E) NORM_BACK(256, E);
     if (n <= 512 * E) NORM_BACK(512, E);
+    if (n <= 8 * 256 * E) {
+        // a cluster of 4 or 8 CTAs to the rows
+        constexpr int G = 256, R = ROWS_AT_ONCE<T, G>;
+        static int known[64], clusters[2][64];
+        auto kernel = k_layer_norm_back<T, VEC, G, E, R, false, true>;
+        const size_t smem = RING_BYTES<T, VEC, G, E, R>;
+        int per_sm = 0, dev = 0;
+        const int e = residency(kernel, G, smem, known, &per_sm);
+        if (e) return e;
+        const int cluster = n <= 4 * G * E ? 4 : 8;
+        A.slab = ((n + cluster - 1) / cluster + 8 - 1) / 8 * 8;            // whole vectors
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)cluster);
+        cfg.blockDim = dim3(G);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)cluster;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        // clusters lie within a group of SMs: fewer of them fit than their CTAs alone would
+        int& fit = clusters[cluster == 8][cudaGetDevice(&dev) == cudaSuccess && dev < 64 ? dev : 0];
+        if (!fit && (cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) != cudaSuccess || fit < 1)) return SSGD_ECUDA;
+        grid = std::min({(A.rows + R - 1) / R, (int64_t)fit, PART_BLOCKS});
+        cfg.gridDim = dim3((unsigned)(grid * cluster));
+        *parts = (int)grid;
+        return cudaLaunchKernelEx(&cfg, kernel, A) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
+    }
 #undef NORM_BACK
     if (A.rows > 0x7fffffff) return SSGD_EINVAL;
     k_norm_back_sums<T, VEC><<<(unsigned)A.rows, WIDE, 0, st>>>(A);
@@ -859,7 +913,7 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
     if (!workspace || workspace_bytes < need) return SSGD_EWORKSPACE;
     int sms = 0;
     if ((e = sm_count_of_current_device(&sms))) return e;
-    NormBackArgs A{dy, ld_dy, x, ld_x, w, fmt_w == SSGD_FMT_F32, stats, rows, (int32_t)n, dx, ld_dx, nullptr, nullptr};
+    NormBackArgs A{dy, ld_dy, x, ld_x, w, fmt_w == SSGD_FMT_F32, stats, rows, (int32_t)n, dx, ld_dx, nullptr, nullptr, 0};
     float* base = static_cast<float*>(workspace);
     A.row_sums = base;
     if (n > BACK_NARROW) base += 2 * rows;
