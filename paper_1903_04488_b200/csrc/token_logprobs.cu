@@ -7,9 +7,9 @@
 // rises.  A row is cut into granules of 16 aligned bytes (its first and last may be partial, so any base and stride will
 // do); granule i of a segment belongs to thread i mod THREADS.
 //
-// Alternatives: the threads' maxima bound the k-th largest logit from below, so only threads whose maximum reaches the bound
-// can hold one of the k.  Their granules -- those of some 20 to 60 of 256 threads -- are read again (from L2), and the
-// logits that reach the bound are sorted, 32 to a warp, and merged.  Order: larger logit first, then smaller index; a NaN
+// Alternatives: the threads' maxima bound the k-th largest logit from below.  Every thread has left the maximum of each of its
+// batches of granules in shared memory; the batches that reach the bound, some 20 to 60, are read again, and the logits that
+// reach it are sorted, 32 to a warp, and merged.  Order: larger logit first, then smaller index; a NaN
 // counts as the largest; -0 and +0 are equal.
 //
 // Few rows: a cluster of CTAs shares a row and joins through distributed shared memory, so there is still one launch
@@ -203,16 +203,16 @@ __device__ __noinline__ Sums add_granule_carefully(Sums a, Vec<T, 16 / sizeof(T)
     return a;
 }
 
-// Granules v[0] .. v[have - 1] (`have` is the same for the whole CTA).  Elements that are not there are -inf: they change neither
+// Granules v[0] .. v[have - 1] (`have` is the same for the whole CTA); returns their maximum.  Elements that are not there are -inf: they change neither
 // the maximum nor the sums.
 template <typename T, int U>
-__device__ __forceinline__ void add_granules(Running& r, const Vec<T, 16 / sizeof(T)> (&v)[U], int have) {
+__device__ __forceinline__ float add_granules(Running& r, const Vec<T, 16 / sizeof(T)> (&v)[U], int have) {
     constexpr int VEC = 16 / sizeof(T);
-    PairMax<T> top(r.a.m);
+    PairMax<T> top(NEG_INF);
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (u < have) top.add(v[u]);
-    const float m = top.value();
+    const float here = top.value(), m = max_nan(r.a.m, here);
     if (!(m == r.a.m)) {
         rebase(r.a, m, r.c);
         r.low = fabsf(m) < fast_limit<T>() && ordinary(m, r.a.shift) ? floor_for<T>(m, r.reach) : NEG_INF;
@@ -240,6 +240,7 @@ __device__ __forceinline__ void add_granules(Running& r, const Vec<T, 16 / sizeo
         for (int u = 0; u < U; ++u)
             if (u < have) r.a = add_granule_carefully<T>(r.a, v[u], r.c);
     }
+    return here;
 }
 
 // Inserts `key` into the warp's list, lane l holding the l-th largest.
@@ -279,16 +280,19 @@ __device__ __forceinline__ uint64_t sort32(uint64_t x) {
     return x;
 }
 
-constexpr int CANDIDATES = 256;
+constexpr int CANDIDATES = 256, ITEMS = 256;
+constexpr int BATCH = 4;                  // granules that a thread reads at once
+constexpr int SLOTS = 16;                 // maxima that a thread leaves behind
 
-template <int NT>
+template <int NT, bool TOP>
 struct Shared {
     Sums part[8];                     // part[0] is the CTA's in the end
     uint64_t list[8][MAX_TOP];        // list[0] is the CTA's in the end
     uint64_t candidate[CANDIDATES];
     uint32_t bound[8];
-    int32_t picked[NT];
-    int32_t npicked, ncandidates;
+    float slot[TOP ? SLOTS : 1][TOP ? NT : 1];     // the maximum of each of the thread's batches (or runs of batches)
+    int32_t item[ITEMS];
+    int32_t nitems, ncandidates;
 };
 
 // The order of the elements of a granule (0 where there is none)
@@ -310,30 +314,30 @@ __device__ __forceinline__ void orders_of(const Granules<T>& G, int32_t i, bool 
     }
 }
 
-// Rare: more than CANDIDATES logits reach the bound (many equal ones, or a few threads with nearly all the large ones).  Each
-// warp goes through the granules of the picked threads and inserts one by one into its list.
+// Granules [g0, g1) of a row are a CTA's; the whole ones among them are [whole0, whole1), and thread t has whole0 + t + i NT.
+struct Segment { int32_t g0, g1, whole0, whole1; };
+
+// Rare: more than CANDIDATES logits reach the bound (many equal ones, or a few batches with nearly all the large ones).  Each
+// warp goes through its share of the segment and inserts one by one into its list.
 template <typename T, int NT>
-__device__ __noinline__ uint64_t best_one_by_one(const Shared<NT>& sh, const Granules<T>& G, int32_t g0, int32_t g1, uint32_t bound, int k) {
+__device__ __noinline__ uint64_t best_one_by_one(const Granules<T>& G, const Segment& S, uint32_t bound, int k) {
     constexpr int VEC = 16 / sizeof(T);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint64_t list = 0, last = 0;                           // lane's entry of the warp's list; the k-th entry
-    for (int q = warp; q < sh.npicked; q += NT / 32) {
-        for (int32_t base = g0 + sh.picked[q]; base < g1; base += 32 * NT) {
-            const int32_t i = base + lane * NT, at = G.first(i);
-            uint32_t order[VEC];
-            orders_of<T>(G, i, i < g1, order);
+    for (int32_t base = S.g0 + ((int)threadIdx.x & ~31); base < S.g1; base += NT) {
+        const int32_t i = base + ((int)threadIdx.x & 31), at = G.first(i);
+        uint32_t order[VEC];
+        orders_of<T>(G, i, i < S.g1, order);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                uint32_t todo = __ballot_sync(0xffffffffu, order[e] >= bound && order[e] >= (uint32_t)(last >> 32) && order[e] != 0);
-                while (todo) {
-                    const int src = __ffs(todo) - 1;
-                    todo &= todo - 1;
-                    const uint64_t key = ((uint64_t)__shfl_sync(0xffffffffu, order[e], src) << 32) |
-                                         (0xffffffffu - (uint32_t)__shfl_sync(0xffffffffu, at + e, src));
-                    if (key > last) {
-                        insert(list, key);
-                        last = __shfl_sync(0xffffffffu, list, k - 1);
-                    }
+        for (int e = 0; e < VEC; ++e) {
+            uint32_t todo = __ballot_sync(0xffffffffu, order[e] >= bound && order[e] >= (uint32_t)(last >> 32) && order[e] != 0);
+            while (todo) {
+                const int src = __ffs(todo) - 1;
+                todo &= todo - 1;
+                const uint64_t key = ((uint64_t)__shfl_sync(0xffffffffu, order[e], src) << 32) |
+                                     (0xffffffffu - (uint32_t)__shfl_sync(0xffffffffu, at + e, src));
+                if (key > last) {
+                    insert(list, key);
+                    last = __shfl_sync(0xffffffffu, list, k - 1);
                 }
             }
         }
@@ -341,16 +345,17 @@ __device__ __noinline__ uint64_t best_one_by_one(const Shared<NT>& sh, const Gra
     return list;
 }
 
-// The CTA's best of its segment [g0, g1) into sh.list[0], in order, at least k of them (0 where there are fewer).
+// The CTA's best of its segment into sh.list[0], in order, at least k of them (0 where there are fewer).  2^log_run batches
+// share a slot of the threads' maxima.
 template <typename T, int NT>
-__device__ __forceinline__ void best_of_segment(Shared<NT>& sh, const Granules<T>& G, int32_t g0, int32_t g1, float thread_max, int k) {
+__device__ __forceinline__ void best_of_segment(Shared<NT, true>& sh, const Granules<T>& G, const Segment& S, float thread_max, int log_run, int k) {
     constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const bool has = g0 + t < g1;
+    const bool has = S.whole0 + t < S.whole1;
     const uint32_t mine = has ? order_of(thread_max) : 0u;
     // The q-th largest maximum of each warp whose 32 threads all have granules, q = ceil(k / number of those warps): k logits
-    // reach the least of these.  (No such warp: every logit is a candidate, fewer than 32 granules.)
-    const int full = min((g1 - g0) / 32, WARPS);
+    // reach the least of these.  (No such warp: every logit is a candidate, fewer than 32 whole granules.)
+    const int full = min((S.whole1 - S.whole0) / 32, WARPS);
     if (warp < full) {
         uint32_t left = mine, best = 0;
         for (int q = 0; q < k; q += full) {
@@ -360,58 +365,52 @@ __device__ __forceinline__ void best_of_segment(Shared<NT>& sh, const Granules<T
         }
         if (lane == 0) sh.bound[warp] = best;
     }
-    if (t == 0) sh.npicked = sh.ncandidates = 0;
+    if (t == 0) sh.nitems = sh.ncandidates = 0;
     __syncthreads();
-    uint32_t bound = full ? 0xffffffffu : 0u;
+    uint32_t bound = full > 0 ? 0xffffffffu : 0u;
     for (int i = 0; i < full; ++i) bound = min(bound, sh.bound[i]);
-    if (has && mine >= bound) sh.picked[atomicAdd(&sh.npicked, 1)] = t;
-    __syncthreads();
-    // All threads share the granules of the picked ones.  Four reads at once: under load each takes microseconds.
-    const int each = (g1 - g0 + NT - 1) / NT, total = sh.npicked * each;
-    const float per = 1.f / (float)each;
-    constexpr int AT_ONCE = 4;
-    for (int p0 = t; p0 < total; p0 += NT * AT_ONCE) {
-        Vec<T, VEC> v[AT_ONCE];
-        int32_t at[AT_ONCE];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const int p = p0 + u * NT, q = (int)(((float)p + 0.5f) * per);     // p / each: p is below 2^20
-            const int32_t i = p < total ? g0 + sh.picked[q] + (p - q * each) * NT : g1;
-            at[u] = i < g1 ? i : -1;
-            if (i < g1 && G.whole(i)) v[u] = load_vec<T, VEC>(G.row + G.first(i));
+    auto candidate = [&](uint32_t order, int32_t index) {
+        if (order >= bound && order != 0) {
+            const int at = atomicAdd(&sh.ncandidates, 1);
+            if (at < CANDIDATES) sh.candidate[at] = ((uint64_t)order << 32) | (0xffffffffu - (uint32_t)index);
         }
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            if (at[u] < 0) continue;
-            uint32_t order[VEC];
-            if (G.whole(at[u])) {                          // mostly there is nothing in it
-                PairMax<T> top(NEG_INF);
-                top.add(v[u]);
-                if (order_of(top.value()) < bound) continue;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) order[e] = order_of(to_f32(v[u].e[e]));
-            } else {
-                orders_of<T>(G, at[u], true, order);
+    };
+    auto partial = [&](int32_t i) {
+        for (int32_t at = max(G.first(i), 0); at < min(G.first(i) + VEC, G.n); ++at) candidate(order_of(to_f32(G.row[at])), at);
+    };
+    if (t == 0 && S.whole0 > S.g0) partial(S.g0);
+    if (t == 32 % NT && S.whole1 < S.g1 && S.g1 - 1 >= S.whole0) partial(S.g1 - 1);
+    if (has && mine >= bound) {
+        const int slots = (((S.whole1 - S.whole0 + NT * BATCH - 1) / (NT * BATCH) - 1) >> log_run) + 1;
+        for (int i = 0; i < slots; ++i) {
+            if (order_of(sh.slot[i][t]) >= bound) {
+                const int at = atomicAdd(&sh.nitems, 1);
+                if (at < ITEMS) sh.item[at] = t | i << 16;
             }
+        }
+    }
+    __syncthreads();
+    // all threads share the granules of these batches
+    const int log_each = log_run + 2, total = min(sh.nitems, ITEMS) << log_each;
+    for (int p = t; p < total; p += NT) {
+        const int32_t item = sh.item[p >> log_each];
+        const int32_t i = S.whole0 + (item & 0xffff) + (((item >> 16) << log_each) + (p & ((1 << log_each) - 1))) * NT;
+        if (i < S.whole1) {
+            const Vec<T, VEC> v = load_vec<T, VEC>(G.row + G.first(i));
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                if (order[e] >= bound && order[e] != 0) {
-                    const int slot = atomicAdd(&sh.ncandidates, 1);
-                    if (slot < CANDIDATES) sh.candidate[slot] = ((uint64_t)order[e] << 32) | (0xffffffffu - (uint32_t)(G.first(at[u]) + e));
-                }
-            }
+            for (int e = 0; e < VEC; ++e) candidate(order_of(to_f32(v.e[e])), G.first(i) + e);
         }
     }
     __syncthreads();
     const int n = sh.ncandidates;
     int lists = WARPS;
     uint64_t list = 0;
-    if (n <= CANDIDATES) {
+    if (n <= CANDIDATES && sh.nitems <= ITEMS) {
         lists = min((n + 31) / 32, WARPS);
         if (warp < lists) list = sort32(t < n ? sh.candidate[t] : 0);
         for (int at = t + NT; at - lane < n; at += NT) list = merge(list, sort32(at < n ? sh.candidate[at] : 0));
     } else {
-        list = best_one_by_one<T, NT>(sh, G, g0, g1, bound, k);
+        list = best_one_by_one<T, NT>(G, S, bound, k);
     }
     sh.list[warp][lane] = list;
     for (int half = WARPS / 2; half > 0; half >>= 1) {
@@ -429,8 +428,8 @@ __device__ __forceinline__ void best_of_segment(Shared<NT>& sh, const Granules<T
 // next batch in registers while one is summed, 3 CTAs: 69).
 template <typename T, bool TOP, int NT>
 __global__ void __launch_bounds__(NT, 6 * 256 / NT) k_token_logprobs(const LogprobArgs A, int split) {
-    constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32, U = 4;
-    __shared__ Shared<NT> sh;
+    constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32, U = BATCH;
+    __shared__ Shared<NT, TOP> sh;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     // split is a power of two
     const int shift = __ffs(split) - 1, part = blockIdx.x & (split - 1);
@@ -443,47 +442,59 @@ __global__ void __launch_bounds__(NT, 6 * 256 / NT) k_token_logprobs(const Logpr
     int64_t id = -1;
     if (part == 0 && t == 0) id = id_of(A.ids, A.ids64, row);
     Running r{no_sums(), NEG_INF, c, __fdiv_ru(160.f, c)};
-    // granules [whole0, whole1) of the segment are vectors; the row's first and last may be parts of one
-    const int32_t whole0 = g0 == 0 && G.phase ? 1 : g0, whole1 = g1 == G.count && !G.whole(G.count - 1) ? g1 - 1 : g1;
+    // the row's first and last granule may be parts of one
+    Segment S{g0, g1, g0 == 0 && G.phase ? 1 : g0, g1 == G.count && !G.whole(G.count - 1) ? g1 - 1 : g1};
+    S.whole1 = max(S.whole1, min(S.whole0, g1));
+    int log_run = 0;
+    if (TOP) {
+        const int batches = (S.whole1 - S.whole0 + NT * U - 1) / (NT * U);
+        while ((batches - 1) >> log_run >= SLOTS) ++log_run;
+    }
     {
-        int32_t i = g0 + t;
+        int32_t i = S.whole0 + t, b0 = S.whole0;
         const T* p = z + G.first(i);
-        int32_t b0 = g0;
-        if (whole0 == g0) {
-            for (; b0 + NT * U <= whole1; b0 += NT * U, i += NT * U, p += NT * U * VEC) {
-                Vec<T, VEC> v[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = TOP ? load_vec<T, VEC>(p + u * (NT * VEC)) : load_vec_stream<T, VEC>(p + u * (NT * VEC));
-                add_granules<T, U>(r, v, U);
+        int batch = 0;
+        float run_max = NEG_INF;
+        auto leave = [&](float m) {
+            if constexpr (TOP) {
+                run_max = (batch & ((1 << log_run) - 1)) ? max_nan(run_max, m) : m;
+                sh.slot[batch >> log_run][t] = run_max;
+                ++batch;
             }
-        }
-        for (; b0 < whole1; b0 += NT * U, i += NT * U, p += NT * U * VEC) {
+        };
+        for (; b0 + NT * U <= S.whole1; b0 += NT * U, i += NT * U, p += NT * U * VEC) {
             Vec<T, VEC> v[U];
-            const int have = (whole1 - b0 + NT - 1) / NT;
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = TOP ? load_vec<T, VEC>(p + u * (NT * VEC)) : load_vec_stream<T, VEC>(p + u * (NT * VEC));
+            leave(add_granules<T, U>(r, v, U));
+        }
+        if (b0 < S.whole1) {
+            Vec<T, VEC> v[U];
+            const int have = (S.whole1 - b0 + NT - 1) / NT;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[u].e[e] = from_f32<T>(NEG_INF);
-                if (i + u * NT >= whole0 && i + u * NT < whole1)
+                if (i + u * NT < S.whole1)
                     v[u] = TOP ? load_vec<T, VEC>(p + u * (NT * VEC)) : load_vec_stream<T, VEC>(p + u * (NT * VEC));
             }
-            add_granules<T, U>(r, v, have);
+            leave(add_granules<T, U>(r, v, have));
         }
     }
+    const float thread_max = r.a.m;
     auto partial = [&](int32_t i) {
         for (int32_t at = max(G.first(i), 0); at < min(G.first(i) + VEC, A.vocab); ++at) add_careful(r.a, to_f32(z[at]), c);
     };
-    if (whole0 > g0 && t == 0) partial(0);
-    if (whole1 < g1 && whole1 >= whole0 && (whole1 - g0) % NT == t) partial(whole1);
+    if (t == 0 && S.whole0 > g0) partial(g0);
+    if (t == 32 % NT && S.whole1 < g1 && g1 - 1 >= S.whole0) partial(g1 - 1);
     Sums& a = r.a;
-    const float thread_max = a.m;
     const bool counted = id >= 0 && id < A.vocab;          // an id outside the vocabulary is ignored
     float z_id = 0.f;
     if (counted) z_id = to_f32(z[id]);
     // join: warp, CTA, cluster
     join_warp(a, c);
     if (lane == 0) sh.part[warp] = a;
-    if (TOP) best_of_segment<T, NT>(sh, G, g0, g1, thread_max, A.top);
+    if constexpr (TOP) best_of_segment<T, NT>(sh, G, S, thread_max, log_run, A.top);
     __syncthreads();
     if (warp == 0) {
         a = lane < WARPS ? sh.part[lane] : no_sums();
