@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
@@ -167,34 +168,38 @@ inline int fmt_bytes(int32_t fmt) {
 inline uint64_t addr(const void* p) { return (uint64_t)reinterpret_cast<uintptr_t>(p); }
 inline bool aligned_to(const void* p, int bytes) { return addr(p) % (uint64_t)bytes == 0; }
 
+// A fact about each device, 0 until it has been asked for
+constexpr int MAX_DEVICES = 64;
+struct PerDevice { std::atomic<int> value[MAX_DEVICES] = {}; };
+
 // Multiprocessors of the current device (looked up once per device).
 inline int sm_count_of_current_device(int* out) {
-    static int known[64] = {};
+    static PerDevice known;
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SSGD_ECUDA;
-    if (!known[dev]) {
-        int n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return SSGD_ECUDA;
+    int n = known.value[dev];
+    if (!n) {
         if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return SSGD_ECUDA;
-        known[dev] = n;      // the same value whichever thread stores it
+        known.value[dev] = n;      // the same value whichever thread stores it
     }
-    *out = known[dev];
+    *out = n;
     return SSGD_OK;
 }
 
 // CTAs of a kernel that fit an SM at once (asked once per kernel and device: the answer does not change, and asking costs as
 // much as a launch).  `known` belongs to the kernel; smem above 40 KB is opted into on the way.
 template <typename K>
-inline int residency(K kernel, int block, size_t smem, int (&known)[64], int* out) {
+inline int residency(K kernel, int block, size_t smem, PerDevice& known, int* out) {
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SSGD_ECUDA;
-    if (!known[dev]) {
-        int n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return SSGD_ECUDA;
+    int n = known.value[dev];
+    if (!n) {
         if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
             return SSGD_ECUDA;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem) != cudaSuccess || n < 1) return SSGD_ECUDA;
-        known[dev] = n;      // the same value whichever thread stores it
+        known.value[dev] = n;      // the same value whichever thread stores it
     }
-    *out = known[dev];
+    *out = n;
     return SSGD_OK;
 }
 

@@ -5,8 +5,9 @@
 //              dx = rstd (a - 1/n sum a - h 1/n sum a h),   dw = sum over rows of dy h,   db = sum over rows of dy
 //
 // Both are bound by HBM: two streams of rows x n elements forward, three backward, a dozen operations per element.
-// So a row is read once and stays in registers (in its own format) from the first sum to the result: the variance is
-// the mean of squared deviations from the mean already known, not a difference of large sums.
+// So a row is read once and stays on the SM, in its own format, from the first sum to the result: the variance is the mean of
+// squared deviations from the mean already known, not a difference of large sums.  What keeps the kernels from the
+// memory's rate is the latency of a row's sums on their way through warps and block, and the instructions around them.
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -135,6 +136,7 @@ struct NormArgs {
 };
 
 // FULL: every thread has E elements (n = G E), so no column needs a check.
+// One row per group and block: for rows too long to keep w and b in registers beside them.
 template <typename T, int VEC, int G, int E, bool FULL>
 __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm(const NormArgs A) {
     constexpr int NV = E / VEC;
@@ -428,15 +430,17 @@ __device__ __forceinline__ Vec<T, VEC> back_result(const Vec<T, VEC>& x, const V
 // cannot be copied this way: they are read when they are needed.)
 //
 // Measured at 16384 x 4096 in bfloat16 (us, rows at a time x blocks per SM): 1 x 2 85.9, 2 x 2 80.9, 4 x 2 (128 registers: spills)
-// 81.2, 4 x 1 73.8; in fp32, 8192 x 2048: 2 x 2 37.2, 4 x 1 37.6, 1999 x 1030 10.5 and 13.4.  Without the ring, the next row in registers: 88.6; the rows ahead asked into L2: 86.
-template <typename T, int G> constexpr int ROWS_AT_ONCE = sizeof(T) == 4 || G >= 512 ? 2 : 4;
+// 81.2, 4 x 1 73.8; in fp32, 8192 x 2048 2 x 2 37.2, 4 x 1 37.6, 1999 x 1030 10.5 and 13.4.  Without the ring: with the next row in
+// registers 88.6, with the rows ahead asked into L2 86.
+template <typename T, int VEC, int G> constexpr int ROWS_AT_ONCE = !STAGED<T, VEC> || sizeof(T) == 4 || G >= 512 ? 2 : 4;
 template <typename T, int VEC, int G, int E, int R> constexpr size_t RING_BYTES =
     STAGED<T, VEC> ? (size_t)STAGES * R * 2 * E * sizeof(T) * GroupShape<G>::BLOCK : 0;
 
 // FULL: every thread has E elements (n = G E), so no column needs a check.  SHARED: a cluster of CTAs shares the rows, each with a
 // slab of A.slab columns; their sums of a row meet in distributed shared memory.
 template <typename T, int VEC, int G, int E, int R, bool FULL, bool SHARED>
-__global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 256 ? 2 : sizeof(T) == 4 && GroupShape<G>::BLOCK == 256 ? 2 : 1) k_layer_norm_back(const NormBackArgs A) {
+__global__ void __launch_bounds__(GroupShape<G>::BLOCK, GroupShape<G>::BLOCK < 256 || (sizeof(T) == 4 && GroupShape<G>::BLOCK == 256) ? 2 : 1)
+k_layer_norm_back(const NormBackArgs A) {
     constexpr int NV = E / VEC, ROWS = GroupShape<G>::ROWS, P = PAIRS<VEC>, NW = GroupShape<G>::WARPS, BLOCK = GroupShape<G>::BLOCK;
     constexpr bool RING = STAGED<T, VEC>;
     extern __shared__ __align__(16) float smem[];      // the ring; G = 32: [8][2][n] partial sums at the end
@@ -717,7 +721,7 @@ int vec_of(int es, int64_t n, std::initializer_list<const void*> bases, std::ini
 
 // A grid that fills the SMs; `smem` depends on the kernel alone
 template <typename K>
-int launch_filling(K kernel, const NormArgs& A, int block, int64_t tile, size_t smem, int (&known)[64], int sms, cudaStream_t st) {
+int launch_filling(K kernel, const NormArgs& A, int block, int64_t tile, size_t smem, PerDevice& known, int sms, cudaStream_t st) {
     int per_sm = 0;
     const int e = residency(kernel, block, smem, known, &per_sm);
     if (e) return e;
@@ -736,12 +740,12 @@ int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
         const bool full = WIDEST && n == G * E;                                                                     \
         if constexpr (sizeof(T) == 2 && VEC > 1 && G <= 512) {                                                      \
             if (A.rows >= 8 * sms) {                                                                                \
-                static int known[2][64];                                                                            \
+                static PerDevice known[2];                                                                            \
                 auto kernel = full ? k_layer_norm_ring<T, VEC, G, E, R, WIDEST> : k_layer_norm_ring<T, VEC, G, E, R, false>; \
                 return launch_filling(kernel, A, BLOCK, ROWS * R, (size_t)STAGES * R * E * sizeof(T) * BLOCK, known[full], sms, st); \
             }                                                                                                       \
         }                                                                                                           \
-        static int known[2][64];                                                                                    \
+        static PerDevice known[2];                                                                                    \
         auto kernel = full ? k_layer_norm_rows<T, VEC, G, E, WIDEST> : k_layer_norm_rows<T, VEC, G, E, false>;      \
         return launch_filling(kernel, A, BLOCK, ROWS, 0, known[full], sms, st);                                     \
     } while (0)
@@ -770,7 +774,7 @@ int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
 }
 
 constexpr int64_t PART_BLOCKS = 148 * 4;         // at most so many partial sums of dw and db
-constexpr int BACK_NARROW = 8 * 256 * 8;         // rows up to here never need the sums of k_norm_back_sums
+constexpr int BACK_NARROW = 512 * 8;             // rows up to here never need the sums of k_norm_back_sums
 
 template <typename T, int VEC>
 int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
@@ -778,9 +782,9 @@ int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
     int64_t grid = 0;
 #define NORM_BACK(G, E)                                                                                             \
     do {                                                                                                            \
-        constexpr int R = ROWS_AT_ONCE<T, G>, BLOCK = GroupShape<G>::BLOCK, TILE = GroupShape<G>::ROWS * R;         \
+        constexpr int R = ROWS_AT_ONCE<T, VEC, G>, BLOCK = GroupShape<G>::BLOCK, TILE = GroupShape<G>::ROWS * R;         \
         constexpr bool WIDEST = VEC * sizeof(T) == 16;                                                              \
-        static int known[2][64];                                                                                    \
+        static PerDevice known[2];                                                                                    \
         const bool full = WIDEST && n == G * E;                                                                     \
         auto kernel = full ? k_layer_norm_back<T, VEC, G, E, R, WIDEST, false> : k_layer_norm_back<T, VEC, G, E, R, false, false>; \
         size_t smem = RING_BYTES<T, VEC, G, E, R>;                                                                  \
@@ -799,10 +803,10 @@ int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
     if (n <= 128 * E) NORM_BACK(128, E);
     if (n <= 256 * E) NORM_BACK(256, E);
     if (n <= 512 * E) NORM_BACK(512, E);
-    if (n <= 8 * 256 * E) {
+    if constexpr (STAGED<T, VEC>) if (n <= 8 * 256 * E) {
         // a cluster of 4 or 8 CTAs to the rows
-        constexpr int G = 256, R = ROWS_AT_ONCE<T, G>;
-        static int known[64], clusters[2][64];
+        constexpr int G = 256, R = ROWS_AT_ONCE<T, VEC, G>;
+        static PerDevice known, clusters[2];
         auto kernel = k_layer_norm_back<T, VEC, G, E, R, false, true>;
         const size_t smem = RING_BYTES<T, VEC, G, E, R>;
         int per_sm = 0, dev = 0;
@@ -822,8 +826,12 @@ int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
         cfg.attrs = at;
         cfg.numAttrs = 1;
         // clusters lie within a group of SMs: fewer of them fit than their CTAs alone would
-        int& fit = clusters[cluster == 8][cudaGetDevice(&dev) == cudaSuccess && dev < 64 ? dev : 0];
-        if (!fit && (cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) != cudaSuccess || fit < 1)) return SSGD_ECUDA;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return SSGD_ECUDA;
+        int fit = clusters[cluster == 8].value[dev];
+        if (!fit) {
+            if (cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) != cudaSuccess || fit < 1) return SSGD_ECUDA;
+            clusters[cluster == 8].value[dev] = fit;
+        }
         grid = std::min({(A.rows + R - 1) / R, (int64_t)fit, PART_BLOCKS});
         cfg.gridDim = dim3((unsigned)(grid * cluster));
         *parts = (int)grid;

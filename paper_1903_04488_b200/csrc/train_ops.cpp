@@ -103,7 +103,12 @@ at::Tensor result_like(const at::Tensor* out, const at::Tensor& like, const char
     if (out->sizes() != like.sizes() || out->scalar_type() != like.scalar_type())
         raise(PyExc_TypeError, std::string(name) + ": need " + of + " shape and type");
     *ld = rows_of(*out, name, dev).ld;
+    if (!out->is_inference()) out->unsafeGetTensorImpl()->bump_version();
     return *out;
+}
+// A tensor of the caller's that is written to: autograd has to know
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 at::Tensor new_f32(at::IntArrayRef shape, const at::Tensor& like) {
     return at::empty(shape, at::TensorOptions().dtype(at::kFloat).device(like.device()));
@@ -176,6 +181,8 @@ PyObject* layer_norm_backward(PyObject* const* a) {
         db = db_in ? *db_in : new_f32({r.n}, x);
     }
     float *dwp = need ? flat_f32(&dw, r.n, "dw", dev) : nullptr, *dbp = need ? flat_f32(&db, r.n, "db", dev) : nullptr;
+    if (need && dw_in) written(*dw_in);
+    if (need && db_in) written(*db_in);
     size_t bytes = 0;
     check(ssgd_layer_norm_backward_workspace(r.rows, r.n, &bytes), "ssgd_layer_norm_backward_workspace");
     at::Tensor ws = new_f32({(int64_t)(bytes / 4)}, x);
@@ -246,25 +253,44 @@ PyObject* token_logprobs_backward(PyObject* const* a) {
     return wrap(out);
 }
 
-// (address of the ssgd_adamw_tensor array, grads, device, fmt_p, fmt_state, fmt_copy, lr, b1, b2, eps, decay, step, grad_scale, seed)
-// The array's g and n are filled in from the gradients; `sizes` are kept in a second array behind it.
+// One member of all descriptors from a list of tensors.  They are looked at in every step: a parameter may have been given
+// other storage in the meantime.
+template <typename F>
+void column(PyObject* list, Py_ssize_t count, const char* name, at::ScalarType type, int dev, const int64_t* sizes, int64_t per, F set) {
+    if (!PyList_Check(list) || PyList_GET_SIZE(list) != count) raise(PyExc_ValueError, std::string(name) + ": need one tensor per parameter");
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor& t = tensor(PyList_GET_ITEM(list, i), name);
+        const int64_t n = (sizes[i] + per - 1) / per;
+        if (t.scalar_type() != type || t.numel() != n || !t.is_contiguous() || !t.is_cuda() || t.get_device() != dev)
+            raise(PyExc_TypeError, std::string(name) + "[" + std::to_string(i) + "]: need a contiguous tensor of " + std::to_string(n) +
+                                       " elements of " + std::string(at::toString(type)) + " on CUDA device " + std::to_string(dev));
+        set(i, t);
+    }
+}
+
+// (buffer, params, m, v, m_scale, v_scale, copies, grads, device, lr, b1, b2, eps, decay, step, grad_scale, seed, count): the buffer's address
+// (room for an ssgd_adamw_tensor and, behind them all, a size per parameter); the lists; None for what there is not
 PyObject* adamw_step(PyObject* const* a) {
     auto* desc = reinterpret_cast<ssgd_adamw_tensor*>((uintptr_t)PyLong_AsUnsignedLongLong(a[0]));
-    const int dev = (int)integer(a[2], "device");
+    const int dev = (int)integer(a[8], "device");
     if (dev != (int)c10::cuda::current_device())
         raise(PyExc_ValueError, "grads: the parameters are on device " + std::to_string(dev) + ", which is not the current one");
-    PyObject* grads = a[1];
-    const int64_t count = integer(a[14], "count");
+    const Py_ssize_t count = (Py_ssize_t)integer(a[17], "count");      // what the buffer has room for
+    if (count < 1 || !PyList_Check(a[1]) || PyList_GET_SIZE(a[1]) != count) raise(PyExc_ValueError, "params: not as many as there were");
+    const auto* sizes = reinterpret_cast<const int64_t*>(desc + count);
+    const at::ScalarType type_p = tensor(PyList_GET_ITEM(a[1], 0), "params").scalar_type();
+    if (type_p != at::kFloat && type_p != at::kBFloat16) raise(PyExc_TypeError, "params: need float32 or bfloat16");
+    const bool small = a[4] != Py_None, copied = a[6] != Py_None;
+    const at::ScalarType type_s = small ? at::kFloat8_e4m3fn : at::kFloat;
+    PyObject* grads = a[7];
     if ((!PyList_Check(grads) && !PyTuple_Check(grads)) || PySequence_Fast_GET_SIZE(grads) != count)
         raise(PyExc_ValueError, "grads: need one tensor per parameter");
     PyObject** items = PySequence_Fast_ITEMS(grads);
-    const auto* sizes = reinterpret_cast<const int64_t*>(desc + count);
     at::ScalarType type = at::kFloat;
     bool known = false;
-    for (int64_t i = 0; i < count; ++i) {
-        desc[i].n = 0;
-        desc[i].g = nullptr;
-        if (items[i] == Py_None) continue;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        desc[i] = ssgd_adamw_tensor{};
+        if (items[i] == Py_None) continue;                 // left alone: no elements
         const at::Tensor& g = tensor(items[i], "grads");
         if (!known) type = g.scalar_type();
         known = true;
@@ -274,17 +300,39 @@ PyObject* adamw_step(PyObject* const* a) {
         desc[i].g = g.data_ptr();
         desc[i].n = sizes[i];
     }
-    int32_t fmt_g = SSGD_FMT_F32;
+    int32_t fmt_g = SSGD_FMT_F32, fmt_copy = SSGD_FMT_BF16;
     if (type == at::kBFloat16) fmt_g = SSGD_FMT_BF16;
     else if (type == at::kHalf) fmt_g = SSGD_FMT_F16;
     else if (type != at::kFloat) raise(PyExc_TypeError, "grads: need float32, bfloat16 or float16");
-    const float* grad_scale = flat_f32(optional_tensor(a[12], "grad_scale"), 1, "grad_scale", dev);
-    const bool stochastic = a[13] != Py_None;
-    const uint64_t seed = stochastic ? PyLong_AsUnsignedLongLongMask(a[13]) : 0;
+    column(a[1], count, "params", type_p, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) {
+        desc[i].p = t.data_ptr();
+        if (desc[i].n) written(t);
+    });
+    column(a[2], count, "m", type_s, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) { desc[i].m = t.data_ptr(); });
+    column(a[3], count, "v", type_s, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) { desc[i].v = t.data_ptr(); });
+    if (small) {
+        column(a[4], count, "m_scale", at::kFloat, dev, sizes, SSGD_ADAMW_BLOCK,
+               [&](Py_ssize_t i, const at::Tensor& t) { desc[i].m_scale = static_cast<float*>(t.data_ptr()); });
+        column(a[5], count, "v_scale", at::kFloat, dev, sizes, SSGD_ADAMW_BLOCK,
+               [&](Py_ssize_t i, const at::Tensor& t) { desc[i].v_scale = static_cast<float*>(t.data_ptr()); });
+    }
+    if (copied) {
+        if (!PyList_Check(a[6]) || PyList_GET_SIZE(a[6]) != count) raise(PyExc_ValueError, "copies: need one tensor per parameter");
+        const at::ScalarType type_c = tensor(PyList_GET_ITEM(a[6], 0), "copies").scalar_type();
+        if (type_c != at::kHalf && type_c != at::kBFloat16) raise(PyExc_TypeError, "copies: need bfloat16 or float16");
+        fmt_copy = type_c == at::kHalf ? SSGD_FMT_F16 : SSGD_FMT_BF16;
+        column(a[6], count, "copies", type_c, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) {
+            desc[i].copy = t.data_ptr();
+            if (desc[i].n) written(t);
+        });
+    }
+    const float* grad_scale = flat_f32(optional_tensor(a[15], "grad_scale"), 1, "grad_scale", dev);
+    const bool stochastic = a[16] != Py_None;
+    const uint64_t seed = stochastic ? PyLong_AsUnsignedLongLongMask(a[16]) : 0;
     if (PyErr_Occurred()) throw Raised{};
-    check(ssgd_adamw_step(desc, (int32_t)count, (int32_t)integer(a[3], "fmt_p"), fmt_g, (int32_t)integer(a[4], "fmt_state"),
-                          (int32_t)integer(a[5], "fmt_copy"), number(a[6], "lr"), number(a[7], "beta1"), number(a[8], "beta2"),
-                          number(a[9], "eps"), number(a[10], "weight_decay"), integer(a[11], "step"), grad_scale, stochastic, seed,
+    check(ssgd_adamw_step(desc, (int32_t)count, type_p == at::kBFloat16 ? SSGD_FMT_BF16 : SSGD_FMT_F32, fmt_g,
+                          small ? SSGD_FMT_E4M3 : SSGD_FMT_F32, fmt_copy, number(a[9], "lr"), number(a[10], "beta1"), number(a[11], "beta2"),
+                          number(a[12], "eps"), number(a[13], "weight_decay"), integer(a[14], "step"), grad_scale, stochastic, seed,
                           stream_of(dev)), "ssgd_adamw_step");
     Py_RETURN_NONE;
 }
@@ -315,7 +363,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(layer_norm, 5), ENTRY(layer_norm_backward, 9), ENTRY(token_logprobs, 4), ENTRY(token_logprobs_backward, 10),
-                         ENTRY(adamw_step, 15), ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(adamw_step, 18), ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -20,7 +20,6 @@ import torch
 from . import ssgd as S
 
 BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_train_ops.so")
-_FMT = {torch.float32: S.FMT_F32, torch.float16: S.FMT_F16, torch.bfloat16: S.FMT_BF16}
 _native = None
 
 
@@ -100,13 +99,12 @@ def token_logprobs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.
 
 # ---- AdamW over many tensors -------------------------------------------------------------------------
 
-_P, _G, _M, _V, _MS, _VS, _COPY, _N = range(8)     # the fields of ssgd_adamw_tensor, 8 bytes each
-
-
-def _address(t: torch.Tensor, dtype, n: int, name: str, dev: torch.device) -> int:
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != dev:
-        raise TypeError(f"{name}: need a contiguous tensor of {n} elements of {dtype} on {dev}")
-    return t.data_ptr()
+def _check(tensors, dtype, lens, name: str, dev: torch.device) -> None:
+    if len(tensors) != len(lens):
+        raise ValueError(f"{name}: need one tensor per parameter")
+    for i, (t, n) in enumerate(zip(tensors, lens)):
+        if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != dev:
+            raise TypeError(f"{name}[{i}]: need a contiguous tensor of {n} elements of {dtype} on {dev}")
 
 
 class AdamW:
@@ -154,27 +152,24 @@ class AdamW:
             raise TypeError("copies: bfloat16 or float16, and only of float32 params")
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.step_count = step_count
-        # an ssgd_adamw_tensor per parameter, and behind them the sizes
-        self._desc = np.zeros(len(params) * 9, dtype=np.uint64)
-        self._desc[len(params) * 8:] = sizes
-        table = self._desc[: len(params) * 8].reshape(-1, 8)
-        columns = [(_P, params, dtype, sizes, "params"), (_M, self.m, sdtype, sizes, "m"), (_V, self.v, sdtype, sizes, "v")]
+        _check(params, dtype, sizes, "params", dev)
+        _check(self.m, sdtype, sizes, "m", dev)
+        _check(self.v, sdtype, sizes, "v", dev)
         if small:
-            columns += [(_MS, self.m_scale, torch.float32, blocks, "m_scale"), (_VS, self.v_scale, torch.float32, blocks, "v_scale")]
+            _check(self.m_scale, torch.float32, blocks, "m_scale", dev)
+            _check(self.v_scale, torch.float32, blocks, "v_scale", dev)
         if self.copies is not None:
-            columns.append((_COPY, self.copies, self.copies[0].dtype, sizes, "copies"))
-        for col, tensors, dt, lens, name in columns:
-            if len(tensors) != len(params):
-                raise ValueError(f"{name}: need one tensor per parameter")
-            table[:, col] = [_address(t, dt, n, f"{name}[{i}]", dev) for i, (t, n) in enumerate(zip(tensors, lens))]
-        self._dev, self._desc_p = dev.index, self._desc.ctypes.data
-        self._fmt = (_FMT[dtype], S.FMT_E4M3 if small else S.FMT_F32,
-                     S.FMT_BF16 if self.copies is None else _FMT[self.copies[0].dtype])
+            _check(self.copies, self.copies[0].dtype, sizes, "copies", dev)
+        # room for an ssgd_adamw_tensor (64 bytes) per parameter, and behind them their sizes
+        self._buffer = np.zeros(len(params) * 9, dtype=np.int64)
+        self._buffer[len(params) * 8:] = sizes
+        self._address, self._dev = self._buffer.ctypes.data, dev.index
 
     def step(self, grads, *, seed: int | None = None, grad_scale: torch.Tensor | None = None, lr: float | None = None) -> None:
         """One step.  grads: one contiguous tensor per parameter (float32, bfloat16 or float16, all the same type), None
         for a parameter that is left alone.  seed: round e4m3 states and bfloat16 parameters stochastically with it (another
         one every step).  grad_scale: float32 scalar on the device that multiplies every gradient."""
-        (_native or native()).adamw_step(self._desc_p, grads, self._dev, *self._fmt, self.lr if lr is None else lr, *self.betas,
-                                        self.eps, self.weight_decay, self.step_count + 1, grad_scale, seed, len(self.params))
+        (_native or native()).adamw_step(self._address, self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies, grads,
+                                         self._dev, self.lr if lr is None else lr, *self.betas, self.eps, self.weight_decay,
+                                         self.step_count + 1, grad_scale, seed, len(self._buffer) // 9)
         self.step_count += 1

@@ -629,6 +629,62 @@ def test_adamw_values_that_are_not_finite_stay_alone(cuda_device):
     assert p[0] == math.inf and p[1] == -math.inf and p[2].isnan() and p[3] == 1
 
 
+def test_adamw_follows_its_parameters_and_refuses_what_does_not_fit(cuda_device):
+    g = gen(3)
+    p = [torch.randn(n, generator=g, device="cuda") for n in (1000, 7)]
+    q = [t.clone() for t in p]
+    grads = [torch.randn(n, generator=g, device="cuda") for n in (1000, 7)]
+    a, b = T.AdamW(p, **HYPER), T.AdamW(q, **HYPER)
+    a.step(grads)
+    p[0].data = p[0].data.clone()                      # other storage: the step goes where the parameter is now
+    version = p[0]._version
+    a.step(grads)
+    assert p[0]._version > version                     # autograd is told
+    b.step(grads)
+    b.step(grads)
+    assert all(torch.equal(x, y) for x, y in zip(p, q))
+    for bad in ([grads[0]], [grads[0], grads[0]], [grads[0].double(), grads[1]], [grads[0], grads[1].half()], [grads[0].cpu(), grads[1]],
+                [torch.randn(2000, device="cuda")[::2], grads[1]], "xy"):
+        with pytest.raises((TypeError, ValueError), match="grads"):
+            a.step(bad)
+    with pytest.raises(TypeError, match="grad_scale"):
+        a.step(grads, grad_scale=torch.ones(2, device="cuda"))
+    assert a.step_count == 2 and all(torch.equal(x, y) for x, y in zip(p, q))
+    a.params.append(p[0])
+    with pytest.raises(ValueError, match="params"):
+        a.step(grads)
+
+
+def test_bindings_refuse_what_the_kernels_could_not_read(cuda_device):
+    x, w, b, dy = norm_inputs(8, 64, torch.float32, 1)
+    z, ids = lp_inputs(8, 64, torch.float32, 1)
+    y, stats = T.layer_norm(x, w, b)
+    r = T.token_logprobs(z, ids, top=2)
+    wide = torch.zeros(8, 128, device="cuda")
+    for call in (lambda: T.layer_norm(wide[:, ::2], w, b), lambda: T.layer_norm(x, w[:32], b), lambda: T.layer_norm(x, w, b.cpu()),
+                 lambda: T.layer_norm(x[:1].expand(8, 64), w, b), lambda: T.layer_norm(x.double()), lambda: T.layer_norm(x, out=x.half()),
+                 lambda: T.layer_norm(torch.zeros(4, 8, 64, device="cuda").transpose(0, 1)),
+                 lambda: T.layer_norm_backward(dy.half(), x, w, stats), lambda: T.layer_norm_backward(dy, x, w, stats[:1]),
+                 lambda: T.layer_norm_backward(dy, x, w, stats, dw=torch.zeros(63, device="cuda")),
+                 lambda: T.token_logprobs(z[0], ids), lambda: T.token_logprobs(z, ids[:4]), lambda: T.token_logprobs(z, ids.float()),
+                 lambda: T.token_logprobs_backward(z, ids, r.lse[:4], r.logp),
+                 lambda: T.token_logprobs_backward(z, ids, r.lse, r.logp, top_idx=r.top_idx.long(), d_top=r.top_logp),
+                 lambda: T.token_logprobs_backward(z, ids, r.lse, r.logp, out=z.half())):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError):
+        T.token_logprobs_backward(z, ids, r.lse, r.logp, top_idx=r.top_idx)
+    with pytest.raises(ValueError):
+        T.token_logprobs_backward(z, ids, r.lse, r.logp, d_entropy=r.entropy)
+    with pytest.raises(ValueError):
+        T.layer_norm_backward(dy, x, w, stats, accumulate=True)
+    for call, code in ((lambda: T.token_logprobs(z, ids, top=33), S.ETOOBIG), (lambda: T.token_logprobs(z, ids, scale=0.0), S.EINVAL),
+                       (lambda: T.layer_norm(x, w.half(), b.half()), S.EINVAL), (lambda: T.layer_norm(x, eps=-1.0), S.EINVAL)):
+        with pytest.raises(S.SsgdError) as e:
+            call()
+        assert e.value.code == code
+
+
 def test_operators_on_another_stream_and_in_a_graph(cuda_device):
     x, w, b, dy = norm_inputs(300, 512, torch.bfloat16, 3)
     z, ids = lp_inputs(1, 100000, torch.bfloat16, 3)
