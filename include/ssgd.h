@@ -49,13 +49,13 @@ extern "C" {
 
 #define SSGD_OK          0
 #define SSGD_EINVAL     -1  /* bad shape, size, NULL pointer, ld < d, k > ncand, ncand > d, even r ... */
-#define SSGD_EALIGN     -2  /* base pointer not 16-byte aligned, or ld not a multiple of 4             */
+#define SSGD_EALIGN     -2  /* a base or ld not aligned as the call needs (the step: 16 bytes, ld % 4 == 0)  */
 #define SSGD_ENOTBOUND  -3  /* ssgd_bind has not been called                                           */
 #define SSGD_EWORKSPACE -4  /* workspace too small for the requested ncand                             */
 #define SSGD_ECUDA      -5  /* a CUDA runtime call failed; ssgd_last_error gives its text              */
 #define SSGD_EDEVICE    -6  /* a kernel recorded an error: bad index in a caller's list, or a wait gave up */
 #define SSGD_ENOMEM     -7  /* host allocation failed                                                  */
-#define SSGD_ETOOBIG    -8  /* size beyond the fixed capacity of ssgd_exact_topk_static                */
+#define SSGD_ETOOBIG    -8  /* beyond a fixed capacity: ssgd_exact_topk_static's scratch, SSGD_MAX_TOP      */
 #define SSGD_EPENDING   -9  /* a deferred zero-out has not been applied yet: ssgd_flush first (or ssgd_unbind) */
 
 #define SSGD_MAX_R 15

@@ -6,6 +6,8 @@
 //                       and Algorithm 1's key kernel
 //   launch_small.cu     Algorithm 3 lines 9-13 in one cooperative kernel (k_small_tail)
 //   ssgd.cu             the C ABI, workspace layout, the selections and everything else
+// The operators of the training step (layer_norm.cu, token_logprobs.cu, adamw.cu over formats.cuh) have no context and share
+// nothing with these.
 #pragma once
 #include <cuda_runtime.h>
 

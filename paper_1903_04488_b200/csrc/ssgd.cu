@@ -963,13 +963,13 @@ const char* ssgd_strerror(int code) {
     switch (code) {
         case SSGD_OK: return "ok";
         case SSGD_EINVAL: return "invalid argument";
-        case SSGD_EALIGN: return "pointer not 16-byte aligned or leading dimension not a multiple of 4";
+        case SSGD_EALIGN: return "pointer or leading dimension not aligned as the call needs";
         case SSGD_ENOTBOUND: return "no state/workspace bound (call ssgd_bind)";
         case SSGD_EWORKSPACE: return "workspace too small for this ncand";
         case SSGD_ECUDA: return "CUDA runtime error (see ssgd_last_error)";
         case SSGD_EDEVICE: return "a kernel reported an error (index out of range, or a bounded wait gave up)";
         case SSGD_ENOMEM: return "out of host memory";
-        case SSGD_ETOOBIG: return "size exceeds the fixed capacity of the built-in scratch";
+        case SSGD_ETOOBIG: return "size exceeds a fixed capacity (built-in scratch, alternatives per token)";
         case SSGD_EPENDING: return "a deferred zero-out is pending: call ssgd_flush first (or ssgd_unbind to discard it)";
         default: return "unknown error";
     }
