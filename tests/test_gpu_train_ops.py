@@ -105,6 +105,18 @@ def test_norm_and_its_gradient(cuda_device, rows, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n", [(1500, 1000), (1301, 2048), (1202, 4096), (1187, 8192), (1300, 130), (2401, 512), (1250, 77), (701, 8704),
+                                    (403, 12000)])
+def test_norm_of_many_rows(cuda_device, rows, n, dtype):
+    """More rows than the blocks take in their first turns, and a last turn that is not full."""
+    x, w, b, dy = norm_inputs(rows, n, dtype, rows + n, torch.float32 if n % 3 else dtype)
+    y, stats = T.layer_norm(x, w, b, 1e-5)
+    check_norm(x, w, b, 1e-5, y, stats)
+    dx, dw, db = T.layer_norm_backward(dy, x, w, stats)
+    check_norm_back(x, w, stats, dy, dx, dw, db)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n,pad,offset", [(512, 8, 8), (512, 1, 3), (2048, 2, 2), (1000, 24, 5), (20000, 7, 1)])
 def test_norm_of_strided_rows(cuda_device, dtype, n, pad, offset):
     x, w, b, dy = norm_inputs(21, n, dtype, n + pad)
@@ -394,6 +406,19 @@ def test_logprobs_alternatives_of_equal_rising_and_not_finite_logits(cuda_device
     assert r.stats[:, 2:].isfinite().all()
 
 
+def test_logprobs_of_rows_with_many_batches(cuda_device):
+    """Enough rows that one CTA has each, long enough that several batches share one of the maxima it keeps."""
+    for dtype, v in ((torch.float32, 200003), (torch.bfloat16, 300001)):
+        z, ids = lp_inputs(600, v, dtype, 17)
+        r = T.token_logprobs(z, ids, top=7)
+        for rows in (slice(0, 40), slice(590, 600)):
+            part = T.TokenLogprobs(r.stats[:, rows], r.top_idx[rows], r.top_logp[rows])
+            check_lp(z[rows], ids[rows], 7, 1.0, part, order=False)
+        order = z[:40].float().sort(dim=1, descending=True, stable=True).indices[:, :7]
+        assert torch.equal(r.top_idx[:40].long(), order)
+        assert torch.equal(z.gather(1, r.top_idx.long()), z.topk(7, dim=1).values)
+
+
 def test_logprobs_gradient_against_differences(cuda_device):
     z, ids = lp_inputs(3, 41, torch.float32, 12)
     zr = z.clone().requires_grad_()
@@ -585,6 +610,27 @@ def test_adamw_8bit_states(cuda_device, pdtype, gdtype, gap):
                   for p, a, b, c, d in zip(params, opt.m, opt.v, opt.m_scale, opt.v_scale)]
         opt.step(grads, seed=seed)
         check_8bit(opt, before, grads, t, seed)
+
+
+def test_adamw_8bit_does_not_depend_on_how_it_is_divided(cuda_device):
+    """With a large tensor behind them the others' blocks are dealt out differently: the same bits come out."""
+    g = gen(9)
+    sizes = [5003, 256, 70001, 1 << 16]
+    big = 12_000_011
+    p = [torch.randn(n, generator=g, device="cuda").to(torch.bfloat16) for n in sizes + [big]]
+    q = [t.clone() for t in p]
+    a, b = T.AdamW(p, state="e4m3", **HYPER), T.AdamW(q[:-1], state="e4m3", **HYPER)
+    for t in (1, 2):
+        grads = [(torch.randn(n, generator=g, device="cuda") * 1e-3).to(torch.bfloat16) for n in sizes + [big]]
+        a.step(grads, seed=t)
+        b.step(grads[:-1], seed=t)
+    for x, y in zip((p, a.m, a.v, a.m_scale, a.v_scale), (q, b.m, b.v, b.m_scale, b.v_scale)):
+        assert all(torch.equal(i.float(), j.float()) for i, j in zip(x[:-1], y[: len(sizes)]))
+    last = T.AdamW([p[-1]], state="e4m3", m=[a.m[-1]], v=[a.v[-1]], m_scale=[a.m_scale[-1]], v_scale=[a.v_scale[-1]], step_count=2, **HYPER)
+    before = [(p[-1].clone(), a.m[-1].clone(), a.v[-1].clone(), a.m_scale[-1].clone(), a.v_scale[-1].clone())]
+    grads = [(torch.randn(big, generator=g, device="cuda") * 1e-3).to(torch.bfloat16)]
+    last.step(grads, seed=77)
+    check_8bit(last, before, grads, 3, 77)
 
 
 def test_adamw_8bit_is_right_on_average_and_moves_slowly(cuda_device):
