@@ -534,9 +534,10 @@ def mix(x):
     return x ^ (x >> 16)
 
 
-def words(seed, tensor, n):
+def words(seed, tensor, n, start=0):
     key = mix((mix(mix(seed & 0xFFFFFFFF) ^ (seed >> 32)) + tensor) & 0xFFFFFFFF)
-    return mix(np.arange(n, dtype=np.int64) ^ key)
+    i = np.arange(start, start + n, dtype=np.int64)
+    return mix((i & 0xFFFFFFFF) ^ ((i >> 32) * 0x9E3779B9 & 0xFFFFFFFF) ^ key)
 
 
 def blocks_of(x):
@@ -550,7 +551,7 @@ def unit_of(y):
     return torch.exp2(torch.floor(torch.log2(y.clamp_min(2.0 ** -6))) - 3)
 
 
-def check_8bit(opt, before, grads, t, seed):
+def check_8bit(opt, before, grads, t, seed, start=0):
     for i, (p0, m0, v0, ms0, vs0) in enumerate(before):
         n = p0.numel()
         if n == 0:
@@ -567,7 +568,7 @@ def check_8bit(opt, before, grads, t, seed):
             # rounded up or down from p1: within one unit of the last place
             ulp = 2.0 ** -7 * torch.exp2(torch.floor(torch.log2(p1.abs().clamp_min(1e-30))))
             near(opt.params[i], p1, ulp * (1 + 1e-3) * (1.0 if seed is not None else 0.5) + 32 * U * upd.abs() + 1e-300, "p")
-        w = words(seed, i, n) if seed is not None else None
+        w = words(seed, i, n, start) if seed is not None else None
         for got, scale, want, shift in ((opt.m[i], opt.m_scale[i], m1, 0), (opt.v[i], opt.v_scale[i], r1, 16)):
             amax = blocks_of(want.abs()).amax(1)
             near(scale, amax / 448, 32 * U * amax / 448 + blocks_of(cancel).amax(1) / 448 + 1e-300, "scale")
@@ -631,6 +632,39 @@ def test_adamw_8bit_does_not_depend_on_how_it_is_divided(cuda_device):
     grads = [(torch.randn(big, generator=g, device="cuda") * 1e-3).to(torch.bfloat16)]
     last.step(grads, seed=77)
     check_8bit(last, before, grads, 3, 77)
+
+
+def test_offsets_beyond_32_bits(cuda_device):
+    """Rows 2^31 elements apart, and a tensor of more than 2^32 elements."""
+    far = (1 << 31) + 8
+    buf = torch.zeros(2 * far + 4096, dtype=torch.bfloat16, device="cuda")
+    x, w, b, dy = norm_inputs(3, 1024, torch.bfloat16, 2)
+    xs, out = buf.as_strided((3, 1024), (far, 1)), buf.as_strided((3, 1024), (far, 1), 2048)
+    xs.copy_(x)
+    y, stats = T.layer_norm(xs, w, b, out=out)
+    check_norm(x, w, b, 1e-5, y, stats)
+    dx, dw, db = T.layer_norm_backward(dy, xs, w, stats, dx=out)
+    check_norm_back(x, w, stats, dy, dx, dw, db)
+    ids = torch.tensor([3, 500, 1023], device="cuda")
+    r = T.token_logprobs(xs, ids, top=3)
+    check_lp(x, ids, 3, 1.0, r)
+    d = torch.ones(3, device="cuda")
+    check_lp_back(x, ids, 1.0, r, d, None, None, T.token_logprobs_backward(xs, ids, r.lse, d, out=out))
+    del xs, out, buf
+    n = (1 << 32) + 777
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    start, gg = (1 << 32) - 1024, gen(6)
+    for t in (p, g):
+        t[start:] = torch.randn(n - start, generator=gg, device="cuda").to(torch.bfloat16)
+    opt = T.AdamW([p], state="e4m3", **HYPER)
+    tail = T.AdamW.__new__(T.AdamW)                    # the same step, seen from `start` on
+    tail.params, tail.m, tail.v, tail.copies = [p[start:]], [opt.m[0][start:]], [opt.v[0][start:]], None
+    tail.m_scale, tail.v_scale = [opt.m_scale[0][start // 256:]], [opt.v_scale[0][start // 256:]]
+    for t in (1, 2):
+        before = [tuple(x[0].clone() for x in (tail.params, tail.m, tail.v, tail.m_scale, tail.v_scale))]
+        opt.step([g], seed=40 + t)
+        check_8bit(tail, before, [g[start:]], t, 40 + t, start)
+    assert not p[:start].any() and not opt.m[0][:4096].float().any()
 
 
 def test_adamw_8bit_is_right_on_average_and_moves_slowly(cuda_device):
