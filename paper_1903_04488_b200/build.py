@@ -55,7 +55,7 @@ def build_binding(force: bool = False) -> str:
         tmp = BINDING + ".tmp.%d" % os.getpid()
         cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
         cmd += [a for i in includes for a in ("-isystem", i)] + [src, "-o", tmp, "-L", HERE, "-l:libssgd.so", "-L", libs]
-        cmd += ["-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
+        cmd += ["-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
         subprocess.check_call(cmd)
         os.replace(tmp, BINDING)
     return BINDING

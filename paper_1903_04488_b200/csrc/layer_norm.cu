@@ -390,6 +390,8 @@ struct NormBackArgs {
     float* partial;      // [grid][2][n]; NULL: neither dw nor db is wanted
     float* row_sums;     // wide rows: [rows][2]
     int32_t slab;        // columns per CTA of a cluster
+    // one block alone has the sums over all rows: it writes them where they belong
+    float* dw; float* db; bool direct, accumulate;
 };
 
 // What a vector adds to the row's two sums (of a and a h) and to the columns' sums over the rows
@@ -588,7 +590,13 @@ k_layer_norm_back(const NormBackArgs A) {
     successor_may_start();                             // k_norm_reduce waits for the partial sums by itself
     if (!A.partial) return;
     float* out = A.partial + block * 2 * A.n + col0;
-    float* mine = G == 32 ? smem + (int64_t)sub * 2 * A.n : out;
+    auto put = [&](int c, float value) {               // c: 0 .. 2 n - 1, dw then db, from this CTA's first column on
+        if (!A.direct) { out[c] = value; return; }
+        float* to = c < A.n ? A.dw : A.db;
+        const int at = (c < A.n ? c : c - A.n) + col0;
+        if (to) to[at] = A.accumulate ? to[at] + value : value;
+    };
+    float* mine = smem + (int64_t)sub * 2 * A.n;       // G = 32: the block's 8 warps add up in shared memory
     if (G == 32) __syncthreads();                      // every warp is done with the ring
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -596,19 +604,24 @@ k_layer_norm_back(const NormBackArgs A) {
         if (i < nv) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                mine[i * VEC + e] = e & 1 ? dw[j][e / 2].y : dw[j][e / 2].x;
-                mine[A.n + i * VEC + e] = e & 1 ? db[j][e / 2].y : db[j][e / 2].x;
+                const float a = e & 1 ? dw[j][e / 2].y : dw[j][e / 2].x, b = e & 1 ? db[j][e / 2].y : db[j][e / 2].x;
+                if constexpr (G == 32) {
+                    mine[i * VEC + e] = a;
+                    mine[A.n + i * VEC + e] = b;
+                } else {
+                    put(i * VEC + e, a);
+                    put(A.n + i * VEC + e, b);
+                }
             }
         }
     }
     if constexpr (G == 32) {
-        // the block's 8 warps add up in shared memory
         __syncthreads();
         for (int c = threadIdx.x; c < 2 * A.n; c += GroupShape<G>::BLOCK) {
             float s = 0.f;
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) s += smem[(int64_t)r * 2 * A.n + c];
-            out[c] = s;
+            put(c, s);
         }
     }
 }
@@ -802,8 +815,9 @@ int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
         const int e = residency(kernel, BLOCK, smem, known[full], &per_sm);                                         \
         if (e) return e;                                                                                            \
         grid = std::min({(A.rows + TILE - 1) / TILE, (int64_t)sms * per_sm, PART_BLOCKS});                          \
+        A.direct = grid == 1;                                                                                       \
         kernel<<<(unsigned)grid, BLOCK, smem, st>>>(A);                                                             \
-        *parts = (int)grid;                                                                                         \
+        *parts = A.direct ? 0 : (int)grid;           /* 0: nothing is left to add up */                             \
         return launched();                                                                                          \
     } while (0)
     // 16 elements of 16 bits per thread or 8 of 32 bits: with their sums, 128 registers
@@ -844,7 +858,8 @@ int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
         }
         grid = std::min({(A.rows + R - 1) / R, (int64_t)fit, PART_BLOCKS});
         cfg.gridDim = dim3((unsigned)(grid * cluster));
-        *parts = (int)grid;
+        A.direct = grid == 1;
+        *parts = A.direct ? 0 : (int)grid;
         return cudaLaunchKernelEx(&cfg, kernel, A) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
     }
 #undef NORM_BACK
@@ -931,7 +946,7 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
     if (!workspace || workspace_bytes < need) return SSGD_EWORKSPACE;
     int sms = 0;
     if ((e = sm_count_of_current_device(&sms))) return e;
-    NormBackArgs A{dy, ld_dy, x, ld_x, w, fmt_w == SSGD_FMT_F32, stats, rows, (int32_t)n, dx, ld_dx, nullptr, nullptr, 0};
+    NormBackArgs A{dy, ld_dy, x, ld_x, w, fmt_w == SSGD_FMT_F32, stats, rows, (int32_t)n, dx, ld_dx, nullptr, nullptr, 0, dw, db, false, accumulate != 0};
     float* base = static_cast<float*>(workspace);
     A.row_sums = base;
     if (n > BACK_NARROW) base += 2 * rows;
@@ -939,7 +954,7 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
     const int vec = vec_of(es, n, {dy, x, dx}, {ld_dy, ld_x, ld_dx}, {w}, A.w_f32);
     int parts = 0;
     e = BY_FORMAT(launch_norm_back, fmt_x, vec, A, sms, &parts, st);
-    if (e || !A.partial) return e;
+    if (e || !A.partial || parts == 0) return e;
     return launch_after(st, k_norm_reduce, dim3((unsigned)((2 * n + 31) / 32)), REDUCE_WARPS * 32, A.partial, parts, (int)n, dw, db,
                         accumulate);
 }

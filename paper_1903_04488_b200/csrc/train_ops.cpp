@@ -6,6 +6,8 @@
 // given to set_error_class.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -94,11 +96,16 @@ float* flat_f32(const at::Tensor* t, int64_t n, const char* name, int dev) {
     return static_cast<float*>(flat(t, at::kFloat, n, name, dev));
 }
 
+// A new tensor, without the detour over the dispatcher
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, int dev) {
+    return at::detail::empty_cuda(shape, type, at::Device(at::kCUDA, (c10::DeviceIndex)dev), std::nullopt);
+}
+
 // The tensor that a result goes to: the caller's, which has to be like `like`, or a new contiguous one
 at::Tensor result_like(const at::Tensor* out, const at::Tensor& like, const char* name, int dev, int64_t* ld, const char* of) {
     if (!out) {
         *ld = like.dim() ? like.size(-1) : 1;
-        return at::empty(like.sizes(), like.options().requires_grad(false).memory_format(at::MemoryFormat::Contiguous));
+        return fresh(like.sizes(), like.scalar_type(), dev);
     }
     if (out->sizes() != like.sizes() || out->scalar_type() != like.scalar_type())
         raise(PyExc_TypeError, std::string(name) + ": need " + of + " shape and type");
@@ -110,9 +117,7 @@ at::Tensor result_like(const at::Tensor* out, const at::Tensor& like, const char
 void written(const at::Tensor& t) {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
-at::Tensor new_f32(at::IntArrayRef shape, const at::Tensor& like) {
-    return at::empty(shape, at::TensorOptions().dtype(at::kFloat).device(like.device()));
-}
+at::Tensor new_f32(at::IntArrayRef shape, int dev) { return fresh(shape, at::kFloat, dev); }
 
 void* stream_of(int dev) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream(); }
 
@@ -151,7 +156,7 @@ PyObject* layer_norm(PyObject* const* a) {
     const void *wp = flat(w, type_w, r.n, "weight", dev), *bp = flat(b, type_w, r.n, "bias", dev);
     int64_t ld_y = 0;
     at::Tensor y = result_like(optional_tensor(a[4], "out"), x, "out", dev, &ld_y, "x's");
-    at::Tensor stats = new_f32({2, r.rows}, x);
+    at::Tensor stats = new_f32({2, r.rows}, dev);
     check(ssgd_layer_norm(x.data_ptr(), r.ld, fmt, wp, bp, fmt_w, r.rows, r.n, (float)number(a[3], "eps"), y.data_ptr(), ld_y,
                           stats.data_ptr<float>(), stream_of(dev)), "ssgd_layer_norm");
     return Py_BuildValue("(NN)", wrap(y), wrap(stats));
@@ -177,17 +182,18 @@ PyObject* layer_norm_backward(PyObject* const* a) {
     at::Tensor dw, db;
     if (need) {
         if (accumulate && (!dw_in || !db_in)) raise(PyExc_ValueError, "accumulate: needs dw and db");
-        dw = dw_in ? *dw_in : new_f32({r.n}, x);
-        db = db_in ? *db_in : new_f32({r.n}, x);
+        dw = dw_in ? *dw_in : new_f32({r.n}, dev);
+        db = db_in ? *db_in : new_f32({r.n}, dev);
     }
     float *dwp = need ? flat_f32(&dw, r.n, "dw", dev) : nullptr, *dbp = need ? flat_f32(&db, r.n, "db", dev) : nullptr;
     if (need && dw_in) written(*dw_in);
     if (need && db_in) written(*db_in);
     size_t bytes = 0;
     check(ssgd_layer_norm_backward_workspace(r.rows, r.n, &bytes), "ssgd_layer_norm_backward_workspace");
-    at::Tensor ws = new_f32({(int64_t)(bytes / 4)}, x);
+    // of the current stream: what is enqueued below runs before anything that gets this memory next
+    const c10::DataPtr ws = c10::cuda::CUDACachingAllocator::get()->allocate(bytes);
     check(ssgd_layer_norm_backward(dy.data_ptr(), rd.ld, x.data_ptr(), r.ld, fmt, wp, fmt_w, stats, r.rows, r.n, dx.data_ptr(), ld_dx, dwp,
-                                   dbp, accumulate ? 1 : 0, ws.data_ptr(), bytes, stream_of(dev)), "ssgd_layer_norm_backward");
+                                   dbp, accumulate ? 1 : 0, ws.get(), bytes, stream_of(dev)), "ssgd_layer_norm_backward");
     return Py_BuildValue("(NNN)", wrap(dx), wrap_or_none(dw), wrap_or_none(db));
 }
 
@@ -211,11 +217,11 @@ PyObject* token_logprobs(PyObject* const* a) {
     const Ids ids = ids_of(tensor(a[1], "ids"), r.rows, dev);
     const int64_t top = integer(a[2], "top");
     if (top < 0 || top > INT32_MAX) check(SSGD_EINVAL, "ssgd_token_logprobs");
-    at::Tensor stats = new_f32({3, r.rows}, z), idx, logp;
+    at::Tensor stats = new_f32({3, r.rows}, dev), idx, logp;
     if (top > SSGD_MAX_TOP) check(SSGD_ETOOBIG, "ssgd_token_logprobs");
     if (top) {
-        idx = at::empty({r.rows, top}, at::TensorOptions().dtype(at::kInt).device(z.device()));
-        logp = new_f32({r.rows, top}, z);
+        idx = fresh({r.rows, top}, at::kInt, dev);
+        logp = new_f32({r.rows, top}, dev);
     }
     check(ssgd_token_logprobs(z.data_ptr(), r.ld, fmt, ids.p, ids.bytes, r.rows, r.n, (float)number(a[3], "scale"), (int32_t)top,
                               stats.data_ptr<float>(), top ? idx.data_ptr<int32_t>() : nullptr, top ? logp.data_ptr<float>() : nullptr,

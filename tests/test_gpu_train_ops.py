@@ -156,6 +156,20 @@ def test_norm_without_parameters_in_place_and_accumulating(cuda_device):
         assert torch.equal(T.layer_norm(x2, w, b, out=x2)[0], y)
 
 
+@pytest.mark.parametrize("rows,n", [(1, 300), (20, 300), (3, 777), (2, 5000), (4, 9000), (33, 300), (5, 777)])
+def test_norm_gradients_add_to_what_is_there(cuda_device, rows, n):
+    """Few rows: one block may have them all and write the sums itself."""
+    for dtype in (torch.float32, torch.bfloat16):
+        x, w, b, dy = norm_inputs(rows, n, dtype, rows + n)
+        y, stats = T.layer_norm(x, w, b)
+        dx, dw, db = T.layer_norm_backward(dy, x, w, stats)
+        check_norm_back(x, w, stats, dy, dx, dw, db)
+        flat = torch.full((2 * n + 3,), 0.5, device="cuda")
+        T.layer_norm_backward(dy, x, w, stats, dw=flat[1: n + 1], db=flat[n + 2: 2 * n + 2], accumulate=True)
+        assert torch.equal(flat[1: n + 1], 0.5 + dw) and torch.equal(flat[n + 2: 2 * n + 2], 0.5 + db)
+        assert (flat[[0, n + 1, 2 * n + 2]] == 0.5).all()
+
+
 def test_norm_repeats_bit_for_bit_and_takes_leading_dimensions(cuda_device):
     x, w, b, dy = norm_inputs(2000, 640, torch.bfloat16, 8)
     y, stats = T.layer_norm(x, w, b)
