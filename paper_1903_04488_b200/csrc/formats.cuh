@@ -57,19 +57,6 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void unpack(const Vec<T, VEC>& v, float (&f)[VEC]) {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = to_f32(v.e[i]);
-}
-template <typename T, int VEC>
-__device__ __forceinline__ Vec<T, VEC> pack(const float (&f)[VEC]) {
-    Vec<T, VEC> v;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v.e[i] = from_f32<T>(f[i]);
-    return v;
-}
-
 // Pairs of fp32 numbers: one instruction works on both (rounding each like the scalar operation).
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;
