@@ -105,6 +105,9 @@ __device__ __forceinline__ uint32_t dither_word(uint32_t key, int64_t i) {
     return mix(key ^ (uint32_t)i ^ ((uint32_t)((uint64_t)i >> 32) * 0x9E3779B9u));
 }
 
+// A chunk of 2048 elements per block: two vectors of four per thread from each of p, g, m, v on their way at once, what has no
+// common alignment element by element.  Measured in fp32: 11,173,962 elements in 62 tensors at any offset 51.2 us, 6.1 TB/s (0.93
+// of a copy); 29,060,773 in 198 tensors 134 us, 6.5 TB/s.
 template <typename P, typename G, int CAP, bool STOCHASTIC>
 __global__ void __launch_bounds__(THREADS) k_adamw_f32(const __grid_constant__ Table<CAP> T) {
     const Hyper& h = T.h;
@@ -445,7 +448,9 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
 
 // A warp takes h.blocks8 blocks, 8 apart (its neighbours have those between); the next one is on its way while one is computed.
 // The chunk's scales are read and written as a whole: a store of 4 bytes per block made the kernel's memory traffic alone
-// 206 instead of 144 us at 90M elements.
+// 206 instead of 144 us at 90M elements.  Measured at 90M bfloat16 parameters and gradients: 172 us, 5.3 TB/s, and up to 195 in
+// sustained work; 56 instructions per element, 14 of them the dither's hash, with the integer pipe at 0.77.  Three stages instead
+// of two 175, 3 CTAs per SM 189, 5 (spills) 196; the next block in registers instead of shared memory 237.
 constexpr int STAGES8 = 2;
 template <typename P, typename G, int CAP, bool STOCHASTIC>
 __global__ void __launch_bounds__(THREADS, 4) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {
