@@ -382,8 +382,13 @@ int ssgd_token_logprobs_backward(const void* logits, int64_t ld, int32_t fmt, co
  * in fmt_copy (SSGD_FMT_BF16 or SSGD_FMT_F16).  No two of these buffers may overlap.
  * States, fmt_state: SSGD_FMT_F32, m and v fp32 [n], scales unused; or SSGD_FMT_E4M3, one byte per element: every
  * SSGD_ADAMW_BLOCK consecutive elements share an fp32 scale (m_scale, v_scale: [ceil(n / SSGD_ADAMW_BLOCK)]), m stands
- * for code * m_scale and v for (code * v_scale)^2, the new scale being the block's largest magnitude / 448.  Zero codes
- * and scales are the initial state.  A positive sqrt(v) is never stored as 0.  A value that is not finite is stored as NaN.
+ * for code * m_scale and v for (code * v_scale)^2.  Zero codes and scales are the initial state.  Every operation on them is
+ * rounded to fp32 by itself, in this order, so that equal states give equal states on any machine:
+ *   m = (code m_scale) b1 + g (1 - b1);   r = code v_scale,  v = (r r) b2 + (g g) (1 - b2),  x = |m| or sqrt(v);
+ *   with a the block's largest x, the new scale is a (1 / 448), y = x ((1 / a) 448), and the new code the multiple
+ *   floor(y / unit + u) of the e4m3 numbers' unit at y; u = 1/2, or the dither (see stochastic).
+ * A block whose a is below 2^-100 gets scale 0.  A positive sqrt(v) gets no smaller code than the least positive one.  A value that
+ * is not finite is stored as NaN and left out of a.
  * stochastic != 0: e4m3 states and bfloat16 parameters are rounded up or down with the probability that makes them
  * right on average, by a hash of (seed, the tensor's place in the list, the element's index): give every step another
  * seed.  stochastic == 0: to nearest. */

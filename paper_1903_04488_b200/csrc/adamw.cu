@@ -13,7 +13,9 @@
 // (1 - b2) g^2, is far below half a unit, and rounding to nearest would never move v.  The dither of an element is a
 // hash of (seed, tensor, index), so a step is reproducible and independent of the schedule.  sqrt(v) > 0 never rounds
 // to 0: the element would be divided by eps alone.  A value that is not finite becomes the format's NaN and does not
-// touch its neighbours' scale.
+// touch its neighbours' scale.  What decides a code or a scale is rounded operation by operation as ssgd.h states it: a code
+// that comes out one higher in one step can be its block's largest in the next, and then the whole block differs by per cents.
+// Only the parameter's own update takes approximate roots and reciprocals (2^-23 each, beside 2^-4 from the state's codes).
 #include <cuda_fp8.h>
 
 #include <cmath>
@@ -39,8 +41,7 @@ struct Entry {
     int32_t head;        // elements before the first aligned vector; -1: no common alignment
 };
 struct Hyper {
-    float b1, omb1, b2, omb2, keep, step_size, inv_bc2, eps;
-    float sqrt_b2, sqrt_omb2;
+    float b1, omb1, b2, omb2, keep, step_size, inv_bc2, eps, one;
     const float* grad_scale;
     int32_t copy_f16;    // the copy is binary16, else bfloat16
     int32_t blocks8;     // blocks per warp and chunk (8-bit states)
@@ -183,9 +184,22 @@ __device__ __forceinline__ float2 e4m3_pair(uint32_t codes) {
     return __half22float2(__half2(r));
 }
 
-// Rounding to e4m3 in the bits of fp32.  y in [-448, 448] times 2^-120 is an fp32 number (a subnormal where e4m3 has
-// subnormals) whose exponent and first three fraction bits ARE the code, at bit 20: adding a dither in [0, 2^20) to the bits
-// and dropping the lower 20 rounds up with the probability of the dropped part, carries into the exponent included.
+// Rounding to e4m3 in the bits of fp32.  The code of a magnitude x in a block whose largest is a: y = x (448 (1 / a)), every
+// operation rounded by itself, and floor(y / unit + u), where the unit is 2^-9 below y = 2^-5 and 2^(e - 9) in [2^(e - 6),
+// 2^(e - 5)), and u in (0, 1) the dither, a multiple of 2^-17.  y times 2^-120 is an fp32 number (a subnormal where y / unit is
+// one in e4m3) whose exponent and first three fraction bits ARE the code, at bit 20: adding u 2^20 to the bits and dropping the
+// lower 20 does it, carries into the exponent included.  Two things make that inexact: a subnormal is rounded to 2^-20 units of
+// the code once more, and the root is sqrt.approx (within 2^-23; with the roundings around it 5 units of y's last place).  Neither
+// decides anything unless the sum ends up within ERROR of a multiple of 2^20; then code_of does what the formula says.
+constexpr uint32_t ERROR = 8;
+constexpr float LARGEST_SCALED = 0x1p14f;                  // of more, 2^-120 448 / a would be a subnormal
+__device__ __forceinline__ uint32_t from_border(uint32_t sum) { return (sum << 12) + (ERROR << 12); }
+__device__ __forceinline__ bool near_border(uint32_t least) { return least < (2 * ERROR) << 12; }
+__device__ __forceinline__ uint32_t code_of(float x, float per_scale, uint32_t u20) {
+    const float y = __fmul_rn(x, per_scale);
+    if (y >= 0x1p-6f) return __float_as_uint(y) + u20 - (120u << 23);
+    return (uint32_t)__fadd_rn(y * 512.f, (float)u20 * 0x1p-20f) << 20;
+}
 // The codes of four such sums x (sign in front), in one word.  Two at a time: their upper halves side by side and shifted left by
 // 4, each half's upper byte is a code once the sign is put in front of it again.
 template <bool SIGNED>
@@ -201,6 +215,12 @@ __device__ __forceinline__ uint32_t e4m3_codes(uint32_t a, uint32_t b, uint32_t 
 __device__ __forceinline__ float sqrt_fast(float x) {
     float y;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Smallest of a, b, c; a NaN does not count
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float y;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
     return y;
 }
 __device__ __forceinline__ float rcp_fast(float x) {
@@ -273,9 +293,9 @@ __device__ __forceinline__ Block<P, G> taken(const Staged<P, G>& s) {
 
 // The step's constants in the form the 8-bit kernel uses them
 struct Hyper8 {
-    float b1, g_m;              // m = (b1 scale) code + g_m g
-    float sqrt_b2, g_v;         // v = ((sqrt b2) scale code)^2 + (g_v g)^2
-    float keep, minus_step, inv_bc2, eps;
+    float gs, b1, omb1, b2, omb2, keep, minus_step, inv_bc2, eps;
+    float one;      // 1, which the compiler does not know: x * one + y is a sum whose operands it cannot leave unrounded (it
+                    // contracts mul.rn.f32x2 and add.rn.f32x2 to one fma, unlike their scalar forms)
 };
 
 __device__ __forceinline__ float part(const float2 (&f)[4], int j) { return j & 1 ? f[j / 2].y : f[j / 2].x; }
@@ -307,111 +327,111 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
             fr[j] = e4m3_pair((in0 ? C.v[i0] : 0u) | (in1 ? C.v[i1] : 0u) << 8);
         }
     }
-    const float2 ms = both(ms_io * h.b1), vs = both(vs_io * h.sqrt_b2);
-    float am = 0.f, ar = 0.f, ap = 0.f;
+    const float2 ms = both(ms_io), vs = both(vs_io);
+    float am = 0.f, av = 0.f, ap = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float2 m = fma2(fm[j], ms, mul2(fg[j], both(h.g_m)));
-        const float2 r0 = mul2(fr[j], vs), gv = mul2(fg[j], both(h.g_v));
-        const float2 v = fma2(r0, r0, mul2(gv, gv));
-        const float2 r = make_float2(sqrt_fast(v.x), sqrt_fast(v.y));
-        const float2 denom = fma2(r, both(h.inv_bc2), both(h.eps));
+        const float2 g = mul2(fg[j], both(h.gs));
+        const float2 m = fma2(mul2(mul2(fm[j], ms), both(h.b1)), both(h.one), mul2(g, both(h.omb1)));
+        const float2 r0 = mul2(fr[j], vs);
+        const float2 v = fma2(mul2(mul2(r0, r0), both(h.b2)), both(h.one), mul2(mul2(g, g), both(h.omb2)));
+        const float2 denom = fma2(make_float2(sqrt_fast(v.x), sqrt_fast(v.y)), both(h.inv_bc2), both(h.eps));
         const float2 q = mul2(m, make_float2(rcp_fast(denom.x), rcp_fast(denom.y)));
         fp[j] = fma2(q, both(h.minus_step), mul2(fp[j], both(h.keep)));
         fm[j] = m;
-        fr[j] = r;
+        fr[j] = v;
         am = max3_nan(am, fabsf(m.x), fabsf(m.y));
-        ar = max3_nan(ar, r.x, r.y);
+        av = max3_nan(av, v.x, v.y);
         if (sizeof(P) == 2) ap = max3_nan(ap, fabsf(fp[j].x), fabsf(fp[j].y));
     }
-    // Rare: a value that is not finite (it must not count for the scale, and its code is NaN), or so large that 2^-120 over its
-    // scale would be subnormal
-    const float large = 0x1p12f;
-    const bool odd = __any_sync(0xffffffffu, !(max3_nan(am, ar, ap) < large));
+    // Rare: a value that is not finite.  It must not count for the scale, and its code is NaN
+    const bool odd = __any_sync(0xffffffffu, !(max3_nan(am, av, ap) < INFINITY));
     if (odd) {
-        am = ar = 0.f;
+        am = av = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (finite(part(fm, j))) am = fmaxf(am, fabsf(part(fm, j)));
-            if (finite(part(fr, j))) ar = fmaxf(ar, part(fr, j));
+            if (finite(part(fr, j))) av = fmaxf(av, part(fr, j));
         }
     }
     am = warp_max(am);
-    ar = warp_max(ar);
-    // Below 2^-100 the block is held as zeros.  value * (1 / scale) is within 5 units of exact: the dither's 16 bits leave
-    // room for 7 before the largest magnitude could round past 448.
+    const float ar = __fsqrt_rn(warp_max(av));             // roots rounded to nearest are in order
+    // Below 2^-100 the block is held as zeros
     const float least = 0x1p-100f, scale_m = am * (1.f / 448.f), scale_r = ar * (1.f / 448.f);
-    float im = am < least ? 0.f : rcp_fast(scale_m) * 0x1p-120f, ir = ar < least ? 0.f : rcp_fast(scale_r) * 0x1p-120f;
-    if (odd) {
-        const float2 down = both(0x1p-120f);
-        if (am >= large) {
-            im = rcp_fast(scale_m * 0x1p-120f) * 0x1p-120f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) fm[j] = mul2(fm[j], down);
-        }
-        if (ar >= large) {
-            ir = rcp_fast(scale_r * 0x1p-120f) * 0x1p-120f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) fr[j] = mul2(fr[j], down);
-        }
-    }
+    const float per_m = am < least ? 0.f : __fmul_rn(__frcp_rn(am), 448.f), per_r = ar < least ? 0.f : __fmul_rn(__frcp_rn(ar), 448.f);
+    const float im = per_m * 0x1p-120f, ir = per_r * 0x1p-120f;
     if (lane == 0) {
         ms_io = am < least ? 0.f : scale_m;
         vs_io = ar < least ? 0.f : scale_r;
     }
     // The dither of element i is the hash of key ^ i (see dither_word).  What belongs to the chunk, to the lane and to j has no
-    // bits in common, and j none above the 16th, so the first step of the mixing is the same for all j.
+    // bits in common, and j none above the 16th, so the first step of the mixing is the same for all j.  16 bits each (m: the
+    // lower half of the word, v: the upper) at bit 4, in the middle of their interval; without a seed 1/2: to nearest.
     uint32_t seed = index ^ (VECTOR ? lane8 : at(0));
     seed ^= seed >> 16;
+    auto mixed = [&](uint32_t seed, int j) {
+        uint32_t r = seed ^ (uint32_t)(VECTOR ? j : 32 * j);
+        r *= 0x6A09E667u;
+        r ^= r >> 15;
+        return r * 0xBB67AE85u;                              // the word is r ^ (r >> 16)
+    };
+    auto dither_m = [&](uint32_t r) { return STOCHASTIC ? ((r >> 12) ^ (r << 4)) & 0xffff0u : 0x80000u - 8u; };
+    auto dither_v = [&](uint32_t r) { return STOCHASTIC ? (r >> 12) & 0xffff0u : 0x80000u - 8u; };
     uint32_t out_m[2], out_v[2], out_p[4];
+    uint32_t border = ~0u, least_v = ~0u;                    // least_v: bits of v less 1, so that zeros do not count
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         uint32_t code_m[4], code_v[4], np[4];
-        uint32_t least_v = ~0u;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int j = half * 4 + q;
-            const float2 ym = mul2(fm[j / 2], both(im)), yr = mul2(fr[j / 2], both(ir));
-            // 16 bits of dither each (m: the lower half of the word, v: the upper), in the middle of their interval; without
-            // a seed 1/2: to nearest
-            uint32_t dm = 0x80000u - 8u, dv = 0x80000u - 8u;
-            if (STOCHASTIC) {
-                uint32_t r = seed ^ (uint32_t)(VECTOR ? j : 32 * j);
-                r *= 0x6A09E667u;
-                r ^= r >> 15;
-                r *= 0xBB67AE85u;                            // the word is r ^ (r >> 16)
-                const uint32_t upper = r >> 12;
-                dm = (upper ^ (r << 4)) & 0xffff0u;
-                dv = upper & 0xffff0u;
-                if (sizeof(P) == 2) np[q] = __float_as_uint(part(fp, j)) + (((r ^ (r >> 16)) * 0x9E3779B9u) >> 16);
-            }
-            code_m[q] = __float_as_uint(j & 1 ? ym.y : ym.x) + dm + 8u;
-            code_v[q] = __float_as_uint(j & 1 ? yr.y : yr.x) + dv + 8u;
-            if (q & 1) least_v = __vimin3_u32(least_v, code_v[q - 1], code_v[q]);
-        }
-        if (least_v < 1u << 20) {                            // a positive value keeps at least the smallest code
-#pragma unroll
-            for (int q = 0; q < 4; ++q) code_v[q] = max(code_v[q], part(fr, half * 4 + q) > 0.f ? 1u << 20 : 0u);
-        }
-        if (odd) {                                           // the format's NaN, 0x7f
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (!finite(part(fm, half * 4 + q))) code_m[q] = 0x7fu << 20;
-                if (!finite(part(fr, half * 4 + q))) code_v[q] = 0x7fu << 20;
+            const float2 v = fr[j / 2], ym = mul2(fm[j / 2], both(im)), yr = mul2(make_float2(sqrt_fast(v.x), sqrt_fast(v.y)), both(ir));
+            const uint32_t r = STOCHASTIC ? mixed(seed, j) : 0u;
+            code_m[q] = __float_as_uint(j & 1 ? ym.y : ym.x) + dither_m(r) + 8u;
+            code_v[q] = __float_as_uint(j & 1 ? yr.y : yr.x) + dither_v(r) + 8u;
+            if (sizeof(P) == 2) np[q] = STOCHASTIC ? __float_as_uint(part(fp, j)) + (((r ^ (r >> 16)) * 0x9E3779B9u) >> 16)
+                                                   : (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(part(fp, j))) << 16;
+            if (q & 1) {
+                least_v = __vimin3_u32(least_v, __float_as_uint(v.x) - 1u, __float_as_uint(v.y) - 1u);
+                border = __vimin3_u32(border, from_border(code_m[q - 1]), from_border(code_m[q]));
+                border = __vimin3_u32(border, from_border(code_v[q - 1]), from_border(code_v[q]));
             }
         }
         out_m[half] = e4m3_codes<true>(code_m[0], code_m[1], code_m[2], code_m[3]);
         out_v[half] = e4m3_codes<false>(code_v[0], code_v[1], code_v[2], code_v[3]);
         if constexpr (sizeof(P) == 2) {                      // bfloat16 parameters: the new value in the upper half of a word
-            if (!STOCHASTIC || odd) {                        // to nearest, or what is not finite, which no dither may touch
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float x = part(fp, half * 4 + q);
-                    if (!STOCHASTIC || !finite(x)) np[q] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x)) << 16;
-                }
-            }
             out_p[half * 2] = __byte_perm(np[0], np[1], 0x7632);
             out_p[half * 2 + 1] = __byte_perm(np[2], np[3], 0x7632);
+        }
+    }
+    // Seldom: everything again, with care.  From the hash on, so that nothing has to be kept for it.
+    const float smallest = least_v == ~0u ? INFINITY : sqrt_fast(__uint_as_float(least_v)) * per_r;    // of the positive ones
+    if (odd || !(fmaxf(am, ar) <= LARGEST_SCALED) || !(smallest >= 0x1p-8f) || near_border(border)) {
+        float again_m = per_m, again_r = per_r;
+        asm volatile("" : "+r"(seed), "+f"(again_m), "+f"(again_r));
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint32_t code_m[4], code_v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int j = half * 4 + q;
+                const float m = part(fm, j), v = part(fr, j);
+                const uint32_t r = STOCHASTIC ? mixed(seed, j) : 0u, dm = dither_m(r) + 8u, dv = dither_v(r) + 8u;
+                code_m[q] = __float_as_uint(__fmul_rn(m, again_m) * 0x1p-120f) + dm;
+                if (near_border(from_border(code_m[q]))) code_m[q] = code_of(fabsf(m), again_m, dm) | (__float_as_uint(m) & 0x80000000u);
+                code_v[q] = __float_as_uint(__fmul_rn(sqrt_fast(v), again_r) * 0x1p-120f) + dv;
+                // a positive value keeps at least the smallest code (and here comes what sqrt.approx has flushed to zero)
+                if (v > 0.f && (code_v[q] < 1u << 20 || near_border(from_border(code_v[q])))) code_v[q] = max(code_of(__fsqrt_rn(v), again_r, dv), 1u << 20);
+                if (!finite(m)) code_m[q] = 0x7fu << 20;     // the format's NaN
+                if (!finite(v)) code_v[q] = 0x7fu << 20;
+                if constexpr (sizeof(P) == 2) {              // no dither may touch what is not finite
+                    const float x = part(fp, j);
+                    const uint32_t np = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x));
+                    if (STOCHASTIC && !finite(x)) out_p[j / 2] = j & 1 ? (out_p[j / 2] & 0xffffu) | np << 16 : (out_p[j / 2] & 0xffff0000u) | np;
+                }
+            }
+            out_m[half] = e4m3_codes<true>(code_m[0], code_m[1], code_m[2], code_m[3]);
+            out_v[half] = e4m3_codes<false>(code_v[0], code_v[1], code_v[2], code_v[3]);
         }
     }
     if (VECTOR) {
@@ -448,9 +468,11 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
 
 // A warp takes h.blocks8 blocks, 8 apart (its neighbours have those between); the next one is on its way while one is computed.
 // The chunk's scales are read and written as a whole: a store of 4 bytes per block made the kernel's memory traffic alone
-// 206 instead of 144 us at 90M elements.  Measured at 90M bfloat16 parameters and gradients: 172 us, 5.3 TB/s, and up to 195 in
-// sustained work; 56 instructions per element, 14 of them the dither's hash, with the integer pipe at 0.77.  Three stages instead
-// of two 175, 3 CTAs per SM 189, 5 (spills) 196; the next block in registers instead of shared memory 237.
+// 206 instead of 144 us at 90M elements.  Measured at 90M bfloat16 parameters and gradients: 203 us, 4.5 TB/s, and 211 in
+// sustained work; 8 of 10 issue slots, the integer pipe at 0.75.  The codes' exactness is 30 us of it: 172 with b1 and b2 folded
+// into the scales and approximate roots alone.  At 30M, 74 us: with sqrt.rn for every element 78, with the careful branch at
+// every four elements 77; where the positive roots of a block span more than 2^16 its lanes take that branch, 115.  Of the form
+// with folded constants at 90M: three stages instead of two 175, the next block in registers instead of shared memory 237.
 constexpr int STAGES8 = 2;
 template <typename P, typename G, int CAP, bool STOCHASTIC>
 __global__ void __launch_bounds__(THREADS, 4) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {
@@ -479,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_adamw_8bit(const __grid_constant
     const bool has_scale = mine < nscales && mine * QBLOCK < C.n;
     if (has_scale) scales[which][mine] = *scale;
     const float gs = T.h.grad_scale ? *T.h.grad_scale : 1.f;
-    const Hyper8 h{T.h.b1, T.h.omb1 * gs, T.h.sqrt_b2, T.h.sqrt_omb2 * gs, T.h.keep, -T.h.step_size, T.h.inv_bc2, T.h.eps};
+    const Hyper8 h{gs, T.h.b1, T.h.omb1, T.h.b2, T.h.omb2, T.h.keep, -T.h.step_size, T.h.inv_bc2, T.h.eps, T.h.one};
     __syncthreads();
     int stage = 0;
 #pragma unroll 1
@@ -594,12 +616,11 @@ extern "C" int ssgd_adamw_step(const ssgd_adamw_tensor* tensors, int32_t count, 
     h.omb1 = (float)(1.0 - beta1);
     h.b2 = (float)beta2;
     h.omb2 = (float)(1.0 - beta2);
-    h.sqrt_b2 = (float)std::sqrt(beta2);
-    h.sqrt_omb2 = (float)std::sqrt(1.0 - beta2);
     h.keep = (float)(1.0 - lr * weight_decay);
     h.step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
     h.inv_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
     h.eps = (float)eps;
+    h.one = 1.f;
     h.grad_scale = grad_scale;
     h.copy_f16 = fmt_copy == SSGD_FMT_F16;
     h.blocks8 = 1;
