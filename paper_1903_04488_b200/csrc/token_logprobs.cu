@@ -49,22 +49,29 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
 template <typename T> __device__ __forceinline__ float fast_limit() { return 1e30f; }
 template <> __device__ __forceinline__ float fast_limit<__half>() { return 6e4f; }
 
-// The running sums of one thread, relative to its maximum logit m, in powers of two: with c = scale * log2 e, shift = m c and
-// d = z c - shift, s = sum 2^d and w = sum 2^d d.  shift is rounded, but as every d is taken from the same shift that only
-// moves the reference.  Beyond HUGE_LOGIT, where masks put their lowest values, z c would overflow: there d = (z - m) c, and
-// nothing from there has weight beside a smaller logit.
+// The running sums of one thread, relative to its maximum logit m, in powers of two: with c = scale * log2 e, s = sum 2^d and
+// w = sum 2^d d.  Two forms of d:
+//   near    d = z c - shift, one fma, shift = m c rounded.  As every d is taken from the same shift, the rounding only moves the
+//           reference: d at the maximum is not 0 but up to half a unit of shift's last place, 2 while |shift| < NEAR = 2^26
+//   far     d = (z - m) c, exact at the maximum however large that is.  Beside a far maximum the logits that matter lie
+//           within a factor 2 of it, and z - m is exact, in the logits' own format too.
+// The far form is for rows or pieces of rows that hold nothing but a mask's large negative numbers, and for logits far from zero.
 struct Sums {
     float m, shift, s, w;
 };
-constexpr float HUGE_LOGIT = 1e30f;
+constexpr float NEAR = 0x1p26f;
+constexpr float HUGE_LOGIT = 1e30f;         // beyond, z c might overflow: logits are taken one by one
 
 __device__ __forceinline__ Sums no_sums() { return Sums{NEG_INF, NEG_INF, 0.f, 0.f}; }
-__device__ __forceinline__ bool ordinary(float m, float shift) { return fabsf(m) < HUGE_LOGIT && fabsf(shift) < HUGE_LOGIT; }
+__device__ __forceinline__ bool near(float shift) { return fabsf(shift) < NEAR; }
 
+// To the maximum m.  What the sums lose is 2^(old reference - new reference); a far form's reference is m c itself, unrounded.
 __device__ __forceinline__ void rebase(Sums& a, float m, float c) {
     const float shift = __fmul_rn(m, c);
     if (a.m > NEG_INF || a.m != a.m) {
-        const float delta = ordinary(m, shift) ? a.shift - shift : (a.m - m) * c, f = ex2(delta);
+        const bool from_near = near(a.shift), to_near = near(shift);
+        const float delta = from_near ? (to_near ? a.shift - shift : -fmaf(m, c, -a.shift)) : (to_near ? fmaf(a.m, c, -shift) : (a.m - m) * c);
+        const float f = ex2(delta);
         a.w = f * fmaf(delta, a.s, a.w);
         if (f == 0.f && a.s == a.s && a.w != a.w) a.w = 0.f;   // 0 * -inf: the old part has vanished
         a.s *= f;
@@ -78,7 +85,7 @@ __device__ __forceinline__ void add_careful(Sums& a, float z, float c) {
     const float m = max_nan(a.m, z);
     if (!(m == a.m)) rebase(a, m, c);
     if (z == NEG_INF && a.m == a.m) return;                // contributes nothing, whatever the maximum
-    const float d = ordinary(a.m, a.shift) ? fmaf(z, c, -a.shift) : (z - a.m) * c, e = ex2(d);
+    const float d = near(a.shift) ? fmaf(z, c, -a.shift) : (z - a.m) * c, e = ex2(d);
     a.s += e;
     if (e > 0.f || e != e) a.w = fmaf(e, d, a.w);
 }
@@ -180,6 +187,27 @@ __device__ __forceinline__ Vec<__half, 8> raised(Vec<__half, 8> v, float low) {
     return v;
 }
 
+// A granule less m (a number of the format)
+__device__ __forceinline__ Vec<float, 4> less(Vec<float, 4> v, float m) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v.e[e] -= m;
+    return v;
+}
+__device__ __forceinline__ Vec<__nv_bfloat16, 8> less(Vec<__nv_bfloat16, 8> v, float m) {
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+    const __nv_bfloat162 l = __float2bfloat162_rn(m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __hsub2(h[e], l);
+    return v;
+}
+__device__ __forceinline__ Vec<__half, 8> less(Vec<__half, 8> v, float m) {
+    __half2* h = reinterpret_cast<__half2*>(&v);
+    const __half2 l = __float2half2_rn(m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __hsub2(h[e], l);
+    return v;
+}
+
 // A value no larger than m - reach, reach = 160 / c rounded up, and below every element that could matter: elements under it
 // are raised to it, so that -inf does not make 0 * -inf.  2^-160 is zero in fp32.
 template <typename T> __device__ __forceinline__ float floor_for(float m, float reach) { return __fsub_rd(m, reach); }
@@ -206,7 +234,7 @@ __device__ __noinline__ Sums add_granule_carefully(Sums a, Vec<T, 16 / sizeof(T)
 // Granules v[0] .. v[have - 1] (`have` is the same for the whole CTA); returns their maximum.  Elements that are not there are -inf: they change neither
 // the maximum nor the sums.
 template <typename T, int U>
-__device__ __forceinline__ float add_granules(Running& r, const Vec<T, 16 / sizeof(T)> (&v)[U], int have) {
+__device__ __forceinline__ float add_granules(Running& r, Vec<T, 16 / sizeof(T)> (&v)[U], int have) {
     constexpr int VEC = 16 / sizeof(T);
     PairMax<T> top(NEG_INF);
 #pragma unroll
@@ -215,16 +243,24 @@ __device__ __forceinline__ float add_granules(Running& r, const Vec<T, 16 / size
     const float here = top.value(), m = max_nan(r.a.m, here);
     if (!(m == r.a.m)) {
         rebase(r.a, m, r.c);
-        r.low = fabsf(m) < fast_limit<T>() && ordinary(m, r.a.shift) ? floor_for<T>(m, r.reach) : NEG_INF;
+        r.low = fabsf(m) < fast_limit<T>() && fabsf(r.a.shift) < HUGE_LOGIT ? floor_for<T>(m, r.reach) : NEG_INF;
     }
     if (r.low > NEG_INF) {
-        const float2 minus_shift = both(-r.a.shift), c2 = both(r.c);
+        float low = r.low, shift = r.a.shift;
+        if (!near(shift)) {                                // (z - m) c + 0
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < have) v[u] = less(raised(v[u], low), m);
+            low = -fast_limit<T>();
+            shift = 0.f;
+        }
+        const float2 minus_shift = both(-shift), c2 = both(r.c);
         float2 s = both(0.f), w = both(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u < have) {
                 float2 f[VEC / 2];
-                unpack_pairs(raised(v[u], r.low), f);
+                unpack_pairs(raised(v[u], low), f);
 #pragma unroll
                 for (int e = 0; e < VEC / 2; ++e) {
                     const float2 d = fma2(f[e], c2, minus_shift), x = make_float2(ex2(d.x), ex2(d.y));
@@ -527,7 +563,7 @@ __global__ void __launch_bounds__(NT, 6 * 256 / NT) k_token_logprobs(const Logpr
         const bool none = a.s == 0.f;                      // every logit is -inf
         // relative to the reference that the sums have: log p = (x c - shift) - log2 s in powers of two; in powers of e from the
         // start where that would overflow
-        const bool plain = ordinary(a.m, a.shift);
+        const bool plain = near(a.shift);
         auto logp_of = [&](float x) {
             if (none || (x == NEG_INF && a.s == a.s)) return NEG_INF;
             return plain && fabsf(x) < HUGE_LOGIT ? (fmaf(x, c, -a.shift) - log2s) * LN2 : fmaf(x - a.m, A.scale, -log2s * LN2);
