@@ -366,7 +366,7 @@ int ssgd_token_logprobs(const void* logits, int64_t ld, int32_t fmt, const void*
                         void* stream);
 /* The gradient with respect to the logits of sum(d_logp logp) + sum(d_entropy entropy) + sum(d_top top_logp):
  *   dlogits_j = scale (d_logp [j = id] + sum_m d_top_m [j = top_idx_m] - p_j (d_logp + sum_m d_top_m + d_entropy (log p_j + entropy)))
- * lse, entropy: [rows], as the forward pass wrote them.  d_logp, d_entropy: [rows], either may be NULL (0).  top_idx, d_top:
+ * with p_j = e^(z_j - lse), at most 1.  lse, entropy: [rows], as the forward pass wrote them.  d_logp, d_entropy: [rows], either may be NULL (0).  top_idx, d_top:
  * [rows][top].  A top_idx outside [0, vocab) adds to the sum only.  dlogits: [rows][vocab] in fmt; may be logits itself
  * (same ld). */
 int ssgd_token_logprobs_backward(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes,

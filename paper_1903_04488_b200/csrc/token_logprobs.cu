@@ -45,6 +45,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
     return y;
 }
 
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
 // Largest magnitude of a format for which the fast path below is taken, with room for the floor.
 template <typename T> __device__ __forceinline__ float fast_limit() { return 1e30f; }
 template <> __device__ __forceinline__ float fast_limit<__half>() { return 6e4f; }
@@ -625,13 +631,14 @@ __global__ void __launch_bounds__(NT) k_token_logprobs_back(const LogprobBackArg
     const float h = ENTROPY ? A.entropy[row] : 0.f;
     const float scale = A.scale;
     const float base = -scale * fmaf(g_h, h, sum), slope = -scale * g_h;
-    // gradient of two logits without the columns' own terms: p (base + slope log p)
+    // gradient of two logits without the columns' own terms: p (base + slope log p).  p <= 1: far from zero the 32 bits of lse can lie
+    // below a logit by hundreds, and 2^x would be inf.  (log p itself keeps the last place that lse has lost: entropy has it too.)
     auto grad = [&](float2 x) {
-        float2 logp = fma2(x, both(scale), both(minus_lse));
-        const float2 t = mul2(logp, both(LOG2E)), p = make_float2(ex2(t.x), ex2(t.y));
+        const float2 logp = fma2(x, both(scale), both(minus_lse));
+        const float2 t = mul2(make_float2(min_nan(logp.x, 0.f), min_nan(logp.y, 0.f)), both(LOG2E)), p = make_float2(ex2(t.x), ex2(t.y));
         if (!ENTROPY) return mul2(p, both(base));
-        logp = make_float2(fmaxf(logp.x, -200.f), fmaxf(logp.y, -200.f));
-        return mul2(p, fma2(logp, both(slope), both(base)));
+        const float2 bounded = make_float2(fminf(fmaxf(logp.x, -200.f), 1.f), fminf(fmaxf(logp.y, -200.f), 1.f));
+        return mul2(p, fma2(bounded, both(slope), both(base)));
     };
     auto one = [&](float x) { return from_f32<T>(grad(both(x)).x); };
     // the columns with a term of their own that this CTA writes

@@ -68,3 +68,38 @@ def test_logprobs_of_large_logits(cuda_device, kind, value, dtype):
                     assert torch.equal(r.top_idx.long(), order)
                     want = every.gather(1, order)
                     assert ((r.top_logp.double() - want).abs() <= rel[:, None] + 6 * U * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("value", [-1e9, -1e10, -1e12, -1e20])
+@pytest.mark.parametrize("kind", ["all", "front", "behind", "random", "one left", "far"])
+def test_gradient_of_large_logits(cuda_device, kind, value, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    rows, v = 5, 9001
+    z = rows_of(kind, value, rows, v, dtype, gen)
+    ids = torch.randint(0, v, (rows,), generator=gen, device="cuda")
+    d, dh = (torch.randn(rows, generator=gen, device="cuda") for _ in range(2))
+    d[1] = dh[1] = 0.0                         # a row that the loss leaves out
+    for scale in (0.1, 1.0, 10.0, 0.37):
+        r = T.token_logprobs(z, ids, scale=scale)
+        for kw in ({}, dict(entropy=r.entropy, d_entropy=dh)):
+            out = T.token_logprobs_backward(z, ids, r.lse, d, scale=scale, **kw)
+            assert out.isfinite().all() and not out[1].any()
+            # a probability is at most 1, and p |log p| at most 1 / e, whatever lse has lost to its 32 bits
+            most = scale * (2 * d.abs() + (dh.abs() * (1 + r.entropy) if kw else 0)) * (1 + 2 * HALF[dtype]) + 1e-30
+            assert (out.float().abs() <= most[:, None]).all()
+            if kind in ("all", "far"):
+                continue                       # lse itself does not tell such logits apart
+            _, h, lse, logp, p = definition(z, ids, scale)
+            one = torch.zeros_like(p).scatter_(1, ids[:, None], d.double()[:, None])
+            gh = dh.double()[:, None] if kw else 0.0
+            lp = torch.where(p > 0, logp, 0.0)
+            want = scale * (one - p * (d.double()[:, None] + gh * (lp + h[:, None])))
+            # lse and entropy come with the forward pass's tolerance
+            given = (v / 256 + 64) * U + 4 * U * (h + 4) + 6 * U * lse.abs()
+            relp = (8 * U + 6 * U * lp.abs()) + given[:, None]
+            size = d.double().abs()[:, None] + (gh * 1.0).abs() * (lp.abs() + h[:, None]) if kw else d.double().abs()[:, None]
+            # 2^x below the smallest normal number is 0
+            tol = scale * ((p * (relp + 40 * U) + 2.0 ** -126) * size + 40 * U * one.abs() + (p * (gh * 1.0).abs() * 2 * (given * (1 + h) + 4 * U * (h + 4))[:, None] if kw else 0.0))
+            near = (out.double() - want).abs() <= tol + HALF[dtype] * (want.abs() + tol) + 1e-37
+            assert near.all(), f"scale {scale}: {int((~near).sum())} outside"
