@@ -274,14 +274,26 @@ void column(PyObject* list, Py_ssize_t count, const char* name, at::ScalarType t
     }
 }
 
-// (buffer, params, m, v, m_scale, v_scale, copies, grads, device, lr, b1, b2, eps, decay, step, grad_scale, seed, count): the buffer's address
-// (room for an ssgd_adamw_tensor and, behind them all, a size per parameter); the lists; None for what there is not
+// An object's memory, held for the duration of a call
+struct Memory {
+    Py_buffer view{};
+    explicit Memory(PyObject* o) {
+        if (PyObject_GetBuffer(o, &view, PyBUF_CONTIG) != 0) throw Raised{};
+    }
+    ~Memory() { PyBuffer_Release(&view); }
+    Memory(const Memory&) = delete;
+    Memory& operator=(const Memory&) = delete;
+};
+
+// (buffer, params, m, v, m_scale, v_scale, copies, grads, device, lr, b1, b2, eps, decay, step, grad_scale, seed): the buffer (int64: room
+// for an ssgd_adamw_tensor per parameter and, behind them all, a size per parameter); the lists; None for what there is not
 PyObject* adamw_step(PyObject* const* a) {
-    auto* desc = reinterpret_cast<ssgd_adamw_tensor*>((uintptr_t)PyLong_AsUnsignedLongLong(a[0]));
+    const Memory memory(a[0]);
+    auto* desc = static_cast<ssgd_adamw_tensor*>(memory.view.buf);
     const int dev = (int)integer(a[8], "device");
     if (dev != (int)c10::cuda::current_device())
         raise(PyExc_ValueError, "grads: the parameters are on device " + std::to_string(dev) + ", which is not the current one");
-    const Py_ssize_t count = (Py_ssize_t)integer(a[17], "count");      // what the buffer has room for
+    const Py_ssize_t count = memory.view.len / (Py_ssize_t)(sizeof(ssgd_adamw_tensor) + 8);
     if (count < 1 || !PyList_Check(a[1]) || PyList_GET_SIZE(a[1]) != count) raise(PyExc_ValueError, "params: not as many as there were");
     const auto* sizes = reinterpret_cast<const int64_t*>(desc + count);
     const at::ScalarType type_p = tensor(PyList_GET_ITEM(a[1], 0), "params").scalar_type();
@@ -369,7 +381,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(layer_norm, 5), ENTRY(layer_norm_backward, 9), ENTRY(token_logprobs, 4), ENTRY(token_logprobs_backward, 10),
-                         ENTRY(adamw_step, 18), ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(adamw_step, 17), ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -163,13 +163,13 @@ class AdamW:
         # room for an ssgd_adamw_tensor (64 bytes) per parameter, and behind them their sizes
         self._buffer = np.zeros(len(params) * 9, dtype=np.int64)
         self._buffer[len(params) * 8:] = sizes
-        self._address, self._dev = self._buffer.ctypes.data, dev.index
+        self._dev = dev.index
 
     def step(self, grads, *, seed: int | None = None, grad_scale: torch.Tensor | None = None, lr: float | None = None) -> None:
         """One step.  grads: one contiguous tensor per parameter (float32, bfloat16 or float16, all the same type), None
         for a parameter that is left alone.  seed: round e4m3 states and bfloat16 parameters stochastically with it (another
         one every step).  grad_scale: float32 scalar on the device that multiplies every gradient."""
-        (_native or native()).adamw_step(self._address, self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies, grads,
+        (_native or native()).adamw_step(self._buffer, self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies, grads,
                                          self._dev, self.lr if lr is None else lr, *self.betas, self.eps, self.weight_decay,
-                                         self.step_count + 1, grad_scale, seed, len(self._buffer) // 9)
+                                         self.step_count + 1, grad_scale, seed)
         self.step_count += 1

@@ -1,0 +1,41 @@
+"""The training operators as a program uses them: optimizers that are copied or share parameters, calls that are refused, tensors that
+autograd hands over as it likes, and derivatives of derivatives."""
+import copy
+import io
+
+import pytest
+import torch
+
+from paper_1903_04488_b200 import train_ops as T
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=1e-2, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1)
+
+
+def rand(*shape, seed=1, dtype=torch.float32):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(dtype)
+
+
+def saved(opt):
+    file = io.BytesIO()
+    torch.save(opt, file)
+    file.seek(0)
+    return torch.load(file, weights_only=False)
+
+
+@pytest.mark.parametrize("again", [copy.deepcopy, saved])
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_a_copied_optimizer_steps_its_own_tensors(cuda_device, state, again):
+    a = T.AdamW([rand(n, seed=n) for n in (1000, 7, 300)], state=state, **HYPER)
+    grads = [rand(n, seed=n + 1) for n in (1000, 7, 300)]
+    a.step(grads, seed=1)
+    b = again(a)
+    before = [p.clone() for p in b.params]
+    a.step(grads, seed=2)
+    assert all(torch.equal(p, q) for p, q in zip(b.params, before)) and b.step_count == 1
+    want = [[t.float().clone() for t in x] for x in (a.params, a.m, a.v)]
+    del a
+    b.step(grads, seed=2)
+    assert b.step_count == 2
+    assert all(torch.equal(p.float(), q) for x, y in zip((b.params, b.m, b.v), want) for p, q in zip(x, y))
