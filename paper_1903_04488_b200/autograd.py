@@ -1,7 +1,9 @@
-"""The differentiable operators of `train_ops` as autograd functions: what a model calls."""
+"""The differentiable operators of `train_ops` as autograd functions: what a model calls.  They can be differentiated once: a
+second derivative through them raises."""
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import train_ops
 
@@ -15,6 +17,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, stats = ctx.saved_tensors
         need = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
@@ -37,6 +40,7 @@ class _TokenLogprobs(torch.autograd.Function):
         return logp, entropy, lse, top_idx, top_logp
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_logp, d_entropy, _lse, _idx, d_top):
         logits, ids, stats, top_idx = ctx.saved_tensors
         whole = lambda t: None if t is None else t.contiguous()  # noqa: E731

@@ -6,6 +6,7 @@ import io
 import pytest
 import torch
 
+from paper_1903_04488_b200 import autograd as A
 from paper_1903_04488_b200 import train_ops as T
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,15 @@ def test_a_copied_optimizer_steps_its_own_tensors(cuda_device, state, again):
     b.step(grads, seed=2)
     assert b.step_count == 2
     assert all(torch.equal(p.float(), q) for x, y in zip((b.params, b.m, b.v), want) for p, q in zip(x, y))
+
+
+def test_a_second_derivative_is_refused(cuda_device):
+    x, w, b = (t.requires_grad_() for t in (rand(6, 32), rand(32, seed=2), rand(32, seed=3)))
+    dx, = torch.autograd.grad(A.layer_norm(x, w, b).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (dx.square().sum() + x.square().sum()).backward()
+    z = rand(6, 32, seed=4).requires_grad_()
+    ids = torch.zeros(6, dtype=torch.int64, device="cuda")
+    dz, = torch.autograd.grad(A.token_logprobs(z, ids)[0].square().sum(), z, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (dz.square().sum() + z.square().sum()).backward()
