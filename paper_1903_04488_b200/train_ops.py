@@ -165,10 +165,14 @@ class AdamW:
         self._buffer[len(params) * 8:] = sizes
         self._dev = dev.index
 
-    def step(self, grads, *, seed: int | None = None, grad_scale: torch.Tensor | None = None, lr: float | None = None) -> None:
+    def step(self, grads, *, seed: int | str | None = "step", grad_scale: torch.Tensor | None = None, lr: float | None = None) -> None:
         """One step.  grads: one contiguous tensor per parameter (float32, bfloat16 or float16, all the same type), None
-        for a parameter that is left alone.  seed: round e4m3 states and bfloat16 parameters stochastically with it (another
-        one every step).  grad_scale: float32 scalar on the device that multiplies every gradient."""
+        for a parameter that is left alone.  grad_scale: float32 scalar on the device that multiplies every gradient.
+
+        seed: round e4m3 states and bfloat16 parameters stochastically with it (another one every step); None: to nearest.  "step": with
+        e4m3 states the step's number, since their second moment, rounded to nearest, would never move; otherwise None."""
+        if seed == "step":
+            seed = None if self.m_scale is None else self.step_count + 1
         (_native or native()).adamw_step(self._buffer, self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies, grads,
                                          self._dev, self.lr if lr is None else lr, *self.betas, self.eps, self.weight_decay,
                                          self.step_count + 1, grad_scale, seed)

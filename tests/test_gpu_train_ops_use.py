@@ -52,3 +52,27 @@ def test_a_second_derivative_is_refused(cuda_device):
     dz, = torch.autograd.grad(A.token_logprobs(z, ids)[0].square().sum(), z, create_graph=True)
     with pytest.raises(RuntimeError):
         (dz.square().sum() + z.square().sum()).backward()
+
+
+def test_8bit_states_round_stochastically_unless_told_otherwise(cuda_device):
+    """A second moment that shrinks by a hundredth a step follows; rounded to nearest it would stay where it is."""
+    n = 1 << 16
+    opt = T.AdamW([torch.zeros(n, device="cuda")], state="e4m3", betas=(0.9, 0.99), lr=0.0)
+    opt.step([torch.rand(n, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda") * 0.1 + 0.01])
+    second = lambda: float((opt.v[0].double() * opt.v_scale[0].double().repeat_interleave(256)).square().mean())  # noqa: E731
+    v0 = second()
+    for _ in range(100):
+        opt.step([torch.zeros(n, device="cuda")])
+    # every rounding adds at most (value / 16)^2 to the square's mean: 0.99 + 1 / 256 a step
+    assert second() < 0.75 * v0
+    # the seed of a step is its number
+    a, b = (T.AdamW([torch.zeros(n, device="cuda")], state="e4m3") for _ in range(2))
+    for t in (1, 2, 3):
+        a.step([rand(n, seed=t)])
+        b.step([rand(n, seed=t)], seed=t)
+    assert torch.equal(a.m[0].float(), b.m[0].float()) and torch.equal(a.v[0].float(), b.v[0].float())
+    # states in fp32 round nothing, and bfloat16 parameters to nearest unless a seed is given
+    p, q = (rand(n, seed=9, dtype=torch.bfloat16) for _ in range(2))
+    T.AdamW([p], **HYPER).step([rand(n, seed=3)])
+    T.AdamW([q], **HYPER).step([rand(n, seed=3)], seed=None)
+    assert torch.equal(p, q)
