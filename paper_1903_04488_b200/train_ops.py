@@ -107,13 +107,22 @@ def _check(tensors, dtype, lens, name: str, dev: torch.device) -> None:
             raise TypeError(f"{name}[{i}]: need a contiguous tensor of {n} elements of {dtype} on {dev}")
 
 
+def _check_apart(groups) -> None:
+    """No two tensors that a step writes to may share memory: different threads have them."""
+    spans = sorted((t.data_ptr(), t.numel() * t.element_size(), f"{name}[{i}]")
+                   for name, tensors in groups if tensors is not None for i, t in enumerate(tensors) if t.numel())
+    for (a, size, first), (b, _, second) in zip(spans, spans[1:]):
+        if a + size > b:
+            raise ValueError(f"{first} and {second} overlap (give a tensor that several layers share once)")
+
+
 class AdamW:
     """AdamW with decoupled weight decay over a list of contiguous tensors, all of them in one launch per step.
 
     params: float32, or bfloat16.  state: "f32", or "e4m3" (one byte per element for each of m and sqrt(v), a scale per
     ADAMW_BLOCK elements).  m, v (and m_scale, v_scale for "e4m3"): existing states, one tensor per parameter; fresh zeros
-    if None.  copies: for float32 params, bfloat16 or float16 tensors that receive the rounded new values.  step_count: steps
-    already taken (with states from a checkpoint)."""
+    if None.  copies: for float32 params, bfloat16 or float16 tensors that receive the rounded new values.  No two of all
+    these tensors may share memory.  step_count: steps already taken (with states from a checkpoint)."""
 
     def __init__(self, params, *, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  state: str = "f32", m=None, v=None, m_scale=None, v_scale=None, copies=None, step_count: int = 0):
@@ -160,6 +169,8 @@ class AdamW:
             _check(self.v_scale, torch.float32, blocks, "v_scale", dev)
         if self.copies is not None:
             _check(self.copies, self.copies[0].dtype, sizes, "copies", dev)
+        _check_apart((("params", params), ("m", self.m), ("v", self.v), ("m_scale", self.m_scale), ("v_scale", self.v_scale),
+                      ("copies", self.copies)))
         # room for an ssgd_adamw_tensor (64 bytes) per parameter, and behind them their sizes
         self._buffer = np.zeros(len(params) * 9, dtype=np.int64)
         self._buffer[len(params) * 8:] = sizes

@@ -76,3 +76,23 @@ def test_8bit_states_round_stochastically_unless_told_otherwise(cuda_device):
     T.AdamW([p], **HYPER).step([rand(n, seed=3)])
     T.AdamW([q], **HYPER).step([rand(n, seed=3)], seed=None)
     assert torch.equal(p, q)
+
+
+def test_tensors_that_share_memory_are_refused(cuda_device):
+    p, flat = rand(100), rand(1000)
+    for params in ([p, p], [p, rand(5), p.view(10, 10)], [flat[:600], flat[599:]]):
+        with pytest.raises(ValueError, match="overlap"):
+            T.AdamW(params)
+    with pytest.raises(ValueError, match="overlap"):
+        T.AdamW([p], m=[p], v=[torch.zeros(100, device="cuda")])
+    m = torch.zeros(100, device="cuda")
+    with pytest.raises(ValueError, match="overlap"):
+        T.AdamW([p], m=[m], v=[m])
+    state = torch.zeros(512, dtype=torch.float8_e4m3fn, device="cuda")
+    s = torch.zeros(2, device="cuda")
+    with pytest.raises(ValueError, match="overlap"):
+        T.AdamW([rand(512)], state="e4m3", m=[state], v=[state.clone()], m_scale=[s], v_scale=[s])
+    c = torch.zeros(150, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="overlap"):
+        T.AdamW([rand(100), rand(100)], copies=[c[:100], c[50:]])
+    T.AdamW([flat[:600], flat[600:], flat[:0], flat[:0]]).step([rand(600), rand(400), rand(0), rand(0)])
