@@ -110,12 +110,12 @@ at::Tensor result_like(const at::Tensor* out, const at::Tensor& like, const char
     if (out->sizes() != like.sizes() || out->scalar_type() != like.scalar_type())
         raise(PyExc_TypeError, std::string(name) + ": need " + of + " shape and type");
     *ld = rows_of(*out, name, dev).ld;
-    if (!out->is_inference()) out->unsafeGetTensorImpl()->bump_version();
     return *out;
 }
-// A tensor of the caller's that is written to: autograd has to know
-void written(const at::Tensor& t) {
-    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+// A tensor of the caller's that has been written to (NULL: none): autograd has to know.  Behind the launch, so that a call that
+// is refused leaves it as it was.
+void written(const at::Tensor* t) {
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
 }
 at::Tensor new_f32(at::IntArrayRef shape, int dev) { return fresh(shape, at::kFloat, dev); }
 
@@ -155,10 +155,12 @@ PyObject* layer_norm(PyObject* const* a) {
     const at::ScalarType type_w = param ? param->scalar_type() : x.scalar_type();
     const void *wp = flat(w, type_w, r.n, "weight", dev), *bp = flat(b, type_w, r.n, "bias", dev);
     int64_t ld_y = 0;
-    at::Tensor y = result_like(optional_tensor(a[4], "out"), x, "out", dev, &ld_y, "x's");
+    const at::Tensor* out = optional_tensor(a[4], "out");
+    at::Tensor y = result_like(out, x, "out", dev, &ld_y, "x's");
     at::Tensor stats = new_f32({2, r.rows}, dev);
     check(ssgd_layer_norm(x.data_ptr(), r.ld, fmt, wp, bp, fmt_w, r.rows, r.n, (float)number(a[3], "eps"), y.data_ptr(), ld_y,
                           stats.data_ptr<float>(), stream_of(dev)), "ssgd_layer_norm");
+    written(out);
     return Py_BuildValue("(NN)", wrap(y), wrap(stats));
 }
 
@@ -176,7 +178,8 @@ PyObject* layer_norm_backward(PyObject* const* a) {
     const void* wp = w ? flat(w, w->scalar_type(), r.n, "weight", dev) : nullptr;
     const float* stats = flat_f32(&tensor(a[3], "stats"), 2 * r.rows, "stats", dev);
     int64_t ld_dx = 0;
-    at::Tensor dx = result_like(optional_tensor(a[4], "dx"), x, "dx", dev, &ld_dx, "x's");
+    const at::Tensor* dx_in = optional_tensor(a[4], "dx");
+    at::Tensor dx = result_like(dx_in, x, "dx", dev, &ld_dx, "x's");
     const at::Tensor *dw_in = optional_tensor(a[5], "dw"), *db_in = optional_tensor(a[6], "db");
     const bool accumulate = PyObject_IsTrue(a[7]), need = PyObject_IsTrue(a[8]);
     at::Tensor dw, db;
@@ -186,14 +189,14 @@ PyObject* layer_norm_backward(PyObject* const* a) {
         db = db_in ? *db_in : new_f32({r.n}, dev);
     }
     float *dwp = need ? flat_f32(&dw, r.n, "dw", dev) : nullptr, *dbp = need ? flat_f32(&db, r.n, "db", dev) : nullptr;
-    if (need && dw_in) written(*dw_in);
-    if (need && db_in) written(*db_in);
     size_t bytes = 0;
     check(ssgd_layer_norm_backward_workspace(r.rows, r.n, &bytes), "ssgd_layer_norm_backward_workspace");
     // of the current stream: what is enqueued below runs before anything that gets this memory next
     const c10::DataPtr ws = c10::cuda::CUDACachingAllocator::get()->allocate(bytes);
     check(ssgd_layer_norm_backward(dy.data_ptr(), rd.ld, x.data_ptr(), r.ld, fmt, wp, fmt_w, stats, r.rows, r.n, dx.data_ptr(), ld_dx, dwp,
                                    dbp, accumulate ? 1 : 0, ws.get(), bytes, stream_of(dev)), "ssgd_layer_norm_backward");
+    written(dx_in);
+    if (need) { written(dw_in); written(db_in); }
     return Py_BuildValue("(NNN)", wrap(dx), wrap_or_none(dw), wrap_or_none(db));
 }
 
@@ -252,10 +255,12 @@ PyObject* token_logprobs_backward(PyObject* const* a) {
     const int32_t* idx_p = static_cast<int32_t*>(flat(idx, at::kInt, r.rows * top, "top_idx", dev));
     const float* d_top_p = flat_f32(d_top, r.rows * top, "d_top", dev);
     int64_t ld_out = 0;
-    at::Tensor out = result_like(optional_tensor(a[9], "out"), z, "out", dev, &ld_out, "the logits'");
+    const at::Tensor* out_in = optional_tensor(a[9], "out");
+    at::Tensor out = result_like(out_in, z, "out", dev, &ld_out, "the logits'");
     check(ssgd_token_logprobs_backward(z.data_ptr(), r.ld, fmt, ids.p, ids.bytes, r.rows, r.n, (float)number(a[8], "scale"), lse, entropy,
                                        d_logp, d_entropy, (int32_t)top, idx_p, d_top_p, out.data_ptr(), ld_out, stream_of(dev)),
           "ssgd_token_logprobs_backward");
+    written(out_in);
     return wrap(out);
 }
 
@@ -322,10 +327,7 @@ PyObject* adamw_step(PyObject* const* a) {
     if (type == at::kBFloat16) fmt_g = SSGD_FMT_BF16;
     else if (type == at::kHalf) fmt_g = SSGD_FMT_F16;
     else if (type != at::kFloat) raise(PyExc_TypeError, "grads: need float32, bfloat16 or float16");
-    column(a[1], count, "params", type_p, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) {
-        desc[i].p = t.data_ptr();
-        if (desc[i].n) written(t);
-    });
+    column(a[1], count, "params", type_p, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) { desc[i].p = t.data_ptr(); });
     column(a[2], count, "m", type_s, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) { desc[i].m = t.data_ptr(); });
     column(a[3], count, "v", type_s, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) { desc[i].v = t.data_ptr(); });
     if (small) {
@@ -339,10 +341,7 @@ PyObject* adamw_step(PyObject* const* a) {
         const at::ScalarType type_c = tensor(PyList_GET_ITEM(a[6], 0), "copies").scalar_type();
         if (type_c != at::kHalf && type_c != at::kBFloat16) raise(PyExc_TypeError, "copies: need bfloat16 or float16");
         fmt_copy = type_c == at::kHalf ? SSGD_FMT_F16 : SSGD_FMT_BF16;
-        column(a[6], count, "copies", type_c, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) {
-            desc[i].copy = t.data_ptr();
-            if (desc[i].n) written(t);
-        });
+        column(a[6], count, "copies", type_c, dev, sizes, 1, [&](Py_ssize_t i, const at::Tensor& t) { desc[i].copy = t.data_ptr(); });
     }
     const float* grad_scale = flat_f32(optional_tensor(a[15], "grad_scale"), 1, "grad_scale", dev);
     const bool stochastic = a[16] != Py_None;
@@ -352,6 +351,11 @@ PyObject* adamw_step(PyObject* const* a) {
                           small ? SSGD_FMT_E4M3 : SSGD_FMT_F32, fmt_copy, number(a[9], "lr"), number(a[10], "beta1"), number(a[11], "beta2"),
                           number(a[12], "eps"), number(a[13], "weight_decay"), integer(a[14], "step"), grad_scale, stochastic, seed,
                           stream_of(dev)), "ssgd_adamw_step");
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        if (!desc[i].n) continue;
+        written(&tensor(PyList_GET_ITEM(a[1], i), "params"));
+        if (copied) written(&tensor(PyList_GET_ITEM(a[6], i), "copies"));
+    }
     Py_RETURN_NONE;
 }
 

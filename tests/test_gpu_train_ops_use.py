@@ -96,3 +96,33 @@ def test_tensors_that_share_memory_are_refused(cuda_device):
     with pytest.raises(ValueError, match="overlap"):
         T.AdamW([rand(100), rand(100)], copies=[c[:100], c[50:]])
     T.AdamW([flat[:600], flat[600:], flat[:0], flat[:0]]).step([rand(600), rand(400), rand(0), rand(0)])
+
+
+def test_a_refused_call_leaves_its_tensors_as_they_were(cuda_device):
+    """Values and autograd's version counters."""
+    p, g = rand(100), rand(100)
+    copies = [torch.zeros(100, dtype=torch.bfloat16, device="cuda")]
+    opt = T.AdamW([p], copies=copies, **HYPER)
+    x, w, stats = rand(8, 64), rand(64), rand(2, 8)
+    z, ids = rand(8, 64), torch.zeros(8, dtype=torch.int64, device="cuda")
+    out, dw, db = torch.zeros(8, 64, device="cuda"), torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda")
+    written = [p, copies[0], out, dw, db] + opt.m + opt.v
+    before = [(t._version, t.clone()) for t in written]
+    for call in (lambda: opt.step([g], grad_scale=torch.ones(2, device="cuda")), lambda: opt.step([g], seed=1.5), lambda: opt.step([g], lr="x"),
+                 lambda: opt.step([g], lr=-1.0), lambda: T.layer_norm(x, w[:3], out=out), lambda: T.layer_norm(x, w, eps=-1.0, out=out),
+                 lambda: T.layer_norm(x, w, eps="x", out=out), lambda: T.layer_norm_backward(x, x, w.half(), stats, dx=out, dw=dw, db=db),
+                 lambda: T.layer_norm_backward(x, x, w, stats, dx=out, dw=dw, db=db[:5]),
+                 lambda: T.token_logprobs_backward(z, ids, z[:, 0].contiguous(), None, scale=0.0, out=out),
+                 lambda: T.token_logprobs_backward(z, ids, z[:, 0].contiguous(), None, scale="x", out=out)):
+        with pytest.raises((TypeError, ValueError, RuntimeError)):
+            call()
+    assert opt.step_count == 0
+    for t, (version, value) in zip(written, before):
+        assert t._version == version and torch.equal(t, value)
+    # what is written to does move on
+    T.layer_norm(x, w, out=out)
+    T.layer_norm_backward(x, x, w, stats, dx=out, dw=dw, db=db)
+    T.token_logprobs_backward(z, ids, z[:, 0].contiguous(), None, out=out)
+    opt.step([g])
+    assert out._version == before[2][0] + 3 and dw._version == before[3][0] + 1 and db._version == before[4][0] + 1
+    assert p._version > before[0][0] and copies[0]._version > before[1][0]
