@@ -126,3 +126,31 @@ def test_a_refused_call_leaves_its_tensors_as_they_were(cuda_device):
     opt.step([g])
     assert out._version == before[2][0] + 3 and dw._version == before[3][0] + 1 and db._version == before[4][0] + 1
     assert p._version > before[0][0] and copies[0]._version > before[1][0]
+
+
+def test_autograd_takes_tensors_however_they_lie(cuda_device):
+    x, w, b, dy = rand(6, 5, 32), rand(64, seed=2)[::2], rand(64, seed=3)[1::2], rand(6, 5, 32, seed=4)
+    for view in (lambda t: t.transpose(0, 1), lambda t: t[:, ::2], lambda t: t[0].t(), lambda t: t[:1].expand(6, 5, 32), lambda t: t[0, :1].expand(5, 32),
+                 lambda t: t[:, 1], lambda t: t[0, 0]):
+        xv = view(x).detach()
+        lies = xv.detach().requires_grad_()
+        plain = xv.clone(memory_format=torch.contiguous_format).requires_grad_()
+        n = xv.shape[-1]
+        params = [(t[:n].detach().requires_grad_() if n <= 32 else None) for t in (w, b)]
+        y = A.layer_norm(lies, *params)
+        d = view(dy)
+        gx, gw, gb = torch.autograd.grad(y, [lies, *params], d)
+        y2 = A.layer_norm(plain, params[0].detach().contiguous(), params[1].detach().contiguous())
+        want = torch.autograd.grad(torch.nn.functional.layer_norm(plain, (n,), *params, 1e-5), [plain, *params], d)
+        assert torch.equal(y, y2)
+        for got, ref in zip((gx, gw, gb), want):
+            assert got.shape == ref.shape and (got - ref).abs().max() <= 1e-4 * (1 + ref.abs().max())
+    z = rand(50, 12)
+    for zv in (z.t(), z[:, ::3], z[:1].expand(4, 12)):
+        rows = zv.shape[0]
+        lies, plain = zv.detach().requires_grad_(), zv.clone(memory_format=torch.contiguous_format).requires_grad_()
+        ids = torch.zeros(rows, 2, dtype=torch.int64, device="cuda")[:, 0]
+        got, want = A.token_logprobs(lies, ids), A.token_logprobs(plain, ids.contiguous())
+        assert torch.equal(got[0], want[0])
+        gl, gp = torch.autograd.grad(got[0].sum(), lies), torch.autograd.grad(want[0].sum(), plain)
+        assert torch.equal(gl[0], gp[0])
