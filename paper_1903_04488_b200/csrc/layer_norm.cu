@@ -67,6 +67,13 @@ __device__ __forceinline__ float group_sum(float x, float* slot) {
     }
 }
 
+// sum / n by the product with 1 / n and what that leaves over: a mean that is a number of fp32 comes out as it is.  (The product alone
+// can be a unit off, and of a row of one value x that unit, divided by the deviation it makes up, would be the result.)
+__device__ __forceinline__ float mean_of(float sum, float n, float inv_n) {
+    const float m = sum * inv_n, left = fmaf(-m, n, sum);
+    return left == left ? fmaf(left, inv_n, m) : m;        // NaN: the sum is not finite
+}
+
 // w or b at column `col`, VEC of them, in fp32 or in the row's format
 template <typename T, int VEC>
 __device__ __forceinline__ void load_param(const void* w, bool w_f32, int col, float2 (&f)[PAIRS<VEC>]) {
@@ -209,7 +216,7 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_rows(const 
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (mine_here(j)) add_sum(now[j], s);
-        const float mean = group_sum<G>(s.x + s.y, slot[0]) * inv_n;
+        const float mean = mean_of(group_sum<G>(s.x + s.y, slot[0]), (float)A.n, inv_n);
         const float2 minus_mean = both(-mean);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -317,7 +324,7 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_ring(const 
         group_sums<G, R>(mean, slot[0]);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            mean[k] *= inv_n;
+            mean[k] = mean_of(mean[k], (float)A.n, inv_n);
             float2 q = both(0.f);
             if (ALL || k < have) {
 #pragma unroll

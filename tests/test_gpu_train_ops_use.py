@@ -154,3 +154,18 @@ def test_autograd_takes_tensors_however_they_lie(cuda_device):
         assert torch.equal(got[0], want[0])
         gl, gp = torch.autograd.grad(got[0].sum(), lies), torch.autograd.grad(want[0].sum(), plain)
         assert torch.equal(gl[0], gp[0])
+
+
+def test_rows_of_one_value_are_normalised_to_zero(cuda_device):
+    """The mean of a row of one value is that value wherever the sum is exact: nothing is left to be divided by a small deviation."""
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for n in (40, 1000, 1030, 2050, 3000, 5000, 7000, 9000, 17000, 40000):
+            for rows in (1, 3, 1500):
+                if rows * n > 1 << 24:
+                    continue
+                for value in (3.0, 48.0, 1000.0, 24064.0, 50000.0):
+                    if dtype == torch.bfloat16 and value == 1000.0:
+                        value = 1008.0
+                    x = torch.full((rows, n), value, device="cuda").to(dtype)
+                    y, stats = T.layer_norm(x, None, None, 1e-5)
+                    assert (stats[0] == x[0, 0].float()).all() and not y.any(), (dtype, rows, n, value, float(stats[0, 0]), float(y.float().abs().max()))
