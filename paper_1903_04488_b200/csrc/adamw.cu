@@ -561,13 +561,13 @@ int launch_group(const ssgd_adamw_tensor* t, int32_t first, int32_t count, bool 
     T.count = k;
     if (small) {
         auto kernel = stochastic ? k_adamw_8bit<P, G, CAP, true> : k_adamw_8bit<P, G, CAP, false>;
-        const int smem = (int)sizeof(Staged<P, G>) * (THREADS / 32) * STAGES8;
-        if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-            return SSGD_ECUDA;
+        constexpr int smem = (int)sizeof(Staged<P, G>) * (THREADS / 32) * STAGES8;
+        static_assert(smem <= 40 * 1024, "a launch needs no permission for so much shared memory beside the scales");
         kernel<<<(unsigned)chunks, THREADS, smem, st>>>(T);
     } else {
-        if (stochastic && sizeof(P) == 2) k_adamw_f32<P, G, CAP, true><<<(unsigned)chunks, THREADS, 0, st>>>(T);
-        else k_adamw_f32<P, G, CAP, false><<<(unsigned)chunks, THREADS, 0, st>>>(T);
+        auto kernel = k_adamw_f32<P, G, CAP, false>;
+        if constexpr (sizeof(P) == 2) if (stochastic) kernel = k_adamw_f32<P, G, CAP, true>;
+        kernel<<<(unsigned)chunks, THREADS, 0, st>>>(T);
     }
     return launched();
 }

@@ -793,7 +793,7 @@ int launch_norm(const NormArgs& A, int sms, cudaStream_t st) {
     if (n <= 128 * E) NORM_ROWS(128, E, 4);
     if (n <= 256 * E) NORM_ROWS(256, E, 4);
     if (n <= 512 * E) NORM_ROWS(512, E, 2);
-    if (VEC == 1 && n <= 1024 * 8) NORM_ROWS(1024, 8, 1);
+    if constexpr (VEC == 1) if (n <= 1024 * 8) NORM_ROWS(1024, 8, 1);
     if (n <= 512 * 32) NORM(512, 32);
 #undef NORM
 #undef NORM_ROWS
@@ -830,7 +830,7 @@ int launch_norm_back(NormBackArgs A, int sms, int* parts, cudaStream_t st) {
     // 16 elements of 16 bits per thread or 8 of 32 bits: with their sums, 128 registers
     constexpr int E = sizeof(T) == 4 || VEC == 1 ? 8 : 16;
     if (n <= 32 * E) NORM_BACK(32, E);
-    if (sizeof(T) == 2 && n <= 64 * E) NORM_BACK(64, E);       // 31296 x 960 binary16 41.1, with 128 threads 45.4
+    if constexpr (sizeof(T) == 2) if (n <= 64 * E) NORM_BACK(64, E);   // 31296 x 960 binary16 41.1, with 128 threads 45.4
     if (n <= 128 * E) NORM_BACK(128, E);
     if (n <= 256 * E) NORM_BACK(256, E);
     if (n <= 512 * E) NORM_BACK(512, E);
