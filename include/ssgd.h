@@ -327,7 +327,9 @@ int ssgd_status(ssgd_ctx* ctx, void* stream);
  * The gradient that ssgd_step compresses comes out of a model's layers and loss, and the parameters that are not
  * sketched (Section 5 of the paper leaves bias terms uncompressed) need an ordinary optimizer step.  These entry
  * points have no context: everything they read or write is an argument.  They allocate nothing, check their arguments
- * before anything is launched, and only enqueue work on `stream` (they can be captured in a CUDA graph).
+ * before anything is launched, and only enqueue work on `stream`, so they can be captured in a CUDA graph.  A graph repeats the
+ * call as it was captured: of ssgd_adamw_step that includes lr, the step's number in its bias corrections and the seed, so a
+ * replayed step has the same dither every time.  Capture it anew for every step (or leave it out of the graph).
  *
  * Element formats are SSGD_FMT_*; all arithmetic is fp32, results are rounded to nearest even once.  Bases need the
  * alignment of their element type only (SSGD_EALIGN); rows may have any stride ld >= n (elements).  Bases and
@@ -358,8 +360,9 @@ int ssgd_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64
  *   top_idx, top_logp [rows][top]   the `top` (0 .. SSGD_MAX_TOP) largest logits, larger first, equal ones by smaller
  *                                   index (NaN counts as the largest), and their log probabilities
  * ids: [rows] of 4 or 8 bytes each (ids_bytes).  An id outside [0, vocab) is ignored: its logp is 0 and has no gradient.
- * A logit of -inf has probability 0.  A row of nothing else has lse = -inf, entropy 0, every log probability -inf and
- * the gradient 0.  A NaN or +inf makes its row's statistics NaN.  1 <= vocab <= 2^27. */
+ * A logit of -inf has probability 0.  A row of nothing else has lse = -inf, entropy 0 and every log probability -inf (of its
+ * gradient, with p = 0, only the terms at id and top_idx themselves are left).  Finite logits may be as far from zero as they
+ * like.  A NaN or +inf makes its row's statistics NaN.  1 <= vocab <= 2^27. */
 #define SSGD_MAX_TOP 32
 int ssgd_token_logprobs(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes, int64_t rows,
                         int64_t vocab, float scale, int32_t top, float* stats, int32_t* top_idx, float* top_logp,

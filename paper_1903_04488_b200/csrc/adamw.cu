@@ -107,8 +107,9 @@ __device__ __forceinline__ uint32_t dither_word(uint32_t key, int64_t i) {
 }
 
 // A chunk of 2048 elements per block: two vectors of four per thread from each of p, g, m, v on their way at once, what has no
-// common alignment element by element.  Measured in fp32: 11,173,962 elements in 62 tensors at any offset 51.2 us, 6.1 TB/s (0.93
-// of a copy); 29,060,773 in 198 tensors 134 us, 6.5 TB/s.
+// common alignment element by element.  Measured in fp32: 11,173,962 elements in 62 tensors at any offset 51.3 us, 6.1 TB/s (0.93
+// of a copy), with a bfloat16 copy 55.4; 29,060,773 in 198 tensors 123 us, 6.6 TB/s, with a copy 134.  bfloat16 parameters and
+// gradients, 11,173,962 in 62 tensors 42.2 us, 5.8 TB/s; without a common alignment 90.
 template <typename P, typename G, int CAP, bool STOCHASTIC>
 __global__ void __launch_bounds__(THREADS) k_adamw_f32(const __grid_constant__ Table<CAP> T) {
     const Hyper& h = T.h;
@@ -468,11 +469,12 @@ __device__ __forceinline__ void block8(const Hyper8& h, uint32_t index, const Ch
 
 // A warp takes h.blocks8 blocks, 8 apart (its neighbours have those between); the next one is on its way while one is computed.
 // The chunk's scales are read and written as a whole: a store of 4 bytes per block made the kernel's memory traffic alone
-// 206 instead of 144 us at 90M elements.  Measured at 90M bfloat16 parameters and gradients: 203 us, 4.5 TB/s, and 211 in
-// sustained work; 8 of 10 issue slots, the integer pipe at 0.75.  The codes' exactness is 30 us of it: 172 with b1 and b2 folded
-// into the scales and approximate roots alone.  At 30M, 74 us: with sqrt.rn for every element 78, with the careful branch at
-// every four elements 77; where the positive roots of a block span more than 2^16 its lanes take that branch, 115.  Of the form
-// with folded constants at 90M: three stages instead of two 175, the next block in registers instead of shared memory 237.
+// 206 instead of 144 us at 90M elements.  Measured at 90M bfloat16 parameters and gradients: 206 us, 4.4 TB/s, at 1965 MHz; after
+// some 2,000 passes on end 222, when the power limit has brought the clock to 1815 MHz.  What bounds it is issue: 66 instructions per
+// element, 8 of 10 slots, the integer pipe at 0.74.  The codes' exactness is 30 us of it: 175 with b1 and b2 folded into the
+// scales and approximate roots alone.  At 30M, 74 us: with sqrt.rn for every element 78, with the careful branch at every four
+// elements 77; where the positive roots of a block span more than 2^16 its lanes take that branch, 115.  Of the form with folded
+// constants at 90M: three stages instead of two 175, the next block in registers instead of shared memory 237.
 constexpr int STAGES8 = 2;
 template <typename P, typename G, int CAP, bool STOCHASTIC>
 __global__ void __launch_bounds__(THREADS, 4) k_adamw_8bit(const __grid_constant__ Table<CAP> T) {

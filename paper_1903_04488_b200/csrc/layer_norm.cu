@@ -242,7 +242,8 @@ __global__ void __launch_bounds__(GroupShape<G>::BLOCK) k_layer_norm_rows(const 
 // warps and block is paid once for R rows; and the next R rows are on their way into shared memory meanwhile.  A thread
 // copies what it will read itself.  (Vectors of 2 bytes cannot be copied this way.)
 //
-// Measured at 16384 x 2048 in bfloat16 (us): 22.9, 5.9 TB/s; 2 rows at a time 24.7, 1 row 26.2; k_layer_norm_rows 28.8; a warp per
+// Measured at 16384 x 2048 in bfloat16 (us): 23, 5.8 TB/s (with new results beside the last ones, which the L2 then does not
+// hold, 26.5); 2 rows at a time 24.7, 1 row 26.2; k_layer_norm_rows 28.8; a warp per
 // row and w, b from L1 29.3, with fp32 w, b 36.9.
 constexpr int STAGES = 2;
 template <typename T, int VEC> constexpr bool STAGED = sizeof(T) * VEC >= 4;
@@ -439,7 +440,7 @@ __device__ __forceinline__ Vec<T, VEC> back_result(const Vec<T, VEC>& x, const V
 // cannot be copied this way: they are read when they are needed.)
 //
 // Measured at 16384 x 4096 in bfloat16 (us, rows at a time x blocks per SM): 1 x 2 85.9, 2 x 2 80.9, 4 x 2 (128 registers: spills)
-// 81.2, 4 x 1 73.8; in fp32, 8192 x 2048 2 x 2 37.2, 4 x 1 37.6, 1999 x 1030 10.5 and 13.4.  Without the ring: with the next row in
+// 81.2, 4 x 1 73.4 (in sustained work 79); in fp32, 8192 x 2048 2 x 2 37.2, 4 x 1 37.6, 1999 x 1030 10.5 and 13.4.  Without the ring: with the next row in
 // registers 88.6, with the rows ahead asked into L2 86.
 template <typename T, int VEC, int G> constexpr int ROWS_AT_ONCE = !STAGED<T, VEC> || sizeof(T) == 4 || G >= 512 ? 2 : 4;
 template <typename T, int VEC, int G, int E, int R> constexpr size_t RING_BYTES =

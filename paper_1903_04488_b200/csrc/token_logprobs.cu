@@ -34,6 +34,8 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -INFINITY;
 
+// 2^x within 2 units of the last place; below 2^-126 it is 0.  One instruction of nine in the loop; the sums' own roundings are of the
+// same size: against 64 bits the results are off by 4.6e-8 of their size, those of 32-bit exp and sums by 3.4e-8 (4096 x 32000).
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -465,8 +467,9 @@ __device__ __forceinline__ void best_of_segment(Shared<NT, true>& sh, const Gran
     }
 }
 
-// At 4096 x 32000 in bfloat16 50 us, 5.2 TB/s.  Per logit 8.5 instructions, one of them a 2^x, of which an SM has 16 a cycle:
-// 36 us for these alone.  The latency of the loads is covered by other CTAs, 6 of 256 threads per SM (with 4: 56 us, 5: 51; the
+// At 4096 x 32000 in bfloat16 50 us, 5.2 TB/s (55 in sustained work).  Per logit 8.8 instructions, 31 us of issue slots at
+// 1965 MHz, one of them a 2^x, of which an SM has 16 a cycle: 28 us.  Neither they nor the memory (40 us) are full; loads and
+// arithmetic take turns.  The latency of the loads is covered by other CTAs, 6 of 256 threads per SM (with 4: 56 us, 5: 51; the
 // next batch in registers while one is summed, 3 CTAs: 69).
 template <typename T, bool TOP, int NT>
 __global__ void __launch_bounds__(NT, 6 * 256 / NT) k_token_logprobs(const LogprobArgs A, int split) {
@@ -606,7 +609,7 @@ struct LogprobBackArgs {
 constexpr int BACK_U = 4;
 
 // CTA (row, part) writes `per` granules of a row, in batches of BACK_U reads per thread.  At 8192 x 32000 in bfloat16 168 us, 6.2 TB/s
-// (0.95 of a copy), 6.4 instructions per logit.
+// (0.95 of a copy; 174 in sustained work), 7.5 instructions per logit.
 template <typename T, bool ENTROPY, int NT>
 __global__ void __launch_bounds__(NT) k_token_logprobs_back(const LogprobBackArgs A) {
     constexpr int VEC = 16 / sizeof(T);

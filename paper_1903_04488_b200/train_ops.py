@@ -181,7 +181,9 @@ class AdamW:
         for a parameter that is left alone.  grad_scale: float32 scalar on the device that multiplies every gradient.
 
         seed: round e4m3 states and bfloat16 parameters stochastically with it (another one every step); None: to nearest.  "step": with
-        e4m3 states the step's number, since their second moment, rounded to nearest, would never move; otherwise None."""
+        e4m3 states the step's number, since their second moment, rounded to nearest, would never move; otherwise None.
+
+        In a CUDA graph a step repeats itself with the lr, step number and seed that it was captured with."""
         if seed == "step":
             seed = None if self.m_scale is None else self.step_count + 1
         (_native or native()).adamw_step(self._buffer, self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies, grads,
