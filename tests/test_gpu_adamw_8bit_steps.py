@@ -118,3 +118,47 @@ def test_a_block_of_what_is_hardly_there_is_held_as_zeros(cuda_device):
         assert bool((opt.m_scale[0] > 0).all()) == there
         if there:
             assert (opt.m[0].float() == 448).all() and math.isclose(float(opt.m_scale[0][0]) * 448, 2.0 ** (exponent - 1), rel_tol=1e-6)
+
+
+@pytest.mark.parametrize("make", [dense, wide, large])
+def test_codes_do_not_depend_on_where_the_tensors_lie(cuda_device, make):
+    """The same step on tensors that start anywhere, whose blocks are read element by element."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    n = 200_003
+    start = torch.randn(n, generator=gen, device="cuda").to(torch.bfloat16)
+
+    def at(offset, dtype):
+        return torch.zeros(n + 16, device="cuda").to(dtype)[offset: offset + n]
+
+    def optimizer(offset):
+        p = at(offset, torch.bfloat16)
+        p.copy_(start)
+        return T.AdamW([p], state="e4m3", m=[at(offset, torch.float8_e4m3fn)], v=[at(offset, torch.float8_e4m3fn)],
+                       m_scale=[torch.zeros(-(-n // BLOCK), device="cuda")], v_scale=[torch.zeros(-(-n // BLOCK), device="cuda")])
+
+    a, b = optimizer(0), optimizer(3)
+    for t in range(1, 7):
+        g = make(n, gen, t)
+        there = at(5, torch.float32)
+        there.copy_(g)
+        a.step([g])
+        b.step([there])
+        for x, y in ((a.params, b.params), (a.m, b.m), (a.v, b.v), (a.m_scale, b.m_scale), (a.v_scale, b.v_scale)):
+            assert torch.equal(x[0].float(), y[0].float())
+
+
+@pytest.mark.parametrize("make", [dense, wide, large])
+def test_what_is_not_finite_leaves_the_others_codes_alone(cuda_device, make):
+    """A block's other elements and its scales are what they would be if the gradient were 0 there."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n = 100_000
+    g = make(n, gen, 1)
+    bad = torch.rand(n, generator=gen, device="cuda") < 0.003
+    values = torch.tensor([math.nan, math.inf, -math.inf], device="cuda")[torch.randint(0, 3, (n,), generator=gen, device="cuda")]
+    a, b = (T.AdamW([torch.zeros(n, device="cuda")], state="e4m3") for _ in range(2))
+    a.step([torch.where(bad, values, g)])
+    b.step([torch.where(bad, 0.0, g)])
+    assert torch.equal(a.m_scale[0], b.m_scale[0]) and torch.equal(a.v_scale[0], b.v_scale[0])
+    for x, y in ((a.m, b.m), (a.v, b.v), (a.params, b.params)):
+        assert torch.equal(x[0].float()[~bad], y[0].float()[~bad])
+    assert a.m[0].float()[bad].isnan().all() and a.v[0].float()[bad].isnan().all()
