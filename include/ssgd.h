@@ -410,6 +410,41 @@ int ssgd_adamw_step(const ssgd_adamw_tensor* tensors, int32_t count, int32_t fmt
                     int32_t fmt_copy, double lr, double beta1, double beta2, double eps, double weight_decay,
                     int64_t step, const float* grad_scale, int32_t stochastic, uint64_t seed, void* stream);
 
+/* Orthogonalised matrices.  With u a matrix and |u| the root of the sum of its squares, x_0 = u / (|u| + eps), and `steps` times
+ *   A = x x',  x <- a x + (b A + c A A) x          (rows <= cols; otherwise A = x' x and x <- a x + x (b A + c A A))
+ * which applies the polynomial a s + b s^3 + c s^5 to the singular values; (3.4445, -4.7750, 2.0315) brings them near 1 in 5 steps.
+ * The products are of fp16 numbers with fp32 sums.  products = 3: every matrix is a sum of two fp16 numbers, so that results are as
+ * exact as those of fp32; 1: one number in the operands of products, two in x itself: the result is off by about 1e-3 of its norm;
+ * 0: 1 for results in bfloat16, otherwise 3.
+ * A matrix of zeros stays one (0 / 0 with eps = 0 is NaN); infinities and NaN spread over their matrix.  Polynomials that take anything
+ * in [0, 1] beyond 4 on the way are refused (SSGD_EINVAL).  1 <= steps <= 32; rows, cols <= 2^20, rows * cols <= 2^32, the shorter
+ * side <= 32768 (SSGD_ETOOBIG).  Matrices without elements are left out. */
+typedef struct {
+    void* out;        /* ssgd_orthogonalize: the result, may be `in` itself (same ld); ssgd_muon_step: the parameter */
+    const void* in;   /* the matrix, or the gradient */
+    float* m;         /* ssgd_muon_step: momentum, [rows][cols]; otherwise unused */
+    int64_t ld_out, ld_in;
+    int64_t rows, cols;
+    double scale;     /* ssgd_muon_step: factor of lr for this matrix */
+} ssgd_matrix;
+/* Device memory that the two below need: 8 bytes per element of the matrices, twice (products 1) or four times (3) 2 bytes per element
+ * of A and B, and a little.  More than 224 matrices or 2^27 elements are worked off in groups, each in the same memory.  Free again
+ * once the stream has passed; its contents mean nothing.  16-byte aligned. */
+int ssgd_orthogonalize_workspace(const ssgd_matrix* matrices, int32_t count, int32_t fmt_out, int32_t products, size_t* out_bytes);
+/* out <- the orthogonalised `in`, for each matrix; both in fmt. */
+int ssgd_orthogonalize(const ssgd_matrix* matrices, int32_t count, int32_t fmt, int32_t products, int32_t steps, double a, double b,
+                       double c, double eps, void* workspace, size_t workspace_bytes, void* stream);
+/* One step of an optimizer for matrices, over `count` of them:
+ *   g <- g * grad_scale (device fp32 scalar, NULL: 1),  m <- momentum m + (1 - momentum) g
+ *   u = momentum m + (1 - momentum) g (nesterov != 0) or m,  p <- p (1 - lr weight_decay) - lr scale O(u)
+ * with O(u) the orthogonalised u.  p: SSGD_FMT_F32 or SSGD_FMT_BF16; g: any of the three formats.  No two p or m may overlap. */
+int ssgd_muon_step(const ssgd_matrix* matrices, int32_t count, int32_t fmt_p, int32_t fmt_g, int32_t products, double lr, double momentum,
+                   int32_t nesterov, double weight_decay, int32_t steps, double a, double b, double c, double eps, const float* grad_scale,
+                   void* workspace, size_t workspace_bytes, void* stream);
+/* Waits for the stream; SSGD_EDEVICE if a wait inside a kernel of the training operators has run out on this device since the last
+ * call (what that call wrote is then worthless), SSGD_ECUDA if the stream reports an error, else SSGD_OK.  Not while capturing. */
+int ssgd_train_ops_status(void* stream);
+
 const char* ssgd_strerror(int code);
 const char* ssgd_last_error(const ssgd_ctx* ctx); /* text of the last CUDA error seen, or "" */
 

@@ -14,6 +14,7 @@
 
 #include <cstdint>
 #include <string>
+#include <vector>
 
 #include "../../include/ssgd.h"
 
@@ -359,6 +360,107 @@ PyObject* adamw_step(PyObject* const* a) {
     Py_RETURN_NONE;
 }
 
+// Memory of the current stream: what is enqueued behind runs before anything that gets it next
+c10::DataPtr scratch(size_t bytes) { return c10::cuda::CUDACachingAllocator::get()->allocate(bytes); }
+
+// (x, steps, a, b, c, eps, products, out) -> the orthogonalised x
+PyObject* orthogonalize(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "x");
+    const int dev = device_of(x, "x");
+    if (x.dim() < 2) raise(PyExc_TypeError, "x: need a matrix, or a batch of them");
+    const int32_t fmt = format_of(x, "x");
+    const Rows r = rows_of(x, "x", dev);
+    int64_t ld_out = 0;
+    const at::Tensor* out_in = optional_tensor(a[7], "out");
+    at::Tensor out = result_like(out_in, x, "out", dev, &ld_out, "x's");
+    const int64_t rows = x.size(-2), cols = x.size(-1), count = rows * cols ? x.numel() / (rows * cols) : 0;
+    if (count > INT32_MAX) check(SSGD_ETOOBIG, "ssgd_orthogonalize");
+    std::vector<ssgd_matrix> list((size_t)count);
+    const int64_t bytes_each = x.element_size();
+    for (int64_t i = 0; i < count; ++i)
+        list[i] = ssgd_matrix{static_cast<char*>(out.data_ptr()) + i * rows * ld_out * bytes_each,
+                              static_cast<const char*>(x.data_ptr()) + i * rows * r.ld * bytes_each, nullptr, ld_out, r.ld, rows, cols, 0.0};
+    const int32_t products = (int32_t)integer(a[6], "products");
+    size_t bytes = 0;
+    check(ssgd_orthogonalize_workspace(list.data(), (int32_t)count, fmt, products, &bytes), "ssgd_orthogonalize_workspace");
+    const c10::DataPtr ws = scratch(bytes);
+    check(ssgd_orthogonalize(list.data(), (int32_t)count, fmt, products, (int32_t)integer(a[1], "steps"), number(a[2], "coefficients"),
+                             number(a[3], "coefficients"), number(a[4], "coefficients"), number(a[5], "eps"), ws.get(), bytes, stream_of(dev)),
+          "ssgd_orthogonalize");
+    written(out_in);
+    return wrap(out);
+}
+
+// (params, m, scales, grads, device, lr, momentum, nesterov, decay, steps, a, b, c, eps, products, grad_scale): lists of as many members
+PyObject* muon_step(PyObject* const* a) {
+    const int dev = (int)integer(a[4], "device");
+    if (dev != (int)c10::cuda::current_device())
+        raise(PyExc_ValueError, "grads: the parameters are on device " + std::to_string(dev) + ", which is not the current one");
+    for (int i = 0; i < 3; ++i)
+        if (!PyList_Check(a[i]) || PyList_GET_SIZE(a[i]) != PyList_GET_SIZE(a[0])) raise(PyExc_ValueError, "params: not as many as there were");
+    const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+    PyObject* grads = a[3];
+    if ((!PyList_Check(grads) && !PyTuple_Check(grads)) || PySequence_Fast_GET_SIZE(grads) != count)
+        raise(PyExc_ValueError, "grads: need one tensor per parameter");
+    PyObject** items = PySequence_Fast_ITEMS(grads);
+    std::vector<ssgd_matrix> list;
+    at::ScalarType type_p = at::kFloat, type_g = at::kFloat;
+    bool known = false;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        if (items[i] == Py_None) continue;                 // left alone
+        const at::Tensor &p = tensor(PyList_GET_ITEM(a[0], i), "params"), &m = tensor(PyList_GET_ITEM(a[1], i), "m"), &g = tensor(items[i], "grads");
+        if (!known) {
+            type_p = p.scalar_type();
+            type_g = g.scalar_type();
+        }
+        known = true;
+        const std::string at = "[" + std::to_string(i) + "]";
+        auto whole = [&](const at::Tensor& t, at::ScalarType type, const char* name) {
+            if (t.scalar_type() != type || t.sizes() != p.sizes() || !t.is_contiguous() || !t.is_cuda() || t.get_device() != dev)
+                raise(PyExc_TypeError, name + at + ": need a contiguous tensor of the parameter's shape of " + std::string(at::toString(type)) +
+                                           " on CUDA device " + std::to_string(dev));
+        };
+        if (p.dim() < 2) raise(PyExc_TypeError, "params" + at + ": need a matrix, or a batch of them");
+        whole(p, type_p, "params");
+        whole(m, at::kFloat, "m");
+        whole(g, type_g, "grads");
+        const double scale = number(PyList_GET_ITEM(a[2], i), "scale");
+        const int64_t rows = p.size(-2), cols = p.size(-1), each = rows * cols, n = each ? p.numel() / each : 0;
+        for (int64_t j = 0; j < n; ++j)
+            list.push_back(ssgd_matrix{static_cast<char*>(p.data_ptr()) + j * each * (int64_t)p.element_size(),
+                                       static_cast<const char*>(g.data_ptr()) + j * each * (int64_t)g.element_size(),
+                                       static_cast<float*>(m.data_ptr()) + j * each, cols, cols, rows, cols, scale});
+    }
+    if (list.empty()) Py_RETURN_NONE;
+    if (list.size() > INT32_MAX) check(SSGD_ETOOBIG, "ssgd_muon_step");
+    if (type_p != at::kFloat && type_p != at::kBFloat16) raise(PyExc_TypeError, "params: need float32 or bfloat16");
+    int32_t fmt_g = SSGD_FMT_F32;
+    const int32_t fmt_p = type_p == at::kBFloat16 ? SSGD_FMT_BF16 : SSGD_FMT_F32;
+    if (type_g == at::kBFloat16) fmt_g = SSGD_FMT_BF16;
+    else if (type_g == at::kHalf) fmt_g = SSGD_FMT_F16;
+    else if (type_g != at::kFloat) raise(PyExc_TypeError, "grads: need float32, bfloat16 or float16");
+    const float* grad_scale = flat_f32(optional_tensor(a[15], "grad_scale"), 1, "grad_scale", dev);
+    const int32_t products = (int32_t)integer(a[14], "products");
+    size_t bytes = 0;
+    check(ssgd_orthogonalize_workspace(list.data(), (int32_t)list.size(), fmt_p, products, &bytes), "ssgd_orthogonalize_workspace");
+    const c10::DataPtr ws = scratch(bytes);
+    check(ssgd_muon_step(list.data(), (int32_t)list.size(), fmt_p, fmt_g, products, number(a[5], "lr"), number(a[6], "momentum"),
+                         PyObject_IsTrue(a[7]), number(a[8], "weight_decay"), (int32_t)integer(a[9], "steps"), number(a[10], "coefficients"),
+                         number(a[11], "coefficients"), number(a[12], "coefficients"), number(a[13], "eps"), grad_scale, ws.get(), bytes,
+                         stream_of(dev)), "ssgd_muon_step");
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        if (items[i] == Py_None) continue;
+        written(&tensor(PyList_GET_ITEM(a[0], i), "params"));
+        written(&tensor(PyList_GET_ITEM(a[1], i), "m"));
+    }
+    Py_RETURN_NONE;
+}
+
+PyObject* status(PyObject* const*) {
+    check(ssgd_train_ops_status(stream_of((int)c10::cuda::current_device())), "ssgd_train_ops_status");
+    Py_RETURN_NONE;
+}
+
 PyObject* set_error_class(PyObject* const* a) {
     Py_INCREF(a[0]);
     Py_XDECREF(g_error_class);
@@ -385,7 +487,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(layer_norm, 5), ENTRY(layer_norm_backward, 9), ENTRY(token_logprobs, 4), ENTRY(token_logprobs_backward, 10),
-                         ENTRY(adamw_step, 17), ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(adamw_step, 17), ENTRY(orthogonalize, 8), ENTRY(muon_step, 16), ENTRY(status, 0),
+                         ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

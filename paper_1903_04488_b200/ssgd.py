@@ -74,6 +74,10 @@ SIGNATURES = {
     "ssgd_token_logprobs": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _i32, _vp, _vp, _vp, _vp],
     "ssgd_token_logprobs_backward": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
                                      _i64, _vp],
+    "ssgd_orthogonalize_workspace": [_vp, _i32, _i32, _i32, C.POINTER(_sz)],
+    "ssgd_orthogonalize": [_vp, _i32, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _vp, _sz, _vp],
+    "ssgd_muon_step": [_vp, _i32, _i32, _i32, _i32, _f64, _f64, _i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp, _sz, _vp],
+    "ssgd_train_ops_status": [_vp],
     "ssgd_adamw_step": [_vp, _i32, _i32, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _f64, _i64, _vp, _i32, _u64, _vp],
 }
 

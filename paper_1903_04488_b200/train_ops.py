@@ -190,3 +190,75 @@ class AdamW:
                                          self._dev, self.lr if lr is None else lr, *self.betas, self.eps, self.weight_decay,
                                          self.step_count + 1, grad_scale, seed)
         self.step_count += 1
+
+
+# ---- orthogonalised matrices -------------------------------------------------------------------------
+
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def orthogonalize(x: torch.Tensor, *, steps: int = 5, coefficients=QUINTIC, eps: float = 1e-7, products: int | None = None,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """x / (norm + eps) with the polynomial a s + b s^3 + c s^5 applied to its singular values `steps` times, in x's type: close to
+    the nearest matrix with orthonormal rows (or columns), but for singular values that are all but zero.
+
+    x: a matrix (with any row stride), or a contiguous batch of them.  products: 3 for results as exact as fp32's, 1 for an error of
+    about 1e-3 at a third of the time; None: 1 for bfloat16, otherwise 3.  out: where the result goes (x's shape and type; may be x)."""
+    a, b, c = coefficients
+    return (_native or native()).orthogonalize(x, steps, a, b, c, eps, 0 if products is None else products, out)
+
+
+class Muon:
+    """Momentum, orthogonalised: the optimizer of the matrices beside AdamW for everything else.  All matrices in the same few
+    launches per step:  m <- momentum m + (1 - momentum) g,  u = momentum m + (1 - momentum) g (nesterov) or m,
+    p <- p (1 - lr weight_decay) - lr scale orthogonalize(u).
+
+    params: contiguous matrices, or batches of them, float32 or bfloat16.  m: existing momenta (float32, of the parameters' shapes);
+    fresh zeros if None.  scale: "spectral" (sqrt(max(1, rows / cols))), "rms" (0.2 sqrt(max(rows, cols)): updates as large as
+    AdamW's) or a number.  products: as in `orthogonalize`, by the parameters' type.  No two of the tensors may share memory."""
+
+    def __init__(self, params, *, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                 steps: int = 5, coefficients=QUINTIC, eps: float = 1e-7, scale: str | float = "spectral", products: int | None = None,
+                 m=None):
+        params = list(params)
+        if not params:
+            raise ValueError("params: need at least one tensor")
+        dtype, dev = params[0].dtype, params[0].device
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("params: need float32 or bfloat16")
+        if dev.type != "cuda":
+            raise TypeError("params: need CUDA tensors")
+        for i, p in enumerate(params):
+            if p.dim() < 2:
+                raise TypeError(f"params[{i}]: need a matrix, or a batch of them")
+        if scale == "spectral":
+            self.scales = [max(1.0, p.shape[-2] / max(1, p.shape[-1])) ** 0.5 for p in params]
+        elif scale == "rms":
+            self.scales = [0.2 * max(p.shape[-2:]) ** 0.5 for p in params]
+        elif isinstance(scale, str):
+            raise ValueError('scale: "spectral", "rms" or a number')
+        else:
+            self.scales = [float(scale)] * len(params)
+        self.params = params
+        self.m = [torch.zeros_like(p, dtype=torch.float32) for p in params] if m is None else list(m)
+        sizes = [p.numel() for p in params]
+        _check(params, dtype, sizes, "params", dev)
+        _check(self.m, torch.float32, sizes, "m", dev)
+        _check_apart((("params", params), ("m", self.m)))
+        self.lr, self.momentum, self.nesterov, self.weight_decay = lr, momentum, nesterov, weight_decay
+        self.steps, self.coefficients, self.eps, self.products = steps, tuple(coefficients), eps, products
+        self._dev = dev.index
+
+    def step(self, grads, *, grad_scale: torch.Tensor | None = None, lr: float | None = None) -> None:
+        """One step.  grads: one contiguous tensor per parameter, of its shape (float32, bfloat16 or float16, all the same type), None
+        for a parameter that is left alone.  grad_scale: float32 scalar on the device that multiplies every gradient."""
+        a, b, c = self.coefficients
+        (_native or native()).muon_step(self.params, self.m, self.scales, grads, self._dev, self.lr if lr is None else lr, self.momentum,
+                                        self.nesterov, self.weight_decay, self.steps, a, b, c, self.eps,
+                                        0 if self.products is None else self.products, grad_scale)
+
+
+def status() -> None:
+    """Waits for the current stream and raises if a wait inside a kernel of these operators has run out since the last call (what it
+    wrote is then worthless) or the stream reports an error."""
+    (_native or native()).status()
