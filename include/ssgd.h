@@ -410,6 +410,43 @@ int ssgd_adamw_step(const ssgd_adamw_tensor* tensors, int32_t count, int32_t fmt
                     int32_t fmt_copy, double lr, double beta1, double beta2, double eps, double weight_decay,
                     int64_t step, const float* grad_scale, int32_t stochastic, uint64_t seed, void* stream);
 
+/* The clipped policy loss of sampled tokens, and its gradient, in one pass over the logits.  For each row of logits [rows][vocab], z, lse,
+ * p, logp = z[id] - lse and the entropy H as above:
+ *   r = e^(logp - old_logp),  kept = A >= 0 ? min(r, 1 + clip_high) : max(r, 1 - clip_low),  A = advantages[row]
+ *   q = ref_logp - logp,  K = e^q - 1 - q                     (0 without ref_logp)
+ *   loss = w (-kept A + kl K - entropy H),   w = weights[row] (NULL: 1; a mean is a matter of the weights)
+ *   c = (kept = r ? -A r : 0) - kl (e^q - 1)
+ *   dlogits_j = w scale (c [j = id] - c p_j + entropy p_j (log p_j + H)), the gradient of the sum of the losses
+ * stats [5][rows] fp32: loss, logp, H, K, r.  dlogits: [rows][vocab] in fmt, may be logits itself (same ld); NULL: not wanted.
+ * A row of weight 0, or with an id outside [0, vocab), has statistics and gradient 0, whatever its logits are: they are not read.
+ * old_logp, advantages, ref_logp, weights: [rows] fp32.  0 <= clip_low <= 1, 0 <= clip_high (infinity: no clipping), kl >= 0 (needs
+ * ref_logp unless 0); entropy may be negative.  -inf logits, rows of nothing else, far logits and NaN: as for ssgd_token_logprobs. */
+int ssgd_policy_loss(const void* logits, int64_t ld, int32_t fmt, const void* ids, int32_t ids_bytes, int64_t rows, int64_t vocab,
+                     float scale, const float* old_logp, const float* advantages, const float* ref_logp, const float* weights,
+                     float clip_low, float clip_high, float kl, float entropy, float* stats, void* dlogits, int64_t ld_d,
+                     void* stream);
+
+/* The preference loss of pairs of token sequences.  Sequence s is tokens [starts[s], starts[s + 1]) (starts: [2 pairs + 1] ascending, of 4 or
+ * 8 bytes each; sequences may be empty); pair p is sequence 2 p, the preferred one, and 2 p + 1.  With
+ *   D_s = sum of (logp - ref_logp) over the sequence, divided by its length if average != 0,   x = beta (D_2p - D_2p+1)
+ * SSGD_PREFERENCE_SIGMOID   l = -(1 - e) log sigmoid(x) - e log sigmoid(-x),  e = label_smoothing, 0 .. 0.5
+ * SSGD_PREFERENCE_IPO       l = ((x - 1/2) / beta)^2
+ * SSGD_PREFERENCE_HINGE     l = max(0, 1 - x)
+ *   loss [pairs] = weights l;  rewards [2][pairs] = beta D, of the preferred sequences and of the others;
+ *   d_logp [tokens] (NULL: not wanted) = the gradient of the sum of the losses; 0 for tokens of no sequence
+ * logp, ref_logp (NULL: 0), d_logp: [tokens] fp32; weights [pairs] fp32 (NULL: 1; a pair of weight 0 has loss and gradient 0 whatever
+ * its tokens hold).  Sums are taken in 64 bits, in an order that depends on nothing but the starts.  starts outside [0, tokens] count as the
+ * nearest of these; where they do not ascend, the results of the pairs concerned are unspecified.
+ * d_logp may be logp or ref_logp itself.  workspace: device memory of at least ssgd_preference_loss_workspace(tokens, pairs) bytes, 8-byte
+ * aligned, free again once the stream has passed.  tokens <= 2^40, pairs <= 2^30. */
+#define SSGD_PREFERENCE_SIGMOID 0
+#define SSGD_PREFERENCE_IPO     1
+#define SSGD_PREFERENCE_HINGE   2
+int ssgd_preference_loss_workspace(int64_t tokens, int64_t pairs, size_t* out_bytes);
+int ssgd_preference_loss(const float* logp, const float* ref_logp, int64_t tokens, const void* starts, int32_t starts_bytes, int64_t pairs,
+                         const float* weights, int32_t kind, float beta, float label_smoothing, int32_t average, float* loss,
+                         float* rewards, float* d_logp, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Orthogonalised matrices.  With u a matrix and |u| the root of the sum of its squares, x_0 = u / (|u| + eps), and `steps` times
  *   A = x x',  x <- a x + (b A + c A A) x          (rows <= cols; otherwise A = x' x and x <- a x + x (b A + c A A))
  * which applies the polynomial a s + b s^3 + c s^5 to the singular values; (3.4445, -4.7750, 2.0315) brings them near 1 in 5 steps.

@@ -69,3 +69,58 @@ def token_logprobs(logits, ids, top: int = 0, scale: float = 1.0):
     """(logp, entropy, lse, top_idx, top_logp) of `train_ops.token_logprobs`.  logp, entropy and top_logp have gradients; lse, which
     the backward pass reads, has none.  Logits that do not lie in rows are copied first."""
     return _TokenLogprobs.apply(logits, ids, top, scale)
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, old_logp, advantages, ref_logp, weights, options):
+        logits = _rows(logits)
+        rows = [None if t is None else t.detach().contiguous() for t in (ids, old_logp, advantages, ref_logp, weights)]
+        stats = train_ops.policy_loss(logits, *rows[:3], ref_logp=rows[3], weights=rows[4], need_grad=False, **options).stats
+        ctx.save_for_backward(logits, *rows)
+        ctx.options = options
+        loss, rest = stats[0].clone(), [t.clone() for t in stats[1:]]
+        ctx.mark_non_differentiable(*rest)
+        return (loss, *rest)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_loss, *_):
+        logits, ids, old_logp, advantages, ref_logp, weights = ctx.saved_tensors
+        # the gradient of a weighted sum of the rows' losses
+        weights = d_loss.contiguous() if weights is None else d_loss * weights
+        return (train_ops.policy_loss(logits, ids, old_logp, advantages, ref_logp=ref_logp, weights=weights, **ctx.options).dlogits,
+                None, None, None, None, None, None)
+
+
+class _PreferenceLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logp, ref_logp, starts, weights, options):
+        ref_logp, starts, weights = (None if t is None else t.detach().contiguous() for t in (ref_logp, starts, weights))
+        logp = logp.contiguous()
+        r = train_ops.preference_loss(logp, ref_logp, starts, weights=weights, need_grad=False, **options)
+        ctx.save_for_backward(logp, ref_logp, starts, weights)
+        ctx.options = options
+        ctx.mark_non_differentiable(r.rewards)
+        return r.loss, r.rewards
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_loss, _):
+        logp, ref_logp, starts, weights = ctx.saved_tensors
+        weights = d_loss.contiguous() if weights is None else d_loss * weights
+        return train_ops.preference_loss(logp, ref_logp, starts, weights=weights, **ctx.options).d_logp, None, None, None, None
+
+
+def policy_loss(logits, ids, old_logp, advantages, *, ref_logp=None, weights=None, clip=(0.2, 0.2), kl: float = 0.0, entropy: float = 0.0,
+                scale: float = 1.0):
+    """(loss, logp, entropy, kl, ratio) of `train_ops.policy_loss`, one value per row; loss has a gradient for the logits, the others
+    none.  It is made in the backward pass, from the logits: where the losses are only summed, `train_ops.policy_loss` has it in one pass
+    with the loss.  Logits that do not lie in rows are copied first."""
+    return _PolicyLoss.apply(logits, ids, old_logp, advantages, ref_logp, weights, dict(clip=tuple(clip), kl=kl, entropy=entropy, scale=scale))
+
+
+def preference_loss(logp, ref_logp, starts, *, beta: float = 0.1, label_smoothing: float = 0.0, kind: str = "sigmoid", average: bool = False,
+                    weights=None):
+    """(loss, rewards) of `train_ops.preference_loss`; loss has a gradient for logp."""
+    return _PreferenceLoss.apply(logp, ref_logp, starts, weights, dict(beta=beta, label_smoothing=label_smoothing, kind=kind, average=average))

@@ -363,6 +363,62 @@ PyObject* adamw_step(PyObject* const* a) {
 // Memory of the current stream: what is enqueued behind runs before anything that gets it next
 c10::DataPtr scratch(size_t bytes) { return c10::cuda::CUDACachingAllocator::get()->allocate(bytes); }
 
+// (logits, ids, old_logp, advantages, ref_logp, weights, low, high, kl, entropy, scale, need_grad, out) -> (stats, dlogits)
+PyObject* policy_loss(PyObject* const* a) {
+    const at::Tensor& z = tensor(a[0], "logits");
+    const int dev = device_of(z, "logits");
+    const Rows r = logits_of(z, dev);
+    const int32_t fmt = format_of(z, "logits");
+    const Ids ids = ids_of(tensor(a[1], "ids"), r.rows, dev);
+    const float *old_logp = flat_f32(&tensor(a[2], "old_logp"), r.rows, "old_logp", dev),
+                *advantages = flat_f32(&tensor(a[3], "advantages"), r.rows, "advantages", dev),
+                *ref_logp = flat_f32(optional_tensor(a[4], "ref_logp"), r.rows, "ref_logp", dev),
+                *weights = flat_f32(optional_tensor(a[5], "weights"), r.rows, "weights", dev);
+    const float low = (float)number(a[6], "clip"), high = (float)number(a[7], "clip"), kl = (float)number(a[8], "kl"),
+                entropy = (float)number(a[9], "entropy"), scale = (float)number(a[10], "scale");
+    if (kl != 0.f && !ref_logp) raise(PyExc_ValueError, "kl: needs ref_logp");
+    const at::Tensor* out_in = optional_tensor(a[12], "out");
+    const bool need = PyObject_IsTrue(a[11]);
+    if (out_in && !need) raise(PyExc_ValueError, "out: only with need_grad");
+    int64_t ld_out = 0;
+    at::Tensor stats = new_f32({5, r.rows}, dev), out;
+    if (need) out = result_like(out_in, z, "out", dev, &ld_out, "the logits'");
+    check(ssgd_policy_loss(z.data_ptr(), r.ld, fmt, ids.p, ids.bytes, r.rows, r.n, scale, old_logp, advantages, ref_logp, weights, low, high, kl,
+                           entropy, stats.data_ptr<float>(), need ? out.data_ptr() : nullptr, ld_out, stream_of(dev)), "ssgd_policy_loss");
+    written(out_in);
+    return Py_BuildValue("(NN)", wrap(stats), wrap_or_none(out));
+}
+
+// (logp, ref_logp, starts, weights, kind, beta, smoothing, average, need_grad, out) -> (loss, rewards, d_logp)
+PyObject* preference_loss(PyObject* const* a) {
+    const at::Tensor& logp = tensor(a[0], "logp");
+    const int dev = device_of(logp, "logp");
+    const int64_t tokens = logp.numel();
+    const float *lp = flat_f32(&logp, tokens, "logp", dev), *ref = flat_f32(optional_tensor(a[1], "ref_logp"), tokens, "ref_logp", dev);
+    const at::Tensor& starts = tensor(a[2], "starts");
+    const at::ScalarType type = starts.scalar_type();
+    if (type != at::kLong && type != at::kInt) raise(PyExc_TypeError, "starts: need int64 or int32");
+    const int64_t n = starts.numel();
+    if (n % 2 != 1) raise(PyExc_ValueError, "starts: need two per pair and the end");
+    const void* sp = flat(&starts, type, n, "starts", dev);
+    const int64_t pairs = n / 2;
+    const float* weights = flat_f32(optional_tensor(a[3], "weights"), pairs, "weights", dev);
+    const at::Tensor* out_in = optional_tensor(a[9], "out");
+    const bool need = PyObject_IsTrue(a[8]);
+    if (out_in && !need) raise(PyExc_ValueError, "out: only with need_grad");
+    at::Tensor loss = new_f32({pairs}, dev), rewards = new_f32({2, pairs}, dev), d;
+    if (need) d = out_in ? *out_in : new_f32(logp.sizes(), dev);
+    float* dp = need ? flat_f32(&d, tokens, "out", dev) : nullptr;
+    size_t bytes = 0;
+    check(ssgd_preference_loss_workspace(tokens, pairs, &bytes), "ssgd_preference_loss_workspace");
+    const c10::DataPtr ws = scratch(bytes);
+    check(ssgd_preference_loss(lp, ref, tokens, sp, type == at::kLong ? 8 : 4, pairs, weights, (int32_t)integer(a[4], "kind"),
+                               (float)number(a[5], "beta"), (float)number(a[6], "label_smoothing"), PyObject_IsTrue(a[7]),
+                               loss.data_ptr<float>(), rewards.data_ptr<float>(), dp, ws.get(), bytes, stream_of(dev)), "ssgd_preference_loss");
+    written(out_in);
+    return Py_BuildValue("(NNN)", wrap(loss), wrap(rewards), wrap_or_none(d));
+}
+
 // (x, steps, a, b, c, eps, products, out) -> the orthogonalised x
 PyObject* orthogonalize(PyObject* const* a) {
     const at::Tensor& x = tensor(a[0], "x");
@@ -487,7 +543,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(layer_norm, 5), ENTRY(layer_norm_backward, 9), ENTRY(token_logprobs, 4), ENTRY(token_logprobs_backward, 10),
-                         ENTRY(adamw_step, 17), ENTRY(orthogonalize, 8), ENTRY(muon_step, 16), ENTRY(status, 0),
+                         ENTRY(adamw_step, 17), ENTRY(policy_loss, 13), ENTRY(preference_loss, 10), ENTRY(orthogonalize, 8),
+                         ENTRY(muon_step, 16), ENTRY(status, 0),
                          ENTRY(set_error_class, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

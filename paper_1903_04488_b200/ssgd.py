@@ -23,6 +23,7 @@ ZERO_DEFERRED, ZERO_EAGER = 0, 1
 SCHED_AUTO, SCHED_COORDINATE_MAJOR, SCHED_WORKER_MAJOR = 0, 1, 2
 FMT_F16, FMT_BF16, FMT_F32, FMT_E4M3 = 0, 1, 2, 3
 MAX_TOP = 32
+PREFERENCE_SIGMOID, PREFERENCE_IPO, PREFERENCE_HINGE = 0, 1, 2
 ADAMW_BLOCK = 256
 MAX_R = 15
 
@@ -74,6 +75,9 @@ SIGNATURES = {
     "ssgd_token_logprobs": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _i32, _vp, _vp, _vp, _vp],
     "ssgd_token_logprobs_backward": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
                                      _i64, _vp],
+    "ssgd_policy_loss": [_vp, _i64, _i32, _vp, _i32, _i64, _i64, _f32, _vp, _vp, _vp, _vp, _f32, _f32, _f32, _f32, _vp, _vp, _i64, _vp],
+    "ssgd_preference_loss_workspace": [_i64, _i64, C.POINTER(_sz)],
+    "ssgd_preference_loss": [_vp, _vp, _i64, _vp, _i32, _i64, _vp, _i32, _f32, _f32, _i32, _vp, _vp, _vp, _vp, _sz, _vp],
     "ssgd_orthogonalize_workspace": [_vp, _i32, _i32, _i32, C.POINTER(_sz)],
     "ssgd_orthogonalize": [_vp, _i32, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _vp, _sz, _vp],
     "ssgd_muon_step": [_vp, _i32, _i32, _i32, _i32, _f64, _f64, _i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp, _sz, _vp],

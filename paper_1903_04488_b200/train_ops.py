@@ -97,6 +97,79 @@ def token_logprobs_backward(logits: torch.Tensor, ids: torch.Tensor, lse: torch.
     return (_native or native()).token_logprobs_backward(logits, ids, lse, d_logp, entropy, d_entropy, top_idx, d_top, scale, out)
 
 
+# ---- losses over log probabilities -------------------------------------------------------------------
+
+
+class PolicyLoss:
+    """stats [5][rows] fp32 (loss, logp, entropy, kl and ratio are its rows); dlogits in the logits' type, or None."""
+    __slots__ = ("stats", "dlogits")
+
+    def __init__(self, stats, dlogits):
+        self.stats, self.dlogits = stats, dlogits
+
+    @property
+    def loss(self) -> torch.Tensor:
+        return self.stats[0]
+
+    @property
+    def logp(self) -> torch.Tensor:
+        return self.stats[1]
+
+    @property
+    def entropy(self) -> torch.Tensor:
+        return self.stats[2]
+
+    @property
+    def kl(self) -> torch.Tensor:
+        return self.stats[3]
+
+    @property
+    def ratio(self) -> torch.Tensor:
+        return self.stats[4]
+
+
+def policy_loss(logits: torch.Tensor, ids: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, *,
+                ref_logp: torch.Tensor | None = None, weights: torch.Tensor | None = None, clip=(0.2, 0.2), kl: float = 0.0,
+                entropy: float = 0.0, scale: float = 1.0, need_grad: bool = True, out: torch.Tensor | None = None) -> PolicyLoss:
+    """The clipped policy loss of sampled tokens and, in the same pass, the gradient of its sum with respect to the logits:
+    loss = weights (-min(r A, clip(r, 1 - clip[0], 1 + clip[1]) A) + kl K - entropy H), r = e^(logp - old_logp), and with q = ref_logp - logp
+    K = e^q - 1 - q, which estimates the divergence from the reference without bias.
+
+    logits [rows][vocab]; ids [rows] int64 or int32; old_logp, advantages, ref_logp, weights: [rows] float32.  For a mean, give weights
+    1 / number of tokens.  Rows of weight 0 (padding, prompts) or with an id outside the vocabulary are not read: their statistics and
+    gradients are 0.  out: where the gradient goes (may be the logits themselves).  need_grad=False: the statistics only."""
+    low, high = clip
+    return PolicyLoss(*(_native or native()).policy_loss(logits, ids, old_logp, advantages, ref_logp, weights, low, high, kl, entropy, scale,
+                                                         need_grad, out))
+
+
+class PreferenceLoss:
+    """loss [pairs], rewards [2][pairs] (of the preferred sequences and of the others) and d_logp (logp's shape), or None; all fp32."""
+    __slots__ = ("loss", "rewards", "d_logp")
+
+    def __init__(self, loss, rewards, d_logp):
+        self.loss, self.rewards, self.d_logp = loss, rewards, d_logp
+
+
+PREFERENCE_KINDS = {"sigmoid": S.PREFERENCE_SIGMOID, "ipo": S.PREFERENCE_IPO, "hinge": S.PREFERENCE_HINGE}
+
+
+def preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor | None, starts: torch.Tensor, *, beta: float = 0.1,
+                    label_smoothing: float = 0.0, kind: str = "sigmoid", average: bool = False, weights: torch.Tensor | None = None,
+                    need_grad: bool = True, out: torch.Tensor | None = None) -> PreferenceLoss:
+    """The loss of pairs of sequences of which one is preferred, and the gradient of its sum with respect to the tokens' log
+    probabilities.  With x = beta (difference of the two sums of logp - ref_logp; with `average` of the means):
+    "sigmoid" -(1 - e) log sigmoid(x) - e log sigmoid(-x), e = label_smoothing; "ipo" ((x - 1/2) / beta)^2; "hinge" max(0, 1 - x).
+
+    logp, ref_logp (None: 0): float32, of all tokens (as `token_logprobs` gives them, 0 where there is nothing to predict).  starts:
+    int32 or int64 [2 pairs + 1], ascending: sequence s is tokens [starts[s], starts[s + 1]), sequence 2 p the preferred one of pair p.
+    weights [pairs].  Tokens of no sequence have gradient 0.  out: where the gradient goes (may be logp itself)."""
+    if kind not in PREFERENCE_KINDS:
+        raise ValueError('kind: "sigmoid", "ipo" or "hinge"')
+    return PreferenceLoss(*(_native or native()).preference_loss(logp, ref_logp, starts, weights, PREFERENCE_KINDS[kind], beta, label_smoothing,
+                                                                 average, need_grad, out))
+
+
 # ---- AdamW over many tensors -------------------------------------------------------------------------
 
 def _check(tensors, dtype, lens, name: str, dev: torch.device) -> None:
