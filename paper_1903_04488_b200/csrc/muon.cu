@@ -31,16 +31,17 @@ namespace {
 constexpr float SCALE = 1024.f;
 constexpr int MAX_GROUP = 224;                      // matrices of one set of launches: their descriptors are arguments of the first
 constexpr int64_t GROUP_ELEMENTS = (int64_t)1 << 27;  // and no more than this many elements, unless one matrix has them
-constexpr int STRIP_BLOCKS = 8;                     // what a CTA of the preparation takes: 64 rows of 512 columns
+constexpr int STRIP_BLOCKS = 4;                     // what a CTA of the preparation takes: 64 rows of 256 columns
 
 struct Matrix {
     void* out; const void* in; float* m;
     int64_t ld_out, ld_in;
     int32_t rows, cols, rb, cb, mb;                 // size; size in blocks; blocks of the shorter side
-    uint32_t x[2], a, b;                            // first blocks: x before and after a step, A, B.  Second numbers lie behind the first
+    uint32_t x0, x1, a, b;                          // first blocks: x at even and at odd steps, A, B.  Second numbers lie behind the first
     uint32_t vec;                                   // d and e, mb * 64 floats each
     int32_t strip0, strips, sym0, full0;            // first strip, first tile of A and B, first tile of x among all
     float update;                                   // lr * scale
+    __host__ __device__ uint32_t x(int which) const { return which ? x1 : x0; }
     __host__ __device__ bool tall() const { return rb > cb || (rb == cb && rows > cols); }
 };
 struct Group { Matrix m[MAX_GROUP]; };
@@ -55,7 +56,7 @@ struct Space {
 };
 struct Common {
     Space at;
-    int32_t count, strips;
+    int32_t count;
     int32_t fmt_in, fmt_out;
     bool split;                                     // two numbers in A and B too, three products
     bool nesterov, update;                          // update: out is a parameter to be moved, otherwise it gets the result
@@ -68,10 +69,9 @@ __device__ int g_error;                             // set by a wait that ran ou
 
 // ---- preparation -------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float load_any(const void* p, int64_t i, int32_t fmt) {
-    return fmt == SSGD_FMT_F32 ? static_cast<const float*>(p)[i]
-         : fmt == SSGD_FMT_F16 ? __half2float(static_cast<const __half*>(p)[i]) : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-}
+// Whether four neighbours may be read at once, where rows begin at multiples of four
+template <typename T>
+__device__ __forceinline__ bool aligned_four(const void* p) { return (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0; }
 
 // The matrix of a strip or tile: the last whose first is not beyond it
 template <typename F>
@@ -98,12 +98,38 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
     return s;
 }
 
+// Four neighbours of a row (fewer at its end, zeros in their place)
+template <typename T>
+__device__ __forceinline__ void load_four(const T* p, int n, bool vector, float (&v)[4]) {
+    if (vector && n >= 4) {
+        const Vec<T, 4> x = load_vec<T, 4>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_f32(x.e[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < n ? to_f32(p[e]) : 0.f;
+    }
+}
+// A block of the preparation: thread t has columns 4 (t mod 16) .. of rows t / 16 + 16 i
+constexpr int SHARE = 4;
+template <typename T>
+__device__ __forceinline__ void load_block(const Matrix& M, int r0, int c0, bool vector_in, bool vector_m, float (&g)[SHARE][4], float (&m)[SHARE][4]) {
+    const int c = c0 + (int)threadIdx.x % 16 * 4;
+#pragma unroll
+    for (int i = 0; i < SHARE; ++i) {
+        const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
+        load_four<T>(static_cast<const T*>(M.in) + (int64_t)r * M.ld_in + c, n, vector_in, g[i]);
+        if (M.m) load_four<float>(M.m + (int64_t)r * M.cols + c, n, vector_m, m[i]);
+    }
+}
+
 // m <- momentum m + (1 - momentum) g, and the sum of squares of what is to be made orthogonal, per strip.  Squares are added in 64
 // bits: they may leave the range of 32.
+template <typename T>
 __global__ void __launch_bounds__(PREPARE_THREADS) k_momentum(const __grid_constant__ Group G, const __grid_constant__ Common C) {
     __shared__ double shared[PREPARE_THREADS / 32];
-    successor_may_start();
     successor_wait();
+    successor_may_start();
     if (blockIdx.x == 0) {
         const uint32_t* from = reinterpret_cast<const uint32_t*>(&G);
         uint32_t* to = reinterpret_cast<uint32_t*>(C.at.matrices);
@@ -111,41 +137,57 @@ __global__ void __launch_bounds__(PREPARE_THREADS) k_momentum(const __grid_const
     }
     const int strip = blockIdx.x;
     const Matrix& M = G.m[matrix_of(C.count, strip, [&](int i) { return G.m[i].strip0; })];
-    const int local = strip - M.strip0, r0 = local % M.rb * BLOCK, c0 = local / M.rb * (STRIP_BLOCKS * BLOCK);
-    const int h = min(BLOCK, M.rows - r0), w = min(STRIP_BLOCKS * BLOCK, M.cols - c0);
+    const int local = strip - M.strip0, r0 = local % M.rb * BLOCK, cblock0 = local / M.rb * STRIP_BLOCKS;
+    const bool vector_in = M.ld_in % 4 == 0 && aligned_four<T>(M.in), vector_m = M.cols % 4 == 0 && aligned_four<float>(M.m);
     const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
     double sum = 0.0;
-    int r = threadIdx.x / w, c = threadIdx.x % w;
-    const int dr = PREPARE_THREADS / w, dc = PREPARE_THREADS % w;
-    while (r < h) {
-        float g = load_any(M.in, (int64_t)(r0 + r) * M.ld_in + c0 + c, C.fmt_in) * scale;
-        if (M.m) {
-            float* at = M.m + (int64_t)(r0 + r) * M.cols + c0 + c;
-            const float m = fmaf(mu, *at, (1.f - mu) * g);
-            *at = m;
-            g = C.nesterov ? fmaf(mu, m, (1.f - mu) * g) : m;
+    for (int cblock = cblock0; cblock < min(cblock0 + STRIP_BLOCKS, M.cb); ++cblock) {
+        float g[SHARE][4], m[SHARE][4];
+        load_block<T>(M, r0, cblock * BLOCK, vector_in, vector_m, g, m);
+        const int c = cblock * BLOCK + (int)threadIdx.x % 16 * 4;
+#pragma unroll
+        for (int i = 0; i < SHARE; ++i) {
+            const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
+            if (n <= 0) continue;
+            if (M.m) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float in = g[i][e] * scale;
+                    m[i][e] = fmaf(mu, m[i][e], (1.f - mu) * in);
+                    g[i][e] = C.nesterov ? fmaf(mu, m[i][e], (1.f - mu) * in) : m[i][e];
+                }
+                float* to = M.m + (int64_t)r * M.cols + c;
+                if (vector_m && n >= 4) store_vec<float, 4>(to, Vec<float, 4>{{m[i][0], m[i][1], m[i][2], m[i][3]}});
+                else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < n) to[e] = m[i][e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += e < n ? (double)g[i][e] * (double)g[i][e] : 0.0;
         }
-        sum += (double)g * (double)g;
-        r += dr;
-        c += dc;
-        if (c >= w) { c -= w; ++r; }
     }
     sum = block_sum(sum, shared);
     if (threadIdx.x == 0) C.at.sums[strip] = sum;
 }
 
-// The nearest fp16 number and what it leaves
-__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
-    hi = __float2half_rn(v);
-    lo = __float2half_rn(v - __half2float(hi));
+// Two numbers as fp16, and what that leaves
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 back = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - back.x, b - back.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
 }
-union Piece { uint4 v; __half h[8]; };
+__device__ __forceinline__ float2 halves(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
 // x = u / (|u| + eps) as blocks
+template <typename T>
 __global__ void __launch_bounds__(PREPARE_THREADS) k_layout(const __grid_constant__ Common C) {
     __shared__ double shared[PREPARE_THREADS / 32];
-    successor_may_start();
     successor_wait();
+    successor_may_start();
     const int strip = blockIdx.x;
     const Matrix M = C.at.matrices[matrix_of(C.count, strip, [&](int i) { return C.at.matrices[i].strip0; })];
     double sum = 0.0;
@@ -157,28 +199,34 @@ __global__ void __launch_bounds__(PREPARE_THREADS) k_layout(const __grid_constan
     const float factor = (float)(inv > 0.0 && inv < (double)INFINITY ? frexp(inv, &exponent) : inv) * SCALE;
     const float power = ldexpf(1.f, min(max(exponent, -126), 127));
     const int local = strip - M.strip0, rblock = local % M.rb, cblock0 = local / M.rb * STRIP_BLOCKS;
+    const bool vector_in = M.ld_in % 4 == 0 && aligned_four<T>(M.in), vector_m = M.cols % 4 == 0 && aligned_four<float>(M.m);
     const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
-    const uint32_t second = (uint32_t)M.rb * (uint32_t)M.cb;
+    const int64_t second = (int64_t)M.rb * M.cb * BLOCK_BYTES;
     for (int cblock = cblock0; cblock < min(cblock0 + STRIP_BLOCKS, M.cb); ++cblock) {
-        uint8_t* block = C.at.blocks + (int64_t)(M.x[0] + (uint32_t)cblock * M.rb + rblock) * BLOCK_BYTES;
-        for (int i = threadIdx.x; i < BLOCK * 8; i += PREPARE_THREADS) {
-            const int rr = i >> 3, piece = i & 7, r = rblock * BLOCK + rr, c = cblock * BLOCK + piece * 8;
-            Piece hi, lo;
+        uint8_t* block = C.at.blocks + (int64_t)(M.x0 + (uint32_t)cblock * M.rb + rblock) * BLOCK_BYTES;
+        float g[SHARE][4], m[SHARE][4];
+        load_block<T>(M, rblock * BLOCK, cblock * BLOCK, vector_in, vector_m, g, m);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float u = 0.f;
-                if (r < M.rows && c + e < M.cols) {
-                    u = load_any(M.in, (int64_t)r * M.ld_in + c + e, C.fmt_in) * scale;
-                    if (M.m) {
-                        const float m = M.m[(int64_t)r * M.cols + c + e];
-                        u = C.nesterov ? fmaf(mu, m, (1.f - mu) * u) : m;
-                    }
-                    u = u * power * factor;
-                }
-                split(u, hi.h[e], lo.h[e]);
+        for (int i = 0; i < SHARE; ++i) {
+            const int rr = (int)threadIdx.x / 16 + 16 * i, cc = (int)threadIdx.x % 16 * 4;
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u[e] = g[i][e];
+                if (M.m) u[e] = C.nesterov ? fmaf(mu, m[i][e], (1.f - mu) * (g[i][e] * scale)) : m[i][e];
+                u[e] = u[e] * power * factor;
             }
-            *reinterpret_cast<uint4*>(block + piece_at(rr, piece)) = hi.v;
-            *reinterpret_cast<uint4*>(block + (int64_t)second * BLOCK_BYTES + piece_at(rr, piece)) = lo.v;
+            if (rblock * BLOCK + rr >= M.rows)                                  // the padding, whatever the factor is
+                u[0] = u[1] = u[2] = u[3] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (cblock * BLOCK + cc + e >= M.cols) u[e] = 0.f;
+            uint2 hi, lo;
+            split2(u[0], u[1], hi.x, lo.x);
+            split2(u[2], u[3], hi.y, lo.y);
+            uint8_t* to = block + piece_at(rr, cc / 8) + cc % 8 * 2;
+            *reinterpret_cast<uint2*>(to) = hi;
+            *reinterpret_cast<uint2*>(to + second) = lo;
         }
     }
     asm volatile("fence.proxy.async.global;" ::: "memory");    // bulk copies read them
@@ -188,281 +236,446 @@ __global__ void __launch_bounds__(PREPARE_THREADS) k_layout(const __grid_constan
 
 enum Kind { GRAM, POLYNOMIAL, APPLY, FINISH };
 
-constexpr int TILE = 128;                           // rows and columns of a tile
-constexpr int STAGES = 6;
-constexpr int STAGE_BYTES = 4 * BLOCK_BYTES;
-constexpr int EPILOGUE_WARPS = 4;
-constexpr int THREADS = 32 * (EPILOGUE_WARPS + 2);
+// A tile is 256 rows and COLS columns, of a pair of CTAs that has half of the rows each.  What a tile loads per block of the contraction
+// grows with its sides, what it computes with their product: 256 x 256 needs 12 TB/s from L2 at the tensor cores' full rate, 128 x 128 by
+// single CTAs 24 TB/s.  Where the larger tiles are too few, 256 x 128.
+constexpr int TILE_ROWS = 256;
+constexpr int RING = 192 * 1024;                    // bytes of operands on their way
+constexpr int RESULT_WARPS = 8;
+constexpr int THREADS = 32 * (RESULT_WARPS + 2);
+constexpr int SCRATCH = 4096;                       // of each result warp: 32 x 32 numbers change hands there
+constexpr int CHUNK = 4;                            // blocks of the contraction that are added up by the tensor cores alone (SPLIT)
+
+// Bytes of a stage of the ring: 128 rows of A and half of the columns of B; with SPLIT the first and the second numbers
+template <int COLS, bool SPLIT> constexpr int STAGE = (2 + COLS / 128) * BLOCK_BYTES * (SPLIT ? 2 : 1);
+template <int COLS, bool SPLIT> constexpr int STAGES = RING / STAGE<COLS, SPLIT>;
 
 struct Shared {
-    uint64_t full[STAGES], empty[STAGES], done[2], taken[2];
+    uint64_t full[8], empty[8], done[2], taken[2];
     uint32_t tmem;
     int gave_up;
     int32_t first[MAX_GROUP];
 };
-constexpr int SHARED_BYTES = 1024 + STAGES * STAGE_BYTES + (int)sizeof(Shared);
+constexpr int SHARED_BYTES = 1024 + RING + RESULT_WARPS * SCRATCH + (int)sizeof(Shared);
+static_assert(SHARED_BYTES <= 227 * 1024, "shared memory of a CTA");
 
-// One operand of a product: blocks [R][C] of which 128 rows or columns are needed at a time
+// One operand of a product: blocks [R][C]
 struct Operand {
-    const uint8_t* hi; const uint8_t* lo;
+    uint32_t base, second;                          // first block; blocks from the first numbers to the second
     int32_t R, mn_blocks;
     bool mn_major;
-    __device__ __forceinline__ const uint8_t* block(bool low, int mn, int k) const {
-        mn = min(mn, mn_blocks - 1);                // beyond the edge: rows or columns that are not stored
-        const int64_t i = mn_major ? (int64_t)mn * R + k : (int64_t)k * R + mn;
-        return (low ? lo : hi) + i * BLOCK_BYTES;
+    // the first block of the contraction at rows or columns 64 mn ..; beyond the edge, rows or columns that are not stored
+    __device__ __forceinline__ int32_t at(int mn) const {
+        mn = min(mn, mn_blocks - 1);
+        return (int32_t)(base + (uint32_t)(mn_major ? mn * R : mn));
     }
+    __device__ __forceinline__ int32_t step() const { return mn_major ? 1 : R; }
 };
 struct Product {
     Operand A, B;
-    int32_t steps, tiles_m;                         // blocks of the contraction; tiles along the rows
+    int32_t steps;                                  // blocks of the contraction
 };
 
 template <Kind KIND>
-__device__ __forceinline__ Product product_of(const Common& C, const Matrix& M, int which) {
-    auto at = [&](uint32_t block) { return C.at.blocks + (int64_t)block * BLOCK_BYTES; };
+__device__ __forceinline__ Product product_of(const Matrix& M, int which) {
     const uint32_t xs = (uint32_t)M.rb * (uint32_t)M.cb, ms = (uint32_t)M.mb * (uint32_t)M.mb;
     const bool tall = M.tall();
     Product P;
     if (KIND == GRAM) {
-        P.A = Operand{at(M.x[which]), at(M.x[which] + xs), M.rb, M.mb, tall};
+        P.A = Operand{M.x(which), xs, M.rb, M.mb, tall};
         P.B = P.A;
         P.steps = tall ? M.rb : M.cb;
-        P.tiles_m = (M.mb + 1) / 2;
     } else if (KIND == POLYNOMIAL) {
-        P.A = Operand{at(M.a), at(M.a + ms), M.mb, M.mb, false};
+        P.A = Operand{M.a, ms, M.mb, M.mb, false};
         P.B = P.A;
         P.steps = M.mb;
-        P.tiles_m = (M.mb + 1) / 2;
     } else {
-        const Operand q{at(M.b), at(M.b + ms), M.mb, M.mb, false};
-        P.A = tall ? Operand{at(M.x[which]), at(M.x[which] + xs), M.rb, M.rb, false} : q;
-        P.B = tall ? q : Operand{at(M.x[which]), at(M.x[which] + xs), M.rb, M.cb, true};
+        const Operand q{M.b, ms, M.mb, M.mb, false};
+        P.A = tall ? Operand{M.x(which), xs, M.rb, M.rb, false} : q;
+        P.B = tall ? q : Operand{M.x(which), xs, M.rb, M.cb, true};
         P.steps = M.mb;
-        P.tiles_m = (M.rb + 1) / 2;
     }
     return P;
 }
 
-__device__ __forceinline__ void store_pieces(uint8_t* hi, uint8_t* lo, uint32_t at, const float (&v)[8], bool both) {
-    Piece h, l;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) split(v[e], h.h[e], l.h[e]);
-    *reinterpret_cast<uint4*>(hi + at) = h.v;
-    if (both) *reinterpret_cast<uint4*>(lo + at) = l.v;
+// Tiles of a symmetric product with n blocks to a side: those that reach the diagonal or lie below it, row by row.  With 256 columns row I has
+// I + 1 of them, with 128 2 I + 2 (but no more than there are).
+template <int COLS>
+__host__ __device__ inline int64_t symmetric_tiles(int64_t n) {
+    const int64_t rows = (n + 3) / 4, cols = (n + COLS / BLOCK - 1) / (COLS / BLOCK);
+    return COLS == 256 ? rows * (rows + 1) / 2 : rows * (rows + 1) - (2 * rows - cols);
 }
-__device__ __forceinline__ void load_pieces(const uint8_t* hi, const uint8_t* lo, uint32_t at, float (&v)[8], bool both) {
-    Piece h, l;
-    h.v = *reinterpret_cast<const uint4*>(hi + at);
-    if (both) l.v = *reinterpret_cast<const uint4*>(lo + at);
+template <int COLS>
+__host__ __device__ inline int64_t all_tiles(int64_t rb, int64_t cb) {
+    return (rb + 3) / 4 * ((cb + COLS / BLOCK - 1) / (COLS / BLOCK));
+}
+struct Tile { int row, col; };                      // first blocks
+template <Kind KIND, int COLS>
+__device__ __forceinline__ Tile tile_of(const Matrix& M, int i) {
+    if (KIND == GRAM || KIND == POLYNOMIAL) {
+        int I;
+        if (COLS == 256) {
+            I = (int)((sqrtf(8.f * (float)i + 1.f) - 1.f) * 0.5f);
+            while (I * (I + 1) / 2 > i) --I;
+            while ((I + 1) * (I + 2) / 2 <= i) ++I;
+            return Tile{I * 4, (i - I * (I + 1) / 2) * 4};
+        }
+        I = (int)((sqrtf(4.f * (float)i + 1.f) - 1.f) * 0.5f);
+        while (I * (I + 1) > i) --I;
+        while ((I + 1) * (I + 2) <= i) ++I;
+        return Tile{I * 4, (i - I * (I + 1)) * 2};
+    }
+    const int rows = (M.rb + 3) / 4;
+    return Tile{i % rows * 4, i / rows * (COLS / BLOCK)};
+}
+
+// ---- results ------------------------------------------------------------------------------------------
+//
+// A warp has 32 rows of the tile and takes 32 columns at a time.  Tensor memory gives a row to a lane; through 4 KB of shared
+// memory they are dealt out anew, eight neighbours of a row to a lane and four lanes to 64 bytes of a block's row, which is how blocks
+// and outputs are read and written.
+
+__device__ __forceinline__ uint32_t word_at(int r, int piece) { return (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4)); }
+// 32 x 32 fp16 numbers; neither eight rows of a column nor rows meet in a bank
+__device__ __forceinline__ uint32_t half_at(int r, int piece) { return (uint32_t)(r * 64 + ((piece ^ (((r >> 1) ^ (r >> 3)) & 3)) << 4)); }
+
+// 32 x 32 numbers of a block, from row 32 rh and column 32 ch on: lane's piece of the i-th eight rows
+struct Quarter {
+    uint8_t* block;
+    int rh, ch;
+    __device__ __forceinline__ uint8_t* at(int i, int lane) const { return block + piece_at(rh * 32 + i * 8 + lane / 4, ch * 4 + lane % 4); }
+};
+
+// What a piece of results needs beside the products
+template <Kind KIND, bool SPLIT> struct Source {
+    static constexpr bool NEEDED = KIND != GRAM, BOTH = KIND != POLYNOMIAL || SPLIT;
+    uint4 hi[NEEDED ? 4 : 1], lo[NEEDED && BOTH ? 4 : 1];
+    float row[4], col[8];                           // d or e of the rows and columns
+};
+
+template <Kind KIND>
+__device__ __forceinline__ Quarter quarter(const Common& C, const Matrix& M, uint32_t first, int row0, int col0) {
+    const int R = KIND == GRAM || KIND == POLYNOMIAL ? M.mb : M.rb;
+    return Quarter{C.at.blocks + (int64_t)(first + (uint32_t)(col0 / BLOCK) * R + row0 / BLOCK) * BLOCK_BYTES, row0 / 32 % 2, col0 / 32 % 2};
+}
+
+template <Kind KIND, bool SPLIT>
+__device__ __forceinline__ void fetch(const Common& C, const Matrix& M, int which, int row0, int col0, int lane, Source<KIND, SPLIT>& s) {
+    if constexpr (KIND == GRAM) return;
+    const int64_t second = (int64_t)(KIND == POLYNOMIAL ? M.mb : M.rb) * (KIND == POLYNOMIAL ? M.mb : M.cb) * BLOCK_BYTES;
+    const Quarter q = quarter<KIND>(C, M, KIND == POLYNOMIAL ? M.a : M.x(which), row0, col0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __half2float(h.h[e]) + (both ? __half2float(l.h[e]) : 0.f);
+    for (int i = 0; i < 4; ++i) {
+        s.hi[i] = *reinterpret_cast<const uint4*>(q.at(i, lane));
+        if constexpr (Source<KIND, SPLIT>::BOTH) s.lo[i] = *reinterpret_cast<const uint4*>(q.at(i, lane) + second);
+    }
+    const float* d = C.at.vec + M.vec + (KIND == POLYNOMIAL ? 0 : M.mb * BLOCK);
+    if (KIND == POLYNOMIAL || !M.tall()) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.row[i] = d[row0 + i * 8 + lane / 4];
+    }
+    if (KIND == POLYNOMIAL || M.tall()) {
+        const float4 a = *reinterpret_cast<const float4*>(d + col0 + lane % 4 * 8), b = *reinterpret_cast<const float4*>(d + col0 + lane % 4 * 8 + 4);
+        s.col[0] = a.x; s.col[1] = a.y; s.col[2] = a.z; s.col[3] = a.w;
+        s.col[4] = b.x; s.col[5] = b.y; s.col[6] = b.z; s.col[7] = b.w;
+    }
 }
 
 // Eight results in a row of the output
 template <typename T>
-__device__ __forceinline__ void finish(const Common& C, const Matrix& M, int row, int col, const float (&v)[8]) {
-    T* out = static_cast<T*>(M.out) + (int64_t)row * M.ld_out + col;
-    const int n = min(8, M.cols - col);
+__device__ __forceinline__ void put_output(const Common& C, const Matrix& M, int row, int col, const float (&v)[8]) {
     constexpr int VEC = 16 / sizeof(T);
-    if (n == 8 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
+    const int n = M.cols - col;
+    if (row >= M.rows || n <= 0) return;
+    T* out = static_cast<T*>(M.out) + (int64_t)row * M.ld_out + col;
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
+        Vec<T, VEC> o[8 / VEC];
+        if (C.update) {
 #pragma unroll
-        for (int i = 0; i < 8; i += VEC) {
-            Vec<T, VEC> o;
-            if (C.update) o = load_vec<T, VEC>(out + i);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                o.e[e] = from_f32<T>(C.update ? fmaf(to_f32(o.e[e]), C.decay, -M.update * v[i + e]) : v[i + e]);
-            store_vec<T, VEC>(out + i, o);
+            for (int i = 0; i < 8 / VEC; ++i) o[i] = load_vec<T, VEC>(out + i * VEC);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            T& to = o[i / VEC].e[i % VEC];
+            to = from_f32<T>(C.update ? fmaf(to_f32(to), C.decay, -M.update * v[i]) : v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8 / VEC; ++i) store_vec<T, VEC>(out + i * VEC, o[i]);
     } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) out[i] = from_f32<T>(C.update ? fmaf(to_f32(out[i]), C.decay, -M.update * v[i]) : v[i]);
+    }
+}
+
+// Exchanges rows and columns of 32 x 32 fp16 numbers, eight of a row to a lane as above, and stores them
+__device__ __forceinline__ void put_transposed(const Quarter& q, uint8_t* scratch, int lane, const uint4 (&h)[4], int64_t offset) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {h[i].x, h[i].y, h[i].z, h[i].w};
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (e < n) out[e] = from_f32<T>(C.update ? fmaf(to_f32(out[e]), C.decay, -M.update * v[e]) : v[e]);
+            *reinterpret_cast<uint16_t*>(scratch + half_at(lane % 4 * 8 + e, i) + lane / 4 * 2) = (uint16_t)(e % 2 ? w[e / 2] >> 16 : w[e / 2]);
     }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint4*>(q.at(i, lane) + offset) = *reinterpret_cast<const uint4*>(scratch + half_at(i * 8 + lane / 4, lane % 4));
 }
 
-// Eight accumulators of one row: what a product becomes
-template <Kind KIND>
-__device__ __forceinline__ void eight(const Common& C, const Matrix& M, int which, int row, int col, const float (&acc)[8], float row_factor) {
-    const int rblock = row / BLOCK, rr = row % BLOCK, cblock = col / BLOCK, piece = col % BLOCK / 8;
-    const uint32_t at = piece_at(rr, piece);
-    auto block = [&](uint32_t first, int R) { return C.at.blocks + (int64_t)(first + (uint32_t)cblock * R + rblock) * BLOCK_BYTES; };
-    const int64_t xs = (int64_t)M.rb * M.cb * BLOCK_BYTES, ms = (int64_t)M.mb * M.mb * BLOCK_BYTES;
-    float* d = C.at.vec + M.vec;
-    float* e = d + M.mb * BLOCK;
-    float v[8];
-    if constexpr (KIND == GRAM) {
+// What 32 rows and columns of a product become.  acc: the lane's row.
+template <Kind KIND, bool SPLIT>
+__device__ __forceinline__ void take(const Common& C, const Matrix& M, int which, int row0, int col0, const float (&acc)[32],
+                                     const Source<KIND, SPLIT>& s, uint8_t* scratch, int lane) {
+    constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
+    __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = acc[i] * (1.f / SCALE);
-            if (row == col + i) {
-                d[row] = v[i] * (1.f / SCALE);
-                v[i] = 0.f;
+    for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<float4*>(scratch + word_at(lane, i)) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
+    __syncwarp();
+    float* diagonal = C.at.vec + M.vec + (KIND == POLYNOMIAL ? M.mb * BLOCK : 0);
+    const bool tall = M.tall();
+    const uint32_t first = KIND == GRAM ? M.a : KIND == POLYNOMIAL ? M.b : M.x(which ^ 1);
+    const int64_t second = (int64_t)(SYMMETRIC ? M.mb : M.rb) * (SYMMETRIC ? M.mb : M.cb) * BLOCK_BYTES;
+    const Quarter to = quarter<KIND>(C, M, first, row0, col0);
+    uint4 hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + lane / 4;
+        const float4 a = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2)), b = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2 + 1));
+        float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        float x[8];
+        if constexpr (KIND != GRAM) {
+            const uint32_t h[4] = {s.hi[i].x, s.hi[i].y, s.hi[i].z, s.hi[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { const float2 f = halves(h[e]); x[2 * e] = f.x; x[2 * e + 1] = f.y; }
+            if constexpr (Source<KIND, SPLIT>::BOTH) {
+                const uint32_t l[4] = {s.lo[i].x, s.lo[i].y, s.lo[i].z, s.lo[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { const float2 f = halves(l[e]); x[2 * e] += f.x; x[2 * e + 1] += f.y; }
             }
         }
-        uint8_t* to = block(M.a, M.mb);
-        store_pieces(to, to + ms, at, v, C.split);
-    } else if constexpr (KIND == POLYNOMIAL) {
-        const uint8_t* from = block(M.a, M.mb);
-        float r[8];
-        load_pieces(from, from + ms, at, r, C.split);
-        const float4 d0 = *reinterpret_cast<const float4*>(d + col), d1 = *reinterpret_cast<const float4*>(d + col + 4);
-        const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float square = fmaf(r[i], row_factor + dj[i], acc[i] * (1.f / SCALE));
-            v[i] = fmaf(C.c, square, C.b * r[i]);
-            if (row == col + i) {
-                e[row] = fmaf(C.c, fmaf(row_factor, row_factor, acc[i] * (1.f / (SCALE * SCALE))), C.b * row_factor);
-                v[i] = 0.f;
+        for (int e = 0; e < 8; ++e) {
+            const bool diag = SYMMETRIC && row0 == col0 && r == lane % 4 * 8 + e;
+            if constexpr (KIND == GRAM) {
+                if (diag) diagonal[row0 + r] = v[e] * (1.f / (SCALE * SCALE));
+                v[e] *= 1.f / SCALE;
+            } else if constexpr (KIND == POLYNOMIAL) {
+                if (diag) diagonal[row0 + r] = fmaf(C.c, fmaf(s.row[i], s.row[i], v[e] * (1.f / (SCALE * SCALE))), C.b * s.row[i]);
+                v[e] = fmaf(C.c, fmaf(x[e], s.row[i] + s.col[e], v[e] * (1.f / SCALE)), C.b * x[e]);
+            } else {
+                v[e] = fmaf((tall ? s.col[e] : s.row[i]) + C.a, x[e], v[e] * (1.f / SCALE));
             }
+            if (diag) v[e] = 0.f;
         }
-        uint8_t* to = block(M.b, M.mb);
-        store_pieces(to, to + ms, at, v, C.split);
-    } else {
-        const uint8_t* from = block(M.x[which], M.rb);
-        float x[8], f[8];
-        load_pieces(from, from + xs, at, x, true);
-        if (M.tall()) {
-            const float4 e0 = *reinterpret_cast<const float4*>(e + col), e1 = *reinterpret_cast<const float4*>(e + col + 4);
-            f[0] = e0.x + C.a; f[1] = e0.y + C.a; f[2] = e0.z + C.a; f[3] = e0.w + C.a;
-            f[4] = e1.x + C.a; f[5] = e1.y + C.a; f[6] = e1.z + C.a; f[7] = e1.w + C.a;
+        if constexpr (KIND == FINISH) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= 1.f / SCALE;
+            const int row = row0 + r, col = col0 + lane % 4 * 8;
+            if (C.fmt_out == SSGD_FMT_F32) put_output<float>(C, M, row, col, v);
+            else if (C.fmt_out == SSGD_FMT_F16) put_output<__half>(C, M, row, col, v);
+            else put_output<__nv_bfloat16>(C, M, row, col, v);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = row_factor + C.a;
+            split2(v[0], v[1], hi[i].x, lo[i].x);
+            split2(v[2], v[3], hi[i].y, lo[i].y);
+            split2(v[4], v[5], hi[i].z, lo[i].z);
+            split2(v[6], v[7], hi[i].w, lo[i].w);
+            *reinterpret_cast<uint4*>(to.at(i, lane)) = hi[i];
+            if (SPLIT || !SYMMETRIC) *reinterpret_cast<uint4*>(to.at(i, lane) + second) = lo[i];
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(f[i], x[i], acc[i] * (1.f / SCALE));
-        if constexpr (KIND == APPLY) {
-            uint8_t* to = block(M.x[which ^ 1], M.rb);
-            store_pieces(to, to + xs, at, v, true);
-        } else if (row < M.rows && col < M.cols) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= 1.f / SCALE;
-            if (C.fmt_out == SSGD_FMT_F32) finish<float>(C, M, row, col, v);
-            else if (C.fmt_out == SSGD_FMT_F16) finish<__half>(C, M, row, col, v);
-            else finish<__nv_bfloat16>(C, M, row, col, v);
+    }
+    if constexpr (SYMMETRIC) {
+        if (row0 / BLOCK > col0 / BLOCK) {
+            const Quarter mirror = quarter<KIND>(C, M, first, col0, row0);
+            put_transposed(mirror, scratch, lane, hi, 0);
+            if (SPLIT) put_transposed(mirror, scratch, lane, lo, second);
         }
     }
 }
 
-template <Kind KIND>
-__global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Common C, int which, int tiles) {
+template <Kind KIND, int COLS, bool SPLIT>
+__global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap map, int which, int tiles) {
+    constexpr int BYTES = STAGE<COLS, SPLIT>, N = STAGES<COLS, SPLIT>, B_BLOCKS = COLS / 128;
+    constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
     extern __shared__ uint8_t raw[];
-    uint8_t* stage = raw + ((1024u - (shared_addr(raw) & 1023u)) & 1023u);
-    Shared& S = *reinterpret_cast<Shared*>(stage + STAGES * STAGE_BYTES);
+    uint8_t* ring = raw + ((1024u - (shared_addr(raw) & 1023u)) & 1023u);
+    uint8_t* scratches = ring + RING;
+    Shared& S = *reinterpret_cast<Shared*>(scratches + RESULT_WARPS * SCRATCH);
     volatile int* gave_up = &S.gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = pair_rank();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < STAGES; ++i) { bar_init(&S.full[i], 1); bar_init(&S.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(&S.done[i], 1); bar_init(&S.taken[i], EPILOGUE_WARPS); }
+        // the first CTA's barriers count for both: what has been copied, and which results have been taken
+        for (int i = 0; i < N; ++i) { bar_init(&S.full[i], 1); bar_init(&S.empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(&S.done[i], 1); bar_init(&S.taken[i], 2 * RESULT_WARPS); }
         bar_init_fence();
         S.gave_up = 0;
     }
-    if (warp == EPILOGUE_WARPS) tmem_alloc(&S.tmem, 2 * TILE);
-    successor_may_start();
-    successor_wait();
-    for (int i = threadIdx.x; i < C.count; i += THREADS)
-        S.first[i] = KIND == GRAM || KIND == POLYNOMIAL ? C.at.matrices[i].sym0 : C.at.matrices[i].full0;
+    if (warp == RESULT_WARPS) tmem_alloc<true>(&S.tmem, 2 * COLS);
+    // The descriptors are there before the predecessor is done: every launch lets the next one start only after it has seen its own
+    // predecessor's end, so that the one before that is over.
+    for (int i = threadIdx.x; i < C.count; i += THREADS) S.first[i] = SYMMETRIC ? C.at.matrices[i].sym0 : C.at.matrices[i].full0;
     fence_before();
     __syncthreads();
+    pair_sync();
     fence_after();
     const uint32_t tmem = S.tmem;
-    const int passes = C.split ? 3 : 1;
     auto find = [&](int tile) { return matrix_of(C.count, tile, [&](int i) { return S.first[i]; }); };
+    const int tile0 = blockIdx.x / 2, stride = gridDim.x / 2;
 
-    if (warp == EPILOGUE_WARPS && lane == 0) {                  // copies
-        asm volatile("fence.proxy.async.global;" ::: "memory");
+    if (warp == RESULT_WARPS && lane == 0) {                    // copies
         int s = 0, issued = 0;
         uint32_t parity = 1;
         bool ok = true;
-        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-            const int which_matrix = find(tile), local = tile - S.first[which_matrix];
-            const Product P = product_of<KIND>(C, C.at.matrices[which_matrix], which);
-            const int bm = local % P.tiles_m * 2, bn = local / P.tiles_m * 2;
-            for (int pass = 0; pass < passes && ok; ++pass) {
-                for (int k = 0; k < P.steps; ++k) {
-                    if (!(ok = bar_wait(&S.empty[s], parity, gave_up))) break;
-                    bar_expect(&S.full[s], STAGE_BYTES);
-                    uint8_t* to = stage + s * STAGE_BYTES;
-                    for (int i = 0; i < 2; ++i) bulk_load(to + i * BLOCK_BYTES, P.A.block(pass == 2, bm + i, k), BLOCK_BYTES, &S.full[s]);
-                    for (int i = 0; i < 2; ++i) bulk_load(to + (2 + i) * BLOCK_BYTES, P.B.block(pass == 1, bn + i, k), BLOCK_BYTES, &S.full[s]);
-                    ++issued;
-                    if (++s == STAGES) { s = 0; parity ^= 1; }
+        for (int tile = tile0; tile < tiles && ok; tile += stride) {
+            const int m = find(tile);
+            const Matrix M = C.at.matrices[m];
+            const Product P = product_of<KIND>(M, which);
+            const Tile T = tile_of<KIND, COLS>(M, tile - S.first[m]);
+            const int bm = T.row + (int)rank * 2, bn = T.col + (int)rank * B_BLOCKS;
+            int32_t from[4] = {P.A.at(bm), P.A.at(bm + 1), P.B.at(bn), B_BLOCKS == 2 ? P.B.at(bn + 1) : 0};
+            const int32_t step[2] = {P.A.step(), P.B.step()}, second[2] = {(int32_t)P.A.second, (int32_t)P.B.second};
+            if (tile == tile0) {
+                successor_wait();
+                asm volatile("fence.proxy.async.global;" ::: "memory");
+            }
+            for (int k = 0; k < P.steps; ++k) {
+                if (!(ok = bar_wait(&S.empty[s], parity, gave_up))) break;
+                if (rank == 0) bar_expect(&S.full[s], 2 * BYTES);
+                uint8_t* to = ring + s * BYTES;
+#pragma unroll
+                for (int i = 0; i < 2 + B_BLOCKS; ++i) {
+                    block_load(to + i * BLOCK_BYTES, &map, from[i], &S.full[s]);
+                    if (SPLIT) block_load(to + (2 + B_BLOCKS + i) * BLOCK_BYTES, &map, from[i] + second[i / 2], &S.full[s]);
+                    from[i] += step[i / 2];
                 }
+                ++issued;
+                if (++s == N) { s = 0; parity ^= 1; }
             }
         }
-        // no copy may land in a CTA that is gone
-        if (!ok)
-            for (int i = 0; i < min(issued, STAGES); ++i) {
+        // no copy may land in a CTA that is gone, nor count there: the first CTA waits for both's, and the second leaves with it
+        if (!ok && rank == 0)
+            for (int i = 0; i < min(issued, N); ++i) {
                 const int last = issued - 1 - i;
                 const uint64_t t0 = now_ns();
-                while (!bar_try(&S.full[last % STAGES], (uint32_t)(last / STAGES) & 1u) && now_ns() - t0 < WAIT_NS) {}
+                while (!bar_try(&S.full[last % N], (uint32_t)(last / N) & 1u) && now_ns() - t0 < WAIT_NS) {}
             }
-    } else if (warp == EPILOGUE_WARPS + 1 && lane == 0) {       // products
+    } else if (warp == RESULT_WARPS + 1 && lane == 0 && rank == 0) {         // products, of both CTAs
         int s = 0, buffer = 0;
         uint32_t parity = 0, parity_taken = 1;
         bool ok = true;
-        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-            const Product P = product_of<KIND>(C, C.at.matrices[find(tile)], which);
-            const uint32_t instr = instruction(TILE, TILE, P.A.mn_major, P.B.mn_major);
+        for (int tile = tile0; tile < tiles && ok; tile += stride) {
+            const Matrix M = C.at.matrices[find(tile)];
+            const Product P = product_of<KIND>(M, which);
+            const uint32_t instr = instruction(TILE_ROWS, COLS, P.A.mn_major, P.B.mn_major);
             const uint64_t step_a = operand_step(P.A.mn_major), step_b = operand_step(P.B.mn_major);
-            const uint32_t d = tmem + buffer * TILE;
-            if (!(ok = bar_wait(&S.taken[buffer], parity_taken, gave_up))) break;
-            fence_after();
-            const int total = passes * P.steps;
-            for (int k = 0; k < total; ++k) {
+            for (int k = 0; k < P.steps && ok; ++k) {
+                const bool begin = SPLIT ? k % CHUNK == 0 : k == 0;
+                if (begin) {
+                    if (!(ok = bar_wait(&S.taken[buffer], parity_taken, gave_up))) break;
+                    fence_after();
+                }
                 if (!(ok = bar_wait(&S.full[s], parity, gave_up))) break;
                 fence_after();
-                const uint32_t at = shared_addr(stage + s * STAGE_BYTES);
+                const uint32_t at = shared_addr(ring + s * BYTES), d = tmem + buffer * COLS;
                 const uint64_t a = operand(at, P.A.mn_major), b = operand(at + 2 * BLOCK_BYTES, P.B.mn_major);
+                constexpr uint64_t LOW = (2 + B_BLOCKS) * BLOCK_BYTES / 16;
+                if (SPLIT) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mma(d, a + i * step_a, b + i * step_b, instr, k > 0 || i > 0);
-                commit(&S.empty[s]);
-                if (++s == STAGES) { s = 0; parity ^= 1; }
+                    for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a, b + i * step_b + LOW, instr, !begin || i > 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a + LOW, b + i * step_b, instr, true);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a, b + i * step_b, instr, SPLIT || !begin || i > 0);
+                commit<true>(&S.empty[s]);
+                if (k + 1 == P.steps || (SPLIT && k % CHUNK == CHUNK - 1)) {
+                    commit<true>(&S.done[buffer]);
+                    if (buffer) parity_taken ^= 1;
+                    buffer ^= 1;
+                }
+                if (++s == N) { s = 0; parity ^= 1; }
             }
-            commit(&S.done[buffer]);
-            if (buffer) parity_taken ^= 1;
-            buffer ^= 1;
         }
-    } else if (warp < EPILOGUE_WARPS) {                         // results
+    } else if (warp < RESULT_WARPS) {                           // results
+        constexpr int MINE = COLS / 2 / 32;                     // pieces of 32 columns of a warp
+        uint8_t* scratch = scratches + warp * SCRATCH;
         int buffer = 0;
         uint32_t parity = 0;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-            const int which_matrix = find(tile), local = tile - S.first[which_matrix];
-            const Matrix& M = C.at.matrices[which_matrix];
-            const int tiles_m = KIND == GRAM || KIND == POLYNOMIAL ? (M.mb + 1) / 2 : (M.rb + 1) / 2;
-            const int row = local % tiles_m * TILE + warp * 32 + lane, col0 = local / tiles_m * TILE;
-            const int R = KIND == GRAM || KIND == POLYNOMIAL ? M.mb : M.rb, K = KIND == GRAM || KIND == POLYNOMIAL ? M.mb : M.cb;
-            float factor = 0.f;
-            const bool stored = row < R * BLOCK;
-            if (stored && KIND == POLYNOMIAL) factor = C.at.vec[M.vec + row];
-            if (stored && (KIND == APPLY || KIND == FINISH) && !M.tall()) factor = C.at.vec[M.vec + M.mb * BLOCK + row];
-            if (!bar_wait(&S.done[buffer], parity, gave_up)) break;
-            __syncwarp();
-            fence_after();
-#pragma unroll 1
-            for (int half = 0; half < TILE / 32; ++half) {
-                const int col = col0 + half * 32;
-                uint32_t acc[32];
-                tmem_load32(tmem + buffer * TILE + half * 32 + ((uint32_t)warp << 21), acc);
-                tmem_wait();
-                if (stored && col < K * BLOCK) {
+        bool ok = true;
+        for (int tile = tile0; tile < tiles; tile += stride) {
+            const int m = find(tile);
+            const Matrix M = C.at.matrices[m];
+            const Tile T = tile_of<KIND, COLS>(M, tile - S.first[m]);
+            const int row0 = T.row * BLOCK + (int)rank * 128 + warp % 4 * 32, col0 = T.col * BLOCK + warp / 4 * (COLS / 2);
+            const int R = SYMMETRIC ? M.mb : M.rb, K = SYMMETRIC ? M.mb : M.cb;
+            // of a symmetric product, what lies above the diagonal comes from below it
+            auto wanted = [&](int i) {
+                const int col = col0 + i * 32;
+                return row0 < R * BLOCK && col < K * BLOCK && (!SYMMETRIC || row0 / BLOCK >= col / BLOCK);
+            };
+            const uint32_t at = tmem + ((uint32_t)(warp % 4) << 21) + warp / 4 * (COLS / 2);
+            auto next = [&] {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_first(&S.taken[buffer]);
+                if (buffer) parity ^= 1;
+                buffer ^= 1;
+            };
+            if (tile == tile0) {
+                successor_wait();
+                successor_may_start();
+            }
+            Source<KIND, SPLIT> source;
+            if (!SPLIT && wanted(0)) fetch(C, M, which, row0, col0, lane, source);
+            if constexpr (SPLIT) {
+                float sum[MINE][32];
+                const int steps = product_of<KIND>(M, which).steps;
+                for (int k = 0; k < steps; k += CHUNK) {
+                    if (!(ok = bar_wait(&S.done[buffer], parity, gave_up))) break;
+                    __syncwarp();
+                    fence_after();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float v[8];
+                    for (int i = 0; i < MINE; ++i) {
+                        uint32_t acc[32];
+                        tmem_load32(at + buffer * COLS + i * 32, acc);
+                        tmem_wait();
+                        if (k == 0) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(acc[i * 8 + j]);
-                        eight<KIND>(C, M, which, row, col + i * 8, v, factor);
+                            for (int j = 0; j < 32; ++j) sum[i][j] = __uint_as_float(acc[j]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[i][j] += __uint_as_float(acc[j]);
+                        }
                     }
+                    next();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < MINE; ++i) {
+                    if (!wanted(i)) continue;
+                    fetch(C, M, which, row0, col0 + i * 32, lane, source);
+                    take<KIND, SPLIT>(C, M, which, row0, col0 + i * 32, sum[i], source, scratch, lane);
+                }
+            } else {
+                if (!bar_wait(&S.done[buffer], parity, gave_up)) break;
+                __syncwarp();
+                fence_after();
+#pragma unroll 1
+                for (int i = 0; i < MINE; ++i) {
+                    uint32_t acc[32];
+                    tmem_load32(at + buffer * COLS + i * 32, acc);
+                    tmem_wait();
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]);
+                    if (i + 1 == MINE) next();
+                    if (wanted(i)) take<KIND, SPLIT>(C, M, which, row0, col0 + i * 32, v, source, scratch, lane);
+                    if (i + 1 < MINE && wanted(i + 1)) fetch(C, M, which, row0, col0 + (i + 1) * 32, lane, source);
                 }
             }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(&S.taken[buffer]);
-            if (buffer) parity ^= 1;
-            buffer ^= 1;
         }
     }
     __syncwarp();
@@ -470,15 +683,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     asm volatile("fence.proxy.async.global;" ::: "memory");
     fence_before();
     __syncthreads();
-    fence_after();
     if (threadIdx.x == 0 && S.gave_up) atomicExch(&g_error, 1);
-    if (warp == EPILOGUE_WARPS) tmem_free(tmem, 2 * TILE);
+    pair_sync();                                    // neither leaves while the other's products read its shared memory
+    fence_after();
+    if (warp == RESULT_WARPS) tmem_free<true>(tmem, 2 * COLS);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
 
 struct Sizes {
-    int64_t blocks = 0, floats = 0, strips = 0, sym = 0, full = 0, elements = 0;
+    int64_t blocks = 0, floats = 0, strips = 0, elements = 0;
+    int64_t sym[2] = {0, 0}, full[2] = {0, 0};      // tiles of 128 and of 256 columns
     int count = 0;
     int64_t sums_at() const { return (int64_t)sizeof(Matrix) * MAX_GROUP; }
     int64_t vec_at() const { return (sums_at() + strips * 8 + 127) / 128 * 128; }
@@ -497,16 +712,15 @@ bool add(Sizes& s, const ssgd_matrix& t, bool split, Matrix* to) {
     M.rb = (int32_t)div_up(t.rows, BLOCK); M.cb = (int32_t)div_up(t.cols, BLOCK);
     M.mb = M.rb < M.cb ? M.rb : M.cb;
     const int64_t xs = (int64_t)M.rb * M.cb, ms = (int64_t)M.mb * M.mb;
-    M.x[0] = (uint32_t)s.blocks; M.x[1] = (uint32_t)(s.blocks + 2 * xs);
+    M.x0 = (uint32_t)s.blocks; M.x1 = (uint32_t)(s.blocks + 2 * xs);
     M.a = (uint32_t)(s.blocks + 4 * xs); M.b = (uint32_t)(s.blocks + 4 * xs + (split ? 2 : 1) * ms);
     s.blocks += 4 * xs + (split ? 4 : 2) * ms;
     M.vec = (uint32_t)s.floats;
     s.floats += 2 * (int64_t)M.mb * BLOCK;
     M.strip0 = (int32_t)s.strips; M.strips = (int32_t)(M.rb * div_up(M.cb, STRIP_BLOCKS));
-    M.sym0 = (int32_t)s.sym; M.full0 = (int32_t)s.full;
     s.strips += M.strips;
-    s.sym += div_up(M.mb, 2) * div_up(M.mb, 2);
-    s.full += div_up(M.rb, 2) * div_up(M.cb, 2);
+    s.sym[0] += symmetric_tiles<128>(M.mb); s.sym[1] += symmetric_tiles<256>(M.mb);
+    s.full[0] += all_tiles<128>(M.rb, M.cb); s.full[1] += all_tiles<256>(M.rb, M.cb);
     s.elements += elements;
     s.count++;
     if (to) {
@@ -532,12 +746,28 @@ int launch(cudaStream_t st, void (*kernel)(P...), int grid, int block, int smem,
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
 }
 
-template <Kind KIND>
-int launch_product(cudaStream_t st, const Common& C, int which, int64_t tiles, int sms) {
+template <typename T>
+int launch_prepare(cudaStream_t st, int strips, const Group& G, const Common& C) {
+    if (int e = launch(st, k_momentum<T>, strips, PREPARE_THREADS, 0, G, C)) return e;
+    return launch(st, k_layout<T>, strips, PREPARE_THREADS, 0, C);
+}
+
+template <Kind KIND, int COLS, bool SPLIT>
+int launch_tiles(cudaStream_t st, const Common& C, const CUtensorMap& map, int which, int64_t tiles, int sms) {
     static PerDevice known;
     int fits = 0;
-    if (int e = residency(k_product<KIND>, THREADS, SHARED_BYTES, known, &fits)) return e;
-    return launch(st, k_product<KIND>, (int)(tiles < sms ? tiles : sms), THREADS, SHARED_BYTES, C, which, (int)tiles);
+    if (int e = residency(k_product<KIND, COLS, SPLIT>, THREADS, SHARED_BYTES, known, &fits)) return e;
+    return launch(st, k_product<KIND, COLS, SPLIT>, (int)(2 * (tiles < sms / 2 ? tiles : sms / 2)), THREADS, SHARED_BYTES, C, map, which, (int)tiles);
+}
+template <Kind KIND>
+int launch_product(cudaStream_t st, const Common& C, const CUtensorMap& map, bool wide, int which, int64_t tiles, int sms) {
+    if (C.split) return wide ? launch_tiles<KIND, 256, true>(st, C, map, which, tiles, sms) : launch_tiles<KIND, 128, true>(st, C, map, which, tiles, sms);
+    return wide ? launch_tiles<KIND, 256, false>(st, C, map, which, tiles, sms) : launch_tiles<KIND, 128, false>(st, C, map, which, tiles, sms);
+}
+
+// Whether tiles of 256 columns take less time than those of 128, which take half as long at least
+bool wide_tiles(const int64_t (&tiles)[2], int sms) {
+    return div_up(tiles[1], sms / 2) * 2 <= div_up(tiles[0], sms / 2);
 }
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 20;
@@ -618,13 +848,25 @@ int run(const ssgd_matrix* t, int32_t count, Common C, int32_t steps, double lr,
         C.at = Space{reinterpret_cast<Matrix*>(base), reinterpret_cast<double*>(base + s.sums_at()),
                      reinterpret_cast<float*>(base + s.vec_at()), base + s.blocks_at()};
         C.count = s.count;
-        C.strips = (int32_t)s.strips;
-        if ((e = launch(st, k_momentum, (int)s.strips, PREPARE_THREADS, 0, G, C))) return e;
-        if ((e = launch(st, k_layout, (int)s.strips, PREPARE_THREADS, 0, C))) return e;
+        CUtensorMap map;
+        if (!blocks_map(&map, C.at.blocks, s.blocks)) return SSGD_ECUDA;
+        const bool wide_sym = wide_tiles(s.sym, sms), wide_full = wide_tiles(s.full, sms);
+        int32_t sym = 0, full = 0;
+        for (int k = 0; k < s.count; ++k) {
+            Matrix& M = G.m[k];
+            M.sym0 = sym;
+            M.full0 = full;
+            sym += (int32_t)(wide_sym ? symmetric_tiles<256>(M.mb) : symmetric_tiles<128>(M.mb));
+            full += (int32_t)(wide_full ? all_tiles<256>(M.rb, M.cb) : all_tiles<128>(M.rb, M.cb));
+        }
+        if ((e = C.fmt_in == SSGD_FMT_F32 ? launch_prepare<float>(st, (int)s.strips, G, C)
+               : C.fmt_in == SSGD_FMT_F16 ? launch_prepare<__half>(st, (int)s.strips, G, C) : launch_prepare<__nv_bfloat16>(st, (int)s.strips, G, C)))
+            return e;
         for (int k = 0; k < steps; ++k) {
-            if ((e = launch_product<GRAM>(st, C, k & 1, s.sym, sms))) return e;
-            if ((e = launch_product<POLYNOMIAL>(st, C, k & 1, s.sym, sms))) return e;
-            if ((e = k + 1 < steps ? launch_product<APPLY>(st, C, k & 1, s.full, sms) : launch_product<FINISH>(st, C, k & 1, s.full, sms))) return e;
+            if ((e = launch_product<GRAM>(st, C, map, wide_sym, k & 1, sym, sms))) return e;
+            if ((e = launch_product<POLYNOMIAL>(st, C, map, wide_sym, k & 1, sym, sms))) return e;
+            if ((e = k + 1 < steps ? launch_product<APPLY>(st, C, map, wide_full, k & 1, full, sms)
+                                   : launch_product<FINISH>(st, C, map, wide_full, k & 1, full, sms))) return e;
         }
     }
     return SSGD_OK;

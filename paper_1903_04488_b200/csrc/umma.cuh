@@ -7,6 +7,7 @@
 // a tensor map moves them, and one block serves as an operand in both directions: its columns along the contraction (K-major) or
 // its rows (MN-major).
 #pragma once
+#include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
@@ -44,6 +45,20 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
         : "=r"(ok) : "r"(shared_addr(bar)), "r"(parity) : "memory");
     return ok != 0;
 }
+// Arrives at the barrier in the same place of the pair's first CTA
+__device__ __forceinline__ void bar_arrive_first(uint64_t* bar) {
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(shared_addr(bar)));
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+}
+__device__ __forceinline__ void pair_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t pair_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
 __device__ __forceinline__ uint64_t now_ns() {
     uint64_t t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
@@ -67,21 +82,33 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, volatil
 
 // ---- copies ------------------------------------------------------------------------------------------
 
-// bytes: a multiple of 16; both addresses 16-byte aligned
-__device__ __forceinline__ void bulk_load(void* shared, const void* global, uint32_t bytes, uint64_t* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_addr(shared)),
-                 "l"(global), "r"(bytes), "r"(shared_addr(bar)) : "memory");
+// A block into the CTA's own shared memory; what has arrived is counted at the barrier in this place of the pair's first CTA.  The
+// tensor map (blocks_map) reads the blocks' memory as rows of 128 bytes, as they are: it is there because a copy without one cannot
+// count at another CTA's barrier.  Forwarding by a thread of the second CTA took 1000 cycles per stage, twice the products' time.
+__device__ __forceinline__ void block_load(void* shared, const CUtensorMap* map, int32_t block, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .b32 first;\n\tmapa.shared::cluster.u32 first, %4, 0;\n\t"
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [first];\n\t}"
+        ::"r"(shared_addr(shared)), "l"(map), "r"(0), "r"(block * BLOCK), "r"(shared_addr(bar)) : "memory");
 }
 
 // ---- tensor memory -----------------------------------------------------------------------------------
 
-// One warp; columns: a power of two of at least 32.  The address goes to shared memory.
+// PAIR: for products of two CTAs, where one warp of each calls.  columns: a power of two of at least 32.  The address goes to shared memory.
+template <bool PAIR>
 __device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t columns) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_addr(where)), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_addr(where)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_addr(where)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
 }
+template <bool PAIR>
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -115,15 +142,47 @@ __device__ __forceinline__ uint64_t operand_step(bool mn_major) { return mn_majo
 __device__ __forceinline__ uint32_t instruction(int m, int n, bool a_mn, bool b_mn) {
     return 1u << 4 | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
+// One thread; PAIR: of the first CTA, for both: each holds half of the rows of A and of the result, and half of the columns of B.
+template <bool PAIR>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"(accumulate ? 1u : 0u) : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"(accumulate ? 1u : 0u) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"(accumulate ? 1u : 0u) : "memory");
 }
-// The barrier is arrived at when everything this thread has issued is done.
+// The barrier (PAIR: of both CTAs) is arrived at when everything this thread has issued is done.
+template <bool PAIR>
 __device__ __forceinline__ void commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_addr(bar)) : "memory");
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_addr(bar)),
+                     "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_addr(bar)) : "memory");
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+
+// Map of `blocks` blocks from `base` on
+inline bool blocks_map(CUtensorMap* map, void* base, int64_t blocks) {
+    using Encode = decltype(&cuTensorMapEncodeTiled);
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<Encode>(f);
+    }();
+    const cuuint64_t dims[2] = {BLOCK, (cuuint64_t)blocks * BLOCK}, strides[1] = {BLOCK * 2};
+    const cuuint32_t box[2] = {BLOCK, BLOCK}, each[2] = {1, 1};
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace umma
