@@ -20,6 +20,8 @@
 // Layout.  All matrices of a call go through every launch together: prepare (momentum and sums of squares; division and layout),
 // then 3 launches per step, whose tiles are dealt out over the SMs.  Matrices live in the workspace as blocks (umma.cuh), padded with
 // zeros to 64; block (r, c) of a matrix of R x C blocks is the (c R + r)-th.
+#include <algorithm>
+
 #include "formats.cuh"
 #include "umma.cuh"
 
@@ -33,13 +35,15 @@ constexpr int MAX_GROUP = 224;                      // matrices of one set of la
 constexpr int64_t GROUP_ELEMENTS = (int64_t)1 << 27;  // and no more than this many elements, unless one matrix has them
 constexpr int STRIP_BLOCKS = 4;                     // what a CTA of the preparation takes: 64 rows of 256 columns
 
+enum Kind { GRAM, POLYNOMIAL, APPLY, FINISH };      // A, B, x of the next step, the result
+
 struct Matrix {
     void* out; const void* in; float* m;
     int64_t ld_out, ld_in;
     int32_t rows, cols, rb, cb, mb;                 // size; size in blocks; blocks of the shorter side
     uint32_t x0, x1, a, b;                          // first blocks: x at even and at odd steps, A, B.  Second numbers lie behind the first
     uint32_t vec;                                   // d and e, mb * 64 floats each
-    int32_t strip0, strips, sym0, full0;            // first strip, first tile of A and B, first tile of x among all
+    int32_t strip0, strips, first[4];               // first strip and first tile of each product among those of all matrices
     float update;                                   // lr * scale
     __host__ __device__ uint32_t x(int which) const { return which ? x1 : x0; }
     __host__ __device__ bool tall() const { return rb > cb || (rb == cb && rows > cols); }
@@ -69,9 +73,12 @@ __device__ int g_error;                             // set by a wait that ran ou
 
 // ---- preparation -------------------------------------------------------------------------------------
 
-// Whether four neighbours may be read at once, where rows begin at multiples of four
+// Whether four neighbours from a multiple of four on may be read and written at once
 template <typename T>
-__device__ __forceinline__ bool aligned_four(const void* p) { return (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0; }
+__device__ __forceinline__ bool may_load_four(const Matrix& M) {
+    return M.ld_in % 4 == 0 && (reinterpret_cast<uintptr_t>(M.in) & (4 * sizeof(T) - 1)) == 0 &&
+           (!M.m || (M.cols % 4 == 0 && (reinterpret_cast<uintptr_t>(M.m) & 15u) == 0));
+}
 
 // The matrix of a strip or tile: the last whose first is not beyond it
 template <typename F>
@@ -98,35 +105,41 @@ __device__ __forceinline__ double block_sum(double v, double* shared) {
     return s;
 }
 
-// Four neighbours of a row (fewer at its end, zeros in their place)
-template <typename T>
-__device__ __forceinline__ void load_four(const T* p, int n, bool vector, float (&v)[4]) {
-    if (vector && n >= 4) {
-        const Vec<T, 4> x = load_vec<T, 4>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = to_f32(x.e[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = e < n ? to_f32(p[e]) : 0.f;
-    }
-}
-// A block of the preparation: thread t has columns 4 (t mod 16) .. of rows t / 16 + 16 i
+// A block of the preparation: thread t has columns 4 (t mod 16) .. of rows t / 16 + 16 i.  What is not there is zero.
 constexpr int SHARE = 4;
+template <typename T> struct Share {
+    Vec<T, 4> g[SHARE];
+    Vec<float, 4> m[SHARE];
+};
 template <typename T>
-__device__ __forceinline__ void load_block(const Matrix& M, int r0, int c0, bool vector_in, bool vector_m, float (&g)[SHARE][4], float (&m)[SHARE][4]) {
-    const int c = c0 + (int)threadIdx.x % 16 * 4;
+__device__ __forceinline__ void load_block(const Matrix& M, int r0, int c0, bool vector, Share<T>& s) {
+    const int c = c0 + (int)threadIdx.x % 16 * 4, r = r0 + (int)threadIdx.x / 16;
+    const T* in = static_cast<const T*>(M.in) + (int64_t)r * M.ld_in + c;
+    const float* m = M.m + (int64_t)r * M.cols + c;
+    if (vector && r0 + BLOCK <= M.rows && c0 + BLOCK <= M.cols) {      // the same for the whole CTA: all loads on their way at once
+#pragma unroll
+        for (int i = 0; i < SHARE; ++i) s.g[i] = load_vec<T, 4>(in + (int64_t)(16 * i) * M.ld_in);
+        if (M.m) {
+#pragma unroll
+            for (int i = 0; i < SHARE; ++i) s.m[i] = load_vec<float, 4>(m + (int64_t)(16 * i) * M.cols);
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < SHARE; ++i) {
-        const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
-        load_four<T>(static_cast<const T*>(M.in) + (int64_t)r * M.ld_in + c, n, vector_in, g[i]);
-        if (M.m) load_four<float>(M.m + (int64_t)r * M.cols + c, n, vector_m, m[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool there = r + 16 * i < M.rows && c + e < M.cols;
+            s.g[i].e[e] = there ? in[(int64_t)(16 * i) * M.ld_in + e] : from_f32<T>(0.f);
+            s.m[i].e[e] = there && M.m ? m[(int64_t)(16 * i) * M.cols + e] : 0.f;
+        }
     }
 }
 
 // m <- momentum m + (1 - momentum) g, and the sum of squares of what is to be made orthogonal, per strip.  Squares are added in 64
 // bits: they may leave the range of 32.
 template <typename T>
-__global__ void __launch_bounds__(PREPARE_THREADS) k_momentum(const __grid_constant__ Group G, const __grid_constant__ Common C) {
+__global__ void __launch_bounds__(PREPARE_THREADS, 4) k_momentum(const __grid_constant__ Group G, const __grid_constant__ Common C) {
     __shared__ double shared[PREPARE_THREADS / 32];
     successor_wait();
     successor_may_start();
@@ -138,34 +151,36 @@ __global__ void __launch_bounds__(PREPARE_THREADS) k_momentum(const __grid_const
     const int strip = blockIdx.x;
     const Matrix& M = G.m[matrix_of(C.count, strip, [&](int i) { return G.m[i].strip0; })];
     const int local = strip - M.strip0, r0 = local % M.rb * BLOCK, cblock0 = local / M.rb * STRIP_BLOCKS;
-    const bool vector_in = M.ld_in % 4 == 0 && aligned_four<T>(M.in), vector_m = M.cols % 4 == 0 && aligned_four<float>(M.m);
+    const bool vector = may_load_four<T>(M);
     const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
     double sum = 0.0;
     for (int cblock = cblock0; cblock < min(cblock0 + STRIP_BLOCKS, M.cb); ++cblock) {
-        float g[SHARE][4], m[SHARE][4];
-        load_block<T>(M, r0, cblock * BLOCK, vector_in, vector_m, g, m);
+        Share<T> s;
+        load_block<T>(M, r0, cblock * BLOCK, vector, s);
         const int c = cblock * BLOCK + (int)threadIdx.x % 16 * 4;
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
-            if (n <= 0) continue;
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = to_f32(s.g[i].e[e]);
             if (M.m) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float in = g[i][e] * scale;
-                    m[i][e] = fmaf(mu, m[i][e], (1.f - mu) * in);
-                    g[i][e] = C.nesterov ? fmaf(mu, m[i][e], (1.f - mu) * in) : m[i][e];
+                    const float in = u[e] * scale;
+                    s.m[i].e[e] = fmaf(mu, s.m[i].e[e], (1.f - mu) * in);
+                    u[e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * in) : s.m[i].e[e];
                 }
                 float* to = M.m + (int64_t)r * M.cols + c;
-                if (vector_m && n >= 4) store_vec<float, 4>(to, Vec<float, 4>{{m[i][0], m[i][1], m[i][2], m[i][3]}});
+                if (vector && n >= 4) store_vec<float, 4>(to, s.m[i]);
                 else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (e < n) to[e] = m[i][e];
+                        if (e < n) to[e] = s.m[i].e[e];
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += e < n ? (double)g[i][e] * (double)g[i][e] : 0.0;
+            for (int e = 0; e < 4; ++e) sum += e < n ? (double)u[e] * (double)u[e] : 0.0;
         }
     }
     sum = block_sum(sum, shared);
@@ -184,12 +199,17 @@ __device__ __forceinline__ float2 halves(uint32_t v) { return __half22float2(*re
 
 // x = u / (|u| + eps) as blocks
 template <typename T>
-__global__ void __launch_bounds__(PREPARE_THREADS) k_layout(const __grid_constant__ Common C) {
+__global__ void __launch_bounds__(PREPARE_THREADS, 4) k_layout(const __grid_constant__ Common C) {
     __shared__ double shared[PREPARE_THREADS / 32];
     successor_wait();
     successor_may_start();
     const int strip = blockIdx.x;
     const Matrix M = C.at.matrices[matrix_of(C.count, strip, [&](int i) { return C.at.matrices[i].strip0; })];
+    const int local = strip - M.strip0, rblock = local % M.rb, cblock0 = local / M.rb * STRIP_BLOCKS, cblock1 = min(cblock0 + STRIP_BLOCKS, M.cb);
+    const bool vector = may_load_four<T>(M);
+    // what is read need not wait for the sum, nor the next block for this one
+    Share<T> s;
+    load_block<T>(M, rblock * BLOCK, cblock0 * BLOCK, vector, s);
     double sum = 0.0;
     for (int i = threadIdx.x; i < M.strips; i += PREPARE_THREADS) sum += C.at.sums[M.strip0 + i];
     sum = block_sum(sum, shared);
@@ -198,32 +218,29 @@ __global__ void __launch_bounds__(PREPARE_THREADS) k_layout(const __grid_constan
     int exponent = 0;
     const float factor = (float)(inv > 0.0 && inv < (double)INFINITY ? frexp(inv, &exponent) : inv) * SCALE;
     const float power = ldexpf(1.f, min(max(exponent, -126), 127));
-    const int local = strip - M.strip0, rblock = local % M.rb, cblock0 = local / M.rb * STRIP_BLOCKS;
-    const bool vector_in = M.ld_in % 4 == 0 && aligned_four<T>(M.in), vector_m = M.cols % 4 == 0 && aligned_four<float>(M.m);
     const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
     const int64_t second = (int64_t)M.rb * M.cb * BLOCK_BYTES;
-    for (int cblock = cblock0; cblock < min(cblock0 + STRIP_BLOCKS, M.cb); ++cblock) {
+    for (int cblock = cblock0; cblock < cblock1; ++cblock) {
         uint8_t* block = C.at.blocks + (int64_t)(M.x0 + (uint32_t)cblock * M.rb + rblock) * BLOCK_BYTES;
-        float g[SHARE][4], m[SHARE][4];
-        load_block<T>(M, rblock * BLOCK, cblock * BLOCK, vector_in, vector_m, g, m);
+        float u[SHARE][4];
+#pragma unroll
+        for (int i = 0; i < SHARE; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u[i][e] = to_f32(s.g[i].e[e]);
+                if (M.m) u[i][e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * (u[i][e] * scale)) : s.m[i].e[e];
+            }
+        }
+        if (cblock + 1 < cblock1) load_block<T>(M, rblock * BLOCK, (cblock + 1) * BLOCK, vector, s);
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int rr = (int)threadIdx.x / 16 + 16 * i, cc = (int)threadIdx.x % 16 * 4;
-            float u[4];
+            const int n = rblock * BLOCK + rr < M.rows ? M.cols - cblock * BLOCK - cc : 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u[e] = g[i][e];
-                if (M.m) u[e] = C.nesterov ? fmaf(mu, m[i][e], (1.f - mu) * (g[i][e] * scale)) : m[i][e];
-                u[e] = u[e] * power * factor;
-            }
-            if (rblock * BLOCK + rr >= M.rows)                                  // the padding, whatever the factor is
-                u[0] = u[1] = u[2] = u[3] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (cblock * BLOCK + cc + e >= M.cols) u[e] = 0.f;
+            for (int e = 0; e < 4; ++e) u[i][e] = e < n ? u[i][e] * power * factor : 0.f;    // the padding is 0 whatever the factor is
             uint2 hi, lo;
-            split2(u[0], u[1], hi.x, lo.x);
-            split2(u[2], u[3], hi.y, lo.y);
+            split2(u[i][0], u[i][1], hi.x, lo.x);
+            split2(u[i][2], u[i][3], hi.y, lo.y);
             uint8_t* to = block + piece_at(rr, cc / 8) + cc % 8 * 2;
             *reinterpret_cast<uint2*>(to) = hi;
             *reinterpret_cast<uint2*>(to + second) = lo;
@@ -234,15 +251,13 @@ __global__ void __launch_bounds__(PREPARE_THREADS) k_layout(const __grid_constan
 
 // ---- products ----------------------------------------------------------------------------------------
 
-enum Kind { GRAM, POLYNOMIAL, APPLY, FINISH };
-
 // A tile is 256 rows and COLS columns, of a pair of CTAs that has half of the rows each.  What a tile loads per block of the contraction
 // grows with its sides, what it computes with their product: 256 x 256 needs 12 TB/s from L2 at the tensor cores' full rate, 128 x 128 by
 // single CTAs 24 TB/s.  Where the larger tiles are too few, 256 x 128.
 constexpr int TILE_ROWS = 256;
 constexpr int RING = 192 * 1024;                    // bytes of operands on their way
 constexpr int RESULT_WARPS = 8;
-constexpr int THREADS = 32 * (RESULT_WARPS + 2);
+constexpr int THREADS = 32 * (RESULT_WARPS + 4);     // one more warp copies, one issues products, two complete a group of four
 constexpr int SCRATCH = 4096;                       // of each result warp: 32 x 32 numbers change hands there
 constexpr int CHUNK = 4;                            // blocks of the contraction that are added up by the tensor cores alone (SPLIT)
 
@@ -336,6 +351,12 @@ __device__ __forceinline__ Tile tile_of(const Matrix& M, int i) {
 // and outputs are read and written.
 
 __device__ __forceinline__ uint32_t word_at(int r, int piece) { return (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4)); }
+// x, of which the compiler knows nothing
+__device__ __forceinline__ int opaque(int x) {
+    asm volatile("" : "+r"(x));
+    return x;
+}
+
 // 32 x 32 fp16 numbers; neither eight rows of a column nor rows meet in a bank
 __device__ __forceinline__ uint32_t half_at(int r, int piece) { return (uint32_t)(r * 64 + ((piece ^ (((r >> 1) ^ (r >> 3)) & 3)) << 4)); }
 
@@ -424,15 +445,15 @@ __device__ __forceinline__ void put_transposed(const Quarter& q, uint8_t* scratc
         *reinterpret_cast<uint4*>(q.at(i, lane) + offset) = *reinterpret_cast<const uint4*>(scratch + half_at(i * 8 + lane / 4, lane % 4));
 }
 
-// What 32 rows and columns of a product become.  acc: the lane's row.
-template <Kind KIND, bool SPLIT>
-__device__ __forceinline__ void take(const Common& C, const Matrix& M, int which, int row0, int col0, const float (&acc)[32],
+// What 32 rows and columns of a product become.  acc: the lane's row; T: the output's type (FINISH).
+template <Kind KIND, bool SPLIT, typename T>
+__device__ __forceinline__ void take(const Common& C, const Matrix& M, int which, int row0, int col0, const uint32_t (&acc)[32],
                                      const Source<KIND, SPLIT>& s, uint8_t* scratch, int lane) {
     constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<float4*>(scratch + word_at(lane, i)) = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
+        *reinterpret_cast<uint4*>(scratch + word_at(lane, i)) = make_uint4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
     __syncwarp();
     float* diagonal = C.at.vec + M.vec + (KIND == POLYNOMIAL ? M.mb * BLOCK : 0);
     const bool tall = M.tall();
@@ -474,9 +495,7 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, int which
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= 1.f / SCALE;
             const int row = row0 + r, col = col0 + lane % 4 * 8;
-            if (C.fmt_out == SSGD_FMT_F32) put_output<float>(C, M, row, col, v);
-            else if (C.fmt_out == SSGD_FMT_F16) put_output<__half>(C, M, row, col, v);
-            else put_output<__nv_bfloat16>(C, M, row, col, v);
+            put_output<T>(C, M, row, col, v);
         } else {
             split2(v[0], v[1], hi[i].x, lo[i].x);
             split2(v[2], v[3], hi[i].y, lo[i].y);
@@ -495,7 +514,7 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, int which
     }
 }
 
-template <Kind KIND, int COLS, bool SPLIT>
+template <Kind KIND, int COLS, bool SPLIT, typename T>
 __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap map, int which, int tiles) {
     constexpr int BYTES = STAGE<COLS, SPLIT>, N = STAGES<COLS, SPLIT>, B_BLOCKS = COLS / 128;
     constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
@@ -516,7 +535,7 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
     if (warp == RESULT_WARPS) tmem_alloc<true>(&S.tmem, 2 * COLS);
     // The descriptors are there before the predecessor is done: every launch lets the next one start only after it has seen its own
     // predecessor's end, so that the one before that is over.
-    for (int i = threadIdx.x; i < C.count; i += THREADS) S.first[i] = SYMMETRIC ? C.at.matrices[i].sym0 : C.at.matrices[i].full0;
+    for (int i = threadIdx.x; i < C.count; i += THREADS) S.first[i] = C.at.matrices[i].first[KIND];
     fence_before();
     __syncthreads();
     pair_sync();
@@ -525,16 +544,19 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
     auto find = [&](int tile) { return matrix_of(C.count, tile, [&](int i) { return S.first[i]; }); };
     const int tile0 = blockIdx.x / 2, stride = gridDim.x / 2;
 
+    // With SPLIT a result warp holds up to 128 sums to a lane: it gets registers from the group that copies (224 + 224 + 56 = 3 x 168).
+    if (warp >= RESULT_WARPS) {
+    if (SPLIT && COLS == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == RESULT_WARPS && lane == 0) {                    // copies
         int s = 0, issued = 0;
         uint32_t parity = 1;
         bool ok = true;
         for (int tile = tile0; tile < tiles && ok; tile += stride) {
             const int m = find(tile);
-            const Matrix M = C.at.matrices[m];
+            const Matrix& M = C.at.matrices[m];
             const Product P = product_of<KIND>(M, which);
-            const Tile T = tile_of<KIND, COLS>(M, tile - S.first[m]);
-            const int bm = T.row + (int)rank * 2, bn = T.col + (int)rank * B_BLOCKS;
+            const Tile at_tile = tile_of<KIND, COLS>(M, tile - S.first[m]);
+            const int bm = at_tile.row + (int)rank * 2, bn = at_tile.col + (int)rank * B_BLOCKS;
             int32_t from[4] = {P.A.at(bm), P.A.at(bm + 1), P.B.at(bn), B_BLOCKS == 2 ? P.B.at(bn + 1) : 0};
             const int32_t step[2] = {P.A.step(), P.B.step()}, second[2] = {(int32_t)P.A.second, (int32_t)P.B.second};
             if (tile == tile0) {
@@ -567,7 +589,7 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
         uint32_t parity = 0, parity_taken = 1;
         bool ok = true;
         for (int tile = tile0; tile < tiles && ok; tile += stride) {
-            const Matrix M = C.at.matrices[find(tile)];
+            const Matrix& M = C.at.matrices[find(tile)];
             const Product P = product_of<KIND>(M, which);
             const uint32_t instr = instruction(TILE_ROWS, COLS, P.A.mn_major, P.B.mn_major);
             const uint64_t step_a = operand_step(P.A.mn_major), step_b = operand_step(P.B.mn_major);
@@ -599,17 +621,17 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
                 if (++s == N) { s = 0; parity ^= 1; }
             }
         }
-    } else if (warp < RESULT_WARPS) {                           // results
+    }
+    } else {                                                    // results
+        if (SPLIT && COLS == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         constexpr int MINE = COLS / 2 / 32;                     // pieces of 32 columns of a warp
-        uint8_t* scratch = scratches + warp * SCRATCH;
         int buffer = 0;
         uint32_t parity = 0;
-        bool ok = true;
         for (int tile = tile0; tile < tiles; tile += stride) {
             const int m = find(tile);
-            const Matrix M = C.at.matrices[m];
-            const Tile T = tile_of<KIND, COLS>(M, tile - S.first[m]);
-            const int row0 = T.row * BLOCK + (int)rank * 128 + warp % 4 * 32, col0 = T.col * BLOCK + warp / 4 * (COLS / 2);
+            const Matrix& M = C.at.matrices[m];
+            const Tile at_tile = tile_of<KIND, COLS>(M, tile - S.first[m]);
+            const int row0 = at_tile.row * BLOCK + (int)rank * 128 + warp % 4 * 32, col0 = at_tile.col * BLOCK + warp / 4 * (COLS / 2);
             const int R = SYMMETRIC ? M.mb : M.rb, K = SYMMETRIC ? M.mb : M.cb;
             // of a symmetric product, what lies above the diagonal comes from below it
             auto wanted = [&](int i) {
@@ -628,53 +650,54 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
                 successor_wait();
                 successor_may_start();
             }
-            Source<KIND, SPLIT> source;
-            if (!SPLIT && wanted(0)) fetch(C, M, which, row0, col0, lane, source);
-            if constexpr (SPLIT) {
-                float sum[MINE][32];
-                const int steps = product_of<KIND>(M, which).steps;
-                for (int k = 0; k < steps; k += CHUNK) {
-                    if (!(ok = bar_wait(&S.done[buffer], parity, gave_up))) break;
-                    __syncwarp();
-                    fence_after();
-#pragma unroll
-                    for (int i = 0; i < MINE; ++i) {
-                        uint32_t acc[32];
-                        tmem_load32(at + buffer * COLS + i * 32, acc);
-                        tmem_wait();
-                        if (k == 0) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[i][j] = __uint_as_float(acc[j]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[i][j] += __uint_as_float(acc[j]);
-                        }
-                    }
-                    next();
-                }
-                if (!ok) break;
-#pragma unroll
-                for (int i = 0; i < MINE; ++i) {
-                    if (!wanted(i)) continue;
-                    fetch(C, M, which, row0, col0 + i * 32, lane, source);
-                    take<KIND, SPLIT>(C, M, which, row0, col0 + i * 32, sum[i], source, scratch, lane);
-                }
-            } else {
-                if (!bar_wait(&S.done[buffer], parity, gave_up)) break;
+            const bool some = wanted(0);                        // the first piece lies farthest to the left
+            const int steps = product_of<KIND>(M, which).steps;
+            auto done = [&] {
+                const bool ok = bar_wait(&S.done[buffer], parity, gave_up);
                 __syncwarp();
                 fence_after();
-#pragma unroll 1
-                for (int i = 0; i < MINE; ++i) {
-                    uint32_t acc[32];
-                    tmem_load32(at + buffer * COLS + i * 32, acc);
-                    tmem_wait();
-                    float v[32];
+                return ok;
+            };
+            const bool summed = SPLIT && steps > CHUNK;
+            if (summed) {
+                // the chunks' sums, in the end back in tensor memory in the place of the last
+                float sum[2 * MINE][16] = {};
+                bool ok = true;
+                for (int k = 0; k < steps; k += CHUNK) {
+                    if (!(ok = done())) break;
+                    if (some) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]);
-                    if (i + 1 == MINE) next();
-                    if (wanted(i)) take<KIND, SPLIT>(C, M, which, row0, col0 + i * 32, v, source, scratch, lane);
-                    if (i + 1 < MINE && wanted(i + 1)) fetch(C, M, which, row0, col0 + (i + 1) * 32, lane, source);
+                        for (int i = 0; i < 2 * MINE; ++i) {
+                            float acc[16];
+                            tmem_load16(at + buffer * COLS + i * 16, acc);
+                            tmem_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sum[i][j] += acc[j];
+                        }
+                    }
+                    if (k + CHUNK < steps) next();
                 }
+                if (!ok) break;
+                if (some) {
+#pragma unroll
+                    for (int i = 0; i < 2 * MINE; ++i) tmem_store16(at + buffer * COLS + i * 16, sum[i]);
+                    tmem_store_wait();
+                }
+            }
+            Source<KIND, SPLIT> source{};
+            if (some) fetch(C, M, which, row0, col0, opaque(lane), source);
+            if (!summed && !done()) break;
+#pragma unroll 1
+            for (int i = 0; i < MINE; ++i) {
+                uint32_t acc[32];
+                tmem_load32(at + buffer * COLS + i * 32, acc);
+                tmem_wait();
+                if (i + 1 == MINE) next();
+                if (!wanted(i)) continue;
+                // addresses are made here each time: kept across the tiles they would take the registers of the sums
+                const int l = opaque(lane);
+                take<KIND, SPLIT, T>(C, M, which, row0, col0 + i * 32, acc, source, scratches + opaque(warp) * SCRATCH, l);
+                if (i + 1 < MINE && wanted(i + 1)) fetch(C, M, which, row0, col0 + (i + 1) * 32, l, source);
             }
         }
     }
@@ -693,7 +716,6 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
 
 struct Sizes {
     int64_t blocks = 0, floats = 0, strips = 0, elements = 0;
-    int64_t sym[2] = {0, 0}, full[2] = {0, 0};      // tiles of 128 and of 256 columns
     int count = 0;
     int64_t sums_at() const { return (int64_t)sizeof(Matrix) * MAX_GROUP; }
     int64_t vec_at() const { return (sums_at() + strips * 8 + 127) / 128 * 128; }
@@ -717,10 +739,8 @@ bool add(Sizes& s, const ssgd_matrix& t, bool split, Matrix* to) {
     s.blocks += 4 * xs + (split ? 4 : 2) * ms;
     M.vec = (uint32_t)s.floats;
     s.floats += 2 * (int64_t)M.mb * BLOCK;
-    M.strip0 = (int32_t)s.strips; M.strips = (int32_t)(M.rb * div_up(M.cb, STRIP_BLOCKS));
+    M.strips = (int32_t)(M.rb * div_up(M.cb, STRIP_BLOCKS));
     s.strips += M.strips;
-    s.sym[0] += symmetric_tiles<128>(M.mb); s.sym[1] += symmetric_tiles<256>(M.mb);
-    s.full[0] += all_tiles<128>(M.rb, M.cb); s.full[1] += all_tiles<256>(M.rb, M.cb);
     s.elements += elements;
     s.count++;
     if (to) {
@@ -752,23 +772,35 @@ int launch_prepare(cudaStream_t st, int strips, const Group& G, const Common& C)
     return launch(st, k_layout<T>, strips, PREPARE_THREADS, 0, C);
 }
 
-template <Kind KIND, int COLS, bool SPLIT>
+template <Kind KIND, int COLS, bool SPLIT, typename T>
 int launch_tiles(cudaStream_t st, const Common& C, const CUtensorMap& map, int which, int64_t tiles, int sms) {
     static PerDevice known;
     int fits = 0;
-    if (int e = residency(k_product<KIND, COLS, SPLIT>, THREADS, SHARED_BYTES, known, &fits)) return e;
-    return launch(st, k_product<KIND, COLS, SPLIT>, (int)(2 * (tiles < sms / 2 ? tiles : sms / 2)), THREADS, SHARED_BYTES, C, map, which, (int)tiles);
+    if (int e = residency(k_product<KIND, COLS, SPLIT, T>, THREADS, SHARED_BYTES, known, &fits)) return e;
+    return launch(st, k_product<KIND, COLS, SPLIT, T>, (int)(2 * (tiles < sms / 2 ? tiles : sms / 2)), THREADS, SHARED_BYTES, C, map, which, (int)tiles);
 }
-template <Kind KIND>
+template <Kind KIND, typename T = void>
 int launch_product(cudaStream_t st, const Common& C, const CUtensorMap& map, bool wide, int which, int64_t tiles, int sms) {
-    if (C.split) return wide ? launch_tiles<KIND, 256, true>(st, C, map, which, tiles, sms) : launch_tiles<KIND, 128, true>(st, C, map, which, tiles, sms);
-    return wide ? launch_tiles<KIND, 256, false>(st, C, map, which, tiles, sms) : launch_tiles<KIND, 128, false>(st, C, map, which, tiles, sms);
+    if (C.split)
+        return wide ? launch_tiles<KIND, 256, true, T>(st, C, map, which, tiles, sms) : launch_tiles<KIND, 128, true, T>(st, C, map, which, tiles, sms);
+    return wide ? launch_tiles<KIND, 256, false, T>(st, C, map, which, tiles, sms) : launch_tiles<KIND, 128, false, T>(st, C, map, which, tiles, sms);
 }
 
-// Whether tiles of 256 columns take less time than those of 128, which take half as long at least
-bool wide_tiles(const int64_t (&tiles)[2], int sms) {
-    return div_up(tiles[1], sms / 2) * 2 <= div_up(tiles[0], sms / 2);
-}
+// Work of a launch with tiles of 128 and of 256 columns, in blocks of the contraction
+struct Work {
+    int64_t blocks[2] = {0, 0}, longest = 0;
+    void add(int64_t narrow, int64_t wide, int64_t steps) {
+        blocks[0] += narrow * steps;
+        blocks[1] += wide * steps;
+        longest = steps > longest ? steps : longest;
+    }
+    // What bounds either is what a tile loads, 3 against 4 blocks to a CTA.  A launch ends when the last tile does: about one tile later
+    // than if all pairs ended together.
+    bool prefers_wide(int sms) const {
+        const int64_t pairs = sms / 2;
+        return 4 * (blocks[1] + longest * pairs) <= 3 * (blocks[0] + longest * pairs);
+    }
+};
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 20;
 constexpr int MAX_STEPS = 32;
@@ -850,23 +882,39 @@ int run(const ssgd_matrix* t, int32_t count, Common C, int32_t steps, double lr,
         C.count = s.count;
         CUtensorMap map;
         if (!blocks_map(&map, C.at.blocks, s.blocks)) return SSGD_ECUDA;
-        const bool wide_sym = wide_tiles(s.sym, sms), wide_full = wide_tiles(s.full, sms);
-        int32_t sym = 0, full = 0;
+        // long tiles first: what is left for the end is short
+        std::stable_sort(G.m, G.m + s.count, [](const Matrix& a, const Matrix& b) { return (a.rb > a.cb ? a.rb : a.cb) > (b.rb > b.cb ? b.rb : b.cb); });
+        Work gram, polynomial, apply;
+        for (int k = 0; k < s.count; ++k) {
+            const Matrix& M = G.m[k];
+            gram.add(symmetric_tiles<128>(M.mb), symmetric_tiles<256>(M.mb), M.rb > M.cb ? M.rb : M.cb);
+            polynomial.add(symmetric_tiles<128>(M.mb), symmetric_tiles<256>(M.mb), M.mb);
+            apply.add(all_tiles<128>(M.rb, M.cb), all_tiles<256>(M.rb, M.cb), M.mb);
+        }
+        const bool wide_gram = gram.prefers_wide(sms), wide_polynomial = polynomial.prefers_wide(sms), wide_apply = apply.prefers_wide(sms);
+        int32_t strips = 0, first_gram = 0, first_polynomial = 0, first_apply = 0;
         for (int k = 0; k < s.count; ++k) {
             Matrix& M = G.m[k];
-            M.sym0 = sym;
-            M.full0 = full;
-            sym += (int32_t)(wide_sym ? symmetric_tiles<256>(M.mb) : symmetric_tiles<128>(M.mb));
-            full += (int32_t)(wide_full ? all_tiles<256>(M.rb, M.cb) : all_tiles<128>(M.rb, M.cb));
+            M.strip0 = strips;
+            M.first[GRAM] = first_gram;
+            M.first[POLYNOMIAL] = first_polynomial;
+            M.first[APPLY] = M.first[FINISH] = first_apply;
+            strips += M.strips;
+            first_gram += (int32_t)(wide_gram ? symmetric_tiles<256>(M.mb) : symmetric_tiles<128>(M.mb));
+            first_polynomial += (int32_t)(wide_polynomial ? symmetric_tiles<256>(M.mb) : symmetric_tiles<128>(M.mb));
+            first_apply += (int32_t)(wide_apply ? all_tiles<256>(M.rb, M.cb) : all_tiles<128>(M.rb, M.cb));
         }
         if ((e = C.fmt_in == SSGD_FMT_F32 ? launch_prepare<float>(st, (int)s.strips, G, C)
                : C.fmt_in == SSGD_FMT_F16 ? launch_prepare<__half>(st, (int)s.strips, G, C) : launch_prepare<__nv_bfloat16>(st, (int)s.strips, G, C)))
             return e;
         for (int k = 0; k < steps; ++k) {
-            if ((e = launch_product<GRAM>(st, C, map, wide_sym, k & 1, sym, sms))) return e;
-            if ((e = launch_product<POLYNOMIAL>(st, C, map, wide_sym, k & 1, sym, sms))) return e;
-            if ((e = k + 1 < steps ? launch_product<APPLY>(st, C, map, wide_full, k & 1, full, sms)
-                                   : launch_product<FINISH>(st, C, map, wide_full, k & 1, full, sms))) return e;
+            if ((e = launch_product<GRAM>(st, C, map, wide_gram, k & 1, first_gram, sms))) return e;
+            if ((e = launch_product<POLYNOMIAL>(st, C, map, wide_polynomial, k & 1, first_polynomial, sms))) return e;
+            if (k + 1 < steps) e = launch_product<APPLY>(st, C, map, wide_apply, k & 1, first_apply, sms);
+            else if (C.fmt_out == SSGD_FMT_F32) e = launch_product<FINISH, float>(st, C, map, wide_apply, k & 1, first_apply, sms);
+            else if (C.fmt_out == SSGD_FMT_F16) e = launch_product<FINISH, __half>(st, C, map, wide_apply, k & 1, first_apply, sms);
+            else e = launch_product<FINISH, __nv_bfloat16>(st, C, map, wide_apply, k & 1, first_apply, sms);
+            if (e) return e;
         }
     }
     return SSGD_OK;
