@@ -265,6 +265,7 @@ constexpr int CHUNK = 4;                            // blocks of the contraction
 template <int COLS, bool SPLIT> constexpr int STAGE = (2 + COLS / 128) * BLOCK_BYTES * (SPLIT ? 2 : 1);
 template <int COLS, bool SPLIT> constexpr int STAGES = RING / STAGE<COLS, SPLIT>;
 
+constexpr int LAUNCH_REGISTERS = 168;
 struct Shared {
     uint64_t full[8], empty[8], done[2], taken[2];
     uint32_t tmem;
@@ -360,46 +361,61 @@ __device__ __forceinline__ int opaque(int x) {
 // 32 x 32 fp16 numbers; neither eight rows of a column nor rows meet in a bank
 __device__ __forceinline__ uint32_t half_at(int r, int piece) { return (uint32_t)(r * 64 + ((piece ^ (((r >> 1) ^ (r >> 3)) & 3)) << 4)); }
 
-// 32 x 32 numbers of a block, from row 32 rh and column 32 ch on: lane's piece of the i-th eight rows
-struct Quarter {
-    uint8_t* block;
-    int rh, ch;
-    __device__ __forceinline__ uint8_t* at(int i, int lane) const { return block + piece_at(rh * 32 + i * 8 + lane / 4, ch * 4 + lane % 4); }
+// What is the same for all results of a tile
+template <Kind KIND> struct Job {
+    uint8_t* blocks;                                // of C.at
+    uint32_t from, to;                              // first blocks of what is added (A, x) and of the result
+    int32_t R;                                      // blocks to a column
+    int32_t second;                                 // blocks from the first numbers to the second
+    float* vec;                                     // d, and behind it e
+    int32_t side;                                   // floats of d
+    bool tall;
+    __device__ __forceinline__ Job(const Common& C, const Matrix& M, int which) {
+        constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
+        blocks = C.at.blocks;
+        from = KIND == POLYNOMIAL ? M.a : M.x(which);
+        to = KIND == GRAM ? M.a : KIND == POLYNOMIAL ? M.b : M.x(which ^ 1);
+        R = SYMMETRIC ? M.mb : M.rb;
+        second = SYMMETRIC ? M.mb * M.mb : M.rb * M.cb;
+        vec = C.at.vec + M.vec;
+        side = M.mb * BLOCK;
+        tall = M.tall();
+    }
+    // The lane's piece of the first eight rows of the 32 x 32 numbers at row0, col0 (multiples of 32); eight rows further is 1 KB further
+    __device__ __forceinline__ uint8_t* at(uint32_t first, int row0, int col0, int lane) const {
+        return blocks + (int64_t)(first + (uint32_t)(col0 / BLOCK * R + row0 / BLOCK)) * BLOCK_BYTES +
+               piece_at(row0 % BLOCK + lane / 4, col0 / 32 % 2 * 4 + lane % 4);
+    }
 };
 
 // What a piece of results needs beside the products
 template <Kind KIND, bool SPLIT> struct Source {
     static constexpr bool NEEDED = KIND != GRAM, BOTH = KIND != POLYNOMIAL || SPLIT;
     uint4 hi[NEEDED ? 4 : 1], lo[NEEDED && BOTH ? 4 : 1];
-    float row[4], col[8];                           // d or e of the rows and columns
+    float row[4], col[8];                           // d or e of the rows and columns, 0 where only the other counts
 };
 
-template <Kind KIND>
-__device__ __forceinline__ Quarter quarter(const Common& C, const Matrix& M, uint32_t first, int row0, int col0) {
-    const int R = KIND == GRAM || KIND == POLYNOMIAL ? M.mb : M.rb;
-    return Quarter{C.at.blocks + (int64_t)(first + (uint32_t)(col0 / BLOCK) * R + row0 / BLOCK) * BLOCK_BYTES, row0 / 32 % 2, col0 / 32 % 2};
-}
-
 template <Kind KIND, bool SPLIT>
-__device__ __forceinline__ void fetch(const Common& C, const Matrix& M, int which, int row0, int col0, int lane, Source<KIND, SPLIT>& s) {
+__device__ __forceinline__ void fetch(const Job<KIND>& J, int row0, int col0, int lane, Source<KIND, SPLIT>& s) {
     if constexpr (KIND == GRAM) return;
-    const int64_t second = (int64_t)(KIND == POLYNOMIAL ? M.mb : M.rb) * (KIND == POLYNOMIAL ? M.mb : M.cb) * BLOCK_BYTES;
-    const Quarter q = quarter<KIND>(C, M, KIND == POLYNOMIAL ? M.a : M.x(which), row0, col0);
+    const uint8_t* p = J.at(J.from, row0, col0, lane);
+    const int64_t second = (int64_t)J.second * BLOCK_BYTES;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        s.hi[i] = *reinterpret_cast<const uint4*>(q.at(i, lane));
-        if constexpr (Source<KIND, SPLIT>::BOTH) s.lo[i] = *reinterpret_cast<const uint4*>(q.at(i, lane) + second);
+        s.hi[i] = *reinterpret_cast<const uint4*>(p + i * 1024);
+        if constexpr (Source<KIND, SPLIT>::BOTH) s.lo[i] = *reinterpret_cast<const uint4*>(p + i * 1024 + second);
     }
-    const float* d = C.at.vec + M.vec + (KIND == POLYNOMIAL ? 0 : M.mb * BLOCK);
-    if (KIND == POLYNOMIAL || !M.tall()) {
+    const float* d = J.vec + (KIND == POLYNOMIAL ? 0 : J.side);
+    const bool rows = KIND == POLYNOMIAL || !J.tall, cols = KIND == POLYNOMIAL || J.tall;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s.row[i] = d[row0 + i * 8 + lane / 4];
+    for (int i = 0; i < 4; ++i) s.row[i] = rows ? d[row0 + i * 8 + lane / 4] : 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (cols) {
+        a = *reinterpret_cast<const float4*>(d + col0 + lane % 4 * 8);
+        b = *reinterpret_cast<const float4*>(d + col0 + lane % 4 * 8 + 4);
     }
-    if (KIND == POLYNOMIAL || M.tall()) {
-        const float4 a = *reinterpret_cast<const float4*>(d + col0 + lane % 4 * 8), b = *reinterpret_cast<const float4*>(d + col0 + lane % 4 * 8 + 4);
-        s.col[0] = a.x; s.col[1] = a.y; s.col[2] = a.z; s.col[3] = a.w;
-        s.col[4] = b.x; s.col[5] = b.y; s.col[6] = b.z; s.col[7] = b.w;
-    }
+    s.col[0] = a.x; s.col[1] = a.y; s.col[2] = a.z; s.col[3] = a.w;
+    s.col[4] = b.x; s.col[5] = b.y; s.col[6] = b.z; s.col[7] = b.w;
 }
 
 // Eight results in a row of the output
@@ -430,7 +446,7 @@ __device__ __forceinline__ void put_output(const Common& C, const Matrix& M, int
 }
 
 // Exchanges rows and columns of 32 x 32 fp16 numbers, eight of a row to a lane as above, and stores them
-__device__ __forceinline__ void put_transposed(const Quarter& q, uint8_t* scratch, int lane, const uint4 (&h)[4], int64_t offset) {
+__device__ __forceinline__ void put_transposed(uint8_t* to, uint8_t* scratch, int lane, const uint4 (&h)[4]) {
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -441,13 +457,12 @@ __device__ __forceinline__ void put_transposed(const Quarter& q, uint8_t* scratc
     }
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint4*>(q.at(i, lane) + offset) = *reinterpret_cast<const uint4*>(scratch + half_at(i * 8 + lane / 4, lane % 4));
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + i * 1024) = *reinterpret_cast<const uint4*>(scratch + half_at(i * 8 + lane / 4, lane % 4));
 }
 
 // What 32 rows and columns of a product become.  acc: the lane's row; T: the output's type (FINISH).
 template <Kind KIND, bool SPLIT, typename T>
-__device__ __forceinline__ void take(const Common& C, const Matrix& M, int which, int row0, int col0, const uint32_t (&acc)[32],
+__device__ __forceinline__ void take(const Common& C, const Matrix& M, const Job<KIND>& J, int row0, int col0, const uint32_t (&acc)[32],
                                      const Source<KIND, SPLIT>& s, uint8_t* scratch, int lane) {
     constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
     __syncwarp();
@@ -455,11 +470,10 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, int which
     for (int i = 0; i < 8; ++i)
         *reinterpret_cast<uint4*>(scratch + word_at(lane, i)) = make_uint4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
     __syncwarp();
-    float* diagonal = C.at.vec + M.vec + (KIND == POLYNOMIAL ? M.mb * BLOCK : 0);
-    const bool tall = M.tall();
-    const uint32_t first = KIND == GRAM ? M.a : KIND == POLYNOMIAL ? M.b : M.x(which ^ 1);
-    const int64_t second = (int64_t)(SYMMETRIC ? M.mb : M.rb) * (SYMMETRIC ? M.mb : M.cb) * BLOCK_BYTES;
-    const Quarter to = quarter<KIND>(C, M, first, row0, col0);
+    float* diagonal = J.vec + (KIND == POLYNOMIAL ? J.side : 0) + row0;
+    const bool on_diagonal = SYMMETRIC && row0 == col0;
+    uint8_t* to = J.at(J.to, row0, col0, lane);
+    const int64_t second = (int64_t)J.second * BLOCK_BYTES;
     uint4 hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -477,39 +491,42 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, int which
                 for (int e = 0; e < 4; ++e) { const float2 f = halves(l[e]); x[2 * e] += f.x; x[2 * e + 1] += f.y; }
             }
         }
+        if (on_diagonal) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (r != lane % 4 * 8 + e) continue;
+                if constexpr (KIND == GRAM) diagonal[r] = v[e] * (1.f / (SCALE * SCALE));
+                if constexpr (KIND == POLYNOMIAL) {
+                    diagonal[r] = fmaf(C.c, fmaf(s.row[i], s.row[i], v[e] * (1.f / (SCALE * SCALE))), C.b * s.row[i]);
+                    x[e] = 0.f;
+                }
+                v[e] = 0.f;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool diag = SYMMETRIC && row0 == col0 && r == lane % 4 * 8 + e;
-            if constexpr (KIND == GRAM) {
-                if (diag) diagonal[row0 + r] = v[e] * (1.f / (SCALE * SCALE));
-                v[e] *= 1.f / SCALE;
-            } else if constexpr (KIND == POLYNOMIAL) {
-                if (diag) diagonal[row0 + r] = fmaf(C.c, fmaf(s.row[i], s.row[i], v[e] * (1.f / (SCALE * SCALE))), C.b * s.row[i]);
-                v[e] = fmaf(C.c, fmaf(x[e], s.row[i] + s.col[e], v[e] * (1.f / SCALE)), C.b * x[e]);
-            } else {
-                v[e] = fmaf((tall ? s.col[e] : s.row[i]) + C.a, x[e], v[e] * (1.f / SCALE));
-            }
-            if (diag) v[e] = 0.f;
+            if constexpr (KIND == GRAM) v[e] *= 1.f / SCALE;
+            else if constexpr (KIND == POLYNOMIAL) v[e] = fmaf(C.c, fmaf(x[e], s.row[i] + s.col[e], v[e] * (1.f / SCALE)), C.b * x[e]);
+            else v[e] = fmaf(C.a + (s.row[i] + s.col[e]), x[e], v[e] * (1.f / SCALE));
         }
         if constexpr (KIND == FINISH) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= 1.f / SCALE;
-            const int row = row0 + r, col = col0 + lane % 4 * 8;
-            put_output<T>(C, M, row, col, v);
+            put_output<T>(C, M, row0 + r, col0 + lane % 4 * 8, v);
         } else {
             split2(v[0], v[1], hi[i].x, lo[i].x);
             split2(v[2], v[3], hi[i].y, lo[i].y);
             split2(v[4], v[5], hi[i].z, lo[i].z);
             split2(v[6], v[7], hi[i].w, lo[i].w);
-            *reinterpret_cast<uint4*>(to.at(i, lane)) = hi[i];
-            if (SPLIT || !SYMMETRIC) *reinterpret_cast<uint4*>(to.at(i, lane) + second) = lo[i];
+            *reinterpret_cast<uint4*>(to + i * 1024) = hi[i];
+            if (SPLIT || !SYMMETRIC) *reinterpret_cast<uint4*>(to + i * 1024 + second) = lo[i];
         }
     }
     if constexpr (SYMMETRIC) {
         if (row0 / BLOCK > col0 / BLOCK) {
-            const Quarter mirror = quarter<KIND>(C, M, first, col0, row0);
-            put_transposed(mirror, scratch, lane, hi, 0);
-            if (SPLIT) put_transposed(mirror, scratch, lane, lo, second);
+            uint8_t* mirror = J.at(J.to, col0, row0, lane);
+            put_transposed(mirror, scratch, lane, hi);
+            if (SPLIT) put_transposed(mirror + second, scratch, lane, lo);
         }
     }
 }
@@ -544,9 +561,10 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
     auto find = [&](int tile) { return matrix_of(C.count, tile, [&](int i) { return S.first[i]; }); };
     const int tile0 = blockIdx.x / 2, stride = gridDim.x / 2;
 
-    // With SPLIT a result warp holds up to 128 sums to a lane: it gets registers from the group that copies (224 + 224 + 56 = 3 x 168).
+    // A result warp holds up to 128 sums to a lane (SPLIT), or two pieces' sources: it gets registers from the group that copies
+    // (224 + 224 + 56 = 3 x 168, what the launch has given: LAUNCH_REGISTERS).
     if (warp >= RESULT_WARPS) {
-    if (SPLIT && COLS == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == RESULT_WARPS && lane == 0) {                    // copies
         int s = 0, issued = 0;
         uint32_t parity = 1;
@@ -623,7 +641,7 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
         }
     }
     } else {                                                    // results
-        if (SPLIT && COLS == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         constexpr int MINE = COLS / 2 / 32;                     // pieces of 32 columns of a warp
         int buffer = 0;
         uint32_t parity = 0;
@@ -632,7 +650,8 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
             const Matrix& M = C.at.matrices[m];
             const Tile at_tile = tile_of<KIND, COLS>(M, tile - S.first[m]);
             const int row0 = at_tile.row * BLOCK + (int)rank * 128 + warp % 4 * 32, col0 = at_tile.col * BLOCK + warp / 4 * (COLS / 2);
-            const int R = SYMMETRIC ? M.mb : M.rb, K = SYMMETRIC ? M.mb : M.cb;
+            const Job<KIND> J(C, M, which);
+            const int R = J.R, K = SYMMETRIC ? M.mb : M.cb;
             // of a symmetric product, what lies above the diagonal comes from below it
             auto wanted = [&](int i) {
                 const int col = col0 + i * 32;
@@ -684,20 +703,25 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
                     tmem_store_wait();
                 }
             }
-            Source<KIND, SPLIT> source{};
-            if (some) fetch(C, M, which, row0, col0, opaque(lane), source);
+            Source<KIND, SPLIT> source[2] = {};
+            if (some) fetch(J, row0, col0, opaque(lane), source[0]);
             if (!summed && !done()) break;
+            // what a piece needs is fetched before the one before it is worked on
 #pragma unroll 1
-            for (int i = 0; i < MINE; ++i) {
-                uint32_t acc[32];
-                tmem_load32(at + buffer * COLS + i * 32, acc);
-                tmem_wait();
-                if (i + 1 == MINE) next();
-                if (!wanted(i)) continue;
-                // addresses are made here each time: kept across the tiles they would take the registers of the sums
-                const int l = opaque(lane);
-                take<KIND, SPLIT, T>(C, M, which, row0, col0 + i * 32, acc, source, scratches + opaque(warp) * SCRATCH, l);
-                if (i + 1 < MINE && wanted(i + 1)) fetch(C, M, which, row0, col0 + (i + 1) * 32, l, source);
+            for (int i0 = 0; i0 < MINE; i0 += 2) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int i = i0 + j;
+                    // addresses are made here each time: kept across the tiles they would take the registers of the sums
+                    const int l = opaque(lane);
+                    uint32_t acc[32];
+                    tmem_load32(at + buffer * COLS + i * 32, acc);
+                    if (i + 1 < MINE && wanted(i + 1)) fetch(J, row0, col0 + (i + 1) * 32, l, source[j ^ 1]);
+                    else source[j ^ 1] = {};
+                    tmem_wait();
+                    if (i + 1 == MINE) next();
+                    if (wanted(i)) take<KIND, SPLIT, T>(C, M, J, row0, col0 + i * 32, acc, source[j], scratches + opaque(warp) * SCRATCH, l);
+                }
             }
         }
     }
@@ -776,6 +800,12 @@ template <Kind KIND, int COLS, bool SPLIT, typename T>
 int launch_tiles(cudaStream_t st, const Common& C, const CUtensorMap& map, int which, int64_t tiles, int sms) {
     static PerDevice known;
     int fits = 0;
+    // the exchange of registers in the kernel would wait forever if it had been launched with others
+    static const bool as_planned = [] {
+        cudaFuncAttributes a{};
+        return cudaFuncGetAttributes(&a, k_product<KIND, COLS, SPLIT, T>) == cudaSuccess && a.numRegs == LAUNCH_REGISTERS;
+    }();
+    if (!as_planned) return SSGD_ECUDA;
     if (int e = residency(k_product<KIND, COLS, SPLIT, T>, THREADS, SHARED_BYTES, known, &fits)) return e;
     return launch(st, k_product<KIND, COLS, SPLIT, T>, (int)(2 * (tiles < sms / 2 ? tiles : sms / 2)), THREADS, SHARED_BYTES, C, map, which, (int)tiles);
 }

@@ -45,11 +45,12 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
         : "=r"(ok) : "r"(shared_addr(bar)), "r"(parity) : "memory");
     return ok != 0;
 }
-// Arrives at the barrier in the same place of the pair's first CTA
+// Arrives at the barrier in the same place of the pair's first CTA.  Relaxed: what it hands over is tensor memory, ordered by the fence
+// before it (fence_before), and a release would wait for all results that are on their way to global memory.
 __device__ __forceinline__ void bar_arrive_first(uint64_t* bar) {
     uint32_t remote;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(shared_addr(bar)));
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
 }
 __device__ __forceinline__ void pair_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
