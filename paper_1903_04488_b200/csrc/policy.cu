@@ -30,11 +30,15 @@ struct Args {
     float* stats;                                   // [5][rows]: loss, logp, entropy, kl, ratio
     void* out; int64_t ld_out;                      // NULL: no gradient
     bool same_phase;                                // rows of logits and of the gradient lie alike within 16 bytes
-    bool kept;                                      // a CTA's segment fits its shared memory; otherwise it is read twice
 };
 
 constexpr int BATCH = 4;                            // granules that a thread takes at once
 constexpr int AHEAD = 4;                            // batches on their way
+
+template <int OFFSET>
+__device__ __forceinline__ void copy_async_at(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %2], 16;" ::"r"(to), "l"(from), "n"(OFFSET) : "memory");
+}
 
 struct Row {                                        // what the gradient needs of a row
     float m, shift, log2s;                          // log2 p = (z c - shift) - log2 s, or (z - m) c - log2 s
@@ -47,23 +51,27 @@ template <int NT> struct Shared {
     Row row;
 };
 
-// Two logits' gradients without the id's own term
+// log2 p of two logits: (z c - shift) - log2 s, or for far rows (z - m) c - log2 s
+__device__ __forceinline__ float2 log2_p(const Row& r, float c, bool plain, float2 x) {
+    const float2 l = plain ? fma2(x, both(c), both(-r.shift)) : make_float2((x.x - r.m) * c, (x.y - r.m) * c);
+    return add2(l, both(-r.log2s));
+}
+// Two logits' gradients from there, without the id's own term
 template <bool ENTROPY>
-__device__ __forceinline__ float2 grad(const Row& r, float c, bool plain, float2 x) {
-    float2 l;
-    if (plain) l = fma2(x, both(c), both(-r.shift));
-    else l = make_float2((x.x - r.m) * c, (x.y - r.m) * c);
-    l = add2(l, both(-r.log2s));
+__device__ __forceinline__ float2 grad(const Row& r, float2 l) {
     const float2 p = make_float2(ex2(l.x), ex2(l.y));
     if (!ENTROPY) return mul2(p, both(r.base));
     // p is zero below; log2 p may be -inf there
     const float2 bounded = make_float2(l.x < -200.f ? -200.f : l.x, l.y < -200.f ? -200.f : l.y);
     return mul2(p, fma2(bounded, both(r.slope), both(r.base)));
 }
+// Where 16 bits are stored, shift + log2 s may be one number: up to FOLD its rounding is 2^-18, 2.6e-6 of p.
+constexpr float FOLD = 64.f;
 
-template <typename T, bool ENTROPY, int NT>
+// KEEP: the CTA's segment stays in shared memory; otherwise it is read again, or there is no gradient to be written.
+template <typename T, bool ENTROPY, bool KEEP, int NT>
 __global__ void __launch_bounds__(NT) k_policy(const Args A, int split) {
-    constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32, U = BATCH;
+    constexpr int VEC = 16 / sizeof(T), WARPS = NT / 32, U = BATCH, STEP = NT * U;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared<NT> sh;
     Vec<T, VEC>* seg = reinterpret_cast<Vec<T, VEC>*>(raw);
@@ -97,37 +105,64 @@ __global__ void __launch_bounds__(NT) k_policy(const Args A, int split) {
     }
     const float c = A.scale * LOG2E;
     const float z_id = to_f32(z[id]);               // before the gradient, which may lie in the same place, is written
+    float adv = 0.f, old_logp = 0.f, ref_logp = 0.f;
+    if (t == 0) {                                   // long before they are needed
+        adv = A.advantages[row];
+        old_logp = A.old_logp[row];
+        if (A.ref_logp) ref_logp = A.ref_logp[row];
+    }
     Running r{no_sums(), NEG_INF, c, __fdiv_ru(160.f, c)};
     // the row's first and last granule may be parts of one
     const int32_t whole0 = g0 == 0 && G.phase ? 1 : g0;
     const int32_t whole1 = max(g1 == G.count && !G.whole(G.count - 1) ? g1 - 1 : g1, min(whole0, g1));
-    const bool keep = A.kept && A.out;
     const int32_t n = whole1 - whole0;
-    const T* first = z + G.first(whole0);
-    auto copy = [&](int32_t b0) {
-        if (keep && b0 < n) {
+    // the thread's granules: t, t + NT, ..
+    const T* mine = z + G.first(whole0) + (int64_t)t * VEC;
+    Vec<T, VEC>* kept = seg + t;
+    {
+        const T* from = mine;
+        uint32_t to = (uint32_t)__cvta_generic_to_shared(kept);
+        int32_t left = n - t;                       // the thread has one more granule for every NT of them
+        auto copy = [&] {
+            if constexpr (KEEP) {
+                if (left > (U - 1) * NT) {
+                    copy_async_at<0>(to, from);
+                    copy_async_at<NT * 16>(to, from);
+                    copy_async_at<2 * NT * 16>(to, from);
+                    copy_async_at<3 * NT * 16>(to, from);
+                } else {
+                    if (left > 0) copy_async_at<0>(to, from);
+                    if (left > NT) copy_async_at<NT * 16>(to, from);
+                    if (left > 2 * NT) copy_async_at<2 * NT * 16>(to, from);
+                }
+                to += STEP * 16;
+                from += STEP * VEC;
+                left -= STEP;
+                copy_async_commit();
+            }
+        };
+        for (int k = 0; k < AHEAD; ++k) copy();
+        const Vec<T, VEC>* at = KEEP ? kept : reinterpret_cast<const Vec<T, VEC>*>(mine);
+        int32_t rest = n;
+        for (; rest >= STEP; rest -= STEP, at += STEP) {
+            Vec<T, VEC> v[U];
+            if (KEEP) copy_async_wait<AHEAD - 1>();
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = KEEP ? at[u * NT] : load_vec<T, VEC>(reinterpret_cast<const T*>(at + u * NT));
+            copy();
+            add_granules<T, U>(r, v, U);
+        }
+        if (rest > 0) {
+            Vec<T, VEC> v[U];
+            if (KEEP) copy_async_wait<0>();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int32_t i = b0 + u * NT + t;
-                if (i < n) copy_async<16>(&seg[i], first + (int64_t)i * VEC);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[u].e[e] = from_f32<T>(NEG_INF);
+                if (u * NT + t < rest) v[u] = KEEP ? at[u * NT] : load_vec<T, VEC>(reinterpret_cast<const T*>(at + u * NT));
             }
+            add_granules<T, U>(r, v, (rest + NT - 1) / NT);
         }
-        copy_async_commit();
-    };
-    for (int k = 0; k < AHEAD; ++k) copy(k * NT * U);
-    for (int32_t b0 = 0; b0 < n; b0 += NT * U) {
-        Vec<T, VEC> v[U];
-        const int have = min((n - b0 + NT - 1) / NT, U);
-        copy_async_wait<AHEAD - 1>();
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t i = b0 + u * NT + t;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[u].e[e] = from_f32<T>(NEG_INF);
-            if (i < n) v[u] = keep ? seg[i] : load_vec<T, VEC>(first + (int64_t)i * VEC);
-        }
-        copy(b0 + AHEAD * NT * U);
-        add_granules<T, U>(r, v, have);
     }
     auto partial = [&](int32_t i) {
         for (int32_t at = max(G.first(i), 0); at < min(G.first(i) + VEC, A.vocab); ++at) add_careful(r.a, to_f32(z[at]), c);
@@ -157,13 +192,13 @@ __global__ void __launch_bounds__(NT) k_policy(const Args A, int split) {
             float logp = plain && fabsf(z_id) < HUGE_LOGIT ? (fmaf(z_id, c, -a.shift) - log2s) * LN2 : fmaf(z_id - a.m, A.scale, -log2s * LN2);
             if (none || (z_id == NEG_INF && a.s == a.s)) logp = NEG_INF;
             const float h = none ? 0.f : (log2s - a.w / a.s) * LN2;
-            const float adv = A.advantages[row], ratio = expf(logp - A.old_logp[row]);
+            const float ratio = expf(logp - old_logp);
             const float kept = adv >= 0.f ? (ratio > 1.f + A.high ? 1.f + A.high : ratio) : (ratio < 1.f - A.low ? 1.f - A.low : ratio);
             float along = kept == ratio ? -adv * ratio : 0.f, kl = 0.f, loss = -kept * adv;
             if (ratio != ratio || adv != adv) along = loss;
             if (A.entropy != 0.f) loss -= A.entropy * h;
             if (A.ref_logp) {
-                const float q = A.ref_logp[row] - logp, e = expm1f(q);
+                const float q = ref_logp - logp, e = expm1f(q);
                 kl = e - q;
                 if (A.kl != 0.f) {
                     loss = fmaf(A.kl, kl, loss);
@@ -187,22 +222,41 @@ __global__ void __launch_bounds__(NT) k_policy(const Args A, int split) {
         const bool plain = near(R.shift);
         // the single elements: of partial granules, and of all where the result lies otherwise than the logits
         auto one = [&](int32_t j, float x) {
-            float v = R.none || (x == NEG_INF && R.log2s == R.log2s) ? 0.f : grad<ENTROPY>(R, c, plain && fabsf(x) < HUGE_LOGIT, both(x)).x;
+            float v = R.none || (x == NEG_INF && R.log2s == R.log2s) ? 0.f : grad<ENTROPY>(R, log2_p(R, c, plain && fabsf(x) < HUGE_LOGIT, both(x))).x;
             if (j == (int32_t)id) v += R.own;
             out[j] = from_f32<T>(v);
         };
-        const int32_t own = ((int32_t)id - G.first(whole0)) / VEC;             // the id's granule, among the whole ones of the CTA
-        for (int32_t i = t; i < n; i += NT) {
-            const Vec<T, VEC> v = keep ? seg[i] : load_vec<T, VEC>(first + (int64_t)i * VEC);
-            const int32_t at = G.first(whole0 + i);
-            if (A.same_phase && i != own && !R.none && plain) {
-                float2 f[VEC / 2];
-                unpack_pairs(v, f);
+        if (A.same_phase && !R.none && plain) {
+            // the id's element among the others first, then once more by the thread that has its granule
+            const int32_t own = ((int32_t)id - G.first(whole0)) / VEC;
+            const bool has_id = (int32_t)id >= G.first(whole0) && own < n && own % NT == t;
+            const float x_id = has_id ? to_f32(z[id]) : 0.f;
+            auto all = [&](auto log2_of) {
+                const Vec<T, VEC>* at = KEEP ? kept : reinterpret_cast<const Vec<T, VEC>*>(mine);
+                T* to = out + G.first(whole0) + (int64_t)t * VEC;
+                auto write = [&](int u) {
+                    const Vec<T, VEC> v = KEEP ? at[u * NT] : load_vec<T, VEC>(reinterpret_cast<const T*>(at + u * NT));
+                    float2 f[VEC / 2];
+                    unpack_pairs(v, f);
 #pragma unroll
-                for (int e = 0; e < VEC / 2; ++e) f[e] = grad<ENTROPY>(R, c, true, f[e]);
-                store_vec<T, VEC>(out + at, pack_pairs<T, VEC>(f));
-            } else {
-                for (int e = 0; e < VEC; ++e) one(at + e, to_f32(v.e[e]));
+                    for (int e = 0; e < VEC / 2; ++e) f[e] = grad<ENTROPY>(R, log2_of(f[e]));
+                    store_vec<T, VEC>(to + u * (NT * VEC), pack_pairs<T, VEC>(f));
+                };
+                int32_t left = n - t;
+                for (; left > (U - 1) * NT; left -= STEP, at += STEP, to += STEP * VEC) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) write(u);
+                }
+                for (; left > 0; left -= NT, at += NT, to += NT * VEC) write(0);
+            };
+            const float fold = R.shift + R.log2s;
+            if (sizeof(T) == 2 && fabsf(fold) < FOLD) all([&](float2 x) { return fma2(x, both(c), both(-fold)); });
+            else all([&](float2 x) { return log2_p(R, c, true, x); });
+            if (has_id) one((int32_t)id, x_id);
+        } else {
+            for (int32_t i = t; i < n; i += NT) {
+                const Vec<T, VEC> v = KEEP ? seg[i] : load_vec<T, VEC>(mine + (int64_t)(i - t) * VEC);
+                for (int e = 0; e < VEC; ++e) one(G.first(whole0 + i) + e, to_f32(v.e[e]));
             }
         }
         if (t == 0 && head)
@@ -218,13 +272,13 @@ __global__ void __launch_bounds__(NT) k_policy(const Args A, int split) {
 constexpr int SEGMENT = 72 * 1024;                  // bytes of a row that a CTA keeps at most while rows can be shared: three CTAs to an SM
 constexpr int MOST = 208 * 1024;                    // and where a cluster of 8 needs more
 
-template <typename T, bool ENTROPY, int NT>
+template <typename T, bool ENTROPY, bool KEEP, int NT>
 int launch_nt(const Args& A, int split, int smem, cudaStream_t st) {
     static PerDevice opted;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return SSGD_ECUDA;
-    if (!opted.value[dev]) {
-        if (cudaFuncSetAttribute(k_policy<T, ENTROPY, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST) != cudaSuccess) return SSGD_ECUDA;
+    if (KEEP && !opted.value[dev]) {
+        if (cudaFuncSetAttribute(k_policy<T, ENTROPY, KEEP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST) != cudaSuccess) return SSGD_ECUDA;
         opted.value[dev] = 1;
     }
     cudaLaunchConfig_t cfg{};
@@ -238,21 +292,25 @@ int launch_nt(const Args& A, int split, int smem, cudaStream_t st) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = split > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, k_policy<T, ENTROPY, NT>, A, split) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
+    return cudaLaunchKernelEx(&cfg, k_policy<T, ENTROPY, KEEP, NT>, A, split) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
 }
 
 template <typename T>
-int launch_policy(Args A, int sms, cudaStream_t st) {
+int launch_policy(const Args& A, int sms, cudaStream_t st) {
     constexpr int VEC = 16 / sizeof(T);
     const int64_t granules = (A.vocab + 2 * VEC - 2) / VEC;                     // whatever the phase
     int split = 1;
     while (split < 8 && (granules * 16 > (int64_t)split * SEGMENT || (A.rows * split < 4 * sms && granules / (split * 2) >= 2 * 256))) split *= 2;
     const int64_t smem = (granules + split - 1) / split * 16;
-    A.kept = smem <= MOST;
-    const int bytes = A.out && A.kept ? (int)smem : 0;
+    const bool keep = A.out && smem <= MOST;
+    // as for the log probabilities: short rows go to small CTAs
     const bool small = granules <= 1024 && A.rows >= 4 * sms;
-    if (A.entropy != 0.f) return small ? launch_nt<T, true, 64>(A, 1, bytes, st) : launch_nt<T, true, 256>(A, split, bytes, st);
-    return small ? launch_nt<T, false, 64>(A, 1, bytes, st) : launch_nt<T, false, 256>(A, split, bytes, st);
+    auto go = [&](auto entropy) {
+        constexpr bool E = decltype(entropy)::value;
+        if (small) return keep ? launch_nt<T, E, true, 64>(A, 1, (int)smem, st) : launch_nt<T, E, false, 64>(A, 1, 0, st);
+        return keep ? launch_nt<T, E, true, 256>(A, split, (int)smem, st) : launch_nt<T, E, false, 256>(A, split, 0, st);
+    };
+    return A.entropy != 0.f && A.out ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace
@@ -275,7 +333,7 @@ extern "C" int ssgd_policy_loss(const void* logits, int64_t ld, int32_t fmt, con
     int sms = 0;
     if (int e = sm_count_of_current_device(&sms)) return e;
     Args A{logits, ld, ids, ids_bytes == 8, old_logp, advantages, ref_logp, weights, rows, (int32_t)vocab, scale, clip_low, clip_high, kl, entropy,
-           stats, dlogits, ld_d, false, false};
+           stats, dlogits, ld_d, false};
     A.same_phase = addr(logits) % 16 == addr(dlogits) % 16 && (rows == 1 || (ld - ld_d) * es % 16 == 0);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return fmt == SSGD_FMT_F32 ? launch_policy<float>(A, sms, st)

@@ -30,8 +30,8 @@ struct Args {
     float* loss; float* rewards;                    // [pairs], [2][pairs]
     float* d_logp;                                  // [tokens] or NULL
     double* pieces;                                 // [chunks + 2 pairs]
+    int64_t* ranges;                                // [chunks][2], see Range
     bool vector;                                    // logp and ref are 16-byte aligned
-    bool vector_out;
 };
 
 // starts[s], kept within the tokens
@@ -40,40 +40,58 @@ __device__ __forceinline__ int64_t start_of(const Args& A, int64_t s) {
     return v < 0 ? 0 : v > A.tokens ? A.tokens : v;
 }
 
-// The first s in [0, n] whose start is at least `token`; n if there is none.  The whole CTA searches: 256 places
-// at a time.
-__device__ __forceinline__ int64_t first_at(const Args& A, int64_t n, int64_t token) {
-    int64_t lo = 0, hi = n;                         // the answer is in [lo, hi]
-    while (lo < hi) {
-        const int64_t step = (hi - lo + THREADS - 1) / THREADS, at = lo + (int64_t)threadIdx.x * step;
-        const bool below = at < hi && start_of(A, at) < token;
-        const int k = __syncthreads_count(below);   // places lo, lo + step, .. that are before the answer
-        const int64_t new_lo = k ? lo + (int64_t)(k - 1) * step + 1 : lo;
-        hi = k ? min(hi, lo + (int64_t)k * step) : lo;
-        lo = new_lo;
-    }
-    return lo;
-}
-
-constexpr int SHORT = 32;                           // pieces below it are summed by one thread, others by a warp
+constexpr int FEW = 64;                             // sequences of a CTA that are gone through one by one
+constexpr int SHORT = 32;                           // where there are more, pieces below it are summed by one thread, others by a warp
+constexpr int LONG = 256;                           // pieces of a pair that the whole CTA joins
 constexpr int32_t NO_MARK = 0x7fa12345;             // the bits of a NaN that no operation makes
 struct Shared {
     float diff[CHUNK];                              // then the gradients
-    int32_t list[CHUNK / SHORT + 1];
+    int32_t bound[FEW + 1];                         // where the sequences begin within the CTA's tokens
+    float value[FEW];                               // their gradients
+    union {
+        double part[WARPS][FEW];
+        int32_t list[CHUNK / SHORT + 1];
+    };
     int32_t listed;
     int32_t last[WARPS];
     double joined[WARPS];
 };
 
-struct Range { int64_t c0, c1, s0, s1; };           // tokens of the CTA; the sequences that may have some of them
+// Tokens of the CTA, and the sequences that may have some of them: from the last one that starts before the first token to the last one
+// that starts before the end.  The last CTA has those too that start at the end.
+struct Range {
+    int64_t c0, c1, s0, s1;
+    __device__ __forceinline__ int within(int64_t token) const { return (int)((token < c0 ? c0 : token > c1 ? c1 : token) - c0); }
+};
 
+// The whole CTA searches, 256 places at a time, for the first starts that are at least c0 and at least c1.
 __device__ __forceinline__ Range range_of(const Args& A, int64_t chunk, bool last) {
     Range R;
     R.c0 = chunk * CHUNK;
     R.c1 = min(R.c0 + CHUNK, A.tokens);
     const int64_t n = 2 * A.pairs + 1;
-    R.s0 = max(first_at(A, n, R.c0) - 1, (int64_t)0);                          // the last sequence that starts before the first token
-    R.s1 = last ? 2 * A.pairs : min(first_at(A, n, R.c1), 2 * A.pairs);        // sequences from here on start behind the last
+    int64_t lo[2] = {0, 0}, hi[2] = {chunk == 0 ? 0 : n, last ? 0 : n};
+    while (lo[0] < hi[0] || lo[1] < hi[1]) {
+        bool below[2];
+        int64_t step[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            step[q] = (hi[q] - lo[q] + THREADS - 1) / THREADS;
+            const int64_t at = lo[q] + (int64_t)threadIdx.x * step[q];
+            below[q] = at < hi[q] && start_of(A, at) < (q ? R.c1 : R.c0);
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = __syncthreads_count(below[q]);   // places lo, lo + step, .. that are before the answer
+            if (lo[q] >= hi[q]) continue;
+            const int64_t from = k ? lo[q] + (int64_t)(k - 1) * step[q] + 1 : lo[q];
+            hi[q] = k ? min(hi[q], lo[q] + (int64_t)k * step[q]) : lo[q];
+            lo[q] = from;
+        }
+    }
+    R.s0 = max(lo[0] - 1, (int64_t)0);
+    R.s1 = last ? 2 * A.pairs : min(lo[1], 2 * A.pairs);
+    if (R.s1 < R.s0) R.s1 = R.s0;                   // starts that do not ascend
     return R;
 }
 
@@ -104,8 +122,41 @@ __device__ __forceinline__ void load_tokens(const Args& A, Shared& S, int64_t c0
 // the lowest number of a mask) stays there.
 __device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, int64_t chunk, const Range& R) {
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    auto join = [&](double v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    };
+    if (R.s1 - R.s0 <= FEW) {                       // every warp takes an eighth of the tokens
+        const int n = (int)(R.s1 - R.s0);
+        if (t <= n) S.bound[t] = R.within(start_of(A, R.s0 + t));
+        __syncthreads();
+        constexpr int SPAN = CHUNK / WARPS;
+        for (int q = 0; q < n; ++q) {
+            const int a = max(S.bound[q], warp * SPAN), b = min(S.bound[q + 1], (warp + 1) * SPAN);
+            double sum[2] = {0.0, 0.0};
+            if (a < b) {
+                int i = a + lane;
+                for (; i + 32 < b; i += 64) {
+                    sum[0] += (double)S.diff[i];
+                    sum[1] += (double)S.diff[i + 32];
+                }
+                if (i < b) sum[0] += (double)S.diff[i];
+                sum[0] = join(sum[0] + sum[1]);
+            }
+            if (lane == 0) S.part[warp][q] = sum[0];
+        }
+        __syncthreads();
+        if (t < n && S.bound[t] < S.bound[t + 1]) {
+            double sum = 0.0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) sum += S.part[w][t];
+            A.pieces[chunk + R.s0 + t] = sum;
+        }
+        return;
+    }
     for (int64_t s = R.s0 + t; s < R.s1; s += THREADS) {
-        const int a = (int)(max(start_of(A, s), R.c0) - R.c0), b = (int)(min(start_of(A, s + 1), R.c1) - R.c0);
+        const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
         if (b - a >= SHORT) {
             const int at = atomicAdd(&S.listed, 1);
             if (at <= CHUNK / SHORT) S.list[at] = (int32_t)(s - R.s0);         // more only where starts do not ascend
@@ -118,18 +169,11 @@ __device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, int64_t chu
     __syncthreads();
     for (int q = warp; q < min(S.listed, CHUNK / SHORT + 1); q += WARPS) {
         const int64_t s = R.s0 + S.list[q];
-        const int a = (int)(max(start_of(A, s), R.c0) - R.c0), b = (int)(min(start_of(A, s + 1), R.c1) - R.c0);
-        double sum[4] = {0.0, 0.0, 0.0, 0.0};
-        int i = a + lane;
-        for (; i + 96 < b; i += 128) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += (double)S.diff[i + 32 * j];
-        }
-        for (; i < b; i += 32) sum[0] += (double)S.diff[i];
-        double all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-        if (lane == 0) A.pieces[chunk + s] = all;
+        const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
+        double sum = 0.0;
+        for (int i = a + lane; i < b; i += 32) sum += (double)S.diff[i];
+        sum = join(sum);
+        if (lane == 0) A.pieces[chunk + s] = sum;
     }
 }
 
@@ -172,53 +216,91 @@ __device__ __forceinline__ Outcome pair_outcome(const Args& A, int64_t p, double
 
 __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R, bool last) {
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    // a token's gradient stands where its sequence begins in this CTA; nothing else does
-    for (int i = t; i < CHUNK; i += THREADS) S.diff[i] = __int_as_float(NO_MARK);
-    __syncthreads();
-    auto mark = [&](int64_t a, int64_t b, float v) {
-        a = max(a, R.c0);
-        b = min(b, R.c1);
-        if (b > a) S.diff[a - R.c0] = v;
+    const bool few = R.s1 - R.s0 <= FEW;
+    const int n = few ? (int)(R.s1 - R.s0) : 0;
+    if (few) {
+        if (t <= n) S.bound[t] = R.within(start_of(A, R.s0 + t));
+    } else {
+        // a sequence's gradient stands where it begins in this CTA
+        for (int i = t; i < CHUNK; i += THREADS) S.diff[i] = __int_as_float(NO_MARK);
+        __syncthreads();
+    }
+    // of sequence s, which is tokens [a, b)
+    auto put = [&](int64_t s, int64_t a, int64_t b, float v) {
+        if (few) {
+            if (s >= R.s0 && s < R.s1) S.value[s - R.s0] = v;
+        } else {
+            const int i = R.within(a), j = R.within(b);
+            if (i < j) S.diff[i] = v;
+        }
+    };
+    auto pair_of = [&](int64_t p, int64_t (&at)[3]) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) at[q] = start_of(A, 2 * p + q);
+    };
+    auto settle = [&](int64_t p, const int64_t (&at)[3], double D0, double D1) {
+        // by the CTA in which the pair begins
+        const bool write = (at[0] >= R.c0 && at[0] < R.c1) || (last && at[0] >= R.c1);
+        const Outcome g = pair_outcome(A, p, D0, D1, at[1] - at[0], at[2] - at[1], write);
+        put(2 * p, at[0], at[1], g.d0);
+        put(2 * p + 1, at[1], at[2], g.d1);
     };
     const int64_t p0 = R.s0 / 2, p1 = (R.s1 + 1) / 2;
-    const int64_t end = start_of(A, 2 * A.pairs);
-    if (t == 0) {                                   // tokens of no sequence
-        mark(0, start_of(A, 0), 0.f);
-        mark(end, A.tokens, 0.f);
-    }
-    // pairs with many pieces are joined by the whole CTA: at most the first and the last have tokens elsewhere
-    for (int64_t p = p0; p < p1; p = p + 1 < p1 - 1 ? p1 - 1 : p + 1) {
-        const int64_t a = start_of(A, 2 * p), m = start_of(A, 2 * p + 1), b = start_of(A, 2 * p + 2);
-        int64_t k0, k1;
-        const int64_t n0 = pieces_of(a, m, &k0), n1 = pieces_of(m, b, &k1);
+    // Pairs of more pieces than one to a sequence have tokens in other CTAs too: they are the first or the last of this one.  A warp joins
+    // one, or all warps where the pieces are many.
+    for (int side = 0; side < 2; ++side) {
+        const int64_t p = side ? p1 - 1 : p0;
+        if (p >= p1 || (side && p == p0)) break;    // the same for the whole CTA
+        int64_t at[3], k[2];
+        pair_of(p, at);
+        const int64_t n0 = pieces_of(at[0], at[1], &k[0]), n1 = pieces_of(at[1], at[2], &k[1]);
+        const bool many = n0 + n1 > LONG;           // the same in every CTA: the order of the sum is
+        if (!many && warp != side) continue;
+        const int stride = many ? THREADS : 32, first = many ? t : lane;
         double D[2] = {0.0, 0.0};
-        for (int64_t i = t; i < n0; i += THREADS) D[0] += A.pieces[k0 + i + 2 * p];
-        for (int64_t i = t; i < n1; i += THREADS) D[1] += A.pieces[k1 + i + 2 * p + 1];
+        for (int64_t i = first; i < n0; i += stride) D[0] += A.pieces[k[0] + i + 2 * p];
+        for (int64_t i = first; i < n1; i += stride) D[1] += A.pieces[k[1] + i + 2 * p + 1];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) D[q] += __shfl_xor_sync(0xffffffffu, D[q], o);
-            __syncthreads();
-            if (lane == 0) S.joined[warp] = D[q];
-            __syncthreads();
-            D[q] = 0.0;
-            for (int w = 0; w < WARPS; ++w) D[q] += S.joined[w];
         }
-        if (t == 0) {
-            const Outcome g = pair_outcome(A, p, D[0], D[1], m - a, b - m, (a >= R.c0 && a < R.c1) || (last && a >= R.c1));
-            mark(a, m, g.d0);
-            mark(m, b, g.d1);
+        if (many) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                __syncthreads();
+                if (lane == 0) S.joined[warp] = D[q];
+                __syncthreads();
+                D[q] = 0.0;
+                for (int w = 0; w < WARPS; ++w) D[q] += S.joined[w];
+            }
         }
+        if (many ? t == 0 : lane == 0) settle(p, at, D[0], D[1]);
     }
     // the others lie within the CTA: one piece per sequence
-    for (int64_t p = p0 + 1 + t; p < p1 - 1; p += THREADS) {
-        const int64_t a = start_of(A, 2 * p), m = start_of(A, 2 * p + 1), b = start_of(A, 2 * p + 2);
-        const Outcome g = pair_outcome(A, p, m > a ? A.pieces[a / CHUNK + 2 * p] : 0.0, b > m ? A.pieces[m / CHUNK + 2 * p + 1] : 0.0,
-                                       m - a, b - m, true);
-        mark(a, m, g.d0);
-        mark(m, b, g.d1);
+    for (int64_t p = p0 + 1 + (t ^ 64); p < p1 - 1; p += THREADS) {            // beginning with warps that join nothing
+        int64_t at[3];
+        pair_of(p, at);
+        settle(p, at, at[1] > at[0] ? A.pieces[at[0] / CHUNK + 2 * p] : 0.0, at[2] > at[1] ? A.pieces[at[1] / CHUNK + 2 * p + 1] : 0.0);
     }
     if (!A.d_logp) return;
+    const int tokens = (int)(R.c1 - R.c0);
+    float* out = A.d_logp + R.c0;
+    if (few) {
+        __syncthreads();
+        const int begin = n ? S.bound[0] : tokens, end = n ? S.bound[n] : tokens;
+        for (int i = t; i < begin; i += THREADS) out[i] = 0.f;                 // tokens of no sequence
+        for (int q = 0; q < n; ++q) {
+            const float v = S.value[q];
+            for (int i = S.bound[q] + t; i < S.bound[q + 1]; i += THREADS) out[i] = v;
+        }
+        for (int i = end + t; i < tokens; i += THREADS) out[i] = 0.f;
+        return;
+    }
+    if (t == 0) {
+        const int end = R.within(start_of(A, 2 * A.pairs));
+        if (end < tokens) S.diff[end] = 0.f;
+    }
     __syncthreads();
     // every token takes the last mark at or before it
     float v[EACH];
@@ -229,14 +311,9 @@ __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R,
         if (__float_as_int(v[i]) != NO_MARK) mine = v[i];
     }
     // the last mark of the threads before this one
-    const bool have = __float_as_int(mine) != NO_MARK;
-    const uint32_t votes = __ballot_sync(0xffffffffu, have);
-    if (votes) {
-        const float of_warp = __shfl_sync(0xffffffffu, mine, 31 - __clz((int)votes));
-        if (lane == 0) S.last[warp] = __float_as_int(of_warp);
-    } else if (lane == 0) {
-        S.last[warp] = NO_MARK;
-    }
+    const uint32_t votes = __ballot_sync(0xffffffffu, __float_as_int(mine) != NO_MARK);
+    const float of_warp = __shfl_sync(0xffffffffu, mine, votes ? 31 - __clz((int)votes) : 0);
+    if (lane == 0) S.last[warp] = __float_as_int(of_warp);
     __syncthreads();
     float carry = 0.f;
     for (int w = 0; w < warp; ++w)
@@ -244,20 +321,13 @@ __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R,
     const uint32_t below = votes & ((1u << lane) - 1u);
     const float of_lane = __shfl_sync(0xffffffffu, mine, below ? 31 - __clz((int)below) : 0);
     if (below) carry = of_lane;
-    const int64_t at = R.c0 + (int64_t)t * EACH;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         if (__float_as_int(v[i]) != NO_MARK) carry = v[i];
-        v[i] = carry;
+        S.diff[t * EACH + i] = carry;
     }
-    if (A.vector_out && at + EACH <= A.tokens) {
-#pragma unroll
-        for (int i = 0; i < EACH; i += 4) store_vec<float, 4>(A.d_logp + at + i, Vec<float, 4>{{v[i], v[i + 1], v[i + 2], v[i + 3]}});
-    } else {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (at + i < A.tokens) A.d_logp[at + i] = v[i];
-    }
+    __syncthreads();
+    for (int i = t; i < tokens; i += THREADS) out[i] = S.diff[i];
 }
 
 enum Part { SUMS, FINISH, ALL };
@@ -269,9 +339,18 @@ __global__ void __launch_bounds__(THREADS) k_preference(const Args A) {
     const bool last = blockIdx.x + 1 == gridDim.x;
     successor_may_start();
     if (PART != FINISH) load_tokens(A, S, chunk * CHUNK);
-    const Range R = range_of(A, chunk, last);
-    if (PART == FINISH) successor_wait();           // the starts are the caller's: the search need not wait
-    if (PART != FINISH) sum_pieces(A, S, chunk, R);
+    Range R;
+    if (PART == FINISH) {
+        successor_wait();
+        R = Range{chunk * CHUNK, min((chunk + 1) * CHUNK, A.tokens), A.ranges[2 * chunk], A.ranges[2 * chunk + 1]};
+    } else {
+        R = range_of(A, chunk, last);
+        if (PART == SUMS && threadIdx.x == 0) {
+            A.ranges[2 * chunk] = R.s0;
+            A.ranges[2 * chunk + 1] = R.s1;
+        }
+        sum_pieces(A, S, chunk, R);
+    }
     if (PART == ALL) __syncthreads();
     if (PART != SUMS) finish(A, S, R, last);
 }
@@ -285,7 +364,7 @@ extern "C" {
 
 int ssgd_preference_loss_workspace(int64_t tokens, int64_t pairs, size_t* out_bytes) {
     if (!out_bytes || tokens < 0 || tokens > MAX_TOKENS || pairs < 0 || pairs > MAX_PAIRS) return SSGD_EINVAL;
-    *out_bytes = (size_t)(chunks_of(tokens) + 2 * pairs) * sizeof(double);
+    *out_bytes = (size_t)(3 * chunks_of(tokens) + 2 * pairs) * 8;
     return SSGD_OK;
 }
 
@@ -305,8 +384,10 @@ int ssgd_preference_loss(const float* logp, const float* ref_logp, int64_t token
         return SSGD_EALIGN;
     if (!workspace || workspace_bytes < need) return SSGD_EWORKSPACE;
     if (!aligned_to(workspace, 8)) return SSGD_EALIGN;
+    double* pieces = static_cast<double*>(workspace);
+    int64_t* ranges = reinterpret_cast<int64_t*>(pieces + chunks_of(tokens) + 2 * pairs);
     const Args A{logp, ref_logp, starts, starts_bytes == 8, weights, tokens, pairs, beta, label_smoothing, kind, average != 0, loss, rewards,
-                 d_logp, static_cast<double*>(workspace), aligned_to(logp, 16) && aligned_to(ref_logp, 16), aligned_to(d_logp, 16)};
+                 d_logp, pieces, ranges, aligned_to(logp, 16) && aligned_to(ref_logp, 16)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t chunks = chunks_of(tokens);
     if (chunks > 0x7fffffff) return SSGD_ETOOBIG;
