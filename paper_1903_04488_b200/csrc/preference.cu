@@ -30,8 +30,8 @@ struct Args {
     float* loss; float* rewards;                    // [pairs], [2][pairs]
     float* d_logp;                                  // [tokens] or NULL
     double* pieces;                                 // [chunks + 2 pairs]
-    int64_t* ranges;                                // [chunks][2], see Range
     bool vector;                                    // logp and ref are 16-byte aligned
+    double per_token;                               // starts to a token
 };
 
 // starts[s], kept within the tokens
@@ -45,114 +45,204 @@ constexpr int SHORT = 32;                           // where there are more, pie
 constexpr int LONG = 256;                           // pieces of a pair that the whole CTA joins
 constexpr int32_t NO_MARK = 0x7fa12345;             // the bits of a NaN that no operation makes
 struct Shared {
-    float diff[CHUNK];                              // then the gradients
-    int32_t bound[FEW + 1];                         // where the sequences begin within the CTA's tokens
+    alignas(16) float logp[CHUNK];                  // then the gradients
+    alignas(16) float ref[CHUNK];
+    int64_t start[FEW + 1];                         // where the sequences begin
+    int32_t bound[FEW + 1];                         // the same within the CTA's tokens
     float value[FEW];                               // their gradients
     union {
-        double part[WARPS][FEW];
+        float2 part[WARPS][FEW];
         int32_t list[CHUNK / SHORT + 1];
     };
+    int2 before[WARPS];
     int32_t listed;
     int32_t last[WARPS];
     double joined[WARPS];
 };
 
-// Tokens of the CTA, and the sequences that may have some of them: from the last one that starts before the first token to the last one
-// that starts before the end.  The last CTA has those too that start at the end.
+// Tokens of the CTA, and the sequences that may have some of them, in whole pairs: from the last one that starts before the first token to
+// the last one that starts before the end.  The last CTA has those too that start at the end.
 struct Range {
     int64_t c0, c1, s0, s1;
+    __device__ __forceinline__ bool few() const { return s1 - s0 <= FEW; }
     __device__ __forceinline__ int within(int64_t token) const { return (int)((token < c0 ? c0 : token > c1 ? c1 : token) - c0); }
 };
 
-// The whole CTA searches, 256 places at a time, for the first starts that are at least c0 and at least c1.
-__device__ __forceinline__ Range range_of(const Args& A, int64_t chunk, bool last) {
-    Range R;
-    R.c0 = chunk * CHUNK;
-    R.c1 = min(R.c0 + CHUNK, A.tokens);
-    const int64_t n = 2 * A.pairs + 1;
-    int64_t lo[2] = {0, 0}, hi[2] = {chunk == 0 ? 0 : n, last ? 0 : n};
-    while (lo[0] < hi[0] || lo[1] < hi[1]) {
-        bool below[2];
-        int64_t step[2];
+// The CTA's range, and the starts of its sequences in shared memory where they are few.  What is looked for are the first starts that
+// are at least c0 and at least c1.  Lengths that are not too unlike put them near chunk / chunks of the way, so the whole CTA looks at
+// 1024 starts there; where they are not among them, it searches, 256 places at a time.
+constexpr int LOOK = 4, WINDOW = LOOK * THREADS;
+struct Window {
+    int64_t w0, v[LOOK];                            // the thread's starts w0 + t + i THREADS
+    __device__ __forceinline__ void load(const Args& A, int64_t chunk) {
+        const int64_t n = 2 * A.pairs + 1;
+        w0 = max(min((int64_t)((double)(chunk * CHUNK + CHUNK / 2) * A.per_token) - WINDOW / 2, n - WINDOW), (int64_t)0);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            step[q] = (hi[q] - lo[q] + THREADS - 1) / THREADS;
-            const int64_t at = lo[q] + (int64_t)threadIdx.x * step[q];
-            below[q] = at < hi[q] && start_of(A, at) < (q ? R.c1 : R.c0);
-        }
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int k = __syncthreads_count(below[q]);   // places lo, lo + step, .. that are before the answer
-            if (lo[q] >= hi[q]) continue;
-            const int64_t from = k ? lo[q] + (int64_t)(k - 1) * step[q] + 1 : lo[q];
-            hi[q] = k ? min(hi[q], lo[q] + (int64_t)k * step[q]) : lo[q];
-            lo[q] = from;
+        for (int i = 0; i < LOOK; ++i) {
+            const int64_t at = w0 + threadIdx.x + i * THREADS;
+            v[i] = at < n ? start_of(A, at) : INT64_MAX;
         }
     }
-    R.s0 = max(lo[0] - 1, (int64_t)0);
-    R.s1 = last ? 2 * A.pairs : min(lo[1], 2 * A.pairs);
-    if (R.s1 < R.s0) R.s1 = R.s0;                   // starts that do not ascend
-    return R;
+    __device__ __forceinline__ Range range(const Args& A, Shared& S, int64_t chunk, int64_t chunks) const {
+        const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+        const bool last = chunk + 1 == chunks;
+        Range R;
+        R.c0 = chunk * CHUNK;
+        R.c1 = min(R.c0 + CHUNK, A.tokens);
+        const int64_t n = 2 * A.pairs + 1;
+        int k0 = 0, k1 = 0;
+#pragma unroll
+        for (int i = 0; i < LOOK; ++i) {
+            k0 += __popc(__ballot_sync(0xffffffffu, v[i] < R.c0));
+            k1 += __popc(__ballot_sync(0xffffffffu, v[i] < R.c1));
+        }
+        if (lane == 0) S.before[warp] = make_int2(k0, k1);
+        __syncthreads();
+        k0 = k1 = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            k0 += S.before[w].x;
+            k1 += S.before[w].y;
+        }
+        int64_t lo[2] = {w0 + k0, w0 + k1};
+        const bool found = (k0 >= 2 || w0 == 0) && (k1 <= WINDOW - 2 || w0 + WINDOW >= n);     // with the starts of whole pairs around them
+        if (!found) {
+            lo[0] = lo[1] = 0;
+            int64_t hi[2] = {n, n};
+            while (lo[0] < hi[0] || lo[1] < hi[1]) {
+                bool below[2];
+                int64_t step[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    step[q] = (hi[q] - lo[q] + THREADS - 1) / THREADS;
+                    const int64_t probe = lo[q] + (int64_t)t * step[q];
+                    below[q] = probe < hi[q] && start_of(A, probe) < (q ? R.c1 : R.c0);
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int k = __syncthreads_count(below[q]);               // places lo, lo + step, .. that are before the answer
+                    if (lo[q] >= hi[q]) continue;
+                    const int64_t from = k ? lo[q] + (int64_t)(k - 1) * step[q] + 1 : lo[q];
+                    hi[q] = k ? min(hi[q], lo[q] + (int64_t)k * step[q]) : lo[q];
+                    lo[q] = from;
+                }
+            }
+        }
+        R.s0 = min(max(lo[0] - 1, (int64_t)0) & ~(int64_t)1, 2 * A.pairs);
+        R.s1 = last ? 2 * A.pairs : min((lo[1] + 1) & ~(int64_t)1, 2 * A.pairs);
+        if (R.s1 < R.s0) R.s1 = R.s0;               // starts that do not ascend
+        if (R.few()) {
+            const int count = (int)(R.s1 - R.s0);
+            auto keep = [&](int i, int64_t start) {
+                S.start[i] = start;
+                S.bound[i] = R.within(start);
+            };
+            if (found && R.s0 >= w0 && R.s1 < w0 + WINDOW) {
+#pragma unroll
+                for (int i = 0; i < LOOK; ++i) {
+                    const int64_t at = w0 + t + i * THREADS - R.s0;
+                    if (at >= 0 && at <= count) keep((int)at, v[i]);
+                }
+            } else if (t <= count) {
+                keep(t, start_of(A, R.s0 + t));
+            }
+        }
+        return R;
+    }
+};
+
+// A sum with what its roundings lost beside it: 48 bits or more, in fp32 arithmetic (an SM converts to 64 bits at 16 numbers a cycle)
+struct Sum {
+    float sum = 0.f, lost = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        const float next = sum + x, back = next - sum;
+        lost += (sum - (next - back)) + (x - back);
+        sum = next;
+    }
+    __device__ __forceinline__ void join_warp() {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const float x = __shfl_xor_sync(0xffffffffu, sum, o), l = __shfl_xor_sync(0xffffffffu, lost, o);
+            add(x);
+            lost += l;
+        }
+    }
+    // an infinity or NaN among the numbers leaves NaN in what was lost
+    __device__ __forceinline__ double value() const { return fabsf(sum) < INFINITY ? (double)sum + (double)lost : (double)sum; }
+};
+
+// A piece's sum from those of the warps
+__device__ __forceinline__ double sum_of_warps(const Shared& S, int q) {
+    Sum sum;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        const float2 p = S.part[w][q];
+        sum.add(p.x);
+        sum.lost += p.y;
+    }
+    return sum.value();
 }
 
-// The CTA's tokens into shared memory
-__device__ __forceinline__ void load_tokens(const Args& A, Shared& S, int64_t c0) {
+// Every warp has an eighth of the CTA's tokens: calls f(q, a, b) for each of n sequences that has some of them, [a, b)
+template <typename F>
+__device__ __forceinline__ void for_pieces(const Shared& S, int n, F f) {
+    const int lane = threadIdx.x & 31, begin = ((int)threadIdx.x >> 5) * (CHUNK / WARPS), end = begin + CHUNK / WARPS;
+    for (int base = 0; base < n; base += 32) {
+        const int q = base + lane;
+        int a = 0, b = 0;
+        if (q < n) {
+            a = max(S.bound[q], begin);
+            b = min(S.bound[q + 1], end);
+        }
+        for (uint32_t todo = __ballot_sync(0xffffffffu, a < b); todo; todo &= todo - 1) {
+            const int src = __ffs(todo) - 1;
+            f(base + src, __shfl_sync(0xffffffffu, a, src), __shfl_sync(0xffffffffu, b, src));
+        }
+    }
+}
+
+// The CTA's tokens on their way to shared memory while it looks for its sequences.  16 bytes at once, or single ones
+__device__ __forceinline__ void start_tokens(const Args& A, Shared& S, int64_t c0) {
     const int64_t left = A.tokens - c0;
-    if (A.vector && left >= CHUNK) {
+    if (A.vector && left >= CHUNK) {                // the same for the whole CTA
 #pragma unroll
         for (int i = 0; i < EACH / 4; ++i) {
             const int at = (i * THREADS + (int)threadIdx.x) * 4;
-            const Vec<float, 4> x = load_vec_stream<float, 4>(A.logp + c0 + at);
-            Vec<float, 4> y{};
-            if (A.ref) y = load_vec_stream<float, 4>(A.ref + c0 + at);
-            store_vec<float, 4>(S.diff + at, Vec<float, 4>{{x.e[0] - y.e[0], x.e[1] - y.e[1], x.e[2] - y.e[2], x.e[3] - y.e[3]}});
+            copy_async<16>(S.logp + at, A.logp + c0 + at);
+            if (A.ref) copy_async<16>(S.ref + at, A.ref + c0 + at);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int at = i * THREADS + (int)threadIdx.x;
-            if (at < left) S.diff[at] = A.logp[c0 + at] - (A.ref ? A.ref[c0 + at] : 0.f);
+            if (at < left) {
+                copy_async<4>(S.logp + at, A.logp + c0 + at);
+                if (A.ref) copy_async<4>(S.ref + at, A.ref + c0 + at);
+            }
         }
     }
-    if (threadIdx.x == 0) S.listed = 0;
-    __syncthreads();
+    copy_async_commit();
 }
+__device__ __forceinline__ float difference(const Args& A, const Shared& S, int i) { return A.ref ? S.logp[i] - S.ref[i] : S.logp[i]; }
 
 // Sums of the pieces of the CTA's tokens, in 64 bits.  Each is added up by itself, so that what one sequence holds (infinities,
-// the lowest number of a mask) stays there.
+// the lowest number of a mask) stays there.  WRITE: for other CTAs; otherwise those of few sequences are left in S.part alone.
+template <bool WRITE>
 __device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, int64_t chunk, const Range& R) {
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    auto join = [&](double v) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
-    };
-    if (R.s1 - R.s0 <= FEW) {                       // every warp takes an eighth of the tokens
+    if (R.few()) {                                  // every warp takes an eighth of the tokens
         const int n = (int)(R.s1 - R.s0);
-        if (t <= n) S.bound[t] = R.within(start_of(A, R.s0 + t));
+        for (int i = lane; i < n; i += 32) S.part[warp][i] = make_float2(0.f, 0.f);
+        __syncwarp();
+        for_pieces(S, n, [&](int q, int a, int b) {
+            Sum sum;
+#pragma unroll 4
+            for (int i = a + lane; i < b; i += 32) sum.add(difference(A, S, i));
+            sum.join_warp();
+            if (lane == 0) S.part[warp][q] = make_float2(sum.sum, sum.lost);
+        });
         __syncthreads();
-        constexpr int SPAN = CHUNK / WARPS;
-        for (int q = 0; q < n; ++q) {
-            const int a = max(S.bound[q], warp * SPAN), b = min(S.bound[q + 1], (warp + 1) * SPAN);
-            double sum[2] = {0.0, 0.0};
-            if (a < b) {
-                int i = a + lane;
-                for (; i + 32 < b; i += 64) {
-                    sum[0] += (double)S.diff[i];
-                    sum[1] += (double)S.diff[i + 32];
-                }
-                if (i < b) sum[0] += (double)S.diff[i];
-                sum[0] = join(sum[0] + sum[1]);
-            }
-            if (lane == 0) S.part[warp][q] = sum[0];
-        }
-        __syncthreads();
-        if (t < n && S.bound[t] < S.bound[t + 1]) {
-            double sum = 0.0;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) sum += S.part[w][t];
-            A.pieces[chunk + R.s0 + t] = sum;
-        }
+        if (WRITE && t < n && S.bound[t] < S.bound[t + 1]) A.pieces[chunk + R.s0 + t] = sum_of_warps(S, t);
         return;
     }
     for (int64_t s = R.s0 + t; s < R.s1; s += THREADS) {
@@ -161,19 +251,19 @@ __device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, int64_t chu
             const int at = atomicAdd(&S.listed, 1);
             if (at <= CHUNK / SHORT) S.list[at] = (int32_t)(s - R.s0);         // more only where starts do not ascend
         } else if (b > a) {
-            double sum = 0.0;
-            for (int i = a; i < b; ++i) sum += (double)S.diff[i];
-            A.pieces[chunk + s] = sum;
+            Sum sum;
+            for (int i = a; i < b; ++i) sum.add(difference(A, S, i));
+            A.pieces[chunk + s] = sum.value();
         }
     }
     __syncthreads();
     for (int q = warp; q < min(S.listed, CHUNK / SHORT + 1); q += WARPS) {
         const int64_t s = R.s0 + S.list[q];
         const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
-        double sum = 0.0;
-        for (int i = a + lane; i < b; i += 32) sum += (double)S.diff[i];
-        sum = join(sum);
-        if (lane == 0) A.pieces[chunk + s] = sum;
+        Sum sum;
+        for (int i = a + lane; i < b; i += 32) sum.add(difference(A, S, i));
+        sum.join_warp();
+        if (lane == 0) A.pieces[chunk + s] = sum.value();
     }
 }
 
@@ -199,12 +289,11 @@ __device__ __forceinline__ int64_t pieces_of(int64_t a, int64_t b, int64_t* firs
 
 // Of one pair: sums -> loss, rewards, gradients
 struct Outcome { float d0, d1; };
-__device__ __forceinline__ Outcome pair_outcome(const Args& A, int64_t p, double D0, double D1, int64_t n0, int64_t n1, bool write) {
+__device__ __forceinline__ Outcome pair_outcome(const Args& A, int64_t p, float w, double D0, double D1, int64_t n0, int64_t n1, bool write) {
     double f0 = 1.0, f1 = 1.0;
     if (A.average) { f0 = n0 > 0 ? 1.0 / (double)n0 : 0.0; f1 = n1 > 0 ? 1.0 / (double)n1 : 0.0; }
     const double r0 = (double)A.beta * (D0 * f0), r1 = (double)A.beta * (D1 * f1);
     const float2 l = loss_of(A, (float)(r0 - r1));
-    const float w = A.weights ? A.weights[p] : 1.f;
     if (write) {
         A.loss[p] = w == 0.f ? 0.f : w * l.x;
         A.rewards[p] = (float)r0;
@@ -214,74 +303,94 @@ __device__ __forceinline__ Outcome pair_outcome(const Args& A, int64_t p, double
     return Outcome{A.average ? (float)((double)slope * f0) : slope, A.average ? (float)(-(double)slope * f1) : -slope};
 }
 
+// ALONE: there is no other CTA
+template <bool ALONE>
 __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R, bool last) {
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const bool few = R.s1 - R.s0 <= FEW;
+    const bool few = R.few();
     const int n = few ? (int)(R.s1 - R.s0) : 0;
-    if (few) {
-        if (t <= n) S.bound[t] = R.within(start_of(A, R.s0 + t));
-    } else {
+    if (!few) {
         // a sequence's gradient stands where it begins in this CTA
-        for (int i = t; i < CHUNK; i += THREADS) S.diff[i] = __int_as_float(NO_MARK);
+        for (int i = t; i < CHUNK; i += THREADS) S.logp[i] = __int_as_float(NO_MARK);
         __syncthreads();
     }
     // of sequence s, which is tokens [a, b)
     auto put = [&](int64_t s, int64_t a, int64_t b, float v) {
         if (few) {
-            if (s >= R.s0 && s < R.s1) S.value[s - R.s0] = v;
+            S.value[s - R.s0] = v;
         } else {
             const int i = R.within(a), j = R.within(b);
-            if (i < j) S.diff[i] = v;
+            if (i < j) S.logp[i] = v;
         }
     };
     auto pair_of = [&](int64_t p, int64_t (&at)[3]) {
 #pragma unroll
-        for (int q = 0; q < 3; ++q) at[q] = start_of(A, 2 * p + q);
+        for (int q = 0; q < 3; ++q) at[q] = few ? S.start[2 * p + q - R.s0] : start_of(A, 2 * p + q);
     };
-    auto settle = [&](int64_t p, const int64_t (&at)[3], double D0, double D1) {
+    auto settle = [&](int64_t p, const int64_t (&at)[3], float w, double D0, double D1) {
         // by the CTA in which the pair begins
         const bool write = (at[0] >= R.c0 && at[0] < R.c1) || (last && at[0] >= R.c1);
-        const Outcome g = pair_outcome(A, p, D0, D1, at[1] - at[0], at[2] - at[1], write);
+        const Outcome g = pair_outcome(A, p, w, D0, D1, at[1] - at[0], at[2] - at[1], write);
         put(2 * p, at[0], at[1], g.d0);
         put(2 * p + 1, at[1], at[2], g.d1);
     };
-    const int64_t p0 = R.s0 / 2, p1 = (R.s1 + 1) / 2;
-    // Pairs of more pieces than one to a sequence have tokens in other CTAs too: they are the first or the last of this one.  A warp joins
-    // one, or all warps where the pieces are many.
-    for (int side = 0; side < 2; ++side) {
-        const int64_t p = side ? p1 - 1 : p0;
-        if (p >= p1 || (side && p == p0)) break;    // the same for the whole CTA
-        int64_t at[3], k[2];
-        pair_of(p, at);
-        const int64_t n0 = pieces_of(at[0], at[1], &k[0]), n1 = pieces_of(at[1], at[2], &k[1]);
-        const bool many = n0 + n1 > LONG;           // the same in every CTA: the order of the sum is
-        if (!many && warp != side) continue;
-        const int stride = many ? THREADS : 32, first = many ? t : lane;
-        double D[2] = {0.0, 0.0};
-        for (int64_t i = first; i < n0; i += stride) D[0] += A.pieces[k[0] + i + 2 * p];
-        for (int64_t i = first; i < n1; i += stride) D[1] += A.pieces[k[1] + i + 2 * p + 1];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) D[q] += __shfl_xor_sync(0xffffffffu, D[q], o);
+    auto weight_of = [&](int64_t p) { return A.weights ? A.weights[p] : 1.f; };
+    const int64_t p0 = R.s0 / 2, p1 = R.s1 / 2;
+    if (ALONE && few) {
+        if (p0 + t < p1) {
+            int64_t at[3];
+            pair_of(p0 + t, at);
+            settle(p0 + t, at, weight_of(p0 + t), sum_of_warps(S, 2 * t), sum_of_warps(S, 2 * t + 1));
         }
-        if (many) {
+    } else {
+        // Pairs of more pieces than one to a sequence have tokens in other CTAs too: they are the first or the last of this one.  A warp
+        // joins one, or all warps where the pieces are many.
+        for (int side = 0; side < 2; ++side) {
+            const int64_t p = side ? p1 - 1 : p0;
+            if (p >= p1 || (side && p == p0)) break;    // the same for the whole CTA
+            int64_t at[3], k[2];
+            pair_of(p, at);
+            const int64_t n0 = pieces_of(at[0], at[1], &k[0]), n1 = pieces_of(at[1], at[2], &k[1]);
+            const bool many = n0 + n1 > LONG;           // the same in every CTA: the order of the sum is
+            if (!many && warp != side) continue;
+            const int stride = many ? THREADS : 32, first = many ? t : lane;
+            const float w = weight_of(p);
+            double D[2] = {0.0, 0.0};
+            if (n0 <= 4 && n1 <= 4) {                   // the usual case: one lane adds them up
+                if (lane != 0) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (i < n0) D[0] += A.pieces[k[0] + i + 2 * p];
+                    if (i < n1) D[1] += A.pieces[k[1] + i + 2 * p + 1];
+                }
+                settle(p, at, w, D[0], D[1]);
+                continue;
+            }
+            for (int64_t i = first; i < n0; i += stride) D[0] += A.pieces[k[0] + i + 2 * p];
+            for (int64_t i = first; i < n1; i += stride) D[1] += A.pieces[k[1] + i + 2 * p + 1];
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                __syncthreads();
-                if (lane == 0) S.joined[warp] = D[q];
-                __syncthreads();
-                D[q] = 0.0;
-                for (int w = 0; w < WARPS; ++w) D[q] += S.joined[w];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) D[q] += __shfl_xor_sync(0xffffffffu, D[q], o);
             }
+            if (many) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    __syncthreads();
+                    if (lane == 0) S.joined[warp] = D[q];
+                    __syncthreads();
+                    D[q] = 0.0;
+                    for (int i = 0; i < WARPS; ++i) D[q] += S.joined[i];
+                }
+            }
+            if (many ? t == 0 : lane == 0) settle(p, at, w, D[0], D[1]);
         }
-        if (many ? t == 0 : lane == 0) settle(p, at, D[0], D[1]);
-    }
-    // the others lie within the CTA: one piece per sequence
-    for (int64_t p = p0 + 1 + (t ^ 64); p < p1 - 1; p += THREADS) {            // beginning with warps that join nothing
-        int64_t at[3];
-        pair_of(p, at);
-        settle(p, at, at[1] > at[0] ? A.pieces[at[0] / CHUNK + 2 * p] : 0.0, at[2] > at[1] ? A.pieces[at[1] / CHUNK + 2 * p + 1] : 0.0);
+        // the others lie within the CTA: one piece per sequence
+        for (int64_t p = p0 + 1 + (t ^ 64); p < p1 - 1; p += THREADS) {        // beginning with warps that join nothing
+            int64_t at[3];
+            pair_of(p, at);
+            settle(p, at, weight_of(p), at[1] > at[0] ? A.pieces[at[0] / CHUNK + 2 * p] : 0.0, at[2] > at[1] ? A.pieces[at[1] / CHUNK + 2 * p + 1] : 0.0);
+        }
     }
     if (!A.d_logp) return;
     const int tokens = (int)(R.c1 - R.c0);
@@ -290,16 +399,16 @@ __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R,
         __syncthreads();
         const int begin = n ? S.bound[0] : tokens, end = n ? S.bound[n] : tokens;
         for (int i = t; i < begin; i += THREADS) out[i] = 0.f;                 // tokens of no sequence
-        for (int q = 0; q < n; ++q) {
+        for_pieces(S, n, [&](int q, int a, int b) {
             const float v = S.value[q];
-            for (int i = S.bound[q] + t; i < S.bound[q + 1]; i += THREADS) out[i] = v;
-        }
+            for (int i = a + lane; i < b; i += 32) out[i] = v;
+        });
         for (int i = end + t; i < tokens; i += THREADS) out[i] = 0.f;
         return;
     }
     if (t == 0) {
         const int end = R.within(start_of(A, 2 * A.pairs));
-        if (end < tokens) S.diff[end] = 0.f;
+        if (end < tokens) S.logp[end] = 0.f;
     }
     __syncthreads();
     // every token takes the last mark at or before it
@@ -307,7 +416,7 @@ __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R,
     float mine = __int_as_float(NO_MARK);
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        v[i] = S.diff[t * EACH + i];
+        v[i] = S.logp[t * EACH + i];
         if (__float_as_int(v[i]) != NO_MARK) mine = v[i];
     }
     // the last mark of the threads before this one
@@ -324,35 +433,41 @@ __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R,
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         if (__float_as_int(v[i]) != NO_MARK) carry = v[i];
-        S.diff[t * EACH + i] = carry;
+        S.logp[t * EACH + i] = carry;
     }
     __syncthreads();
-    for (int i = t; i < tokens; i += THREADS) out[i] = S.diff[i];
+    for (int i = t; i < tokens; i += THREADS) out[i] = S.logp[i];
 }
 
 enum Part { SUMS, FINISH, ALL };
 
 template <Part PART>
-__global__ void __launch_bounds__(THREADS) k_preference(const Args A) {
+__global__ void __launch_bounds__(THREADS, 6) k_preference(const Args A) {
     __shared__ Shared S;
     const int64_t chunk = blockIdx.x;
     const bool last = blockIdx.x + 1 == gridDim.x;
-    successor_may_start();
-    if (PART != FINISH) load_tokens(A, S, chunk * CHUNK);
-    Range R;
-    if (PART == FINISH) {
+    if constexpr (PART == FINISH) {
+        Window W;
+        W.load(A, chunk);
+        const Range R = W.range(A, S, chunk, gridDim.x);                       // what the caller gave need not wait for the sums
         successor_wait();
-        R = Range{chunk * CHUNK, min((chunk + 1) * CHUNK, A.tokens), A.ranges[2 * chunk], A.ranges[2 * chunk + 1]};
+        __syncthreads();
+        finish<false>(A, S, R, last);
     } else {
-        R = range_of(A, chunk, last);
-        if (PART == SUMS && threadIdx.x == 0) {
-            A.ranges[2 * chunk] = R.s0;
-            A.ranges[2 * chunk + 1] = R.s1;
+        successor_may_start();
+        Window W;
+        W.load(A, chunk);
+        start_tokens(A, S, chunk * CHUNK);
+        const Range R = W.range(A, S, chunk, gridDim.x);
+        if (threadIdx.x == 0) S.listed = 0;
+        copy_async_wait<0>();
+        __syncthreads();
+        sum_pieces<PART == SUMS>(A, S, chunk, R);
+        if constexpr (PART == ALL) {
+            __syncthreads();
+            finish<true>(A, S, R, last);
         }
-        sum_pieces(A, S, chunk, R);
     }
-    if (PART == ALL) __syncthreads();
-    if (PART != SUMS) finish(A, S, R, last);
 }
 
 constexpr int64_t MAX_TOKENS = (int64_t)1 << 40, MAX_PAIRS = (int64_t)1 << 30;
@@ -364,7 +479,7 @@ extern "C" {
 
 int ssgd_preference_loss_workspace(int64_t tokens, int64_t pairs, size_t* out_bytes) {
     if (!out_bytes || tokens < 0 || tokens > MAX_TOKENS || pairs < 0 || pairs > MAX_PAIRS) return SSGD_EINVAL;
-    *out_bytes = (size_t)(3 * chunks_of(tokens) + 2 * pairs) * 8;
+    *out_bytes = (size_t)(chunks_of(tokens) + 2 * pairs) * sizeof(double);
     return SSGD_OK;
 }
 
@@ -384,12 +499,11 @@ int ssgd_preference_loss(const float* logp, const float* ref_logp, int64_t token
         return SSGD_EALIGN;
     if (!workspace || workspace_bytes < need) return SSGD_EWORKSPACE;
     if (!aligned_to(workspace, 8)) return SSGD_EALIGN;
-    double* pieces = static_cast<double*>(workspace);
-    int64_t* ranges = reinterpret_cast<int64_t*>(pieces + chunks_of(tokens) + 2 * pairs);
-    const Args A{logp, ref_logp, starts, starts_bytes == 8, weights, tokens, pairs, beta, label_smoothing, kind, average != 0, loss, rewards,
-                 d_logp, pieces, ranges, aligned_to(logp, 16) && aligned_to(ref_logp, 16)};
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t chunks = chunks_of(tokens);
+    const Args A{logp, ref_logp, starts, starts_bytes == 8, weights, tokens, pairs, beta, label_smoothing, kind, average != 0, loss, rewards,
+                 d_logp, static_cast<double*>(workspace), aligned_to(logp, 16) && aligned_to(ref_logp, 16),
+                 tokens ? (double)(2 * pairs + 1) / (double)tokens : 0.0};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (chunks > 0x7fffffff) return SSGD_ETOOBIG;
     if (chunks == 1) {
         k_preference<ALL><<<1, THREADS, 0, st>>>(A);
