@@ -1,7 +1,7 @@
 """A small language model trained by simulated data-parallel workers on one GPU: the operators around the compression step
 and the step itself, together.
 
-    python -m paper_1903_04488_b200.train_lm [--steps 150] [--workers 4] [--state e4m3] ...
+    python -m paper_1903_04488_b200.train_lm [--steps 150] [--workers 4] [--state e4m3] [--tune 20 --tune-loss policy] ...
 
 Every worker computes the gradient of its own batch: a residual network over token embeddings whose norms are
 `autograd.layer_norm` and whose loss is `autograd.token_logprobs`.  The matrices live in one flat vector, and their
@@ -10,10 +10,15 @@ accumulation, sketch, second round); the model moves along these.  Biases and no
 leaves bias terms uncompressed, Section 5): their gradients are averaged and `train_ops.AdamW` takes them in one launch.
 
 The data is synthetic: the next token is a fixed permutation of the current one, or, one time in ten, any token.
+
+`tune` goes on from there as fine-tuning does, on one worker and without compression: the model's own samples are rewarded where they
+are the permutation's token (`train_ops.policy_loss`, with the trained model as the reference), or compared with it in pairs
+(`autograd.preference_loss`); `train_ops.Muon` takes the blocks' matrices and AdamW everything else.
 """
 from __future__ import annotations
 
 import argparse
+import copy
 import math
 
 import torch
@@ -63,8 +68,10 @@ def batch(vocab: int, n: int, perm: torch.Tensor, gen: torch.Generator):
 
 
 def train(steps: int = 150, workers: int = 4, vocab: int = 256, dim: int = 64, layers: int = 2, tokens: int = 1024,
-          lr: float = 0.1, rho: float = 0.9, small_lr: float = 3e-3, state: str = "f32", report_every: int = 25, quiet: bool = False):
-    """Returns [(step, mean loss, mean entropy, share of tokens that are the model's best)] at the reported steps."""
+          lr: float = 0.1, rho: float = 0.9, small_lr: float = 3e-3, state: str = "f32", report_every: int = 25, quiet: bool = False,
+          tune_steps: int = 0, tune_loss: str = "policy"):
+    """Returns [(step, mean loss, mean entropy, share of tokens that are the model's best)] at the reported steps.  tune_steps: `tune`
+    the model afterwards."""
     device = torch.device("cuda", torch.cuda.current_device())
     model = Model(vocab, dim, layers, device)
     W, d = workers, model.d
@@ -103,7 +110,79 @@ def train(steps: int = 150, workers: int = 4, vocab: int = 256, dim: int = 64, l
     if eng.status() != ssgd.OK:
         raise RuntimeError("the compression step reported an error")
     eng.flush()
+    if tune_steps:
+        tune(model, perm, gen, tune_steps, tokens, tune_loss, quiet=quiet)
     return report
+
+
+class Tuner:
+    """What `tune` keeps: the reference, and an optimizer for the blocks' matrices and one for the rest."""
+
+    def __init__(self, model: Model, lr: float = 2e-3, matrix_lr: float = 5e-3):
+        self.model, self.reference = model, copy.deepcopy(model)
+        self.blocks = model.matrices[1:-1]
+        self.rest = [model.matrices[0], model.matrices[-1], *model.small]
+        self.muon = train_ops.Muon(self.blocks, lr=matrix_lr) if self.blocks else None
+        self.adamw = train_ops.AdamW(self.rest, lr=lr, weight_decay=0.0)
+
+    def policy(self, cur, sampled, old_logp, advantages, kl: float = 0.05):
+        """Gradients of the clipped policy loss of sampled tokens; its statistics."""
+        with torch.no_grad():
+            ref = train_ops.token_logprobs(self.reference.logits(cur), sampled).logp
+        logits = self.model.logits(cur)
+        r = train_ops.policy_loss(logits.detach(), sampled, old_logp, advantages, ref_logp=ref, weights=torch.full_like(ref, 1.0 / ref.numel()),
+                                  kl=kl, entropy=0.001)
+        logits.backward(r.dlogits)
+        return r
+
+    def preference(self, cur, chosen, rejected, length: int = 8, beta: float = 0.5):
+        """Gradients of the preference loss of pairs of `length` tokens; the mean loss."""
+        n = cur.numel() // length * length
+        inputs = cur[:n].view(-1, 1, length).expand(-1, 2, length).reshape(-1)
+        ids = torch.stack([chosen[:n].view(-1, length), rejected[:n].view(-1, length)], 1).reshape(-1)
+        starts = torch.arange(0, 2 * n + 1, length, device=cur.device)
+        with torch.no_grad():
+            ref = train_ops.token_logprobs(self.reference.logits(inputs), ids).logp
+        loss, _ = autograd.preference_loss(autograd.token_logprobs(self.model.logits(inputs), ids)[0], ref, starts, beta=beta)
+        loss.mean().backward()
+        return loss.mean().detach()
+
+    def step(self):
+        if self.muon is not None:
+            self.muon.step([p.grad for p in self.blocks])
+        self.adamw.step([p.grad for p in self.rest])
+        for p in [*self.blocks, *self.rest]:
+            p.grad = None
+
+
+def tune(model: Model, perm: torch.Tensor, gen: torch.Generator, steps: int, tokens: int, loss: str = "policy", updates: int = 2, quiet: bool = False):
+    """Returns the share of sampled tokens that were the permutation's, at each step."""
+    if loss not in ("policy", "preference"):
+        raise ValueError('loss: "policy" or "preference"')
+    tuner = Tuner(model)
+    for p in [*tuner.blocks, *tuner.rest]:
+        p.grad = None                                               # it was a piece of the workers' rows
+    shares = []
+    for step in range(steps):
+        cur, _ = batch(perm.numel(), tokens, perm, gen)
+        with torch.no_grad():
+            logits = model.logits(cur)
+            sampled = torch.multinomial(torch.softmax(logits, -1), 1, generator=gen).squeeze(1)
+            old_logp = train_ops.token_logprobs(logits, sampled).logp
+            reward = (sampled == perm[cur]).float()
+        shares.append(reward.mean())
+        for _ in range(updates):
+            if loss == "policy":
+                tuner.policy(cur, sampled, old_logp, reward - reward.mean())
+            else:
+                tuner.preference(cur, perm[cur], sampled)
+            with torch.no_grad():
+                tuner.step()
+    train_ops.status()
+    shares = torch.stack(shares).tolist() if shares else []
+    if shares and not quiet:
+        print("tuned: samples right %.3f -> %.3f" % (shares[0], shares[-1]))
+    return shares
 
 
 def main() -> None:
@@ -116,8 +195,10 @@ def main() -> None:
     ap.add_argument("--tokens", type=int, default=1024, help="tokens per worker and step")
     ap.add_argument("--lr", type=float, default=0.1)
     ap.add_argument("--state", choices=("f32", "e4m3"), default="f32", help="how AdamW holds its states")
+    ap.add_argument("--tune", type=int, default=0, help="steps of fine-tuning afterwards")
+    ap.add_argument("--tune-loss", choices=("policy", "preference"), default="policy")
     a = ap.parse_args()
-    train(a.steps, a.workers, a.vocab, a.dim, a.layers, a.tokens, a.lr, state=a.state)
+    train(a.steps, a.workers, a.vocab, a.dim, a.layers, a.tokens, a.lr, state=a.state, tune_steps=a.tune, tune_loss=a.tune_loss)
 
 
 if __name__ == "__main__":
