@@ -136,6 +136,55 @@ __device__ __forceinline__ void load_block(const Matrix& M, int r0, int c0, bool
     }
 }
 
+// The thread's i-th four numbers of a block: the new momentum, left in s.m, and what is to be made orthogonal
+template <typename T>
+__device__ __forceinline__ float4 momentum_of(const Common& C, const Matrix& M, Share<T>& s, int i, float mu, float scale) {
+    float u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        u[e] = to_f32(s.g[i].e[e]);
+        if (M.m) {
+            const float in = u[e] * scale;
+            s.m[i].e[e] = fmaf(mu, s.m[i].e[e], (1.f - mu) * in);
+            u[e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * in) : s.m[i].e[e];
+        }
+    }
+    return make_float4(u[0], u[1], u[2], u[3]);
+}
+// The same where the momentum is the new one already
+template <typename T>
+__device__ __forceinline__ float4 stored_momentum_of(const Common& C, const Matrix& M, const Share<T>& s, int i, float mu, float scale) {
+    float u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        u[e] = to_f32(s.g[i].e[e]);
+        if (M.m) u[e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * (u[e] * scale)) : s.m[i].e[e];
+    }
+    return make_float4(u[0], u[1], u[2], u[3]);
+}
+// n: how many of the four there are
+template <typename T>
+__device__ __forceinline__ void put_momentum(const Matrix& M, const Share<T>& s, int i, int r, int c, int n, bool vector) {
+    float* to = M.m + (int64_t)r * M.cols + c;
+    if (vector && n >= 4) store_vec<float, 4>(to, s.m[i]);
+    else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) to[e] = s.m[i].e[e];
+    }
+}
+// 1 / (norm + eps), from the sum of squares, as a power of two and a factor near one: either alone may be out of range
+struct Inverse {
+    float power, factor;
+    __device__ __forceinline__ Inverse(double sum, float eps) {
+        const double inv = 1.0 / (sqrt(sum) + (double)eps);
+        int exponent = 0;
+        factor = (float)(inv > 0.0 && inv < (double)INFINITY ? frexp(inv, &exponent) : inv) * SCALE;
+        power = ldexpf(1.f, min(max(exponent, -126), 127));
+    }
+    __device__ __forceinline__ float of(float u) const { return u * power * factor; }
+};
+
 // m <- momentum m + (1 - momentum) g, and the sum of squares of what is to be made orthogonal, per strip.  Squares are added in 64
 // bits: they may leave the range of 32.
 template <typename T>
@@ -161,26 +210,9 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_momentum(const __grid_co
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
-            float u[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) u[e] = to_f32(s.g[i].e[e]);
-            if (M.m) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float in = u[e] * scale;
-                    s.m[i].e[e] = fmaf(mu, s.m[i].e[e], (1.f - mu) * in);
-                    u[e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * in) : s.m[i].e[e];
-                }
-                float* to = M.m + (int64_t)r * M.cols + c;
-                if (vector && n >= 4) store_vec<float, 4>(to, s.m[i]);
-                else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < n) to[e] = s.m[i].e[e];
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum += e < n ? (double)u[e] * (double)u[e] : 0.0;
+            const float4 u = momentum_of(C, M, s, i, mu, scale);
+            if (M.m) put_momentum(M, s, i, r, c, n, vector);
+            sum += (n > 0 ? (double)u.x * u.x : 0.0) + (n > 1 ? (double)u.y * u.y : 0.0) + (n > 2 ? (double)u.z * u.z : 0.0) + (n > 3 ? (double)u.w * u.w : 0.0);
         }
     }
     sum = block_sum(sum, shared);
@@ -213,34 +245,22 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_layout(const __grid_cons
     double sum = 0.0;
     for (int i = threadIdx.x; i < M.strips; i += PREPARE_THREADS) sum += C.at.sums[M.strip0 + i];
     sum = block_sum(sum, shared);
-    // 1 / (norm + eps) as a power of two and a factor near one: either alone may be out of range
-    const double inv = 1.0 / (sqrt(sum) + (double)C.eps);
-    int exponent = 0;
-    const float factor = (float)(inv > 0.0 && inv < (double)INFINITY ? frexp(inv, &exponent) : inv) * SCALE;
-    const float power = ldexpf(1.f, min(max(exponent, -126), 127));
+    const Inverse inv(sum, C.eps);
     const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
     const int64_t second = (int64_t)M.rb * M.cb * BLOCK_BYTES;
     for (int cblock = cblock0; cblock < cblock1; ++cblock) {
         uint8_t* block = C.at.blocks + (int64_t)(M.x0 + (uint32_t)cblock * M.rb + rblock) * BLOCK_BYTES;
-        float u[SHARE][4];
+        float4 u[SHARE];
 #pragma unroll
-        for (int i = 0; i < SHARE; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u[i][e] = to_f32(s.g[i].e[e]);
-                if (M.m) u[i][e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * (u[i][e] * scale)) : s.m[i].e[e];
-            }
-        }
+        for (int i = 0; i < SHARE; ++i) u[i] = stored_momentum_of(C, M, s, i, mu, scale);
         if (cblock + 1 < cblock1) load_block<T>(M, rblock * BLOCK, (cblock + 1) * BLOCK, vector, s);
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int rr = (int)threadIdx.x / 16 + 16 * i, cc = (int)threadIdx.x % 16 * 4;
             const int n = rblock * BLOCK + rr < M.rows ? M.cols - cblock * BLOCK - cc : 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) u[i][e] = e < n ? u[i][e] * power * factor : 0.f;    // the padding is 0 whatever the factor is
-            uint2 hi, lo;
-            split2(u[i][0], u[i][1], hi.x, lo.x);
-            split2(u[i][2], u[i][3], hi.y, lo.y);
+            uint2 hi, lo;                           // the padding is 0 whatever the factor is
+            split2(n > 0 ? inv.of(u[i].x) : 0.f, n > 1 ? inv.of(u[i].y) : 0.f, hi.x, lo.x);
+            split2(n > 2 ? inv.of(u[i].z) : 0.f, n > 3 ? inv.of(u[i].w) : 0.f, hi.y, lo.y);
             uint8_t* to = block + piece_at(rr, cc / 8) + cc % 8 * 2;
             *reinterpret_cast<uint2*>(to) = hi;
             *reinterpret_cast<uint2*>(to + second) = lo;
@@ -736,7 +756,238 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
     if (warp == RESULT_WARPS) tmem_free<true>(tmem, 2 * COLS);
 }
 
+// ---- small matrices ----------------------------------------------------------------------------------
+//
+// Where x and A fit the shared memory of one CTA (the shorter side up to 128, the longer up to 256), one CTA does all of it for one matrix:
+// momentum, division, every step.  The launches above would each wait for the one before, 6 us for a microsecond's work (four matrices of
+// 64 x 128: 98 us; this way LATENCY).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
+// number by number: both halves of the symmetric products are computed, so that each thread needs its own numbers alone.
+
+constexpr int SMALL_SHORT = 2, SMALL_LONG = 4;      // blocks of the sides
+constexpr int SMALL_THREADS = 256;
+struct SmallShared {
+    uint64_t done;
+    uint32_t tmem;
+    int gave_up;
+    double sums[PREPARE_THREADS / 32];
+    float d[SMALL_SHORT * BLOCK], e[SMALL_SHORT * BLOCK];
+};
+static_assert(SMALL_THREADS == PREPARE_THREADS, "blocks are loaded as by the preparation");
+
+struct SmallPlan {
+    int32_t x_blocks, a_blocks;                     // of the largest matrix
+    int32_t columns;                                // of tensor memory
+};
+
+template <typename TIN, typename T, bool SPLIT>
+__global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__ Group G, const __grid_constant__ Common C, const SmallPlan plan, int steps) {
+    extern __shared__ uint8_t raw[];
+    uint8_t* const x_hi = raw + ((1024u - (shared_addr(raw) & 1023u)) & 1023u);
+    uint8_t* const x_lo = x_hi + plan.x_blocks * BLOCK_BYTES;
+    uint8_t* const a_hi = x_lo + plan.x_blocks * BLOCK_BYTES;
+    uint8_t* const a_lo = a_hi + plan.a_blocks * BLOCK_BYTES;
+    __shared__ SmallShared S;
+    volatile int* gave_up = &S.gave_up;
+    const Matrix& M = G.m[blockIdx.x];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int R = M.rb, K = M.cb, side = M.mb;
+    const bool tall = M.tall();
+    if (t == 0) {
+        bar_init(&S.done, 1);
+        bar_init_fence();
+        S.gave_up = 0;
+    }
+    if (warp == 0) tmem_alloc<false>(&S.tmem, plan.columns);
+    successor_wait();
+    successor_may_start();
+
+    // momentum and the sum of squares, then x
+    const bool vector = may_load_four<TIN>(M);
+    const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
+    double sum = 0.0;
+    for (int block = 0; block < R * K; ++block) {
+        const int r0 = block % R * BLOCK, c0 = block / R * BLOCK;
+        Share<TIN> s;
+        load_block<TIN>(M, r0, c0, vector, s);
+        const int c = c0 + t % 16 * 4;
+#pragma unroll
+        for (int i = 0; i < SHARE; ++i) {
+            const int r = r0 + t / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
+            const float4 u = momentum_of(C, M, s, i, mu, scale);
+            if (M.m) put_momentum(M, s, i, r, c, n, vector);
+            sum += (n > 0 ? (double)u.x * u.x : 0.0) + (n > 1 ? (double)u.y * u.y : 0.0) + (n > 2 ? (double)u.z * u.z : 0.0) + (n > 3 ? (double)u.w * u.w : 0.0);
+        }
+    }
+    sum = block_sum(sum, S.sums);
+    const Inverse inv(sum, C.eps);
+    for (int block = 0; block < R * K; ++block) {
+        const int r0 = block % R * BLOCK, c0 = block / R * BLOCK;
+        Share<TIN> s;
+        load_block<TIN>(M, r0, c0, vector, s);      // the momentum as this thread has just stored it
+#pragma unroll
+        for (int i = 0; i < SHARE; ++i) {
+            const int rr = t / 16 + 16 * i, cc = t % 16 * 4, n = r0 + rr < M.rows ? M.cols - c0 - cc : 0;
+            const float4 u = stored_momentum_of(C, M, s, i, mu, scale);
+            uint2 hi, lo;
+            split2(n > 0 ? inv.of(u.x) : 0.f, n > 1 ? inv.of(u.y) : 0.f, hi.x, lo.x);
+            split2(n > 2 ? inv.of(u.z) : 0.f, n > 3 ? inv.of(u.w) : 0.f, hi.y, lo.y);
+            const uint32_t at = block * BLOCK_BYTES + piece_at(rr, cc / 8) + cc % 8 * 2;
+            *reinterpret_cast<uint2*>(x_hi + at) = hi;
+            *reinterpret_cast<uint2*>(x_lo + at) = lo;
+        }
+    }
+
+    uint32_t parity = 0;
+    bool ok = true;
+    // One product: operands as stacks of blocks whose first numbers begin at a and b, to the accumulators at `column`
+    struct Side { const uint8_t *hi, *lo; int first, step, leading; bool mn_major; };
+    auto issue = [&](const Side& A, const Side& B, int n, int count, uint32_t column) {
+        const uint32_t instr = instruction(128, n, A.mn_major, B.mn_major);
+        const uint64_t step_a = operand_step(A.mn_major), step_b = operand_step(B.mn_major);
+        const uint32_t d = S.tmem + column;
+        for (int k = 0; k < count; ++k) {
+            auto of = [&](const Side& s, bool low) { return operand(shared_addr((low ? s.lo : s.hi) + (s.first + k * s.step) * BLOCK_BYTES), s.mn_major, s.leading); };
+            const uint64_t a = of(A, false), b = of(B, false);
+            if (SPLIT) {
+                const uint64_t al = of(A, true), bl = of(B, true);
+                for (int i = 0; i < 4; ++i) mma<false>(d, a + i * step_a, bl + i * step_b, instr, k > 0 || i > 0);
+                for (int i = 0; i < 4; ++i) mma<false>(d, al + i * step_a, b + i * step_b, instr, true);
+            }
+            for (int i = 0; i < 4; ++i) mma<false>(d, a + i * step_a, b + i * step_b, instr, SPLIT || k > 0 || i > 0);
+        }
+    };
+    // What was written by threads is read by the products; then their results are there for all
+    auto products = [&](auto f) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        fence_before();
+        __syncthreads();
+        if (t == 0) {
+            fence_after();
+            f();
+            commit<false>(&S.done);
+        }
+        ok = __syncthreads_and(bar_wait(&S.done, parity, gave_up));            // all go on, or none
+        parity ^= 1;
+        fence_after();
+    };
+    // f(row, col, acc) for the warp's pieces of `rows` x `cols` results (32 columns of the lane's row), tiles of 128 rows side by side
+    auto results = [&](int rows, int cols, auto f) {
+        const int pieces = cols / 32;
+        for (int tile = 0; tile * 128 < rows; ++tile) {
+            const int row = tile * 128 + warp % 4 * 32;
+            if (row >= rows) continue;
+            for (int i = warp / 4; i < pieces; i += 2) {
+                uint32_t acc[32];
+                tmem_load32(S.tmem + ((uint32_t)(warp % 4) << 21) + tile * cols + i * 32, acc);
+                tmem_wait();
+                f(row + lane, i * 32, acc);
+            }
+        }
+    };
+    auto at = [&](int row, int col, int blocks, int piece) {   // of a matrix of `blocks` blocks to a column
+        return (uint32_t)((col / BLOCK * blocks + row / BLOCK) * BLOCK_BYTES) + piece_at(row % BLOCK, col % BLOCK / 8 + piece);
+    };
+    auto load8 = [&](const uint8_t* hi, const uint8_t* lo, uint32_t where, bool both, float (&x)[8]) {
+        const uint4 h = *reinterpret_cast<const uint4*>(hi + where);
+        const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { const float2 f = halves(w[e]); x[2 * e] = f.x; x[2 * e + 1] = f.y; }
+        if (both) {
+            const uint4 l = *reinterpret_cast<const uint4*>(lo + where);
+            const uint32_t v[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { const float2 f = halves(v[e]); x[2 * e] += f.x; x[2 * e + 1] += f.y; }
+        }
+    };
+    auto store8 = [&](uint8_t* hi, uint8_t* lo, uint32_t where, bool both, const float (&v)[8]) {
+        uint4 h, l;
+        split2(v[0], v[1], h.x, l.x);
+        split2(v[2], v[3], h.y, l.y);
+        split2(v[4], v[5], h.z, l.z);
+        split2(v[6], v[7], h.w, l.w);
+        *reinterpret_cast<uint4*>(hi + where) = h;
+        if (both) *reinterpret_cast<uint4*>(lo + where) = l;
+    };
+
+    const Side x_rows{x_hi, x_lo, 0, R, 1, false}, x_down{x_hi, x_lo, 0, 1, R, true}, q{a_hi, a_lo, 0, side, 1, false};
+    for (int step = 0; step < steps && ok; ++step) {
+        products([&] {
+            if (tall) issue(x_down, x_down, side * BLOCK, R, 0);
+            else issue(x_rows, x_rows, side * BLOCK, K, 0);
+        });
+        if (!ok) break;
+        results(side * BLOCK, side * BLOCK, [&](int row, int col, const uint32_t (&acc)[32]) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = __uint_as_float(acc[p * 8 + e]) * (1.f / SCALE);
+                    if (row == col + p * 8 + e) {
+                        S.d[row] = v[e] * (1.f / SCALE);
+                        v[e] = 0.f;
+                    }
+                }
+                store8(a_hi, a_lo, at(row, col, side, p), SPLIT, v);
+            }
+        });
+        products([&] { issue(q, q, side * BLOCK, side, 0); });
+        if (!ok) break;
+        results(side * BLOCK, side * BLOCK, [&](int row, int col, const uint32_t (&acc)[32]) {
+            const float mine = S.d[row];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                float v[8];
+                load8(a_hi, a_lo, at(row, col, side, p), SPLIT, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float a = __uint_as_float(acc[p * 8 + e]) * (1.f / SCALE);
+                    const int c = col + p * 8 + e;
+                    if (row == c) S.e[row] = fmaf(C.c, fmaf(mine, mine, a * (1.f / SCALE)), C.b * mine);
+                    v[e] = row == c ? 0.f : fmaf(C.c, fmaf(v[e], mine + S.d[c], a), C.b * v[e]);
+                }
+                store8(a_hi, a_lo, at(row, col, side, p), SPLIT, v);
+            }
+        });
+        products([&] {
+            if (tall)
+                for (int tile = 0; tile * 2 < R; ++tile) issue(Side{x_hi, x_lo, 2 * tile, R, 1, false}, q, side * BLOCK, side, tile * side * BLOCK);
+            else issue(q, x_down, K * BLOCK, side, 0);
+        });
+        if (!ok) break;
+        results(R * BLOCK, K * BLOCK, [&](int row, int col, const uint32_t (&acc)[32]) {
+            const float mine = tall ? 0.f : S.e[row];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                float v[8];
+                load8(x_hi, x_lo, at(row, col, R, p), true, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] = fmaf(C.a + (tall ? S.e[col + p * 8 + e] : mine), v[e], __uint_as_float(acc[p * 8 + e]) * (1.f / SCALE));
+                if (step + 1 < steps) {
+                    store8(x_hi, x_lo, at(row, col, R, p), true, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= 1.f / SCALE;
+                    put_output<T>(C, M, row, col + p * 8, v);
+                }
+            }
+        });
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (t == 0 && S.gave_up) atomicExch(&g_error, 1);
+    if (warp == 0) tmem_free<false>(S.tmem, plan.columns);
+}
+
 // ---- host side ---------------------------------------------------------------------------------------
+
+// Whether one CTA has room for a matrix
+bool is_small(const ssgd_matrix& t) {
+    const int64_t rb = (t.rows + BLOCK - 1) / BLOCK, cb = (t.cols + BLOCK - 1) / BLOCK;
+    return (rb < cb ? rb : cb) <= SMALL_SHORT && (rb < cb ? cb : rb) <= SMALL_LONG;
+}
 
 struct Sizes {
     int64_t blocks = 0, floats = 0, strips = 0, elements = 0;
@@ -832,6 +1083,29 @@ struct Work {
     }
 };
 
+template <typename TIN, typename T, bool SPLIT>
+int launch_small(cudaStream_t st, const Group& G, const Common& C, const SmallPlan& plan, int steps) {
+    const int smem = 1024 + 2 * (plan.x_blocks + plan.a_blocks) * BLOCK_BYTES;
+    static PerDevice opted;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return SSGD_ECUDA;
+    if (!opted.value[dev]) {
+        constexpr int MOST = 1024 + 2 * (SMALL_SHORT * SMALL_LONG + SMALL_SHORT * SMALL_SHORT) * BLOCK_BYTES;
+        if (cudaFuncSetAttribute(k_small<TIN, T, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST) != cudaSuccess) return SSGD_ECUDA;
+        opted.value[dev] = 1;
+    }
+    return launch(st, k_small<TIN, T, SPLIT>, C.count, SMALL_THREADS, smem, G, C, plan, steps);
+}
+template <typename TIN, typename T>
+int launch_small(cudaStream_t st, const Group& G, const Common& C, const SmallPlan& plan, int steps) {
+    return C.split ? launch_small<TIN, T, true>(st, G, C, plan, steps) : launch_small<TIN, T, false>(st, G, C, plan, steps);
+}
+template <typename T>
+int launch_small(cudaStream_t st, const Group& G, const Common& C, const SmallPlan& plan, int steps) {
+    if (C.fmt_in == SSGD_FMT_F32) return launch_small<float, T>(st, G, C, plan, steps);
+    return C.fmt_in == SSGD_FMT_F16 ? launch_small<__half, T>(st, G, C, plan, steps) : launch_small<__nv_bfloat16, T>(st, G, C, plan, steps);
+}
+
 constexpr int64_t MAX_SIDE = (int64_t)1 << 20;
 constexpr int MAX_STEPS = 32;
 
@@ -879,7 +1153,7 @@ int64_t workspace_of(const ssgd_matrix* t, int32_t count, bool split) {
     int64_t most = 0;
     Sizes s;
     for (int32_t i = 0; i < count; ++i) {
-        if (!t[i].rows || !t[i].cols) continue;
+        if (!t[i].rows || !t[i].cols || is_small(t[i])) continue;
         if (!add(s, t[i], split, nullptr)) {
             s = Sizes{};
             add(s, t[i], split, nullptr);
@@ -891,17 +1165,41 @@ int64_t workspace_of(const ssgd_matrix* t, int32_t count, bool split) {
 
 int run(const ssgd_matrix* t, int32_t count, Common C, int32_t steps, double lr, void* workspace, size_t bytes, cudaStream_t st) {
     const int64_t need = workspace_of(t, count, C.split);
-    if (need == 0) return SSGD_OK;
-    if (!workspace || (int64_t)bytes < need) return SSGD_EWORKSPACE;
-    if (!aligned_to(workspace, 16)) return SSGD_EALIGN;
+    if (need) {
+        if (!workspace || (int64_t)bytes < need) return SSGD_EWORKSPACE;
+        if (!aligned_to(workspace, 16)) return SSGD_EALIGN;
+    }
     int sms = 0, e = sm_count_of_current_device(&sms);
     if (e) return e;
+    // the small ones
+    for (int32_t i = 0; i < count;) {
+        Group G;
+        Sizes s;
+        SmallPlan plan{0, 0, 32};
+        for (; i < count && s.count < MAX_GROUP; ++i) {
+            if (!t[i].rows || !t[i].cols || !is_small(t[i])) continue;
+            Matrix& M = G.m[s.count];
+            add(s, t[i], C.split, &M);
+            M.update = (float)(lr * t[i].scale);
+            const int32_t tiles = M.tall() ? (M.rb + 1) / 2 : 1, columns = BLOCK * (M.tall() ? tiles * M.cb : M.cb);
+            plan.x_blocks = std::max(plan.x_blocks, M.rb * M.cb);
+            // rows beyond a matrix of one block are read, and their results left
+            plan.a_blocks = std::max(plan.a_blocks, std::max(2, M.mb * M.mb));
+            while (plan.columns < columns) plan.columns *= 2;
+        }
+        if (!s.count) break;
+        C.count = s.count;
+        e = C.fmt_out == SSGD_FMT_F32 ? launch_small<float>(st, G, C, plan, steps)
+          : C.fmt_out == SSGD_FMT_F16 ? launch_small<__half, __half>(st, G, C, plan, steps)                // never of another type
+                                      : launch_small<__nv_bfloat16>(st, G, C, plan, steps);
+        if (e) return e;
+    }
     int32_t i = 0;
     while (i < count) {
         Group G;
         Sizes s;
         for (; i < count; ++i) {
-            if (!t[i].rows || !t[i].cols) continue;
+            if (!t[i].rows || !t[i].cols || is_small(t[i])) continue;
             if (!add(s, t[i], C.split, s.count < MAX_GROUP ? &G.m[s.count] : nullptr)) break;
             G.m[s.count - 1].update = (float)(lr * t[i].scale);
         }

@@ -145,9 +145,9 @@ __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.syn
 
 // Operands are stacks of blocks.  K-major (rows along M or N, 64 columns of the contraction): groups of 8 rows are 1024 bytes apart.
 // MN-major (columns along M or N, 64 rows of the contraction): 8 rows of the contraction are 1024 bytes apart, and the next 64
-// columns are the next block.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, bool mn_major) {
-    const uint64_t leading = mn_major ? BLOCK_BYTES / 16 : 1, stride = 1024 / 16;
+// columns are the next block, or `blocks` blocks further.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, bool mn_major, int blocks = 1) {
+    const uint64_t leading = mn_major ? (uint64_t)(blocks * (BLOCK_BYTES / 16)) : 1, stride = 1024 / 16;
     return (uint64_t)((addr & 0x3ffff) >> 4) | leading << 16 | stride << 32 | 1ull << 46 | 2ull << 61;
 }
 // What 16 steps of the contraction add to a descriptor: 32 bytes of a row, or 16 rows
