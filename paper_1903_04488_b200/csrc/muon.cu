@@ -266,7 +266,6 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_layout(const __grid_cons
             *reinterpret_cast<uint2*>(to + second) = lo;
         }
     }
-    asm volatile("fence.proxy.async.global;" ::: "memory");    // bulk copies read them
 }
 
 // ---- products ----------------------------------------------------------------------------------------
@@ -723,35 +722,31 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
                     tmem_store_wait();
                 }
             }
-            Source<KIND, SPLIT> source[2] = {};
-            if (some) fetch(J, row0, col0, opaque(lane), source[0]);
+            Source<KIND, SPLIT> source{};
+            if (some) fetch(J, row0, col0, opaque(lane), source);
             if (!summed && !done()) break;
-            // what a piece needs is fetched before the one before it is worked on
+            // What a piece needs is fetched before the one before it is worked on.  One copy of the code: a launch of few tiles waits for
+            // every line of it.
 #pragma unroll 1
-            for (int i0 = 0; i0 < MINE; i0 += 2) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int i = i0 + j;
-                    // addresses are made here each time: kept across the tiles they would take the registers of the sums
-                    const int l = opaque(lane);
-                    uint32_t acc[32];
-                    tmem_load32(at + buffer * COLS + i * 32, acc);
-                    if (i + 1 < MINE && wanted(i + 1)) fetch(J, row0, col0 + (i + 1) * 32, l, source[j ^ 1]);
-                    else source[j ^ 1] = {};
-                    tmem_wait();
-                    if (i + 1 == MINE) next();
-                    if (wanted(i)) take<KIND, SPLIT, T>(C, M, J, row0, col0 + i * 32, acc, source[j], scratches + opaque(warp) * SCRATCH, l);
-                }
+            for (int i = 0; i < MINE; ++i) {
+                // addresses are made here each time: kept across the tiles they would take the registers of the sums
+                const int l = opaque(lane);
+                uint32_t acc[32];
+                tmem_load32(at + buffer * COLS + i * 32, acc);
+                Source<KIND, SPLIT> following{};
+                if (i + 1 < MINE && wanted(i + 1)) fetch(J, row0, col0 + (i + 1) * 32, l, following);
+                tmem_wait();
+                if (i + 1 == MINE) next();
+                if (wanted(i)) take<KIND, SPLIT, T>(C, M, J, row0, col0 + i * 32, acc, source, scratches + opaque(warp) * SCRATCH, l);
+                source = following;
             }
         }
     }
     __syncwarp();
-    // the results were written by ordinary stores and are read by bulk copies, of the next launch
-    asm volatile("fence.proxy.async.global;" ::: "memory");
     fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && S.gave_up) atomicExch(&g_error, 1);
-    pair_sync();                                    // neither leaves while the other's products read its shared memory
+    pair_meet();                                    // neither leaves while the other's products read its shared memory
     fence_after();
     if (warp == RESULT_WARPS) tmem_free<true>(tmem, 2 * COLS);
 }

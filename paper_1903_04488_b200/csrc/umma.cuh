@@ -55,6 +55,10 @@ __device__ __forceinline__ void bar_arrive_first(uint64_t* bar) {
 __device__ __forceinline__ void pair_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Only that both have come here: nothing written before is handed over (a release would wait for all of it, some 2 us)
+__device__ __forceinline__ void pair_meet() {
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
 __device__ __forceinline__ uint32_t pair_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
