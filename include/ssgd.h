@@ -453,9 +453,9 @@ int ssgd_preference_loss(const float* logp, const float* ref_logp, int64_t token
  * The products are of fp16 numbers with fp32 sums.  products = 3: every matrix is a sum of two fp16 numbers, so that results are as
  * exact as those of fp32; 1: one number in the operands of products, two in x itself: the result is off by about 1e-3 of its norm;
  * 0: 1 for results in bfloat16, otherwise 3.
- * A matrix of zeros stays one (0 / 0 with eps = 0 is NaN), and numbers of x_0 below 2^-35 count as zero; infinities and NaN spread over their matrix.  Polynomials that take anything
- * in [0, 1] beyond 4 on the way are refused (SSGD_EINVAL).  1 <= steps <= 32; rows, cols <= 2^20, rows * cols <= 2^32, the shorter
- * side <= 32768 (SSGD_ETOOBIG).  Matrices without elements are left out. */
+ * A matrix of zeros stays one (0 / 0 with eps = 0 is NaN), and numbers of x_0 below 2^-35 count as zero; infinities and NaN spread
+ * over their matrix.  Polynomials that take anything in [0, 1] beyond 4 on the way are refused (SSGD_EINVAL).  1 <= steps <= 32; rows,
+ * cols <= 2^20, rows * cols <= 2^32, the shorter side <= 32768 (SSGD_ETOOBIG).  Matrices without elements are left out. */
 typedef struct {
     void* out;        /* ssgd_orthogonalize: the result, may be `in` itself (same ld); ssgd_muon_step: the parameter */
     const void* in;   /* the matrix, or the gradient */
@@ -465,8 +465,8 @@ typedef struct {
     double scale;     /* ssgd_muon_step: factor of lr for this matrix */
 } ssgd_matrix;
 /* Device memory that the two below need: 8 bytes per element of the matrices, twice (products 1) or four times (3) 2 bytes per element
- * of A and B, and a little.  More than 224 matrices or 2^27 elements are worked off in groups, each in the same memory.  Free again
- * once the stream has passed; its contents mean nothing.  16-byte aligned. */
+ * of A and B, and a little; none for matrices of up to 128 x 256 or 256 x 128.  More than 224 matrices or 2^27 elements are worked off in
+ * groups, each in the same memory.  Free again once the stream has passed; its contents mean nothing.  16-byte aligned. */
 int ssgd_orthogonalize_workspace(const ssgd_matrix* matrices, int32_t count, int32_t fmt_out, int32_t products, size_t* out_bytes);
 /* out <- the orthogonalised `in`, for each matrix; both in fmt. */
 int ssgd_orthogonalize(const ssgd_matrix* matrices, int32_t count, int32_t fmt, int32_t products, int32_t steps, double a, double b,

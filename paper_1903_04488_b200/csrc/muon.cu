@@ -162,6 +162,11 @@ __device__ __forceinline__ float4 stored_momentum_of(const Common& C, const Matr
     }
     return make_float4(u[0], u[1], u[2], u[3]);
 }
+// The first n of the four, squared and added in 64 bits
+__device__ __forceinline__ double squares(const float4& u, int n) {
+    return (n > 0 ? (double)u.x * u.x : 0.0) + (n > 1 ? (double)u.y * u.y : 0.0) + (n > 2 ? (double)u.z * u.z : 0.0) +
+           (n > 3 ? (double)u.w * u.w : 0.0);
+}
 // n: how many of the four there are
 template <typename T>
 __device__ __forceinline__ void put_momentum(const Matrix& M, const Share<T>& s, int i, int r, int c, int n, bool vector) {
@@ -212,7 +217,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_momentum(const __grid_co
             const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
             const float4 u = momentum_of(C, M, s, i, mu, scale);
             if (M.m) put_momentum(M, s, i, r, c, n, vector);
-            sum += (n > 0 ? (double)u.x * u.x : 0.0) + (n > 1 ? (double)u.y * u.y : 0.0) + (n > 2 ? (double)u.z * u.z : 0.0) + (n > 3 ? (double)u.w * u.w : 0.0);
+            sum += squares(u, n);
         }
     }
     sum = block_sum(sum, shared);
@@ -497,7 +502,8 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, const Job
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = i * 8 + lane / 4;
-        const float4 a = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2)), b = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2 + 1));
+        const float4 a = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2));
+        const float4 b = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2 + 1));
         float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         float x[8];
         if constexpr (KIND != GRAM) {
@@ -551,7 +557,8 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, const Job
 }
 
 template <Kind KIND, int COLS, bool SPLIT, typename T>
-__global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap map, int which, int tiles) {
+__global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1)
+k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap map, int which, int tiles) {
     constexpr int BYTES = STAGE<COLS, SPLIT>, N = STAGES<COLS, SPLIT>, B_BLOCKS = COLS / 128;
     constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLYNOMIAL;
     extern __shared__ uint8_t raw[];
@@ -583,82 +590,82 @@ __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1) k_produc
     // A result warp holds up to 128 sums to a lane (SPLIT), or two pieces' sources: it gets registers from the group that copies
     // (224 + 224 + 56 = 3 x 168, what the launch has given: LAUNCH_REGISTERS).
     if (warp >= RESULT_WARPS) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == RESULT_WARPS && lane == 0) {                    // copies
-        int s = 0, issued = 0;
-        uint32_t parity = 1;
-        bool ok = true;
-        for (int tile = tile0; tile < tiles && ok; tile += stride) {
-            const int m = find(tile);
-            const Matrix& M = C.at.matrices[m];
-            const Product P = product_of<KIND>(M, which);
-            const Tile at_tile = tile_of<KIND, COLS>(M, tile - S.first[m]);
-            const int bm = at_tile.row + (int)rank * 2, bn = at_tile.col + (int)rank * B_BLOCKS;
-            int32_t from[4] = {P.A.at(bm), P.A.at(bm + 1), P.B.at(bn), B_BLOCKS == 2 ? P.B.at(bn + 1) : 0};
-            const int32_t step[2] = {P.A.step(), P.B.step()}, second[2] = {(int32_t)P.A.second, (int32_t)P.B.second};
-            if (tile == tile0) {
-                successor_wait();
-                asm volatile("fence.proxy.async.global;" ::: "memory");
-            }
-            for (int k = 0; k < P.steps; ++k) {
-                if (!(ok = bar_wait(&S.empty[s], parity, gave_up))) break;
-                if (rank == 0) bar_expect(&S.full[s], 2 * BYTES);
-                uint8_t* to = ring + s * BYTES;
-#pragma unroll
-                for (int i = 0; i < 2 + B_BLOCKS; ++i) {
-                    block_load(to + i * BLOCK_BYTES, &map, from[i], &S.full[s]);
-                    if (SPLIT) block_load(to + (2 + B_BLOCKS + i) * BLOCK_BYTES, &map, from[i] + second[i / 2], &S.full[s]);
-                    from[i] += step[i / 2];
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == RESULT_WARPS && lane == 0) {                    // copies
+            int s = 0, issued = 0;
+            uint32_t parity = 1;
+            bool ok = true;
+            for (int tile = tile0; tile < tiles && ok; tile += stride) {
+                const int m = find(tile);
+                const Matrix& M = C.at.matrices[m];
+                const Product P = product_of<KIND>(M, which);
+                const Tile at_tile = tile_of<KIND, COLS>(M, tile - S.first[m]);
+                const int bm = at_tile.row + (int)rank * 2, bn = at_tile.col + (int)rank * B_BLOCKS;
+                int32_t from[4] = {P.A.at(bm), P.A.at(bm + 1), P.B.at(bn), B_BLOCKS == 2 ? P.B.at(bn + 1) : 0};
+                const int32_t step[2] = {P.A.step(), P.B.step()}, second[2] = {(int32_t)P.A.second, (int32_t)P.B.second};
+                if (tile == tile0) {
+                    successor_wait();
+                    asm volatile("fence.proxy.async.global;" ::: "memory");
                 }
-                ++issued;
-                if (++s == N) { s = 0; parity ^= 1; }
+                for (int k = 0; k < P.steps; ++k) {
+                    if (!(ok = bar_wait(&S.empty[s], parity, gave_up))) break;
+                    if (rank == 0) bar_expect(&S.full[s], 2 * BYTES);
+                    uint8_t* to = ring + s * BYTES;
+#pragma unroll
+                    for (int i = 0; i < 2 + B_BLOCKS; ++i) {
+                        block_load(to + i * BLOCK_BYTES, &map, from[i], &S.full[s]);
+                        if (SPLIT) block_load(to + (2 + B_BLOCKS + i) * BLOCK_BYTES, &map, from[i] + second[i / 2], &S.full[s]);
+                        from[i] += step[i / 2];
+                    }
+                    ++issued;
+                    if (++s == N) { s = 0; parity ^= 1; }
+                }
             }
-        }
-        // no copy may land in a CTA that is gone, nor count there: the first CTA waits for both's, and the second leaves with it
-        if (!ok && rank == 0)
-            for (int i = 0; i < min(issued, N); ++i) {
-                const int last = issued - 1 - i;
-                const uint64_t t0 = now_ns();
-                while (!bar_try(&S.full[last % N], (uint32_t)(last / N) & 1u) && now_ns() - t0 < WAIT_NS) {}
-            }
-    } else if (warp == RESULT_WARPS + 1 && lane == 0 && rank == 0) {         // products, of both CTAs
-        int s = 0, buffer = 0;
-        uint32_t parity = 0, parity_taken = 1;
-        bool ok = true;
-        for (int tile = tile0; tile < tiles && ok; tile += stride) {
-            const Matrix& M = C.at.matrices[find(tile)];
-            const Product P = product_of<KIND>(M, which);
-            const uint32_t instr = instruction(TILE_ROWS, COLS, P.A.mn_major, P.B.mn_major);
-            const uint64_t step_a = operand_step(P.A.mn_major), step_b = operand_step(P.B.mn_major);
-            for (int k = 0; k < P.steps && ok; ++k) {
-                const bool begin = SPLIT ? k % CHUNK == 0 : k == 0;
-                if (begin) {
-                    if (!(ok = bar_wait(&S.taken[buffer], parity_taken, gave_up))) break;
+            // no copy may land in a CTA that is gone, nor count there: the first CTA waits for both's, and the second leaves with it
+            if (!ok && rank == 0)
+                for (int i = 0; i < min(issued, N); ++i) {
+                    const int last = issued - 1 - i;
+                    const uint64_t t0 = now_ns();
+                    while (!bar_try(&S.full[last % N], (uint32_t)(last / N) & 1u) && now_ns() - t0 < WAIT_NS) {}
+                }
+        } else if (warp == RESULT_WARPS + 1 && lane == 0 && rank == 0) {         // products, of both CTAs
+            int s = 0, buffer = 0;
+            uint32_t parity = 0, parity_taken = 1;
+            bool ok = true;
+            for (int tile = tile0; tile < tiles && ok; tile += stride) {
+                const Matrix& M = C.at.matrices[find(tile)];
+                const Product P = product_of<KIND>(M, which);
+                const uint32_t instr = instruction(TILE_ROWS, COLS, P.A.mn_major, P.B.mn_major);
+                const uint64_t step_a = operand_step(P.A.mn_major), step_b = operand_step(P.B.mn_major);
+                for (int k = 0; k < P.steps && ok; ++k) {
+                    const bool begin = SPLIT ? k % CHUNK == 0 : k == 0;
+                    if (begin) {
+                        if (!(ok = bar_wait(&S.taken[buffer], parity_taken, gave_up))) break;
+                        fence_after();
+                    }
+                    if (!(ok = bar_wait(&S.full[s], parity, gave_up))) break;
                     fence_after();
-                }
-                if (!(ok = bar_wait(&S.full[s], parity, gave_up))) break;
-                fence_after();
-                const uint32_t at = shared_addr(ring + s * BYTES), d = tmem + buffer * COLS;
-                const uint64_t a = operand(at, P.A.mn_major), b = operand(at + 2 * BLOCK_BYTES, P.B.mn_major);
-                constexpr uint64_t LOW = (2 + B_BLOCKS) * BLOCK_BYTES / 16;
-                if (SPLIT) {
+                    const uint32_t at = shared_addr(ring + s * BYTES), d = tmem + buffer * COLS;
+                    const uint64_t a = operand(at, P.A.mn_major), b = operand(at + 2 * BLOCK_BYTES, P.B.mn_major);
+                    constexpr uint64_t LOW = (2 + B_BLOCKS) * BLOCK_BYTES / 16;
+                    if (SPLIT) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a, b + i * step_b + LOW, instr, !begin || i > 0);
+                        for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a, b + i * step_b + LOW, instr, !begin || i > 0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a + LOW, b + i * step_b, instr, true);
-                }
+                        for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a + LOW, b + i * step_b, instr, true);
+                    }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a, b + i * step_b, instr, SPLIT || !begin || i > 0);
-                commit<true>(&S.empty[s]);
-                if (k + 1 == P.steps || (SPLIT && k % CHUNK == CHUNK - 1)) {
-                    commit<true>(&S.done[buffer]);
-                    if (buffer) parity_taken ^= 1;
-                    buffer ^= 1;
+                    for (int i = 0; i < 4; ++i) mma<true>(d, a + i * step_a, b + i * step_b, instr, SPLIT || !begin || i > 0);
+                    commit<true>(&S.empty[s]);
+                    if (k + 1 == P.steps || (SPLIT && k % CHUNK == CHUNK - 1)) {
+                        commit<true>(&S.done[buffer]);
+                        if (buffer) parity_taken ^= 1;
+                        buffer ^= 1;
+                    }
+                    if (++s == N) { s = 0; parity ^= 1; }
                 }
-                if (++s == N) { s = 0; parity ^= 1; }
             }
         }
-    }
     } else {                                                    // results
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         constexpr int MINE = COLS / 2 / 32;                     // pieces of 32 columns of a warp
@@ -810,7 +817,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
             const int r = r0 + t / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
             const float4 u = momentum_of(C, M, s, i, mu, scale);
             if (M.m) put_momentum(M, s, i, r, c, n, vector);
-            sum += (n > 0 ? (double)u.x * u.x : 0.0) + (n > 1 ? (double)u.y * u.y : 0.0) + (n > 2 ? (double)u.z * u.z : 0.0) + (n > 3 ? (double)u.w * u.w : 0.0);
+            sum += squares(u, n);
         }
     }
     sum = block_sum(sum, S.sums);
@@ -841,7 +848,9 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
         const uint64_t step_a = operand_step(A.mn_major), step_b = operand_step(B.mn_major);
         const uint32_t d = S.tmem + column;
         for (int k = 0; k < count; ++k) {
-            auto of = [&](const Side& s, bool low) { return operand(shared_addr((low ? s.lo : s.hi) + (s.first + k * s.step) * BLOCK_BYTES), s.mn_major, s.leading); };
+            auto of = [&](const Side& s, bool low) {
+                return operand(shared_addr((low ? s.lo : s.hi) + (s.first + k * s.step) * BLOCK_BYTES), s.mn_major, s.leading);
+            };
             const uint64_t a = of(A, false), b = of(B, false);
             if (SPLIT) {
                 const uint64_t al = of(A, true), bl = of(B, true);
@@ -1160,6 +1169,7 @@ int64_t workspace_of(const ssgd_matrix* t, int32_t count, bool split) {
 
 int run(const ssgd_matrix* t, int32_t count, Common C, int32_t steps, double lr, void* workspace, size_t bytes, cudaStream_t st) {
     const int64_t need = workspace_of(t, count, C.split);
+    if (std::all_of(t, t + count, [](const ssgd_matrix& m) { return !m.rows || !m.cols; })) return SSGD_OK;
     if (need) {
         if (!workspace || (int64_t)bytes < need) return SSGD_EWORKSPACE;
         if (!aligned_to(workspace, 16)) return SSGD_EALIGN;

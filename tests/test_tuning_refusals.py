@@ -68,7 +68,7 @@ def matrices(*rows):
     """ssgd_matrix: out, in, m, ld_out, ld_in, rows, cols, scale"""
     out = np.zeros((len(rows), 8), dtype=np.int64)
     for i, r in enumerate(rows):
-        one = dict(out=P, x=P, m=P, ld_out=70, ld_in=70, rows=40, cols=70)
+        one = dict(out=P, x=P, m=P, ld_out=700, ld_in=700, rows=300, cols=700)
         one.update(r)
         out[i, :7] = list(one.values())
         out[i, 7] = np.float64(1.0).view(np.int64)
@@ -84,13 +84,14 @@ def test_orthogonalize_and_muon_refuse(lib):
     d = matrices({}, {})
     assert size(d) == S.OK
     three = need.value
-    assert size(d, products=1) == S.OK and 8 * 2 * 40 * 70 <= need.value < three
+    assert size(d, products=1) == S.OK and 8 * 2 * 300 * 700 <= need.value < three
     for bad in (dict(rows=-1), dict(cols=-1), dict(rows=(1 << 20) + 1), dict(cols=(1 << 20) + 1)):
         assert size(matrices(bad)) == S.EINVAL, bad
     for bad in (dict(rows=1 << 20, cols=8192), dict(rows=32769, cols=32769)):
         assert size(matrices(bad)) == S.ETOOBIG, bad
     assert size(d, fmt=7) == S.EINVAL and size(d, products=2) == S.EINVAL
     assert lib.ssgd_orthogonalize_workspace(d.ctypes.data, 2, 2, 0, None) == S.EINVAL
+    assert size(matrices(dict(rows=128, cols=256), dict(rows=256, cols=1))) == S.OK and need.value == 0     # small ones need none
     # the workspace of many matrices is that of the largest group of them
     assert size(matrices(*[{}] * 224)) == S.OK
     full = need.value
@@ -105,7 +106,7 @@ def test_orthogonalize_and_muon_refuse(lib):
     for bad in (dict(count=-1), dict(fmt=S.FMT_E4M3), dict(products=2), dict(steps=0), dict(steps=33), dict(a=D(NAN)), dict(a=D(9)), dict(b=D(50)),
                 dict(eps=D(-1)), dict(eps=D(NAN)), dict(eps=D(INF))):
         assert ortho(**bad) == S.EINVAL, bad
-    for row in (dict(out=0), dict(x=0), dict(ld_out=69), dict(ld_in=69), dict(rows=-1)):
+    for row in (dict(out=0), dict(x=0), dict(ld_out=699), dict(ld_in=699), dict(rows=-1)):
         assert ortho(row) == S.EINVAL, row
     for row in (dict(out=P + 1), dict(x=P + 1)):
         assert ortho(row) == S.EALIGN, row
