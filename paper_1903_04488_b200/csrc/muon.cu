@@ -17,6 +17,10 @@
 // The stored numbers are 1024 times the true ones: x is at most 1.2 and an element mostly far below, so that the second number stays
 // clear of fp16's subnormals.
 //
+// Measured: 8 x 1024 x 2816 bf16 0.71 ms, 557 TFLOP/s of what has to be computed; the matrices of two transformer blocks (2048, 5632) bf16
+// 2.4 ms, 810; of eight (768, 2048) fp32 with three products 1.66 ms, 240.  What bounds the large ones is what an SM takes from L2: 48 to 50
+// bytes per cycle, 681 cycles for 64 of the contraction of a 256 x 256 tile, of which the products are 512.
+//
 // Layout.  All matrices of a call go through every launch together: prepare (momentum and sums of squares; division and layout),
 // then 3 launches per step, whose tiles are dealt out over the SMs.  Matrices live in the workspace as blocks (umma.cuh), padded with
 // zeros to 64; block (r, c) of a matrix of R x C blocks is the (c R + r)-th.
@@ -762,7 +766,7 @@ k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap 
 //
 // Where x and A fit the shared memory of one CTA (the shorter side up to 128, the longer up to 256), one CTA does all of it for one matrix:
 // momentum, division, every step.  The launches above would each wait for the one before, 6 us for a microsecond's work (four matrices of
-// 64 x 128: 98 us; this way LATENCY).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
+// 64 x 128: 98 us; this way 38).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
 // number by number: both halves of the symmetric products are computed, so that each thread needs its own numbers alone.
 
 constexpr int SMALL_SHORT = 2, SMALL_LONG = 4;      // blocks of the sides
