@@ -502,12 +502,18 @@ __device__ __forceinline__ void take(const Common& C, const Matrix& M, const Job
     const bool on_diagonal = SYMMETRIC && row0 == col0;
     uint8_t* to = J.at(J.to, row0, col0, lane);
     const int64_t second = (int64_t)J.second * BLOCK_BYTES;
+    // all of it before the first result is stored: the compiler cannot know that these are other places
+    float4 sums[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) sums[i][j] = *reinterpret_cast<const float4*>(scratch + word_at(i * 8 + lane / 4, lane % 4 * 2 + j));
+    }
     uint4 hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = i * 8 + lane / 4;
-        const float4 a = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2));
-        const float4 b = *reinterpret_cast<const float4*>(scratch + word_at(r, lane % 4 * 2 + 1));
+        const float4 a = sums[i][0], b = sums[i][1];
         float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         float x[8];
         if constexpr (KIND != GRAM) {
@@ -776,7 +782,8 @@ struct SmallShared {
     uint32_t tmem;
     int gave_up;
     double sums[PREPARE_THREADS / 32];
-    float d[SMALL_SHORT * BLOCK], e[SMALL_SHORT * BLOCK];
+    alignas(16) float d[SMALL_SHORT * BLOCK];
+    alignas(16) float e[SMALL_SHORT * BLOCK];
 };
 static_assert(SMALL_THREADS == PREPARE_THREADS, "blocks are loaded as by the preparation");
 
@@ -895,26 +902,44 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
     auto at = [&](int row, int col, int blocks, int piece) {   // of a matrix of `blocks` blocks to a column
         return (uint32_t)((col / BLOCK * blocks + row / BLOCK) * BLOCK_BYTES) + piece_at(row % BLOCK, col % BLOCK / 8 + piece);
     };
-    auto load8 = [&](const uint8_t* hi, const uint8_t* lo, uint32_t where, bool both, float (&x)[8]) {
-        const uint4 h = *reinterpret_cast<const uint4*>(hi + where);
-        const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+    // All loads before the first store: the compiler cannot know that they are of other places, and one warp alone waits for each
+    auto load32 = [&](const uint8_t* hi, const uint8_t* lo, int row, int col, int blocks, bool both, float (&x)[32]) {
+        uint4 h[4], l[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { const float2 f = halves(w[e]); x[2 * e] = f.x; x[2 * e + 1] = f.y; }
-        if (both) {
-            const uint4 l = *reinterpret_cast<const uint4*>(lo + where);
-            const uint32_t v[4] = {l.x, l.y, l.z, l.w};
+        for (int p = 0; p < 4; ++p) {
+            h[p] = *reinterpret_cast<const uint4*>(hi + at(row, col, blocks, p));
+            if (both) l[p] = *reinterpret_cast<const uint4*>(lo + at(row, col, blocks, p));
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { const float2 f = halves(v[e]); x[2 * e] += f.x; x[2 * e + 1] += f.y; }
+        for (int p = 0; p < 4; ++p) {
+            const uint32_t w[4] = {h[p].x, h[p].y, h[p].z, h[p].w}, u[4] = {l[p].x, l[p].y, l[p].z, l[p].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float2 f = halves(w[e]);
+                if (both) f = add2(f, halves(u[e]));
+                x[p * 8 + 2 * e] = f.x;
+                x[p * 8 + 2 * e + 1] = f.y;
+            }
         }
     };
-    auto store8 = [&](uint8_t* hi, uint8_t* lo, uint32_t where, bool both, const float (&v)[8]) {
-        uint4 h, l;
-        split2(v[0], v[1], h.x, l.x);
-        split2(v[2], v[3], h.y, l.y);
-        split2(v[4], v[5], h.z, l.z);
-        split2(v[6], v[7], h.w, l.w);
-        *reinterpret_cast<uint4*>(hi + where) = h;
-        if (both) *reinterpret_cast<uint4*>(lo + where) = l;
+    auto store32 = [&](uint8_t* hi, uint8_t* lo, int row, int col, int blocks, bool both, const float (&v)[32]) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            uint4 h, l;
+            split2(v[p * 8], v[p * 8 + 1], h.x, l.x);
+            split2(v[p * 8 + 2], v[p * 8 + 3], h.y, l.y);
+            split2(v[p * 8 + 4], v[p * 8 + 5], h.z, l.z);
+            split2(v[p * 8 + 6], v[p * 8 + 7], h.w, l.w);
+            *reinterpret_cast<uint4*>(hi + at(row, col, blocks, p)) = h;
+            if (both) *reinterpret_cast<uint4*>(lo + at(row, col, blocks, p)) = l;
+        }
+    };
+    auto load_vector = [&](const float* from, float (&v)[32]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 f = *reinterpret_cast<const float4*>(from + 4 * i);
+            v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
+        }
     };
 
     const Side x_rows{x_hi, x_lo, 0, R, 1, false}, x_down{x_hi, x_lo, 0, 1, R, true}, q{a_hi, a_lo, 0, side, 1, false};
@@ -925,37 +950,33 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
         });
         if (!ok) break;
         results(side * BLOCK, side * BLOCK, [&](int row, int col, const uint32_t (&acc)[32]) {
+            float v[32];
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = __uint_as_float(acc[p * 8 + e]) * (1.f / SCALE);
-                    if (row == col + p * 8 + e) {
-                        S.d[row] = v[e] * (1.f / SCALE);
-                        v[e] = 0.f;
-                    }
+            for (int e = 0; e < 32; ++e) {
+                v[e] = __uint_as_float(acc[e]) * (1.f / SCALE);
+                if (row == col + e) {
+                    S.d[row] = v[e] * (1.f / SCALE);
+                    v[e] = 0.f;
                 }
-                store8(a_hi, a_lo, at(row, col, side, p), SPLIT, v);
             }
+            store32(a_hi, a_lo, row, col, side, SPLIT, v);
         });
         products([&] { issue(q, q, side * BLOCK, side, 0); });
         if (!ok) break;
         results(side * BLOCK, side * BLOCK, [&](int row, int col, const uint32_t (&acc)[32]) {
             const float mine = S.d[row];
+            float v[32];
+            load32(a_hi, a_lo, row, col, side, SPLIT, v);
+            float other[32];
+            load_vector(S.d + col, other);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                float v[8];
-                load8(a_hi, a_lo, at(row, col, side, p), SPLIT, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float a = __uint_as_float(acc[p * 8 + e]) * (1.f / SCALE);
-                    const int c = col + p * 8 + e;
-                    if (row == c) S.e[row] = fmaf(C.c, fmaf(mine, mine, a * (1.f / SCALE)), C.b * mine);
-                    v[e] = row == c ? 0.f : fmaf(C.c, fmaf(v[e], mine + S.d[c], a), C.b * v[e]);
-                }
-                store8(a_hi, a_lo, at(row, col, side, p), SPLIT, v);
+            for (int e = 0; e < 32; ++e) {
+                const float a = __uint_as_float(acc[e]) * (1.f / SCALE);
+                const bool diag = row == col + e;
+                if (diag) S.e[row] = fmaf(C.c, fmaf(mine, mine, a * (1.f / SCALE)), C.b * mine);
+                v[e] = diag ? 0.f : fmaf(C.c, fmaf(v[e], mine + other[e], a), C.b * v[e]);
             }
+            store32(a_hi, a_lo, row, col, side, SPLIT, v);
         });
         products([&] {
             if (tall)
@@ -964,20 +985,25 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
         });
         if (!ok) break;
         results(R * BLOCK, K * BLOCK, [&](int row, int col, const uint32_t (&acc)[32]) {
-            const float mine = tall ? 0.f : S.e[row];
+            float v[32], f[32];
+            load32(x_hi, x_lo, row, col, R, true, v);
+            if (tall) load_vector(S.e + col, f);
+            else {
+                const float mine = S.e[row];
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                float v[8];
-                load8(x_hi, x_lo, at(row, col, R, p), true, v);
+                for (int e = 0; e < 32; ++e) f[e] = mine;
+            }
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] = fmaf(C.a + (tall ? S.e[col + p * 8 + e] : mine), v[e], __uint_as_float(acc[p * 8 + e]) * (1.f / SCALE));
-                if (step + 1 < steps) {
-                    store8(x_hi, x_lo, at(row, col, R, p), true, v);
-                } else {
+            for (int e = 0; e < 32; ++e) v[e] = fmaf(C.a + f[e], v[e], __uint_as_float(acc[e]) * (1.f / SCALE));
+            if (step + 1 < steps) {
+                store32(x_hi, x_lo, row, col, R, true, v);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= 1.f / SCALE;
-                    put_output<T>(C, M, row, col + p * 8, v);
+                for (int p = 0; p < 4; ++p) {
+                    float o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = v[p * 8 + e] * (1.f / SCALE);
+                    put_output<T>(C, M, row, col + p * 8, o);
                 }
             }
         });
