@@ -4,12 +4,14 @@
 //   D_s = sum of (logp - ref)  (over its length, with `average`),  x = beta (D_2p - D_2p+1)
 //   loss = w l(x),  d_logp of a token of sequence s = +-w beta l'(x)  (over the length, with `average`)
 // What bounds it is memory: 8 bytes read and 4 written per token, and every token of a sequence has the same gradient, so nothing is
-// read twice.  Lengths are known on the device alone and may be anything, so the work is cut by tokens, 4096 to a CTA, and not by
+// read twice.  Lengths are known on the device alone and may be anything, so the work is cut by tokens, 8192 to a CTA, and not by
 // pairs: the first launch leaves the sum of every piece of a sequence (a CTA's tokens that belong to it), the second joins the pieces
 // of its pairs, each CTA for itself and all in the same order, and writes.  The piece of sequence s in CTA k has place k + s: between
 // two pieces that follow one another either grows by one, so no two share a place, and there are CTAs + sequences places.
 // A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 49 us (2.9 TB/s; what bounds it is the latency of a
 // CTA's way through search, sums and joins, some 6000 cycles), 262144 tokens 10 us, 2000 tokens 8 to 9 us.
+#include <cstddef>
+
 #include "formats.cuh"
 
 using namespace ssgd;
@@ -17,7 +19,7 @@ using namespace ssgd;
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int EACH = 16;                            // consecutive tokens of a thread
+constexpr int EACH = 32;                            // tokens of a thread
 constexpr int CHUNK = THREADS * EACH;
 
 struct Args {
@@ -35,19 +37,12 @@ struct Args {
     double per_token;                               // starts to a token
 };
 
-// starts[s], kept within the tokens
-__device__ __forceinline__ int64_t start_of(const Args& A, int64_t s) {
-    const int64_t v = A.starts64 ? static_cast<const int64_t*>(A.starts)[s] : (int64_t)static_cast<const int32_t*>(A.starts)[s];
-    return v < 0 ? 0 : v > A.tokens ? A.tokens : v;
-}
-
 constexpr int FEW = 64;                             // sequences of a CTA that are gone through one by one
 constexpr int SHORT = 32;                           // where there are more, pieces below it are summed by one thread, others by a warp
 constexpr int LONG = 256;                           // pieces of a pair that the whole CTA joins
 constexpr int32_t NO_MARK = 0x7fa12345;             // the bits of a NaN that no operation makes
 struct Shared {
     alignas(16) float logp[CHUNK];                  // then the gradients
-    alignas(16) float ref[CHUNK];
     int64_t start[FEW + 1];                         // where the sequences begin
     int32_t bound[FEW + 1];                         // the same within the CTA's tokens
     float value[FEW];                               // their gradients
@@ -59,416 +54,459 @@ struct Shared {
     int32_t listed;
     int32_t last[WARPS];
     double joined[WARPS];
+    alignas(16) float ref[CHUNK];                   // (not there in the second launch)
 };
-
-// Tokens of the CTA, and the sequences that may have some of them, in whole pairs: from the last one that starts before the first token to
-// the last one that starts before the end.  The last CTA has those too that start at the end.
-struct Range {
-    int64_t c0, c1, s0, s1;
-    __device__ __forceinline__ bool few() const { return s1 - s0 <= FEW; }
-    __device__ __forceinline__ int within(int64_t token) const { return (int)((token < c0 ? c0 : token > c1 ? c1 : token) - c0); }
-};
-
-// The CTA's range, and the starts of its sequences in shared memory where they are few.  What is looked for are the first starts that
-// are at least c0 and at least c1.  Lengths that are not too unlike put them near chunk / chunks of the way, so the whole CTA looks at
-// 1024 starts there; where they are not among them, it searches, 256 places at a time.
 constexpr int LOOK = 4, WINDOW = LOOK * THREADS;
-struct Window {
-    int64_t w0, v[LOOK];                            // the thread's starts w0 + t + i THREADS
-    __device__ __forceinline__ void load(const Args& A, int64_t chunk) {
-        const int64_t n = 2 * A.pairs + 1;
-        w0 = max(min((int64_t)((double)(chunk * CHUNK + CHUNK / 2) * A.per_token) - WINDOW / 2, n - WINDOW), (int64_t)0);
-#pragma unroll
-        for (int i = 0; i < LOOK; ++i) {
-            const int64_t at = w0 + threadIdx.x + i * THREADS;
-            v[i] = at < n ? start_of(A, at) : INT64_MAX;
+
+// I: what counts tokens and sequences, 32 bits where they suffice.  Half of the instructions are such counting.
+template <typename I> struct Work {
+    // starts[s], kept within the tokens
+    static __device__ __forceinline__ I start_of(const Args& A, I s) {
+        if (A.starts64) {
+            const long long v = static_cast<const long long*>(A.starts)[s];
+            return (I)(v < 0 ? 0 : v > A.tokens ? A.tokens : v);
         }
+        return min(max((I)static_cast<const int32_t*>(A.starts)[s], (I)0), (I)A.tokens);
     }
-    __device__ __forceinline__ Range range(const Args& A, Shared& S, int64_t chunk, int64_t chunks) const {
-        const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-        const bool last = chunk + 1 == chunks;
-        Range R;
-        R.c0 = chunk * CHUNK;
-        R.c1 = min(R.c0 + CHUNK, A.tokens);
-        const int64_t n = 2 * A.pairs + 1;
-        int k0 = 0, k1 = 0;
+
+    // Tokens of the CTA, and the sequences that may have some of them, in whole pairs: from the last one that starts before the first token to
+    // the last one that starts before the end.  The last CTA has those too that start at the end.
+    struct Range {
+        I c0, c1, s0, s1;
+        __device__ __forceinline__ bool few() const { return s1 - s0 <= FEW; }
+        __device__ __forceinline__ int within(I token) const { return (int)((token < c0 ? c0 : token > c1 ? c1 : token) - c0); }
+    };
+
+    // The CTA's range, and the starts of its sequences in shared memory where they are few.  What is looked for are the first starts that
+    // are at least c0 and at least c1.  Lengths that are not too unlike put them near chunk / chunks of the way, so the whole CTA looks at
+    // 1024 starts there; where they are not among them, it searches, 256 places at a time.
+    struct Window {
+        I w0, v[LOOK];                            // the thread's starts w0 + t + i THREADS
+        __device__ __forceinline__ void load(const Args& A, I chunk) {
+            const I n = 2 * (I)A.pairs + 1;
+            w0 = max(min((I)((double)(chunk * CHUNK + CHUNK / 2) * A.per_token) - WINDOW / 2, n - WINDOW), (I)0);
 #pragma unroll
-        for (int i = 0; i < LOOK; ++i) {
-            k0 += __popc(__ballot_sync(0xffffffffu, v[i] < R.c0));
-            k1 += __popc(__ballot_sync(0xffffffffu, v[i] < R.c1));
+            for (int i = 0; i < LOOK; ++i) {
+                const I at = w0 + threadIdx.x + i * THREADS;
+                v[i] = at < n ? start_of(A, at) : (I)(sizeof(I) == 4 ? (long long)INT32_MAX : (long long)INT64_MAX);
+            }
         }
-        if (lane == 0) S.before[warp] = make_int2(k0, k1);
-        __syncthreads();
-        k0 = k1 = 0;
+        __device__ __forceinline__ Range range(const Args& A, Shared& S, I chunk, I chunks) const {
+            const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+            const bool last = chunk + 1 == chunks;
+            Range R;
+            R.c0 = chunk * CHUNK;
+            R.c1 = min(R.c0 + CHUNK, (I)A.tokens);
+            const I n = 2 * (I)A.pairs + 1;
+            int k0 = 0, k1 = 0;
+#pragma unroll
+            for (int i = 0; i < LOOK; ++i) {
+                k0 += __popc(__ballot_sync(0xffffffffu, v[i] < R.c0));
+                k1 += __popc(__ballot_sync(0xffffffffu, v[i] < R.c1));
+            }
+            if (lane == 0) S.before[warp] = make_int2(k0, k1);
+            __syncthreads();
+            k0 = k1 = 0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                k0 += S.before[w].x;
+                k1 += S.before[w].y;
+            }
+            I lo[2] = {w0 + k0, w0 + k1};
+            const bool found = (k0 >= 2 || w0 == 0) && (k1 <= WINDOW - 2 || w0 + WINDOW >= n);     // with the starts of whole pairs around them
+            if (!found) {
+                lo[0] = lo[1] = 0;
+                I hi[2] = {n, n};
+                while (lo[0] < hi[0] || lo[1] < hi[1]) {
+                    bool below[2];
+                    I step[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        step[q] = (hi[q] - lo[q] + THREADS - 1) / THREADS;
+                        const I probe = lo[q] + (I)t * step[q];
+                        below[q] = probe < hi[q] && start_of(A, probe) < (q ? R.c1 : R.c0);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int k = __syncthreads_count(below[q]);               // places lo, lo + step, .. that are before the answer
+                        if (lo[q] >= hi[q]) continue;
+                        const I from = k ? lo[q] + (I)(k - 1) * step[q] + 1 : lo[q];
+                        hi[q] = k ? min(hi[q], lo[q] + (I)k * step[q]) : lo[q];
+                        lo[q] = from;
+                    }
+                }
+            }
+            R.s0 = min(max(lo[0] - 1, (I)0) & ~(I)1, 2 * (I)A.pairs);
+            R.s1 = last ? 2 * (I)A.pairs : min((lo[1] + 1) & ~(I)1, 2 * (I)A.pairs);
+            if (R.s1 < R.s0) R.s1 = R.s0;               // starts that do not ascend
+            if (R.few()) {
+                const int count = (int)(R.s1 - R.s0);
+                auto keep = [&](int i, I start) {
+                    S.start[i] = start;
+                    S.bound[i] = R.within(start);
+                };
+                if (found && R.s0 >= w0 && R.s1 < w0 + WINDOW) {
+#pragma unroll
+                    for (int i = 0; i < LOOK; ++i) {
+                        const I at = w0 + t + i * THREADS - R.s0;
+                        if (at >= 0 && at <= count) keep((int)at, v[i]);
+                    }
+                } else if (t <= count) {
+                    keep(t, start_of(A, R.s0 + t));
+                }
+            }
+            return R;
+        }
+    };
+
+    // A sum with what its roundings lost beside it: 48 bits or more, in fp32 arithmetic (an SM converts to 64 bits at 16 numbers a cycle)
+    struct Sum {
+        float sum = 0.f, lost = 0.f;
+        __device__ __forceinline__ void add(float x) {
+            const float next = sum + x, back = next - sum;
+            lost += (sum - (next - back)) + (x - back);
+            sum = next;
+        }
+        __device__ __forceinline__ void join_warp() {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const float x = __shfl_xor_sync(0xffffffffu, sum, o), l = __shfl_xor_sync(0xffffffffu, lost, o);
+                add(x);
+                lost += l;
+            }
+        }
+        // an infinity or NaN among the numbers leaves NaN in what was lost
+        __device__ __forceinline__ double value() const { return fabsf(sum) < INFINITY ? (double)sum + (double)lost : (double)sum; }
+    };
+
+    // A piece's sum from those of the warps
+    static __device__ __forceinline__ double sum_of_warps(const Shared& S, int q) {
+        Sum sum;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            k0 += S.before[w].x;
-            k1 += S.before[w].y;
+            const float2 p = S.part[w][q];
+            sum.add(p.x);
+            sum.lost += p.y;
         }
-        int64_t lo[2] = {w0 + k0, w0 + k1};
-        const bool found = (k0 >= 2 || w0 == 0) && (k1 <= WINDOW - 2 || w0 + WINDOW >= n);     // with the starts of whole pairs around them
-        if (!found) {
-            lo[0] = lo[1] = 0;
-            int64_t hi[2] = {n, n};
-            while (lo[0] < hi[0] || lo[1] < hi[1]) {
-                bool below[2];
-                int64_t step[2];
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    step[q] = (hi[q] - lo[q] + THREADS - 1) / THREADS;
-                    const int64_t probe = lo[q] + (int64_t)t * step[q];
-                    below[q] = probe < hi[q] && start_of(A, probe) < (q ? R.c1 : R.c0);
-                }
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int k = __syncthreads_count(below[q]);               // places lo, lo + step, .. that are before the answer
-                    if (lo[q] >= hi[q]) continue;
-                    const int64_t from = k ? lo[q] + (int64_t)(k - 1) * step[q] + 1 : lo[q];
-                    hi[q] = k ? min(hi[q], lo[q] + (int64_t)k * step[q]) : lo[q];
-                    lo[q] = from;
-                }
+        return sum.value();
+    }
+
+    // Every warp has an eighth of the CTA's tokens: calls f(q, a, b) for each of n sequences that has some of them, [a, b)
+    template <typename F>
+    static __device__ __forceinline__ void for_pieces(const Shared& S, int n, F f) {
+        const int lane = threadIdx.x & 31, begin = ((int)threadIdx.x >> 5) * (CHUNK / WARPS), end = begin + CHUNK / WARPS;
+        for (int base = 0; base < n; base += 32) {
+            const int q = base + lane;
+            int a = 0, b = 0;
+            if (q < n) {
+                a = max(S.bound[q], begin);
+                b = min(S.bound[q + 1], end);
             }
-        }
-        R.s0 = min(max(lo[0] - 1, (int64_t)0) & ~(int64_t)1, 2 * A.pairs);
-        R.s1 = last ? 2 * A.pairs : min((lo[1] + 1) & ~(int64_t)1, 2 * A.pairs);
-        if (R.s1 < R.s0) R.s1 = R.s0;               // starts that do not ascend
-        if (R.few()) {
-            const int count = (int)(R.s1 - R.s0);
-            auto keep = [&](int i, int64_t start) {
-                S.start[i] = start;
-                S.bound[i] = R.within(start);
-            };
-            if (found && R.s0 >= w0 && R.s1 < w0 + WINDOW) {
-#pragma unroll
-                for (int i = 0; i < LOOK; ++i) {
-                    const int64_t at = w0 + t + i * THREADS - R.s0;
-                    if (at >= 0 && at <= count) keep((int)at, v[i]);
-                }
-            } else if (t <= count) {
-                keep(t, start_of(A, R.s0 + t));
-            }
-        }
-        return R;
-    }
-};
-
-// A sum with what its roundings lost beside it: 48 bits or more, in fp32 arithmetic (an SM converts to 64 bits at 16 numbers a cycle)
-struct Sum {
-    float sum = 0.f, lost = 0.f;
-    __device__ __forceinline__ void add(float x) {
-        const float next = sum + x, back = next - sum;
-        lost += (sum - (next - back)) + (x - back);
-        sum = next;
-    }
-    __device__ __forceinline__ void join_warp() {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float x = __shfl_xor_sync(0xffffffffu, sum, o), l = __shfl_xor_sync(0xffffffffu, lost, o);
-            add(x);
-            lost += l;
-        }
-    }
-    // an infinity or NaN among the numbers leaves NaN in what was lost
-    __device__ __forceinline__ double value() const { return fabsf(sum) < INFINITY ? (double)sum + (double)lost : (double)sum; }
-};
-
-// A piece's sum from those of the warps
-__device__ __forceinline__ double sum_of_warps(const Shared& S, int q) {
-    Sum sum;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-        const float2 p = S.part[w][q];
-        sum.add(p.x);
-        sum.lost += p.y;
-    }
-    return sum.value();
-}
-
-// Every warp has an eighth of the CTA's tokens: calls f(q, a, b) for each of n sequences that has some of them, [a, b)
-template <typename F>
-__device__ __forceinline__ void for_pieces(const Shared& S, int n, F f) {
-    const int lane = threadIdx.x & 31, begin = ((int)threadIdx.x >> 5) * (CHUNK / WARPS), end = begin + CHUNK / WARPS;
-    for (int base = 0; base < n; base += 32) {
-        const int q = base + lane;
-        int a = 0, b = 0;
-        if (q < n) {
-            a = max(S.bound[q], begin);
-            b = min(S.bound[q + 1], end);
-        }
-        for (uint32_t todo = __ballot_sync(0xffffffffu, a < b); todo; todo &= todo - 1) {
-            const int src = __ffs(todo) - 1;
-            f(base + src, __shfl_sync(0xffffffffu, a, src), __shfl_sync(0xffffffffu, b, src));
-        }
-    }
-}
-
-// The CTA's tokens on their way to shared memory while it looks for its sequences.  16 bytes at once, or single ones
-__device__ __forceinline__ void start_tokens(const Args& A, Shared& S, int64_t c0) {
-    const int64_t left = A.tokens - c0;
-    if (A.vector && left >= CHUNK) {                // the same for the whole CTA
-#pragma unroll
-        for (int i = 0; i < EACH / 4; ++i) {
-            const int at = (i * THREADS + (int)threadIdx.x) * 4;
-            copy_async<16>(S.logp + at, A.logp + c0 + at);
-            if (A.ref) copy_async<16>(S.ref + at, A.ref + c0 + at);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int at = i * THREADS + (int)threadIdx.x;
-            if (at < left) {
-                copy_async<4>(S.logp + at, A.logp + c0 + at);
-                if (A.ref) copy_async<4>(S.ref + at, A.ref + c0 + at);
+            for (uint32_t todo = __ballot_sync(0xffffffffu, a < b); todo; todo &= todo - 1) {
+                const int src = __ffs(todo) - 1;
+                f(base + src, __shfl_sync(0xffffffffu, a, src), __shfl_sync(0xffffffffu, b, src));
             }
         }
     }
-    copy_async_commit();
-}
-__device__ __forceinline__ float difference(const Args& A, const Shared& S, int i) { return A.ref ? S.logp[i] - S.ref[i] : S.logp[i]; }
 
-// Sums of the pieces of the CTA's tokens, in 64 bits.  Each is added up by itself, so that what one sequence holds (infinities,
-// the lowest number of a mask) stays there.  WRITE: for other CTAs; otherwise those of few sequences are left in S.part alone.
-template <bool WRITE>
-__device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, int64_t chunk, const Range& R) {
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    if (R.few()) {                                  // every warp takes an eighth of the tokens
-        const int n = (int)(R.s1 - R.s0);
-        for (int i = lane; i < n; i += 32) S.part[warp][i] = make_float2(0.f, 0.f);
-        __syncwarp();
-        for_pieces(S, n, [&](int q, int a, int b) {
-            Sum sum;
+    // The CTA's tokens on their way to shared memory while it looks for its sequences, 16 bytes at once where they may be
+    static __device__ __forceinline__ void start_tokens(const Args& A, Shared& S, I c0) {
+        const int left = (int)min((I)A.tokens - c0, (I)CHUNK);
+        auto some = [&](int at, auto bytes) {
+            copy_async<decltype(bytes)::value>(S.logp + at, A.logp + c0 + at);
+            if (A.ref) copy_async<decltype(bytes)::value>(S.ref + at, A.ref + c0 + at);
+        };
+        const int whole = A.vector ? left & ~3 : 0;
+        for (int at = (int)threadIdx.x * 4; at < whole; at += THREADS * 4) some(at, std::integral_constant<int, 16>{});
+        for (int at = whole + (int)threadIdx.x; at < left; at += THREADS) some(at, std::integral_constant<int, 4>{});
+        copy_async_commit();
+    }
+    static __device__ __forceinline__ float difference(const Args& A, const Shared& S, int i) { return A.ref ? S.logp[i] - S.ref[i] : S.logp[i]; }
+
+    // Sums of the pieces of the CTA's tokens, in 64 bits.  Each is added up by itself, so that what one sequence holds (infinities,
+    // the lowest number of a mask) stays there.  WRITE: for other CTAs; otherwise those of few sequences are left in S.part alone.
+    template <bool WRITE>
+    static __device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, I chunk, const Range& R) {
+        const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+        if (R.few()) {                                  // every warp takes an eighth of the tokens
+            const int n = (int)(R.s1 - R.s0);
+            for (int i = lane; i < n; i += 32) S.part[warp][i] = make_float2(0.f, 0.f);
+            __syncwarp();
+            for_pieces(S, n, [&](int q, int a, int b) {
+                // pairs of tokens, and what is left of them at the ends
+                const int a2 = (a + 1) & ~1, b2 = b & ~1;
+                float2 two = both(0.f), off = both(0.f);
 #pragma unroll 4
+                for (int i = a2 + 2 * lane; i < b2; i += 64) {
+                    float2 x = *reinterpret_cast<const float2*>(S.logp + i);
+                    if (A.ref) x = fma2(*reinterpret_cast<const float2*>(S.ref + i), both(-1.f), x);
+                    const float2 next = add2(two, x), back = fma2(two, both(-1.f), next);
+                    off = add2(off, add2(fma2(fma2(back, both(-1.f), next), both(-1.f), two), fma2(back, both(-1.f), x)));
+                    two = next;
+                }
+                Sum sum;
+                sum.add(two.x);
+                sum.add(two.y);
+                sum.lost += off.x + off.y;
+                if (lane == 0 && a < a2) sum.add(difference(A, S, a));
+                if (lane == 1 && b2 < b && b2 >= a) sum.add(difference(A, S, b2));
+                sum.join_warp();
+                if (lane == 0) S.part[warp][q] = make_float2(sum.sum, sum.lost);
+            });
+            __syncthreads();
+            if (WRITE && t < n && S.bound[t] < S.bound[t + 1]) A.pieces[chunk + R.s0 + t] = sum_of_warps(S, t);
+            return;
+        }
+        for (I s = R.s0 + t; s < R.s1; s += THREADS) {
+            const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
+            if (b - a >= SHORT) {
+                const int at = atomicAdd(&S.listed, 1);
+                if (at <= CHUNK / SHORT) S.list[at] = (int32_t)(s - R.s0);         // more only where starts do not ascend
+            } else if (b > a) {
+                Sum sum;
+                for (int i = a; i < b; ++i) sum.add(difference(A, S, i));
+                A.pieces[chunk + s] = sum.value();
+            }
+        }
+        __syncthreads();
+        for (int q = warp; q < min(S.listed, CHUNK / SHORT + 1); q += WARPS) {
+            const I s = R.s0 + S.list[q];
+            const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
+            Sum sum;
             for (int i = a + lane; i < b; i += 32) sum.add(difference(A, S, i));
             sum.join_warp();
-            if (lane == 0) S.part[warp][q] = make_float2(sum.sum, sum.lost);
-        });
-        __syncthreads();
-        if (WRITE && t < n && S.bound[t] < S.bound[t + 1]) A.pieces[chunk + R.s0 + t] = sum_of_warps(S, t);
-        return;
-    }
-    for (int64_t s = R.s0 + t; s < R.s1; s += THREADS) {
-        const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
-        if (b - a >= SHORT) {
-            const int at = atomicAdd(&S.listed, 1);
-            if (at <= CHUNK / SHORT) S.list[at] = (int32_t)(s - R.s0);         // more only where starts do not ascend
-        } else if (b > a) {
-            Sum sum;
-            for (int i = a; i < b; ++i) sum.add(difference(A, S, i));
-            A.pieces[chunk + s] = sum.value();
+            if (lane == 0) A.pieces[chunk + s] = sum.value();
         }
     }
-    __syncthreads();
-    for (int q = warp; q < min(S.listed, CHUNK / SHORT + 1); q += WARPS) {
-        const int64_t s = R.s0 + S.list[q];
-        const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
-        Sum sum;
-        for (int i = a + lane; i < b; i += 32) sum.add(difference(A, S, i));
-        sum.join_warp();
-        if (lane == 0) A.pieces[chunk + s] = sum.value();
-    }
-}
 
-// l(x) and l'(x)
-__device__ __forceinline__ float2 loss_of(const Args& A, float x) {
-    if (A.kind == SSGD_PREFERENCE_IPO) {            // (x - 1/2)^2 / beta^2 = (h - 1 / (2 beta))^2 with x = beta h
-        const float d = (x - 0.5f) / A.beta;
-        return make_float2(d * d, 2.f * d / A.beta);
+    // l(x) and l'(x)
+    static __device__ __forceinline__ float2 loss_of(const Args& A, float x) {
+        if (A.kind == SSGD_PREFERENCE_IPO) {            // (x - 1/2)^2 / beta^2 = (h - 1 / (2 beta))^2 with x = beta h
+            const float d = (x - 0.5f) / A.beta;
+            return make_float2(d * d, 2.f * d / A.beta);
+        }
+        if (A.kind == SSGD_PREFERENCE_HINGE) return x < 1.f ? make_float2(1.f - x, -1.f) : x >= 1.f ? make_float2(0.f, 0.f) : make_float2(x, x);
+        const float e = expf(-fabsf(x)), soft = log1pf(e);
+        const float lose = x >= 0.f ? e / (1.f + e) : 1.f / (1.f + e);              // sigmoid(-x)
+        float loss = (1.f - A.smoothing) * (fmaxf(-x, 0.f) + soft);
+        if (A.smoothing > 0.f) loss += A.smoothing * (fmaxf(x, 0.f) + soft);
+        return make_float2(x != x ? x : loss, A.smoothing - lose);
     }
-    if (A.kind == SSGD_PREFERENCE_HINGE) return x < 1.f ? make_float2(1.f - x, -1.f) : x >= 1.f ? make_float2(0.f, 0.f) : make_float2(x, x);
-    const float e = expf(-fabsf(x)), soft = log1pf(e);
-    const float lose = x >= 0.f ? e / (1.f + e) : 1.f / (1.f + e);              // sigmoid(-x)
-    float loss = (1.f - A.smoothing) * (fmaxf(-x, 0.f) + soft);
-    if (A.smoothing > 0.f) loss += A.smoothing * (fmaxf(x, 0.f) + soft);
-    return make_float2(x != x ? x : loss, A.smoothing - lose);
-}
 
-// Number of pieces of tokens [a, b), and the first one's CTA
-__device__ __forceinline__ int64_t pieces_of(int64_t a, int64_t b, int64_t* first) {
-    *first = a / CHUNK;
-    return b > a ? (b - 1) / CHUNK - *first + 1 : 0;
-}
-
-// Of one pair: sums -> loss, rewards, gradients
-struct Outcome { float d0, d1; };
-__device__ __forceinline__ Outcome pair_outcome(const Args& A, int64_t p, float w, double D0, double D1, int64_t n0, int64_t n1, bool write) {
-    double f0 = 1.0, f1 = 1.0;
-    if (A.average) { f0 = n0 > 0 ? 1.0 / (double)n0 : 0.0; f1 = n1 > 0 ? 1.0 / (double)n1 : 0.0; }
-    const double r0 = (double)A.beta * (D0 * f0), r1 = (double)A.beta * (D1 * f1);
-    const float2 l = loss_of(A, (float)(r0 - r1));
-    if (write) {
-        A.loss[p] = w == 0.f ? 0.f : w * l.x;
-        A.rewards[p] = (float)r0;
-        A.rewards[A.pairs + p] = (float)r1;
+    // Number of pieces of tokens [a, b), and the first one's CTA
+    static __device__ __forceinline__ I pieces_of(I a, I b, I* first) {
+        *first = a / CHUNK;
+        return b > a ? (b - 1) / CHUNK - *first + 1 : 0;
     }
-    const float slope = w == 0.f ? 0.f : w * A.beta * l.y;
-    return Outcome{A.average ? (float)((double)slope * f0) : slope, A.average ? (float)(-(double)slope * f1) : -slope};
-}
 
-// ALONE: there is no other CTA
-template <bool ALONE>
-__device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R, bool last) {
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const bool few = R.few();
-    const int n = few ? (int)(R.s1 - R.s0) : 0;
-    if (!few) {
-        // a sequence's gradient stands where it begins in this CTA
-        for (int i = t; i < CHUNK; i += THREADS) S.logp[i] = __int_as_float(NO_MARK);
-        __syncthreads();
+    // Of one pair: sums -> loss, rewards, gradients
+    struct Outcome { float d0, d1; };
+    static __device__ __forceinline__ Outcome pair_outcome(const Args& A, I p, float w, double D0, double D1, I n0, I n1, bool write) {
+        double f0 = 1.0, f1 = 1.0;
+        if (A.average) { f0 = n0 > 0 ? 1.0 / (double)n0 : 0.0; f1 = n1 > 0 ? 1.0 / (double)n1 : 0.0; }
+        const double r0 = (double)A.beta * (D0 * f0), r1 = (double)A.beta * (D1 * f1);
+        const float2 l = loss_of(A, (float)(r0 - r1));
+        if (write) {
+            A.loss[p] = w == 0.f ? 0.f : w * l.x;
+            A.rewards[p] = (float)r0;
+            A.rewards[A.pairs + p] = (float)r1;
+        }
+        const float slope = w == 0.f ? 0.f : w * A.beta * l.y;
+        return Outcome{A.average ? (float)((double)slope * f0) : slope, A.average ? (float)(-(double)slope * f1) : -slope};
     }
-    // of sequence s, which is tokens [a, b)
-    auto put = [&](int64_t s, int64_t a, int64_t b, float v) {
-        if (few) {
-            S.value[s - R.s0] = v;
+
+    // ALONE: there is no other CTA
+    template <bool ALONE>
+    static __device__ __forceinline__ void finish(const Args& A, Shared& S, const Range& R, bool last) {
+        const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+        const bool few = R.few();
+        const int n = few ? (int)(R.s1 - R.s0) : 0;
+        if (!few) {
+            // a sequence's gradient stands where it begins in this CTA
+            for (int i = t; i < CHUNK; i += THREADS) S.logp[i] = __int_as_float(NO_MARK);
+            __syncthreads();
+        }
+        // of sequence s, which is tokens [a, b)
+        auto put = [&](I s, I a, I b, float v) {
+            if (few) {
+                S.value[s - R.s0] = v;
+            } else {
+                const int i = R.within(a), j = R.within(b);
+                if (i < j) S.logp[i] = v;
+            }
+        };
+        auto pair_of = [&](I p, I (&at)[3]) {
+#pragma unroll
+            for (int q = 0; q < 3; ++q) at[q] = few ? S.start[2 * p + q - R.s0] : start_of(A, 2 * p + q);
+        };
+        auto settle = [&](I p, const I (&at)[3], float w, double D0, double D1) {
+            // by the CTA in which the pair begins
+            const bool write = (at[0] >= R.c0 && at[0] < R.c1) || (last && at[0] >= R.c1);
+            const Outcome g = pair_outcome(A, p, w, D0, D1, at[1] - at[0], at[2] - at[1], write);
+            put(2 * p, at[0], at[1], g.d0);
+            put(2 * p + 1, at[1], at[2], g.d1);
+        };
+        auto weight_of = [&](I p) { return A.weights ? A.weights[p] : 1.f; };
+        const I p0 = R.s0 / 2, p1 = R.s1 / 2;
+        if (ALONE && few) {
+            if (p0 + t < p1) {
+                I at[3];
+                pair_of(p0 + t, at);
+                settle(p0 + t, at, weight_of(p0 + t), sum_of_warps(S, 2 * t), sum_of_warps(S, 2 * t + 1));
+            }
         } else {
-            const int i = R.within(a), j = R.within(b);
-            if (i < j) S.logp[i] = v;
-        }
-    };
-    auto pair_of = [&](int64_t p, int64_t (&at)[3]) {
+            // Pairs of more pieces than one to a sequence have tokens in other CTAs too: they are the first or the last of this one.  A warp
+            // joins one, or all warps where the pieces are many.
+            for (int side = 0; side < 2; ++side) {
+                const I p = side ? p1 - 1 : p0;
+                if (p >= p1 || (side && p == p0)) break;    // the same for the whole CTA
+                I at[3], k[2];
+                pair_of(p, at);
+                const I n0 = pieces_of(at[0], at[1], &k[0]), n1 = pieces_of(at[1], at[2], &k[1]);
+                const bool many = n0 + n1 > LONG;           // the same in every CTA: the order of the sum is
+                if (!many && warp != side) continue;
+                const int stride = many ? THREADS : 32, first = many ? t : lane;
+                const float w = weight_of(p);
+                double D[2] = {0.0, 0.0};
+                if (n0 <= 4 && n1 <= 4) {                   // the usual case: one lane adds them up
+                    if (lane != 0) continue;
 #pragma unroll
-        for (int q = 0; q < 3; ++q) at[q] = few ? S.start[2 * p + q - R.s0] : start_of(A, 2 * p + q);
-    };
-    auto settle = [&](int64_t p, const int64_t (&at)[3], float w, double D0, double D1) {
-        // by the CTA in which the pair begins
-        const bool write = (at[0] >= R.c0 && at[0] < R.c1) || (last && at[0] >= R.c1);
-        const Outcome g = pair_outcome(A, p, w, D0, D1, at[1] - at[0], at[2] - at[1], write);
-        put(2 * p, at[0], at[1], g.d0);
-        put(2 * p + 1, at[1], at[2], g.d1);
-    };
-    auto weight_of = [&](int64_t p) { return A.weights ? A.weights[p] : 1.f; };
-    const int64_t p0 = R.s0 / 2, p1 = R.s1 / 2;
-    if (ALONE && few) {
-        if (p0 + t < p1) {
-            int64_t at[3];
-            pair_of(p0 + t, at);
-            settle(p0 + t, at, weight_of(p0 + t), sum_of_warps(S, 2 * t), sum_of_warps(S, 2 * t + 1));
-        }
-    } else {
-        // Pairs of more pieces than one to a sequence have tokens in other CTAs too: they are the first or the last of this one.  A warp
-        // joins one, or all warps where the pieces are many.
-        for (int side = 0; side < 2; ++side) {
-            const int64_t p = side ? p1 - 1 : p0;
-            if (p >= p1 || (side && p == p0)) break;    // the same for the whole CTA
-            int64_t at[3], k[2];
-            pair_of(p, at);
-            const int64_t n0 = pieces_of(at[0], at[1], &k[0]), n1 = pieces_of(at[1], at[2], &k[1]);
-            const bool many = n0 + n1 > LONG;           // the same in every CTA: the order of the sum is
-            if (!many && warp != side) continue;
-            const int stride = many ? THREADS : 32, first = many ? t : lane;
-            const float w = weight_of(p);
-            double D[2] = {0.0, 0.0};
-            if (n0 <= 4 && n1 <= 4) {                   // the usual case: one lane adds them up
-                if (lane != 0) continue;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (i < n0) D[0] += A.pieces[k[0] + i + 2 * p];
-                    if (i < n1) D[1] += A.pieces[k[1] + i + 2 * p + 1];
+                    for (int i = 0; i < 4; ++i) {
+                        if (i < n0) D[0] += A.pieces[k[0] + i + 2 * p];
+                        if (i < n1) D[1] += A.pieces[k[1] + i + 2 * p + 1];
+                    }
+                    settle(p, at, w, D[0], D[1]);
+                    continue;
                 }
-                settle(p, at, w, D[0], D[1]);
-                continue;
-            }
-            for (int64_t i = first; i < n0; i += stride) D[0] += A.pieces[k[0] + i + 2 * p];
-            for (int64_t i = first; i < n1; i += stride) D[1] += A.pieces[k[1] + i + 2 * p + 1];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) D[q] += __shfl_xor_sync(0xffffffffu, D[q], o);
-            }
-            if (many) {
+                for (I i = first; i < n0; i += stride) D[0] += A.pieces[k[0] + i + 2 * p];
+                for (I i = first; i < n1; i += stride) D[1] += A.pieces[k[1] + i + 2 * p + 1];
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    __syncthreads();
-                    if (lane == 0) S.joined[warp] = D[q];
-                    __syncthreads();
-                    D[q] = 0.0;
-                    for (int i = 0; i < WARPS; ++i) D[q] += S.joined[i];
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) D[q] += __shfl_xor_sync(0xffffffffu, D[q], o);
                 }
+                if (many) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        __syncthreads();
+                        if (lane == 0) S.joined[warp] = D[q];
+                        __syncthreads();
+                        D[q] = 0.0;
+                        for (int i = 0; i < WARPS; ++i) D[q] += S.joined[i];
+                    }
+                }
+                if (many ? t == 0 : lane == 0) settle(p, at, w, D[0], D[1]);
             }
-            if (many ? t == 0 : lane == 0) settle(p, at, w, D[0], D[1]);
+            // the others lie within the CTA: one piece per sequence
+            for (I p = p0 + 1 + (t ^ 64); p < p1 - 1; p += THREADS) {        // beginning with warps that join nothing
+                I at[3];
+                pair_of(p, at);
+                settle(p, at, weight_of(p), at[1] > at[0] ? A.pieces[at[0] / CHUNK + 2 * p] : 0.0, at[2] > at[1] ? A.pieces[at[1] / CHUNK + 2 * p + 1] : 0.0);
+            }
         }
-        // the others lie within the CTA: one piece per sequence
-        for (int64_t p = p0 + 1 + (t ^ 64); p < p1 - 1; p += THREADS) {        // beginning with warps that join nothing
-            int64_t at[3];
-            pair_of(p, at);
-            settle(p, at, weight_of(p), at[1] > at[0] ? A.pieces[at[0] / CHUNK + 2 * p] : 0.0, at[2] > at[1] ? A.pieces[at[1] / CHUNK + 2 * p + 1] : 0.0);
+        if (!A.d_logp) return;
+        const int tokens = (int)(R.c1 - R.c0);
+        float* out = A.d_logp + R.c0;
+        if (few) {
+            __syncthreads();
+            const int begin = n ? S.bound[0] : tokens, end = n ? S.bound[n] : tokens;
+            for (int i = t; i < begin; i += THREADS) out[i] = 0.f;                 // tokens of no sequence
+            for_pieces(S, n, [&](int q, int a, int b) {
+                const float v = S.value[q];
+                for (int i = a + lane; i < b; i += 32) out[i] = v;
+            });
+            for (int i = end + t; i < tokens; i += THREADS) out[i] = 0.f;
+            return;
         }
-    }
-    if (!A.d_logp) return;
-    const int tokens = (int)(R.c1 - R.c0);
-    float* out = A.d_logp + R.c0;
-    if (few) {
+        if (t == 0) {
+            const int end = R.within(start_of(A, 2 * (I)A.pairs));
+            if (end < tokens) S.logp[end] = 0.f;
+        }
         __syncthreads();
-        const int begin = n ? S.bound[0] : tokens, end = n ? S.bound[n] : tokens;
-        for (int i = t; i < begin; i += THREADS) out[i] = 0.f;                 // tokens of no sequence
-        for_pieces(S, n, [&](int q, int a, int b) {
-            const float v = S.value[q];
-            for (int i = a + lane; i < b; i += 32) out[i] = v;
-        });
-        for (int i = end + t; i < tokens; i += THREADS) out[i] = 0.f;
-        return;
-    }
-    if (t == 0) {
-        const int end = R.within(start_of(A, 2 * A.pairs));
-        if (end < tokens) S.logp[end] = 0.f;
-    }
-    __syncthreads();
-    // every token takes the last mark at or before it
-    float v[EACH];
-    float mine = __int_as_float(NO_MARK);
+        // every token takes the last mark at or before it
+        float v[EACH];
+        float mine = __int_as_float(NO_MARK);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        v[i] = S.logp[t * EACH + i];
-        if (__float_as_int(v[i]) != NO_MARK) mine = v[i];
-    }
-    // the last mark of the threads before this one
-    const uint32_t votes = __ballot_sync(0xffffffffu, __float_as_int(mine) != NO_MARK);
-    const float of_warp = __shfl_sync(0xffffffffu, mine, votes ? 31 - __clz((int)votes) : 0);
-    if (lane == 0) S.last[warp] = __float_as_int(of_warp);
-    __syncthreads();
-    float carry = 0.f;
-    for (int w = 0; w < warp; ++w)
-        if (S.last[w] != NO_MARK) carry = __int_as_float(S.last[w]);
-    const uint32_t below = votes & ((1u << lane) - 1u);
-    const float of_lane = __shfl_sync(0xffffffffu, mine, below ? 31 - __clz((int)below) : 0);
-    if (below) carry = of_lane;
+        for (int i = 0; i < EACH; ++i) {
+            v[i] = S.logp[t * EACH + i];
+            if (__float_as_int(v[i]) != NO_MARK) mine = v[i];
+        }
+        // the last mark of the threads before this one
+        const uint32_t votes = __ballot_sync(0xffffffffu, __float_as_int(mine) != NO_MARK);
+        const float of_warp = __shfl_sync(0xffffffffu, mine, votes ? 31 - __clz((int)votes) : 0);
+        if (lane == 0) S.last[warp] = __float_as_int(of_warp);
+        __syncthreads();
+        float carry = 0.f;
+        for (int w = 0; w < warp; ++w)
+            if (S.last[w] != NO_MARK) carry = __int_as_float(S.last[w]);
+        const uint32_t below = votes & ((1u << lane) - 1u);
+        const float of_lane = __shfl_sync(0xffffffffu, mine, below ? 31 - __clz((int)below) : 0);
+        if (below) carry = of_lane;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        if (__float_as_int(v[i]) != NO_MARK) carry = v[i];
-        S.logp[t * EACH + i] = carry;
+        for (int i = 0; i < EACH; ++i) {
+            if (__float_as_int(v[i]) != NO_MARK) carry = v[i];
+            S.logp[t * EACH + i] = carry;
+        }
+        __syncthreads();
+        for (int i = t; i < tokens; i += THREADS) out[i] = S.logp[i];
     }
-    __syncthreads();
-    for (int i = t; i < tokens; i += THREADS) out[i] = S.logp[i];
-}
+};
 
 enum Part { SUMS, FINISH, ALL };
 
-template <Part PART>
-__global__ void __launch_bounds__(THREADS, 6) k_preference(const Args A) {
-    __shared__ Shared S;
-    const int64_t chunk = blockIdx.x;
+template <Part PART, typename I>
+__global__ void __launch_bounds__(THREADS, 4) k_preference(const Args A) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    Shared& S = *reinterpret_cast<Shared*>(raw);
+    using W = Work<I>;
+    const I chunk = blockIdx.x;
     const bool last = blockIdx.x + 1 == gridDim.x;
+    typename W::Window window;
     if constexpr (PART == FINISH) {
-        Window W;
-        W.load(A, chunk);
-        const Range R = W.range(A, S, chunk, gridDim.x);                       // what the caller gave need not wait for the sums
+        window.load(A, chunk);
+        const typename W::Range R = window.range(A, S, chunk, gridDim.x);     // what the caller gave need not wait for the sums
         successor_wait();
         __syncthreads();
-        finish<false>(A, S, R, last);
+        W::template finish<false>(A, S, R, last);
     } else {
         successor_may_start();
-        Window W;
-        W.load(A, chunk);
-        start_tokens(A, S, chunk * CHUNK);
-        const Range R = W.range(A, S, chunk, gridDim.x);
+        window.load(A, chunk);
+        W::start_tokens(A, S, chunk * CHUNK);
+        const typename W::Range R = window.range(A, S, chunk, gridDim.x);
         if (threadIdx.x == 0) S.listed = 0;
         copy_async_wait<0>();
         __syncthreads();
-        sum_pieces<PART == SUMS>(A, S, chunk, R);
+        W::template sum_pieces<PART == SUMS>(A, S, chunk, R);
         if constexpr (PART == ALL) {
             __syncthreads();
-            finish<true>(A, S, R, last);
+            W::template finish<true>(A, S, R, last);
         }
     }
+}
+
+template <Part PART, typename I>
+int launch_part(const Args& A, int64_t chunks, cudaStream_t st) {
+    constexpr int smem = PART == FINISH ? (int)offsetof(Shared, ref) : (int)sizeof(Shared);
+    static PerDevice known;
+    int fits = 0;
+    if (int e = residency(k_preference<PART, I>, THREADS, smem, known, &fits)) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)chunks);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = PART == FINISH ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, k_preference<PART, I>, A) == cudaSuccess ? SSGD_OK : SSGD_ECUDA;
+}
+template <typename I>
+int launch_all(const Args& A, int64_t chunks, cudaStream_t st) {
+    if (chunks == 1) return launch_part<ALL, I>(A, chunks, st);
+    if (int e = launch_part<SUMS, I>(A, chunks, st)) return e;
+    return launch_part<FINISH, I>(A, chunks, st);
 }
 
 constexpr int64_t MAX_TOKENS = (int64_t)1 << 40, MAX_PAIRS = (int64_t)1 << 30;
@@ -506,13 +544,7 @@ int ssgd_preference_loss(const float* logp, const float* ref_logp, int64_t token
                  tokens ? (double)(2 * pairs + 1) / (double)tokens : 0.0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (chunks > 0x7fffffff) return SSGD_ETOOBIG;
-    if (chunks == 1) {
-        k_preference<ALL><<<1, THREADS, 0, st>>>(A);
-        return launched();
-    }
-    k_preference<SUMS><<<(unsigned)chunks, THREADS, 0, st>>>(A);
-    if (int e = launched()) return e;
-    return launch_after(st, k_preference<FINISH>, dim3((unsigned)chunks), THREADS, A);
+    return tokens < (int64_t)1 << 30 && pairs < (int64_t)1 << 28 ? launch_all<int32_t>(A, chunks, st) : launch_all<int64_t>(A, chunks, st);
 }
 
 }  // extern "C"

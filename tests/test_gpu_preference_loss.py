@@ -79,7 +79,8 @@ def lengths(pairs, mean, seed):
 
 CASES = [([1, 1], 0, 0), ([0, 0], 3, 2), ([5, 0], 0, 0), ([0, 7], 0, 1), ([4096, 4096], 0, 0), ([4095, 1, 1, 4095], 0, 5), ([1] * 400, 0, 0),
          ([0] * 300 + [1, 2] + [0] * 300, 1, 1), ([20000, 3], 0, 0), ([3, 1200000], 7, 9), (lengths(8, 100, 1), 0, 40), (lengths(500, 30, 2), 5000, 9000),
-         (lengths(3, 30000, 3), 0, 0), (lengths(4000, 3, 4), 0, 0), ([16] * 6000, 100, 0)]
+         (lengths(3, 30000, 3), 0, 0), (lengths(4000, 3, 4), 0, 0), ([16] * 6000, 100, 0),
+         ([8192, 8192], 0, 0), ([8191, 1, 1, 8191], 0, 3), ([8192, 0, 0, 8192], 0, 0), ([128] * 256, 0, 0), ([100] * 64 + [0] * 2000, 3, 3)]
 
 
 @pytest.mark.parametrize("case", range(len(CASES)))
@@ -152,6 +153,25 @@ def test_preference_loss_of_nothing_and_of_starts_beyond_the_tokens(cuda_device)
     a = T.preference_loss(logp, ref, torch.tensor([-5, 4000, 1 << 40], device="cuda"))
     b = T.preference_loss(logp, ref, torch.tensor([0, 4000, 10000], device="cuda"))
     assert torch.equal(a.loss, b.loss) and torch.equal(a.d_logp, b.d_logp)
+
+
+def test_preference_loss_of_more_tokens_than_32_bits_count(cuda_device):
+    n = (1 << 30) + 5
+    logp = torch.zeros(n, device="cuda")
+    cuts = [0, 1 << 29, (1 << 30) - 3, (1 << 30) - 1, n - 2]
+    for a, b, v in zip(cuts, cuts[1:], (-2.0 ** -20, -2.0 ** -21, -1.0, -0.5)):      # powers of two: every sum is exact
+        logp[a:b] = v
+    starts = torch.tensor(cuts, device="cuda")
+    r = T.preference_loss(logp, None, starts, beta=0.01)
+    D = [(b - a) * v for a, b, v in zip(cuts, cuts[1:], (-2.0 ** -20, -2.0 ** -21, -1.0, -0.5))]
+    want = torch.tensor(D, dtype=torch.float64).view(2, 2) * float(np.float32(0.01))
+    assert (r.rewards.cpu().double().t() - want).abs().max() <= 2 * U * want.abs().max()
+    x = want[:, 0] - want[:, 1]
+    slope = -torch.sigmoid(-x) * float(np.float32(0.01))
+    for a, b, v in zip(cuts, cuts[1:], (slope[0], -slope[0], slope[1], -slope[1])):
+        piece = r.d_logp[a:b]
+        assert float(piece.min()) == float(piece.max()) and abs(float(piece[0]) - float(v)) <= 64 * U * 0.01
+    assert (r.d_logp[-2:] == 0).all()
 
 
 def test_preference_loss_gradient_against_differences(cuda_device):
