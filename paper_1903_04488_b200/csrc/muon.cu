@@ -182,16 +182,18 @@ __device__ __forceinline__ void put_momentum(const Matrix& M, const Share<T>& s,
             if (e < n) to[e] = s.m[i].e[e];
     }
 }
-// 1 / (norm + eps), from the sum of squares, as a power of two and a factor near one: either alone may be out of range
+// 1 / (norm + eps), from the sum of squares, as a factor near one and two powers of two: the norm may lie beyond fp32
 struct Inverse {
-    float power, factor;
+    float power[2], factor;
     __device__ __forceinline__ Inverse(double sum, float eps) {
         const double inv = 1.0 / (sqrt(sum) + (double)eps);
         int exponent = 0;
         factor = (float)(inv > 0.0 && inv < (double)INFINITY ? frexp(inv, &exponent) : inv) * SCALE;
-        power = ldexpf(1.f, min(max(exponent, -126), 127));
+        exponent = min(max(exponent, -252), 254);
+        power[0] = ldexpf(1.f, exponent / 2);
+        power[1] = ldexpf(1.f, exponent - exponent / 2);
     }
-    __device__ __forceinline__ float of(float u) const { return u * power * factor; }
+    __device__ __forceinline__ float of(float u) const { return u * power[0] * power[1] * factor; }
 };
 
 // m <- momentum m + (1 - momentum) g, and the sum of squares of what is to be made orthogonal, per strip.  Squares are added in 64

@@ -191,10 +191,10 @@ template <typename I> struct Work {
         return sum.value();
     }
 
-    // Every warp has an eighth of the CTA's tokens: calls f(q, a, b) for each of n sequences that has some of them, [a, b)
+    // Every warp has an eighth of the CTA's tokens: calls f(q, a, b) for each of the n sequences that has some of them, [a, b)
     template <typename F>
-    static __device__ __forceinline__ void for_pieces(const Shared& S, int n, F f) {
-        const int lane = threadIdx.x & 31, begin = ((int)threadIdx.x >> 5) * (CHUNK / WARPS), end = begin + CHUNK / WARPS;
+    static __device__ __forceinline__ void for_pieces(const Shared& S, int n, int tokens, F f) {
+        const int lane = threadIdx.x & 31, span = (tokens + WARPS - 1) / WARPS, begin = ((int)threadIdx.x >> 5) * span, end = begin + span;
         for (int base = 0; base < n; base += 32) {
             const int q = base + lane;
             int a = 0, b = 0;
@@ -232,7 +232,7 @@ template <typename I> struct Work {
             const int n = (int)(R.s1 - R.s0);
             for (int i = lane; i < n; i += 32) S.part[warp][i] = make_float2(0.f, 0.f);
             __syncwarp();
-            for_pieces(S, n, [&](int q, int a, int b) {
+            for_pieces(S, n, (int)(R.c1 - R.c0), [&](int q, int a, int b) {
                 // pairs of tokens, and what is left of them at the ends
                 const int a2 = (a + 1) & ~1, b2 = b & ~1;
                 float2 two = both(0.f), off = both(0.f);
@@ -411,7 +411,7 @@ template <typename I> struct Work {
             __syncthreads();
             const int begin = n ? S.bound[0] : tokens, end = n ? S.bound[n] : tokens;
             for (int i = t; i < begin; i += THREADS) out[i] = 0.f;                 // tokens of no sequence
-            for_pieces(S, n, [&](int q, int a, int b) {
+            for_pieces(S, n, (int)(R.c1 - R.c0), [&](int q, int a, int b) {
                 const float v = S.value[q];
                 for (int i = a + lane; i < b; i += 32) out[i] = v;
             });

@@ -104,6 +104,11 @@ def test_orthogonalize_of_zeros_magnitudes_and_values_that_are_not_finite(cuda_d
     assert T.orthogonalize(tiny).abs().max() < 1e-10
     exact = T.orthogonalize(tiny, eps=0.0)
     assert off(exact, iterate(rand(70, 90, seed=5).double(), eps=0.0)) < 1e-5
+    for big in (3e36, 5e37):                   # the norm itself is beyond fp32
+        for shape in ((70, 90), (300, 200)):
+            y = rand(*shape, seed=6).clamp(-6, 6)
+            assert off(T.orthogonalize(y * big), iterate((y * big).double())) < 1e-5
+            assert off(T.orthogonalize((y * big).bfloat16()), iterate((y * big).bfloat16().double())) < ONE_PRODUCT + 2.0 ** -8
     x[1, 0, 0] = math.inf
     assert T.orthogonalize(x[1]).isnan().any() and T.orthogonalize(torch.zeros(3, 3, device="cuda"), eps=0.0).isnan().all()
 
