@@ -774,7 +774,7 @@ k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap 
 //
 // Where x and A fit the shared memory of one CTA (the shorter side up to 128, the longer up to 256), one CTA does all of it for one matrix:
 // momentum, division, every step.  The launches above would each wait for the one before, 6 us for a microsecond's work (four matrices of
-// 64 x 128: 98 us; this way 38).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
+// 64 x 128: 98 us; this way 36).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
 // number by number: both halves of the symmetric products are computed, so that each thread needs its own numbers alone.
 
 constexpr int SMALL_SHORT = 2, SMALL_LONG = 4;      // blocks of the sides

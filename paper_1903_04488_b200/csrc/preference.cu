@@ -8,8 +8,8 @@
 // pairs: the first launch leaves the sum of every piece of a sequence (a CTA's tokens that belong to it), the second joins the pieces
 // of its pairs, each CTA for itself and all in the same order, and writes.  The piece of sequence s in CTA k has place k + s: between
 // two pieces that follow one another either grows by one, so no two share a place, and there are CTAs + sequences places.
-// A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 49 us (2.9 TB/s; what bounds it is the latency of a
-// CTA's way through search, sums and joins, some 6000 cycles), 262144 tokens 10 us, 2000 tokens 8 to 9 us.
+// A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 41 us (3.5 TB/s;
+// 25 for the sums, where an SM has three CTAs that load and add by turns, 15 for the rest), 262144 tokens 10 us, 2000 tokens 8 us.
 #include <cstddef>
 
 #include "formats.cuh"
