@@ -33,9 +33,6 @@ __device__ __forceinline__ void bar_init_fence() { asm volatile("fence.mbarrier_
 __device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_addr(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_addr(bar)) : "memory");
-}
 __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
