@@ -1,4 +1,5 @@
-"""Operators of the training step around the compression: layer norm, log probabilities of given tokens, AdamW.
+"""Operators of the training step around the compression: layer norm, log probabilities of given tokens, AdamW; and of fine-tuning: the
+policy loss, the preference loss, orthogonalised matrices and Muon.
 
 The gradient that `Ssgd.step` compresses comes out of a model's layers and loss, and the parameters that are not sketched
 need an ordinary optimizer step.  The work is done by kernels of libssgd.so, enqueued on the current stream; the checks of
