@@ -223,7 +223,7 @@ template <typename I> struct Work {
     }
     static __device__ __forceinline__ float difference(const Args& A, const Shared& S, int i) { return A.ref ? S.logp[i] - S.ref[i] : S.logp[i]; }
 
-    // Sums of the pieces of the CTA's tokens, in 64 bits.  Each is added up by itself, so that what one sequence holds (infinities,
+    // Sums of the pieces of the CTA's tokens, of 48 bits or more.  Each is added up by itself, so that what one sequence holds (infinities,
     // the lowest number of a mask) stays there.  WRITE: for other CTAs; otherwise those of few sequences are left in S.part alone.
     template <bool WRITE>
     static __device__ __forceinline__ void sum_pieces(const Args& A, Shared& S, I chunk, const Range& R) {
