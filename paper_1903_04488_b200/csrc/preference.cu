@@ -8,7 +8,7 @@
 // pairs: the first launch leaves the sum of every piece of a sequence (a CTA's tokens that belong to it), the second joins the pieces
 // of its pairs, each CTA for itself and all in the same order, and writes.  The piece of sequence s in CTA k has place k + s: between
 // two pieces that follow one another either grows by one, so no two share a place, and there are CTAs + sequences places.
-// A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 41 us (3.5 TB/s;
+// A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 40 us (3.6 TB/s;
 // 25 for the sums, where an SM has three CTAs that load and add by turns, 15 for the rest), 262144 tokens 10 us, 2000 tokens 8 us.
 #include <cstddef>
 
@@ -56,6 +56,12 @@ struct Shared {
     double joined[WARPS];
     alignas(16) float ref[CHUNK];                   // (not there in the second launch)
 };
+// Where token i's mark stands while each thread goes through EACH tokens that follow one another: the threads of a warp meet no bank twice
+// (12M tokens in 200,000 pairs 86 us against 103).
+__device__ __forceinline__ int place_of(int i) {
+    static_assert(EACH == 32, "a row of all banks to a thread");
+    return i ^ (i >> 5 & 31);
+}
 constexpr int LOOK = 4, WINDOW = LOOK * THREADS;
 
 // I: what counts tokens and sequences, 32 bits where they suffice.  Half of the instructions are such counting.
@@ -332,7 +338,7 @@ template <typename I> struct Work {
                 S.value[s - R.s0] = v;
             } else {
                 const int i = R.within(a), j = R.within(b);
-                if (i < j) S.logp[i] = v;
+                if (i < j) S.logp[place_of(i)] = v;
             }
         };
         auto pair_of = [&](I p, I (&at)[3]) {
@@ -420,16 +426,15 @@ template <typename I> struct Work {
         }
         if (t == 0) {
             const int end = R.within(start_of(A, 2 * (I)A.pairs));
-            if (end < tokens) S.logp[end] = 0.f;
+            if (end < tokens) S.logp[place_of(end)] = 0.f;
         }
         __syncthreads();
         // every token takes the last mark at or before it
-        float v[EACH];
         float mine = __int_as_float(NO_MARK);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            v[i] = S.logp[t * EACH + i];
-            if (__float_as_int(v[i]) != NO_MARK) mine = v[i];
+            const float v = S.logp[place_of(t * EACH + i)];
+            if (__float_as_int(v) != NO_MARK) mine = v;
         }
         // the last mark of the threads before this one
         const uint32_t votes = __ballot_sync(0xffffffffu, __float_as_int(mine) != NO_MARK);
@@ -444,18 +449,21 @@ template <typename I> struct Work {
         if (below) carry = of_lane;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            if (__float_as_int(v[i]) != NO_MARK) carry = v[i];
-            S.logp[t * EACH + i] = carry;
+            float& v = S.logp[place_of(t * EACH + i)];
+            if (__float_as_int(v) != NO_MARK) carry = v;
+            v = carry;
         }
         __syncthreads();
-        for (int i = t; i < tokens; i += THREADS) out[i] = S.logp[i];
+        for (int i = t; i < tokens; i += THREADS) out[i] = S.logp[place_of(i)];
     }
 };
 
 enum Part { SUMS, FINISH, ALL };
 
 template <Part PART, typename I>
-__global__ void __launch_bounds__(THREADS, 4) k_preference(const Args A) {
+// The second launch waits for starts, pieces and weights one after the other and has the shared memory for 5 CTAs to an SM: 12M
+// tokens in 4099 pairs 39.7 us against 41 for both launches, in 4M pairs 184 against 196.  A sixth gains nothing.
+__global__ void __launch_bounds__(THREADS, PART == FINISH ? 5 : 4) k_preference(const Args A) {
     extern __shared__ __align__(16) uint8_t raw[];
     Shared& S = *reinterpret_cast<Shared*>(raw);
     using W = Work<I>;
