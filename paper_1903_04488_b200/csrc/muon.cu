@@ -633,6 +633,12 @@ k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap 
                     if (++s == N) { s = 0; parity ^= 1; }
                 }
             }
+            // Nor may a CTA be gone before the last commits have arrived at its barriers: that of the results (done) says nothing of where the
+            // others are.  A stage that was not used passes at once.
+            for (int i = 0; i < N && ok; ++i) {
+                ok = bar_wait(&S.empty[s], parity, gave_up);
+                if (++s == N) { s = 0; parity ^= 1; }
+            }
             // no copy may land in a CTA that is gone, nor count there: the first CTA waits for both's, and the second leaves with it
             if (!ok && rank == 0)
                 for (int i = 0; i < min(issued, N); ++i) {
@@ -676,6 +682,12 @@ k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap 
                     }
                     if (++s == N) { s = 0; parity ^= 1; }
                 }
+            }
+            // the second CTA's last arrivals, which the meeting at the end does not wait for
+            for (int i = 0; i < 2 && ok; ++i) {
+                ok = bar_wait(&S.taken[buffer], parity_taken, gave_up);
+                if (buffer) parity_taken ^= 1;
+                buffer ^= 1;
             }
         }
     } else {                                                    // results
