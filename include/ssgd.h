@@ -481,6 +481,10 @@ int ssgd_muon_step(const ssgd_matrix* matrices, int32_t count, int32_t fmt_p, in
 /* Waits for the stream; SSGD_EDEVICE if a wait inside a kernel of the training operators has run out on this device since the last
  * call (what that call wrote is then worthless), SSGD_ECUDA if the stream reports an error, else SSGD_OK.  Not while capturing. */
 int ssgd_train_ops_status(void* stream);
+/* Test hook: a kernel of which one warp waits at a barrier as those kernels do, half of its lanes for limit_ns (1000 .. 1e9), the others until
+ * another warp arrives there, after the first have given up.  told: 32 numbers on the device, whether each lane was told that the wait
+ * succeeded.  ssgd_train_ops_status reports it. */
+int ssgd_test_run_out(int64_t limit_ns, int32_t* told, void* stream);
 
 const char* ssgd_strerror(int code);
 const char* ssgd_last_error(const ssgd_ctx* ctx); /* text of the last CUDA error seen, or "" */

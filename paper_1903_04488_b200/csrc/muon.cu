@@ -722,8 +722,7 @@ k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap 
             const bool some = wanted(0);                        // the first piece lies farthest to the left
             const int steps = product_of<KIND>(M, which).steps;
             auto done = [&] {
-                const bool ok = bar_wait(&S.done[buffer], parity, gave_up);
-                __syncwarp();
+                const bool ok = bar_wait_warp(&S.done[buffer], parity, gave_up);
                 fence_after();
                 return ok;
             };
@@ -1027,6 +1026,32 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
     fence_after();
     if (t == 0 && S.gave_up) atomicExch(&g_error, 1);
     if (warp == 0) tmem_free<false>(S.tmem, plan.columns);
+}
+
+// ---- a wait that runs out ----------------------------------------------------------------------------
+
+// One warp waits at a barrier, half of its lanes for `limit`, the others until a thread of another warp arrives, which it does once the
+// first have given up.  told[lane]: what the lane's wait returned.  Every wait is bounded.
+__global__ void __launch_bounds__(64) k_run_out(uint64_t limit, int32_t* told) {
+    __shared__ uint64_t late;
+    __shared__ int gave_up, patient;
+    volatile int* seen = &gave_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        bar_init(&late, 1);
+        bar_init_fence();
+        gave_up = patient = 0;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        told[lane] = bar_wait_warp(&late, 0, lane < 16 ? &gave_up : &patient, lane < 16 ? limit : WAIT_NS);
+    } else if (lane == 0) {
+        const uint64_t t0 = now_ns();
+        while (!*seen && now_ns() - t0 < WAIT_NS) {}
+        bar_arrive(&late);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && gave_up) atomicExch(&g_error, 1);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
@@ -1338,6 +1363,13 @@ int ssgd_muon_step(const ssgd_matrix* matrices, int32_t count, int32_t fmt_p, in
     C.a = (float)a; C.b = (float)b; C.c = (float)c;
     C.grad_scale = grad_scale;
     return run(matrices, count, C, steps, lr, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int ssgd_test_run_out(int64_t limit_ns, int32_t* told, void* stream) {
+    if (limit_ns < 1000 || limit_ns > 1000000000 || !told) return SSGD_EINVAL;
+    if (!aligned_to(told, 4)) return SSGD_EALIGN;
+    k_run_out<<<1, 64, 0, static_cast<cudaStream_t>(stream)>>>((uint64_t)limit_ns, told);
+    return launched();
 }
 
 int ssgd_train_ops_status(void* stream) {

@@ -66,20 +66,28 @@ __device__ __forceinline__ uint64_t now_ns() {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-// False after two seconds, or when another thread of the CTA has given up.  Nothing here takes a thousandth of that.
+__device__ __forceinline__ void bar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_addr(bar)) : "memory");
+}
+// False after two seconds (`limit`), or when another thread of the CTA has given up.  Nothing here takes a thousandth of that.
 constexpr uint64_t WAIT_NS = 2000000000ull;
-__device__ __forceinline__ bool bar_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
+__device__ __forceinline__ bool bar_wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint64_t limit) {
     const uint64_t t0 = now_ns();
     for (uint32_t i = 1;; ++i) {
         if (bar_try(bar, parity)) return true;
-        if ((i & 63u) == 0 && (*gave_up || now_ns() - t0 > WAIT_NS)) {
+        if ((i & 63u) == 0 && (*gave_up || now_ns() - t0 > limit)) {
             *gave_up = 1;
             return false;
         }
     }
 }
-__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
-    return bar_try(bar, parity) || bar_wait_long(bar, parity, gave_up);
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint64_t limit = WAIT_NS) {
+    return bar_try(bar, parity) || bar_wait_long(bar, parity, gave_up, limit);
+}
+// By a whole warp, with one answer for all of it: its lanes wait each for itself, and where some give up just before the barrier completes for
+// the others, what follows (instructions of the whole warp) would be done by a part of it.
+__device__ __forceinline__ bool bar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* gave_up, uint64_t limit = WAIT_NS) {
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up, limit));
 }
 
 // ---- copies ------------------------------------------------------------------------------------------

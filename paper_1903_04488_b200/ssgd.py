@@ -82,6 +82,7 @@ SIGNATURES = {
     "ssgd_orthogonalize": [_vp, _i32, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _vp, _sz, _vp],
     "ssgd_muon_step": [_vp, _i32, _i32, _i32, _i32, _f64, _f64, _i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp, _sz, _vp],
     "ssgd_train_ops_status": [_vp],
+    "ssgd_test_run_out": [_i64, _vp, _vp],
     "ssgd_adamw_step": [_vp, _i32, _i32, _i32, _i32, _i32, _f64, _f64, _f64, _f64, _f64, _i64, _vp, _i32, _u64, _vp],
 }
 

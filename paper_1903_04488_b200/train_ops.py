@@ -277,7 +277,8 @@ def orthogonalize(x: torch.Tensor, *, steps: int = 5, coefficients=QUINTIC, eps:
     the nearest matrix with orthonormal rows (or columns), but for singular values that are all but zero.
 
     x: a matrix (with any row stride), or a contiguous batch of them.  products: 3 for results as exact as fp32's, 1 for an error of
-    about 1e-3 at a third of the time; None: 1 for bfloat16, otherwise 3.  out: where the result goes (x's shape and type; may be x)."""
+    about 1e-3 at a third of the time; None: 1 for bfloat16, otherwise 3.  out: where the result goes (x's shape and type; may be x).
+    Waits inside the kernels are bounded; `status` says whether one ran out."""
     a, b, c = coefficients
     return (_native or native()).orthogonalize(x, steps, a, b, c, eps, 0 if products is None else products, out)
 
@@ -289,7 +290,8 @@ class Muon:
 
     params: contiguous matrices, or batches of them, float32 or bfloat16.  m: existing momenta (float32, of the parameters' shapes);
     fresh zeros if None.  scale: "spectral" (sqrt(max(1, rows / cols))), "rms" (0.2 sqrt(max(rows, cols)): updates as large as
-    AdamW's) or a number.  products: as in `orthogonalize`, by the parameters' type.  No two of the tensors may share memory."""
+    AdamW's) or a number.  products: as in `orthogonalize`, by the parameters' type.  No two of the tensors may share memory.
+    Waits inside the kernels are bounded; `status` says whether one ran out."""
 
     def __init__(self, params, *, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
                  steps: int = 5, coefficients=QUINTIC, eps: float = 1e-7, scale: str | float = "spectral", products: int | None = None,
