@@ -823,9 +823,13 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
         bar_init_fence();
         S.gave_up = 0;
     }
-    if (warp == 0) tmem_alloc<false>(&S.tmem, plan.columns);
+    // The next launch may come when every CTA has its tensor memory: beside two of another plan (256 columns each) one of this would have to wait
+    // for memory that they keep until this launch is over.
+    if (warp == 0) {
+        tmem_alloc<false>(&S.tmem, plan.columns);
+        successor_may_start();
+    }
     successor_wait();
-    successor_may_start();
 
     // momentum and the sum of squares, then x
     const bool vector = may_load_four<TIN>(M);
