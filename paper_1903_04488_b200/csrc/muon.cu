@@ -825,11 +825,9 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
     }
     // The next launch may come when every CTA has its tensor memory: beside two of another plan (256 columns each) one of this would have to wait
     // for memory that they keep until this launch is over.
-    if (warp == 0) {
-        tmem_alloc<false>(&S.tmem, plan.columns);
-        successor_may_start();
-    }
+    if (warp == 0) tmem_alloc<false>(&S.tmem, plan.columns);
     successor_wait();
+    if (warp == 0) successor_may_start();
 
     // momentum and the sum of squares, then x
     const bool vector = may_load_four<TIN>(M);
