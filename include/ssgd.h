@@ -435,7 +435,7 @@ int ssgd_policy_loss(const void* logits, int64_t ld, int32_t fmt, const void* id
  *   loss [pairs] = weights l;  rewards [2][pairs] = beta D, of the preferred sequences and of the others;
  *   d_logp [tokens] (NULL: not wanted) = the gradient of the sum of the losses; 0 for tokens of no sequence
  * logp, ref_logp (NULL: 0), d_logp: [tokens] fp32; weights [pairs] fp32 (NULL: 1; a pair of weight 0 has loss and gradient 0 whatever
- * its tokens hold).  Sums hold 48 bits or more, in an order that depends on nothing but the starts.  starts outside [0, tokens] count as the
+ * its tokens hold).  Differences and sums hold 48 bits or more and the range of 64-bit numbers, in an order that depends on nothing but the starts.  starts outside [0, tokens] count as the
  * nearest of these; where they do not ascend, the results of the pairs concerned are unspecified.
  * d_logp may be logp or ref_logp itself.  workspace: device memory of at least ssgd_preference_loss_workspace(tokens, pairs) bytes, 8-byte
  * aligned, free again once the stream has passed.  tokens <= 2^40, pairs <= 2^30. */

@@ -47,7 +47,7 @@ struct Shared {
     int32_t bound[FEW + 1];                         // the same within the CTA's tokens
     float value[FEW];                               // their gradients
     union {
-        float2 part[WARPS][FEW];
+        double part[WARPS][FEW];
         int32_t list[CHUNK / SHORT + 1];
     };
     int2 before[WARPS];
@@ -165,13 +165,21 @@ template <typename I> struct Work {
         }
     };
 
-    // A sum with what its roundings lost beside it: 48 bits or more, in fp32 arithmetic (an SM converts to 64 bits at 16 numbers a cycle)
+    // A sum with what its roundings lost beside it: 48 bits or more, in fp32 arithmetic (an SM converts to 64 bits at 16 numbers a cycle).  The
+    // range is that of fp32: two masks of the lowest number leave it, and what they lost is NaN then.  Such a piece, and one that holds
+    // infinities or NaN, is not `sound` and is added up once more in 64 bits.
     struct Sum {
         float sum = 0.f, lost = 0.f;
         __device__ __forceinline__ void add(float x) {
             const float next = sum + x, back = next - sum;
             lost += (sum - (next - back)) + (x - back);
             sum = next;
+        }
+        // a - b, with what the difference loses
+        __device__ __forceinline__ void add_difference(float a, float b) {
+            const float d = a - b, back = d - a;
+            lost += (a - (d - back)) - (b + back);
+            add(d);
         }
         __device__ __forceinline__ void join_warp() {
 #pragma unroll
@@ -181,20 +189,16 @@ template <typename I> struct Work {
                 lost += l;
             }
         }
-        // an infinity or NaN among the numbers leaves NaN in what was lost
-        __device__ __forceinline__ double value() const { return fabsf(sum) < INFINITY ? (double)sum + (double)lost : (double)sum; }
+        __device__ __forceinline__ bool sound() const { return fabsf(sum) < INFINITY && fabsf(lost) < INFINITY; }
+        __device__ __forceinline__ double value() const { return (double)sum + (double)lost; }
     };
 
     // A piece's sum from those of the warps
     static __device__ __forceinline__ double sum_of_warps(const Shared& S, int q) {
-        Sum sum;
+        double sum = 0.0;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float2 p = S.part[w][q];
-            sum.add(p.x);
-            sum.lost += p.y;
-        }
-        return sum.value();
+        for (int w = 0; w < WARPS; ++w) sum += S.part[w][q];
+        return sum;
     }
 
     // Every warp has an eighth of the CTA's tokens: calls f(q, a, b) for each of the n sequences that has some of them, [a, b)
@@ -227,7 +231,25 @@ template <typename I> struct Work {
         for (int at = whole + (int)threadIdx.x; at < left; at += THREADS) some(at, std::integral_constant<int, 4>{});
         copy_async_commit();
     }
-    static __device__ __forceinline__ float difference(const Args& A, const Shared& S, int i) { return A.ref ? S.logp[i] - S.ref[i] : S.logp[i]; }
+    static __device__ __forceinline__ void add_token(const Args& A, const Shared& S, int i, Sum& sum) {
+        if (A.ref) sum.add_difference(S.logp[i], S.ref[i]);
+        else sum.add(S.logp[i]);
+    }
+    // Tokens [a, b), every `stride`-th from `first` on, in 64 bits
+    static __device__ __forceinline__ double wide_sum(const Args& A, const Shared& S, int a, int b, int first, int stride) {
+        double sum = 0.0;
+        for (int i = a + first; i < b; i += stride) sum += A.ref ? (double)S.logp[i] - (double)S.ref[i] : (double)S.logp[i];
+        return sum;
+    }
+    // The sum of [a, b), of which every lane of the warp has some: the same answer in all lanes
+    static __device__ __forceinline__ double joined(const Args& A, const Shared& S, int a, int b, Sum sum) {
+        sum.join_warp();
+        if (__all_sync(0xffffffffu, sum.sound())) return sum.value();
+        double wide = wide_sum(A, S, a, b, threadIdx.x & 31, 32);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+        return wide;
+    }
 
     // Sums of the pieces of the CTA's tokens, of 48 bits or more.  Each is added up by itself, so that what one sequence holds (infinities,
     // the lowest number of a mask) stays there.  WRITE: for other CTAs; otherwise those of few sequences are left in S.part alone.
@@ -236,7 +258,7 @@ template <typename I> struct Work {
         const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
         if (R.few()) {                                  // every warp takes an eighth of the tokens
             const int n = (int)(R.s1 - R.s0);
-            for (int i = lane; i < n; i += 32) S.part[warp][i] = make_float2(0.f, 0.f);
+            for (int i = lane; i < n; i += 32) S.part[warp][i] = 0.0;
             __syncwarp();
             for_pieces(S, n, (int)(R.c1 - R.c0), [&](int q, int a, int b) {
                 // pairs of tokens, and what is left of them at the ends
@@ -245,7 +267,11 @@ template <typename I> struct Work {
 #pragma unroll 4
                 for (int i = a2 + 2 * lane; i < b2; i += 64) {
                     float2 x = *reinterpret_cast<const float2*>(S.logp + i);
-                    if (A.ref) x = fma2(*reinterpret_cast<const float2*>(S.ref + i), both(-1.f), x);
+                    if (A.ref) {
+                        const float2 r = *reinterpret_cast<const float2*>(S.ref + i), d = fma2(r, both(-1.f), x), back = fma2(x, both(-1.f), d);
+                        off = add2(off, fma2(add2(r, back), both(-1.f), fma2(fma2(back, both(-1.f), d), both(-1.f), x)));
+                        x = d;
+                    }
                     const float2 next = add2(two, x), back = fma2(two, both(-1.f), next);
                     off = add2(off, add2(fma2(fma2(back, both(-1.f), next), both(-1.f), two), fma2(back, both(-1.f), x)));
                     two = next;
@@ -254,10 +280,10 @@ template <typename I> struct Work {
                 sum.add(two.x);
                 sum.add(two.y);
                 sum.lost += off.x + off.y;
-                if (lane == 0 && a < a2) sum.add(difference(A, S, a));
-                if (lane == 1 && b2 < b && b2 >= a) sum.add(difference(A, S, b2));
-                sum.join_warp();
-                if (lane == 0) S.part[warp][q] = make_float2(sum.sum, sum.lost);
+                if (lane == 0 && a < a2) add_token(A, S, a, sum);
+                if (lane == 1 && b2 < b && b2 >= a) add_token(A, S, b2, sum);
+                const double all = joined(A, S, a, b, sum);
+                if (lane == 0) S.part[warp][q] = all;
             });
             __syncthreads();
             if (WRITE && t < n && S.bound[t] < S.bound[t + 1]) A.pieces[chunk + R.s0 + t] = sum_of_warps(S, t);
@@ -270,8 +296,8 @@ template <typename I> struct Work {
                 if (at <= CHUNK / SHORT) S.list[at] = (int32_t)(s - R.s0);         // more only where starts do not ascend
             } else if (b > a) {
                 Sum sum;
-                for (int i = a; i < b; ++i) sum.add(difference(A, S, i));
-                A.pieces[chunk + s] = sum.value();
+                for (int i = a; i < b; ++i) add_token(A, S, i, sum);
+                A.pieces[chunk + s] = sum.sound() ? sum.value() : wide_sum(A, S, a, b, 0, 1);
             }
         }
         __syncthreads();
@@ -279,9 +305,9 @@ template <typename I> struct Work {
             const I s = R.s0 + S.list[q];
             const int a = R.within(start_of(A, s)), b = R.within(start_of(A, s + 1));
             Sum sum;
-            for (int i = a + lane; i < b; i += 32) sum.add(difference(A, S, i));
-            sum.join_warp();
-            if (lane == 0) A.pieces[chunk + s] = sum.value();
+            for (int i = a + lane; i < b; i += 32) add_token(A, S, i, sum);
+            const double all = joined(A, S, a, b, sum);
+            if (lane == 0) A.pieces[chunk + s] = all;
         }
     }
 
