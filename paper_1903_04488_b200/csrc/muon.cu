@@ -68,7 +68,7 @@ struct Common {
     int32_t fmt_in, fmt_out;
     bool split;                                     // two numbers in A and B too, three products
     bool nesterov, update;                          // update: out is a parameter to be moved, otherwise it gets the result
-    float momentum, decay, eps;
+    float momentum, share, decay, eps;              // share: 1 - momentum, which fp32 would not hold as 1 less a rounded momentum
     float a, b, c;
     const float* grad_scale;
 };
@@ -142,27 +142,27 @@ __device__ __forceinline__ void load_block(const Matrix& M, int r0, int c0, bool
 
 // The thread's i-th four numbers of a block: the new momentum, left in s.m, and what is to be made orthogonal
 template <typename T>
-__device__ __forceinline__ float4 momentum_of(const Common& C, const Matrix& M, Share<T>& s, int i, float mu, float scale) {
+__device__ __forceinline__ float4 momentum_of(const Common& C, const Matrix& M, Share<T>& s, int i, float scale) {
     float u[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         u[e] = to_f32(s.g[i].e[e]);
         if (M.m) {
             const float in = u[e] * scale;
-            s.m[i].e[e] = fmaf(mu, s.m[i].e[e], (1.f - mu) * in);
-            u[e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * in) : s.m[i].e[e];
+            s.m[i].e[e] = fmaf(C.momentum, s.m[i].e[e], C.share * in);
+            u[e] = C.nesterov ? fmaf(C.momentum, s.m[i].e[e], C.share * in) : s.m[i].e[e];
         }
     }
     return make_float4(u[0], u[1], u[2], u[3]);
 }
 // The same where the momentum is the new one already
 template <typename T>
-__device__ __forceinline__ float4 stored_momentum_of(const Common& C, const Matrix& M, const Share<T>& s, int i, float mu, float scale) {
+__device__ __forceinline__ float4 stored_momentum_of(const Common& C, const Matrix& M, const Share<T>& s, int i, float scale) {
     float u[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         u[e] = to_f32(s.g[i].e[e]);
-        if (M.m) u[e] = C.nesterov ? fmaf(mu, s.m[i].e[e], (1.f - mu) * (u[e] * scale)) : s.m[i].e[e];
+        if (M.m) u[e] = C.nesterov ? fmaf(C.momentum, s.m[i].e[e], C.share * (u[e] * scale)) : s.m[i].e[e];
     }
     return make_float4(u[0], u[1], u[2], u[3]);
 }
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_momentum(const __grid_co
     const Matrix& M = G.m[matrix_of(C.count, strip, [&](int i) { return G.m[i].strip0; })];
     const int local = strip - M.strip0, r0 = local % M.rb * BLOCK, cblock0 = local / M.rb * STRIP_BLOCKS;
     const bool vector = may_load_four<T>(M);
-    const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
+    const float scale = C.grad_scale ? *C.grad_scale : 1.f;
     double sum = 0.0;
     for (int cblock = cblock0; cblock < min(cblock0 + STRIP_BLOCKS, M.cb); ++cblock) {
         Share<T> s;
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_momentum(const __grid_co
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int r = r0 + (int)threadIdx.x / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
-            const float4 u = momentum_of(C, M, s, i, mu, scale);
+            const float4 u = momentum_of(C, M, s, i, scale);
             if (M.m) put_momentum(M, s, i, r, c, n, vector);
             sum += squares(u, n);
         }
@@ -257,13 +257,13 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_layout(const __grid_cons
     for (int i = threadIdx.x; i < M.strips; i += PREPARE_THREADS) sum += C.at.sums[M.strip0 + i];
     sum = block_sum(sum, shared);
     const Inverse inv(sum, C.eps);
-    const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
+    const float scale = C.grad_scale ? *C.grad_scale : 1.f;
     const int64_t second = (int64_t)M.rb * M.cb * BLOCK_BYTES;
     for (int cblock = cblock0; cblock < cblock1; ++cblock) {
         uint8_t* block = C.at.blocks + (int64_t)(M.x0 + (uint32_t)cblock * M.rb + rblock) * BLOCK_BYTES;
         float4 u[SHARE];
 #pragma unroll
-        for (int i = 0; i < SHARE; ++i) u[i] = stored_momentum_of(C, M, s, i, mu, scale);
+        for (int i = 0; i < SHARE; ++i) u[i] = stored_momentum_of(C, M, s, i, scale);
         if (cblock + 1 < cblock1) load_block<T>(M, rblock * BLOCK, (cblock + 1) * BLOCK, vector, s);
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
 
     // momentum and the sum of squares, then x
     const bool vector = may_load_four<TIN>(M);
-    const float scale = C.grad_scale ? *C.grad_scale : 1.f, mu = C.momentum;
+    const float scale = C.grad_scale ? *C.grad_scale : 1.f;
     double sum = 0.0;
     for (int block = 0; block < R * K; ++block) {
         const int r0 = block % R * BLOCK, c0 = block / R * BLOCK;
@@ -841,7 +841,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int r = r0 + t / 16 + 16 * i, n = r < M.rows ? M.cols - c : 0;
-            const float4 u = momentum_of(C, M, s, i, mu, scale);
+            const float4 u = momentum_of(C, M, s, i, scale);
             if (M.m) put_momentum(M, s, i, r, c, n, vector);
             sum += squares(u, n);
         }
@@ -855,7 +855,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) k_small(const __grid_constant__
 #pragma unroll
         for (int i = 0; i < SHARE; ++i) {
             const int rr = t / 16 + 16 * i, cc = t % 16 * 4, n = r0 + rr < M.rows ? M.cols - c0 - cc : 0;
-            const float4 u = stored_momentum_of(C, M, s, i, mu, scale);
+            const float4 u = stored_momentum_of(C, M, s, i, scale);
             uint2 hi, lo;
             split2(n > 0 ? inv.of(u.x) : 0.f, n > 1 ? inv.of(u.y) : 0.f, hi.x, lo.x);
             split2(n > 2 ? inv.of(u.z) : 0.f, n > 3 ? inv.of(u.w) : 0.f, hi.y, lo.y);
@@ -1360,6 +1360,7 @@ int ssgd_muon_step(const ssgd_matrix* matrices, int32_t count, int32_t fmt_p, in
     C.nesterov = nesterov != 0;
     C.update = true;
     C.momentum = (float)momentum;
+    C.share = (float)(1.0 - momentum);
     C.decay = (float)(1.0 - lr * weight_decay);
     C.eps = (float)eps;
     C.a = (float)a; C.b = (float)b; C.c = (float)c;
