@@ -465,8 +465,10 @@ typedef struct {
     double scale;     /* ssgd_muon_step: factor of lr for this matrix */
 } ssgd_matrix;
 /* Device memory that the two below need: 8 bytes per element of the matrices, twice (products 1) or four times (3) 2 bytes per element
- * of A and B, and a little; none for matrices of up to 128 x 256 or 256 x 128.  More than 224 matrices or 2^27 elements are worked off in
- * groups, each in the same memory.  Free again once the stream has passed; its contents mean nothing.  16-byte aligned. */
+ * of A, where both sides count as rounded up to 64, and a little; none for matrices of up to 128 x 256 or 256 x 128.  More than 224 matrices
+ * or 2^27 elements (rounded up likewise) are worked off in groups, each in the same memory: 1.1 GB, and as much again at most for A (square
+ * matrices, products 3), unless a single matrix needs more.  Free again once the stream has passed; its contents mean nothing.  16-byte
+ * aligned. */
 int ssgd_orthogonalize_workspace(const ssgd_matrix* matrices, int32_t count, int32_t fmt_out, int32_t products, size_t* out_bytes);
 /* out <- the orthogonalised `in`, for each matrix; both in fmt. */
 int ssgd_orthogonalize(const ssgd_matrix* matrices, int32_t count, int32_t fmt, int32_t products, int32_t steps, double a, double b,

@@ -36,7 +36,7 @@ namespace {
 
 constexpr float SCALE = 1024.f;
 constexpr int MAX_GROUP = 224;                      // matrices of one set of launches: their descriptors are arguments of the first
-constexpr int64_t GROUP_ELEMENTS = (int64_t)1 << 27;  // and no more than this many elements, unless one matrix has them
+constexpr int64_t GROUP_ELEMENTS = (int64_t)1 << 27;  // and no more than this many elements, sides rounded up to 64, unless one matrix has them
 constexpr int STRIP_BLOCKS = 4;                     // what a CTA of the preparation takes: 64 rows of 256 columns
 
 enum Kind { GRAM, POLYNOMIAL, APPLY, FINISH };      // A, B, x of the next step, the result
@@ -1077,7 +1077,8 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Adds a matrix to a group; false if there is no room
 bool add(Sizes& s, const ssgd_matrix& t, bool split, Matrix* to) {
-    const int64_t elements = (int64_t)t.rows * t.cols;
+    // with the padding, which the workspace holds too: it is most of a matrix of few rows
+    const int64_t elements = div_up(t.rows, BLOCK) * div_up(t.cols, BLOCK) * BLOCK * BLOCK;
     if (s.count == MAX_GROUP || (s.count && s.elements + elements > GROUP_ELEMENTS)) return false;
     Matrix M{};
     M.rows = (int32_t)t.rows; M.cols = (int32_t)t.cols;
