@@ -454,7 +454,8 @@ int ssgd_preference_loss(const float* logp, const float* ref_logp, int64_t token
  * exact as those of fp32; 1: one number in the operands of products, two in x itself: the result is off by about 1e-3 of its norm;
  * 0: 1 for results in bfloat16, otherwise 3.
  * A matrix of zeros stays one (0 / 0 with eps = 0 is NaN), and numbers of x_0 below 2^-35 count as zero; infinities and NaN spread
- * over their matrix.  Polynomials that take anything in [0, 1] beyond 4 on the way are refused (SSGD_EINVAL).  1 <= steps <= 32; rows,
+ * over their matrix.  Polynomials that take anything in [0, 1] beyond 4 on the way, or beyond 8 at the end, are refused
+ * (SSGD_EINVAL).  1 <= steps <= 32; rows,
  * cols <= 2^20, rows * cols <= 2^32, the shorter side <= 32768 (SSGD_ETOOBIG).  Matrices without elements are left out. */
 typedef struct {
     void* out;        /* ssgd_orthogonalize: the result, may be `in` itself (same ld); ssgd_muon_step: the parameter */

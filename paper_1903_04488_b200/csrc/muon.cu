@@ -25,6 +25,7 @@
 // then 3 launches per step, whose tiles are dealt out over the SMs.  Matrices live in the workspace as blocks (umma.cuh), padded with
 // zeros to 64; block (r, c) of a matrix of R x C blocks is the (c R + r)-th.
 #include <algorithm>
+#include <cmath>
 
 #include "formats.cuh"
 #include "umma.cuh"
@@ -1185,18 +1186,38 @@ int launch_small(cudaStream_t st, const Group& G, const Common& C, const SmallPl
 constexpr int64_t MAX_SIDE = (int64_t)1 << 20;
 constexpr int MAX_STEPS = 32;
 
-// The polynomial has to keep what starts within [0, 1] well inside the range of the stored numbers.
+// The polynomial f(s) = a s + b s^3 + c s^5 has to keep what starts within [0, 1] well inside the range of the stored numbers: no more than 4 on
+// the way and 8 at the end, and b s^2 + c s^4 within 48.  f is continuous and f(0) = 0, so that it makes of an interval around 0 exactly the
+// interval between its extremes there: at the ends, or where a + 3 b t + 5 c t^2 = 0 with t = s^2.
 bool stays_in_range(int steps, double a, double b, double c) {
-    for (int i = 0; i <= 64; ++i) {
-        double s = i / 64.0;
-        for (int k = 0; k < steps; ++k) {
-            const double q = s * s, p = b * q + c * q * q;
-            if (!(q <= 16.0) || !(p > -48.0 && p < 48.0)) return false;
-            s *= a + p;
-        }
-        if (!(s > -8.0 && s < 8.0)) return false;
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    auto f = [&](double s) { return s * (a + s * s * (b + c * s * s)); };
+    double flat[2] = {-1.0, -1.0};                  // t of these places
+    const double d = 9.0 * b * b - 20.0 * a * c;
+    if (d >= 0.0) {
+        const double h = -0.5 * (3.0 * b + std::copysign(std::sqrt(d), b));     // no cancellation
+        if (c != 0.0) flat[0] = h / (5.0 * c);
+        if (h != 0.0) flat[1] = a / h;
     }
-    return true;
+    double lo = 0.0, hi = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const double top = std::max(-lo, hi), q = top * top;
+        if (!(top <= 4.0)) return false;
+        const double end = b * q + c * q * q, middle = c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < q ? -b * b / (4.0 * c) : 0.0;
+        if (!(std::fabs(end) < 48.0) || !(std::fabs(middle) < 48.0)) return false;
+        double places[6] = {lo, hi, 0.0, 0.0, 0.0, 0.0};
+        for (int i = 0; i < 2; ++i) {
+            const double s = flat[i] > 0.0 ? std::sqrt(flat[i]) : 0.0;
+            if (s <= hi) places[2 + i] = s;
+            if (-s >= lo) places[4 + i] = -s;
+        }
+        lo = hi = 0.0;
+        for (double s : places) {
+            lo = std::min(lo, f(s));
+            hi = std::max(hi, f(s));
+        }
+    }
+    return lo > -8.0 && hi < 8.0;
 }
 
 // One product or three (0: by the type of the result)

@@ -49,3 +49,61 @@ def test_the_workspace_counts_sides_rounded_up_and_stops_growing(lib, shape, pro
     for more in (group + 1, 3 * group, 1000):
         assert workspace(lib, shape, more, products) == full
     assert 8 * group * rows * cols <= 8 << 27 or group == 1
+
+
+def accepted(lib, steps, a, b, c):
+    """Whether a call with this polynomial gets as far as asking for its workspace, which comes after the polynomial and before the device"""
+    m = matrices((300, 700), 1)
+    D = C.c_double
+    code = lib.ssgd_orthogonalize(m.ctypes.data, 1, S.FMT_F32, 1, steps, D(a), D(b), D(c), D(1e-7), None, 0, None)
+    assert code in (S.EINVAL, S.EWORKSPACE)
+    return code == S.EWORKSPACE
+
+
+def reach(steps, a, b, c, points=200_001):
+    """The largest that the polynomial makes of many singular values on the way, and at the end (or once it is far beyond)"""
+    s, way = np.linspace(0, 1, points), 1.0
+    for _ in range(steps):
+        way = max(way, np.abs(s).max())
+        if way > 1e6:
+            break
+        q = s * s
+        s = s * (a + q * (b + c * q))
+    return way, np.abs(s).max()
+
+
+# between the points of a coarse grid on [0, 1] these leave every range
+@pytest.mark.parametrize("steps,a,b,c", [(8, 2.5820751723704674, -5.537853914649217, 1.9408113825834064),
+                                         (7, 2.5156164553125673, -4.720735474494571, 1.1852813270571287),
+                                         (6, 3.234364782498459, -6.501583412432502, 2.1991137019973506),
+                                         (5, 3.7428638927267945, -8.380319386742006, 3.4978279724879764),
+                                         (5, 2.653961100954992, -4.808708104907779, 1.1347372981776571),
+                                         (3, 3.5222579363973665, -8.513114138869676, 3.6355787279214278)])
+def test_polynomials_that_leave_the_range_between_the_points_of_a_grid(lib, steps, a, b, c):
+    assert max(reach(steps, a, b, c)) > 8
+    assert not accepted(lib, steps, a, b, c)
+
+
+def test_polynomials_that_stay_in_range_are_accepted(lib):
+    for steps in (1, 2, 5, 10, 32):
+        for poly in ((3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5), (1.0, 0.0, 0.0), (0.0, 0.0, 0.0), (-1.5, 0.5, 0.0)):
+            assert accepted(lib, steps, *poly), (steps, poly)
+    assert accepted(lib, 1, 2.0, 0.0, 0.0) and accepted(lib, 2, 2.0, 0.0, 0.0) and accepted(lib, 1, 7.9, 0.0, 0.0)
+    assert not accepted(lib, 3, 2.0, 0.0, 0.0) and not accepted(lib, 2, 7.9, 0.0, 0.0) and not accepted(lib, 1, 8.1, 0.0, 0.0)
+    for bad in (float("nan"), float("inf"), -float("inf"), 1e200):
+        for poly in ((bad, 0.0, 0.0), (1.0, bad, 0.0), (1.0, 0.0, bad)):
+            assert not accepted(lib, 1, *poly)
+
+
+def test_the_range_is_that_of_a_fine_grid(lib):
+    rng = np.random.default_rng(1)
+    for i in range(300):
+        a, b, c = rng.uniform(0, 6), rng.uniform(-12, 6), rng.uniform(-5, 6)
+        if i % 2:
+            a, b, c = 3.4445 * rng.uniform(0.8, 1.25), -4.775 * rng.uniform(0.8, 1.25), 2.0315 * rng.uniform(0.8, 1.25)
+        steps = int(rng.integers(1, 8))
+        way, end = reach(steps, a, b, c, 20_001)
+        if way > 4 or end > 8:
+            assert not accepted(lib, steps, a, b, c), (steps, a, b, c)
+        elif way < 3.9 and end < 7.8 and 16 * abs(b) + 256 * abs(c) * (way / 4) ** 4 < 47:
+            assert accepted(lib, steps, a, b, c), (steps, a, b, c)
