@@ -116,13 +116,14 @@ def train(steps: int = 150, workers: int = 4, vocab: int = 256, dim: int = 64, l
 
 
 class Tuner:
-    """What `tune` keeps: the reference, and an optimizer for the blocks' matrices and one for the rest."""
+    """What `tune` keeps: the reference, and an optimizer for the blocks' matrices and one for the rest.  matrix_scale: how the matrices'
+    updates are scaled.  The model stores them [in][out], for which it is "spectral_t"; the default is that of `train_ops.Muon`."""
 
-    def __init__(self, model: Model, lr: float = 2e-3, matrix_lr: float = 5e-3):
+    def __init__(self, model: Model, lr: float = 2e-3, matrix_lr: float = 5e-3, matrix_scale: str | float = "spectral"):
         self.model, self.reference = model, copy.deepcopy(model)
         self.blocks = model.matrices[1:-1]
         self.rest = [model.matrices[0], model.matrices[-1], *model.small]
-        self.muon = train_ops.Muon(self.blocks, lr=matrix_lr) if self.blocks else None
+        self.muon = train_ops.Muon(self.blocks, lr=matrix_lr, scale=matrix_scale) if self.blocks else None
         self.adamw = train_ops.AdamW(self.rest, lr=lr, weight_decay=0.0)
 
     def policy(self, cur, sampled, old_logp, advantages, kl: float = 0.05):
@@ -159,7 +160,7 @@ def tune(model: Model, perm: torch.Tensor, gen: torch.Generator, steps: int, tok
     """Returns the share of sampled tokens that were the permutation's, at each step."""
     if loss not in ("policy", "preference"):
         raise ValueError('loss: "policy" or "preference"')
-    tuner = Tuner(model)
+    tuner = Tuner(model, matrix_scale="spectral_t")
     for p in [*tuner.blocks, *tuner.rest]:
         p.grad = None                                               # it was a piece of the workers' rows
     shares = []

@@ -289,8 +289,8 @@ class Muon:
     p <- p (1 - lr weight_decay) - lr scale orthogonalize(u).
 
     params: contiguous matrices, or batches of them, float32 or bfloat16.  m: existing momenta (float32, of the parameters' shapes);
-    fresh zeros if None.  scale: "spectral" (sqrt(max(1, rows / cols))), "rms" (0.2 sqrt(max(rows, cols)): updates as large as
-    AdamW's) or a number.  products: as in `orthogonalize`, by the parameters' type.  No two of the tensors may share memory.
+    fresh zeros if None.  scale: "spectral" (sqrt(max(1, rows / cols)), for weights stored [out][in]), "spectral_t" (sqrt(max(1, cols / rows)),
+    for weights stored [in][out], as x @ W takes them), "rms" (0.2 sqrt(max(rows, cols)): updates as large as AdamW's) or a number.  products: as in `orthogonalize`, by the parameters' type.  No two of the tensors may share memory.
     Waits inside the kernels are bounded; `status` says whether one ran out."""
 
     def __init__(self, params, *, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
@@ -309,10 +309,12 @@ class Muon:
                 raise TypeError(f"params[{i}]: need a matrix, or a batch of them")
         if scale == "spectral":
             self.scales = [max(1.0, p.shape[-2] / max(1, p.shape[-1])) ** 0.5 for p in params]
+        elif scale == "spectral_t":
+            self.scales = [max(1.0, p.shape[-1] / max(1, p.shape[-2])) ** 0.5 for p in params]
         elif scale == "rms":
             self.scales = [0.2 * max(p.shape[-2:]) ** 0.5 for p in params]
         elif isinstance(scale, str):
-            raise ValueError('scale: "spectral", "rms" or a number')
+            raise ValueError('scale: "spectral", "spectral_t", "rms" or a number')
         else:
             self.scales = [float(scale)] * len(params)
         self.params = params
