@@ -10,6 +10,7 @@ from __future__ import annotations
 import concurrent.futures
 import glob
 import os
+import re
 import subprocess
 import sys
 
@@ -38,6 +39,47 @@ def stale() -> bool:
     if not os.path.exists(LIB):
         return True
     return os.path.getmtime(LIB) < max(os.path.getmtime(p) for p in _deps())
+
+
+class RegisterError(RuntimeError):
+    pass
+
+
+def planned_registers(source: str) -> int | None:
+    """Registers to a thread that the kernels of a source which hand registers over between their warps (setmaxnreg) have to be launched with;
+    None if there are no such kernels."""
+    found = re.search(r"constexpr int LAUNCH_REGISTERS = (\d+);", source)
+    return int(found.group(1)) if found and "setmaxnreg" in source else None
+
+
+def check_registers(log: str, planned: int, kernel: str = "k_product") -> int:
+    """Reads the assembler's report (-Xptxas -v): every instance of `kernel` has to have `planned` registers to a thread.  With fewer, what its
+    warps ask for is never given up by others, and the library refuses to launch it.  Returns the number of instances."""
+    entries = [(name, int(n)) for name, n in re.findall(r"Compiling entry function '([^']+)'(?:(?!Compiling entry function).)*?Used (\d+) registers", log, re.S)
+               if kernel in name]
+    if not entries:
+        raise RegisterError(f"no instance of {kernel} in the assembler's report")
+    for name, n in entries:
+        if n != planned:
+            raise RegisterError(f"{name} has {n} registers, its launch is planned with {planned}")
+    return len(entries)
+
+
+def compile_one(cmd: list[str], src: str, obj: str, verbose: bool = False) -> int:
+    """Compiles one source; nvcc's exit code.  Raises RegisterError (and leaves no object) where a kernel is not as its launch is planned."""
+    with open(src) as f:
+        planned = planned_registers(f.read())
+    done = subprocess.run(cmd + (["-Xptxas", "-v"] if verbose or planned else []), stderr=subprocess.PIPE, text=True)
+    # without the report, unless it was asked for, but with warnings and errors
+    shown = [line for line in done.stderr.splitlines(True) if verbose or not (line.startswith("ptxas info") or "bytes stack frame" in line)]
+    sys.stderr.write("".join(shown))
+    if done.returncode == 0 and planned:
+        try:
+            check_registers(done.stderr, planned)
+        except RegisterError:
+            os.remove(obj)
+            raise
+    return done.returncode
 
 
 def build_binding(force: bool = False) -> str:
@@ -71,10 +113,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         for src in sources():
             obj = os.path.join(OBJ, os.path.basename(src)[:-3] + ".o")
             if force or not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(src), newest_header):
-                jobs.append([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) +
-                            ["-I", INCLUDE, "-c", "-o", obj, src])
+                jobs.append(([nvcc] + NVCC_FLAGS + ["-I", INCLUDE, "-c", "-o", obj, src], src, obj, verbose))
         with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(len(jobs), os.cpu_count() or 1))) as pool:
-            for rc in pool.map(subprocess.call, jobs):
+            for rc in pool.map(lambda job: compile_one(*job), jobs):
                 if rc:
                     raise subprocess.CalledProcessError(rc, "nvcc")
         objs = [os.path.join(OBJ, os.path.basename(s)[:-3] + ".o") for s in sources()]

@@ -1128,7 +1128,8 @@ template <Kind KIND, int COLS, bool SPLIT, typename T>
 int launch_tiles(cudaStream_t st, const Common& C, const CUtensorMap& map, int which, int64_t tiles, int sms) {
     static PerDevice known;
     int fits = 0;
-    // the exchange of registers in the kernel would wait forever if it had been launched with others
+    // The exchange of registers in the kernel would wait forever if it had been launched with others.  The build looks at what the assembler
+    // reports; this is for libraries that were built otherwise.
     static const bool as_planned = [] {
         cudaFuncAttributes a{};
         return cudaFuncGetAttributes(&a, k_product<KIND, COLS, SPLIT, T>) == cudaSuccess && a.numRegs == LAUNCH_REGISTERS;
