@@ -1242,7 +1242,8 @@ int check_matrices(const ssgd_matrix* t, int32_t count, int32_t fmt_in, int32_t 
     for (int32_t i = 0; i < count; ++i) {
         if (!t[i].rows || !t[i].cols) continue;
         if (t[i].ld_in < t[i].cols || t[i].ld_out < t[i].cols || !t[i].in || !t[i].out || (with_m && !t[i].m)) return SSGD_EINVAL;
-        if (!aligned_to(t[i].in, fmt_bytes(fmt_in)) || !aligned_to(t[i].out, fmt_bytes(fmt_out)) || !aligned_to(t[i].m, 4)) return SSGD_EALIGN;
+        if (!aligned_to(t[i].in, fmt_bytes(fmt_in)) || !aligned_to(t[i].out, fmt_bytes(fmt_out)) || (with_m && !aligned_to(t[i].m, 4)))
+            return SSGD_EALIGN;
     }
     return SSGD_OK;
 }
@@ -1280,6 +1281,7 @@ int run(const ssgd_matrix* t, int32_t count, Common C, int32_t steps, double lr,
             Matrix& M = G.m[s.count];
             add(s, t[i], C.split, &M);
             M.update = (float)(lr * t[i].scale);
+            if (!C.update) M.m = nullptr;           // whatever the caller left there
             const int32_t tiles = M.tall() ? (M.rb + 1) / 2 : 1, columns = BLOCK * (M.tall() ? tiles * M.cb : M.cb);
             plan.x_blocks = std::max(plan.x_blocks, M.rb * M.cb);
             // rows beyond a matrix of one block are read, and their results left
@@ -1301,6 +1303,7 @@ int run(const ssgd_matrix* t, int32_t count, Common C, int32_t steps, double lr,
             if (!t[i].rows || !t[i].cols || is_small(t[i])) continue;
             if (!add(s, t[i], C.split, s.count < MAX_GROUP ? &G.m[s.count] : nullptr)) break;
             G.m[s.count - 1].update = (float)(lr * t[i].scale);
+            if (!C.update) G.m[s.count - 1].m = nullptr;
         }
         if (!s.count) break;
         uint8_t* base = static_cast<uint8_t*>(workspace);
