@@ -11,14 +11,14 @@
 //     only the operands of the products are rounded, and their error lies along the large singular values
 //   - the diagonals of A and B, which all but carry the matrices when x is nearly orthogonal, are kept in fp32 beside them:
 //       A = R + D:  A A = R R + R (d_i + d_j) + D D;    B = Q + E:  a x + B x = (a + e_i) x + Q x
-// leaving 5e-4 to 1.4e-3 of the result (less than its rounding to bfloat16, 1.7e-3).  Where the result has more bits than bfloat16,
-// or the caller says so, every matrix is a sum of two fp16 numbers and a product takes three (high high, high low, low high): 3e-7
-// to 4e-6, less than the same iteration in fp32.
+// leaving 1e-4 to 1.5e-3 of the result (less than its rounding to bfloat16, 1.7e-3).  Where the result has more bits than bfloat16,
+// or the caller says so, every matrix is a sum of two fp16 numbers and a product takes three (high high, high low, low high): 1e-6
+// to 5e-6, where the same iteration in fp32 is off by 1.3e-6 to 1.5e-5.
 // The stored numbers are 1024 times the true ones: x is at most 1.2 and an element mostly far below, so that the second number stays
 // clear of fp16's subnormals.
 //
-// Measured: 8 x 1024 x 2816 bf16 0.71 ms, 557 TFLOP/s of what has to be computed; the matrices of two transformer blocks (2048, 5632) bf16
-// 2.4 ms, 810; of eight (768, 2048) fp32 with three products 1.66 ms, 240.  What bounds the large ones is what an SM takes from L2: 48 to 50
+// Measured: 8 x 1024 x 2816 bf16 0.72 ms, 550 TFLOP/s of what has to be computed; the matrices of two transformer blocks (2048, 5632) bf16
+// 2.4 to 2.5 ms, 780 to 810; of eight (768, 2048) fp32 with three products 1.7 ms, 235.  What bounds the large ones is what an SM takes from L2: 48 to 50
 // bytes per cycle, 681 cycles for 64 of the contraction of a 256 x 256 tile, of which the products are 512.
 //
 // Layout.  All matrices of a call go through every launch together: prepare (momentum and sums of squares; division and layout),
@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(PREPARE_THREADS, 4) k_layout(const __grid_cons
 // ---- products ----------------------------------------------------------------------------------------
 
 // A tile is 256 rows and COLS columns, of a pair of CTAs that has half of the rows each.  What a tile loads per block of the contraction
-// grows with its sides, what it computes with their product: 256 x 256 needs 12 TB/s from L2 at the tensor cores' full rate, 128 x 128 by
-// single CTAs 24 TB/s.  Where the larger tiles are too few, 256 x 128.
+// grows with its sides, what it computes with their product: 256 x 256 needs 32 KB into each SM per 512 cycles at the tensor cores' full rate,
+// 18 TB/s from L2 at 1.9 GHz, 128 x 128 by single CTAs twice that.  Where the larger tiles are too few, 256 x 128.
 constexpr int TILE_ROWS = 256;
 constexpr int RING = 192 * 1024;                    // bytes of operands on their way
 constexpr int RESULT_WARPS = 8;
@@ -786,7 +786,7 @@ k_product(const __grid_constant__ Common C, const __grid_constant__ CUtensorMap 
 //
 // Where x and A fit the shared memory of one CTA (the shorter side up to 128, the longer up to 256), one CTA does all of it for one matrix:
 // momentum, division, every step.  The launches above would each wait for the one before, 6 us for a microsecond's work (four matrices of
-// 64 x 128: 98 us; this way 36).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
+// 64 x 128: 98 us; this way 37).  x, A and B are blocks in shared memory as elsewhere; results replace what they are made from,
 // number by number: both halves of the symmetric products are computed, so that each thread needs its own numbers alone.
 
 constexpr int SMALL_SHORT = 2, SMALL_LONG = 4;      // blocks of the sides

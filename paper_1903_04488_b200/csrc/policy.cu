@@ -10,8 +10,9 @@
 // stays in shared memory in between (a cluster of CTAs shares one that is too long, or where rows are few), so that every
 // logit is read once and every gradient written once, and the memory is what bounds it.  A token of weight 0 is not even read.
 //
-// At 8192 x 32000 bfloat16 201 us, 5.2 TB/s (0.80 of a copy): 15 instructions per logit are 109 us of issue slots, two 2^x 58 us of the
-// special-function unit each; three CTAs of 64 KB share an SM, and their loads, sums and stores overlap only so far.
+// At 8192 x 32000 bfloat16 205 us over the same logits again and again, 212 to 216 over new ones: 4.9 to 5.1 TB/s (0.74 to 0.78 of a
+// copy).  15 instructions per logit are 109 us of issue slots, two 2^x 58 us of the special-function unit each; three CTAs of 64 KB share
+// an SM, and their loads, sums and stores overlap only so far.
 //
 // Granule i of a CTA's segment belongs to thread i mod threads, which copies it to shared memory (cp.async, up to four batches ahead),
 // adds it to its running sums (logits.cuh), and makes its gradient: no barrier but those of the row's sums.

@@ -8,8 +8,9 @@
 // pairs: the first launch leaves the sum of every piece of a sequence (a CTA's tokens that belong to it), the second joins the pieces
 // of its pairs, each CTA for itself and all in the same order, and writes.  The piece of sequence s in CTA k has place k + s: between
 // two pieces that follow one another either grows by one, so no two share a place, and there are CTAs + sequences places.
-// A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 40 us (3.6 TB/s;
-// 25 for the sums, where an SM has three CTAs that load and add by turns, 15 for the rest), 262144 tokens 10 us, 2000 tokens 8 us.
+// A call of one CTA does both in one launch.  Measured: 12,000,000 tokens in 4099 pairs 42 us (3.4 TB/s;
+// 27 for the sums, where an SM has three CTAs that load and add by turns, 16 for the rest), 262144 tokens 12 us, 2000 tokens 8 us.  What the
+// differences logp - ref lose is 2 of the 27: with differences rounded to 24 bits both launches took 40.
 #include <cstddef>
 
 #include "formats.cuh"
@@ -57,7 +58,7 @@ struct Shared {
     alignas(16) float ref[CHUNK];                   // (not there in the second launch)
 };
 // Where token i's mark stands while each thread goes through EACH tokens that follow one another: the threads of a warp meet no bank twice
-// (12M tokens in 200,000 pairs 86 us against 103).
+// (12M tokens in 200,000 pairs took 86 us with it and 103 without).
 __device__ __forceinline__ int place_of(int i) {
     static_assert(EACH == 32, "a row of all banks to a thread");
     return i ^ (i >> 5 & 31);
@@ -488,7 +489,7 @@ enum Part { SUMS, FINISH, ALL };
 
 template <Part PART, typename I>
 // The second launch waits for starts, pieces and weights one after the other and has the shared memory for 5 CTAs to an SM: 12M
-// tokens in 4099 pairs 39.7 us against 41 for both launches, in 4M pairs 184 against 196.  A sixth gains nothing.
+// tokens in 4099 pairs 1.3 us less than with 4, in 4M pairs 12 less.  A sixth gains nothing.
 __global__ void __launch_bounds__(THREADS, PART == FINISH ? 5 : 4) k_preference(const Args A) {
     extern __shared__ __align__(16) uint8_t raw[];
     Shared& S = *reinterpret_cast<Shared*>(raw);
