@@ -12,8 +12,10 @@
 //   - the diagonals of A and B, which all but carry the matrices when x is nearly orthogonal, are kept in fp32 beside them:
 //       A = R + D:  A A = R R + R (d_i + d_j) + D D;    B = Q + E:  a x + B x = (a + e_i) x + Q x
 // leaving 1e-4 to 1.5e-3 of the result (less than its rounding to bfloat16, 1.7e-3).  Where the result has more bits than bfloat16,
-// or the caller says so, every matrix is a sum of two fp16 numbers and a product takes three (high high, high low, low high): 1e-6
-// to 5e-6, where the same iteration in fp32 is off by 1.3e-6 to 1.5e-5.
+// or the caller says so, every matrix is a sum of two fp16 numbers and a product takes three (high high, high low, low high): 4e-7
+// to 7e-6, where the same iteration in fp32 is off by 4e-7 to 1.5e-5.  The tensor cores' sums truncate, which shows where few long rows are
+// multiplied with themselves (4 x 536: 3.7e-6, fp32 1.3e-6).  Roundings that do not average out take matrices of less than 512 numbers
+// to 7e-3 with one product.
 // The stored numbers are 1024 times the true ones: x is at most 1.2 and an element mostly far below, so that the second number stays
 // clear of fp16's subnormals.
 //

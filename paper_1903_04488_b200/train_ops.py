@@ -276,8 +276,8 @@ def orthogonalize(x: torch.Tensor, *, steps: int = 5, coefficients=QUINTIC, eps:
     """x / (norm + eps) with the polynomial a s + b s^3 + c s^5 applied to its singular values `steps` times, in x's type: close to
     the nearest matrix with orthonormal rows (or columns), but for singular values that are all but zero.
 
-    x: a matrix (with any row stride), or a contiguous batch of them.  products: 3 for results as exact as fp32's, 1 for an error of
-    about 1e-3 at a third of the time; None: 1 for bfloat16, otherwise 3.  out: where the result goes (x's shape and type; may be x).
+    x: a matrix (with any row stride), or a contiguous batch of them.  products: 3 for results about as exact as fp32's, 1 for an
+    error of about 1e-3 (matrices of less than 512 numbers: up to 7e-3) at a third of the time; None: 1 for bfloat16, otherwise 3.  out: where the result goes (x's shape and type; may be x).
     Waits inside the kernels are bounded; `status` says whether one ran out."""
     a, b, c = coefficients
     return (_native or native()).orthogonalize(x, steps, a, b, c, eps, 0 if products is None else products, out)
